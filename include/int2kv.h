@@ -318,6 +318,92 @@ int int2kv_output_error(const int2kv_cache* cache, const uint16_t* q, int batch,
                         float* stats, float* dy, void* workspace, size_t workspace_bytes,
                         hipStream_t stream);
 
+/* ---- Around the decode step: a chunk's rotary positions, its attention, and rows read back.
+ *
+ * Rotary positions with several axes (time, height and width of image and video tokens) of a chunk's
+ * queries and keys, in one launch. Rotate-half pairs (i, i + 64), i < 64; pair i turns by its axis'
+ * position of the token:
+ *     y_i = x_i cos - x_{i+64} sin,   y_{i+64} = x_{i+64} cos + x_i sin,
+ *     (cos, sin) = cos_sin[positions[pair_axis[i]][token]][i], [... 64 + i],
+ * each evaluated exactly in fp64 and rounded once to bf16, as in int2kv_quantize_append_rope (with
+ * one axis the keys equal its k_rope_out). The turned keys go to int2kv_quantize_append and
+ * int2kv_chunk_attention, the turned queries to the latter or to int2kv_decode.
+ *   q, k         : bf16, head j of token t at t * stride + 128 j (elements); 16-byte aligned; either
+ *                  may be NULL with 0 heads. The strides let them be views of a layer's fused
+ *                  projection; multiples of 8, at least 128 * heads
+ *   positions    : int32 [num_axes, num_tokens]; a token with a position outside [0, max_pos) on any
+ *                  axis is skipped: its output rows are left as they were
+ *   num_axes     : 1 .. 8;  pair_axis: HOST uint8 [64], the axis of each pair
+ *   cos_sin      : fp32 [max_pos, 128], as in int2kv_quantize_append_rope; 16-byte aligned
+ *   q_out, k_out : bf16 rows as q, k with strides of their own; may be q, k themselves (same stride),
+ *                  otherwise no output row may overlap an input's or the other output's rows */
+int int2kv_rope_axes(const uint16_t* q, int num_q_heads, int64_t q_stride, const uint16_t* k, int num_kv_heads,
+                     int64_t k_stride, const int32_t* positions, int num_axes, const uint8_t* pair_axis,
+                     int num_tokens, const float* cos_sin, int max_pos, uint16_t* q_out, int64_t q_out_stride,
+                     uint16_t* k_out, int64_t k_out_stride, hipStream_t stream);
+
+/* Row formats of int2kv_read_rows. */
+enum {
+  INT2KV_ROWS_BF16 = 0,
+  INT2KV_ROWS_F32 = 1
+};
+
+/* Rows read back from the cache: the keys and values that the decode attends to, for another cache
+ * (other rotations, group size or paging), a full-precision consumer, or diagnostics.
+ *     k_out[i] = k^ R_K^T + mu,   v_out[i] = v^ R_V^T,   k^, v^ = code * s + z of slot slot_mapping[i];
+ * without R_k (R_v) the row as stored, k^ (v^), in the rotated basis.
+ *   slot_mapping : int32 [num_tokens], in any order, repeats allowed; a slot outside the cache (also a
+ *                  negative one) leaves its output rows as they were
+ *   R_k, R_v     : fp32 [H_kv, 128, 128], 16-byte aligned, or NULL;  mu: fp32 [H_kv, 128] or NULL (keys
+ *                  stay centered); mu needs R_k
+ *   row_format   : INT2KV_ROWS_BF16 or INT2KV_ROWS_F32
+ *   k_out, v_out : bf16 or fp32 [num_tokens, H_kv, 128], 16-byte aligned; one of them may be NULL; they
+ *                  may not overlap
+ * Stored rows are exact before the format's one rounding. The un-rotation runs on the matrix cores in
+ * fp16 terms with fp32 sums: one term each for bf16 rows (about 3e-4 of the row's root mean square,
+ * under the rounding of bf16), two for fp32 rows (below 1e-6). Dequantized values and rotations have
+ * to lie within fp16's range (|x| <= 65504). */
+int int2kv_read_rows(const int2kv_cache* cache, const int32_t* slot_mapping, int num_tokens, const float* R_k,
+                     const float* R_v, const float* mu, int row_format, void* k_out, void* v_out,
+                     hipStream_t stream);
+
+/* Attention of several new tokens per sequence over the INT2 cache: a prompt or a chunk of one, a
+ * turn after a cached history, drafted tokens. Token i (0 .. n_b - 1) of sequence b is row
+ * q_starts[b] + i of q and out. Two forms:
+ *   k_new given: the chunk's keys and values are the caller's bf16 rows, the cache holds what came
+ *     before: token i sees the ctx_lens[b] cached tokens and the new tokens 0 .. i of its sequence,
+ *       a_s = (q R_K) k^_s^T / sqrt(d),  a_t = q (k_t - mu)^T / sqrt(d),
+ *       o = (sum_s p_s v^_s) R_V^T + sum_t p_t v_t,   one softmax over both;
+ *   k_new NULL: the cache holds the new tokens too (appended first, as for int2kv_decode), ctx_lens[b]
+ *     counts them: token i sees the cached tokens 0 .. ctx_lens[b] - n_b + i (for n_b = 1 this is
+ *     int2kv_decode without W_O, up to rounding).
+ * A token that sees nothing gets zeros.
+ *   q            : bf16, head j of token t at t * q_stride + 128 j (elements); post-RoPE; 16-byte
+ *                  aligned; q_stride a multiple of 8, at least 128 * H_q
+ *   q_starts     : int32 [batch + 1], ascending offsets into 0 .. total_q; rows of q and out outside
+ *                  every sequence (padding behind the last one) are not written; a sequence may be empty
+ *   total_q, max_q : rows of q and out; host-side upper bound of n_b (larger sequences are cut to it)
+ *   block_table, max_blocks_per_seq, ctx_lens, max_ctx : as int2kv_decode (same clamping, blocks
+ *                  outside the cache are skipped)
+ *   R_k, R_v     : fp32 [H_kv, 128, 128], 16-byte aligned
+ *   k_new, v_new : bf16 rows as q with H_kv heads and strides of their own (raw post-RoPE keys, not
+ *                  centered; values), with mu: fp32 [H_kv, 128]; or NULL, NULL, NULL
+ *   out          : bf16 [total_q, H_q, 128], 16-byte aligned, model basis; must not overlap q, k_new, v_new
+ *   workspace    : int2kv_chunk_attention_workspace_bytes(...) bytes, 256-byte aligned; nothing in it
+ *                  needs to be kept or cleared between calls, calls that overlap need one each
+ * Products run on the matrix cores with fp32 sums: rotated queries, dequantized rows and the
+ * probabilities over the INT2 tokens in fp16, those over the chunk's own tokens in bf16, each rounded
+ * once; softmax statistics in fp32. Dequantized values have to lie within fp16's range (|x| <= 65504).
+ * A non-finite key or value reaches only the tokens that see it. Deterministic; no atomics on results. */
+size_t int2kv_chunk_attention_workspace_bytes(int batch, int num_q_heads, int num_kv_heads, int total_q, int max_q,
+                                              int max_ctx);
+int int2kv_chunk_attention(const int2kv_cache* cache, const uint16_t* q, int64_t q_stride, const int32_t* q_starts,
+                           int batch, int total_q, int max_q, int num_q_heads, const int32_t* block_table,
+                           int max_blocks_per_seq, const int32_t* ctx_lens, int max_ctx, const float* R_k,
+                           const float* R_v, const uint16_t* k_new, int64_t k_stride, const uint16_t* v_new,
+                           int64_t v_stride, const float* mu, uint16_t* out, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream);
+
 /* ---- OptR offline calibration (Sec. 4.2 - 4.5; Algorithm 1 of the appendix), fp64 on the GPU.
  * For every KV head h the corrected rotations R = R^0 exp(A - A^T) (eq:OptR_skew) are fitted to
  * calibration traces: first A_K on the key objective (eq:OptR_key_loss)

@@ -622,6 +622,139 @@ int int2kv_output_error(const int2kv_cache* cache, const uint16_t* q, int batch,
 
 }  // extern "C"
 
+// ---- a chunk's rotary positions, rows read back, attention of a chunk
+namespace {
+
+// Rows of `heads` heads, n of them, `stride` elements apart
+struct Rows {
+  const void* p;
+  int64_t stride;
+  int heads, n, bytes;  // bytes of an element
+  uintptr_t first() const { return reinterpret_cast<uintptr_t>(p); }
+  uint64_t step() const { return (uint64_t)stride * bytes; }
+  uint64_t len() const { return (uint64_t)heads * kHeadDim * bytes; }
+  uintptr_t end() const { return first() + (uint64_t)(n - 1) * step() + len(); }
+};
+
+// Whether two sets of rows share a byte; rows of different strides count as sharing where their spans meet
+bool rows_meet(const Rows& a, const Rows& b) {
+  if (!a.p || !b.p || a.first() >= b.end() || b.first() >= a.end()) return false;
+  if (a.step() != b.step()) return true;
+  const uint64_t d = (b.first() >= a.first() ? b.first() - a.first() : a.step() - (a.first() - b.first()) % a.step()) % a.step();
+  return d < a.len() || a.step() - d < b.len();
+}
+
+bool valid_stride(int64_t stride, int heads) { return stride >= (int64_t)heads * kHeadDim && stride % 8 == 0 && stride <= INT32_MAX; }
+
+}  // namespace
+
+extern "C" {
+
+int int2kv_rope_axes(const uint16_t* q, int num_q_heads, int64_t q_stride, const uint16_t* k, int num_kv_heads,
+                     int64_t k_stride, const int32_t* positions, int num_axes, const uint8_t* pair_axis, int num_tokens,
+                     const float* cos_sin, int max_pos, uint16_t* q_out, int64_t q_out_stride, uint16_t* k_out,
+                     int64_t k_out_stride, hipStream_t stream) {
+  if (num_tokens < 0) return fail(INT2KV_EINVAL, "num_tokens must be >= 0");
+  if (num_q_heads < 0 || num_kv_heads < 0 || num_q_heads > 65535 || num_kv_heads > 65535)
+    return fail(INT2KV_EINVAL, "head counts must be in [0, 65535]");
+  if (num_axes < 1 || num_axes > 8) return fail(INT2KV_EINVAL, "num_axes must be in [1, 8]");
+  if (!pair_axis) return fail(INT2KV_EINVAL, "NULL pointer argument");
+  for (int i = 0; i < kHeadDim / 2; ++i)
+    if (pair_axis[i] >= num_axes) return fail(INT2KV_EINVAL, "pair_axis names an axis outside [0, num_axes)");
+  if (num_tokens == 0 || num_q_heads + num_kv_heads == 0) return ok();
+  if (!positions || !cos_sin || (num_q_heads && (!q || !q_out)) || (num_kv_heads && (!k || !k_out)))
+    return fail(INT2KV_EINVAL, "NULL pointer argument");
+  if (max_pos <= 0) return fail(INT2KV_EINVAL, "max_pos must be positive");
+  if ((num_q_heads && (!valid_stride(q_stride, num_q_heads) || !valid_stride(q_out_stride, num_q_heads))) ||
+      (num_kv_heads && (!valid_stride(k_stride, num_kv_heads) || !valid_stride(k_out_stride, num_kv_heads))))
+    return fail(INT2KV_EINVAL, "strides must be multiples of 8, at least 128 * heads and below 2^31");
+  if (!aligned(cos_sin, 16) || !aligned(positions, 4) ||
+      (num_q_heads && (!aligned(q, 16) || !aligned(q_out, 16))) || (num_kv_heads && (!aligned(k, 16) || !aligned(k_out, 16))))
+    return fail(INT2KV_EINVAL, "q, k, their outputs and cos_sin must be 16-byte aligned");
+  const Rows rq{num_q_heads ? q : nullptr, q_stride, num_q_heads, num_tokens, 2};
+  const Rows rk{num_kv_heads ? k : nullptr, k_stride, num_kv_heads, num_tokens, 2};
+  const Rows oq{num_q_heads ? q_out : nullptr, q_out_stride, num_q_heads, num_tokens, 2};
+  const Rows ok_{num_kv_heads ? k_out : nullptr, k_out_stride, num_kv_heads, num_tokens, 2};
+  const bool q_place = rq.p == oq.p && q_stride == q_out_stride, k_place = rk.p == ok_.p && k_stride == k_out_stride;
+  if ((!q_place && rows_meet(oq, rq)) || (!k_place && rows_meet(ok_, rk)) || rows_meet(oq, rk) || rows_meet(ok_, rq) ||
+      rows_meet(oq, ok_))
+    return fail(INT2KV_EINVAL, "output rows overlap rows of an input or of the other output");
+  RopeAxesArgs a{};
+  a.q = q, a.k = k, a.q_out = q_out, a.k_out = k_out;
+  a.q_stride = q_stride, a.k_stride = k_stride, a.q_out_stride = q_out_stride, a.k_out_stride = k_out_stride;
+  a.hq = num_q_heads, a.hk = num_kv_heads, a.n = num_tokens;
+  a.positions = positions, a.num_axes = num_axes, a.max_pos = max_pos, a.cos_sin = cos_sin;
+  return hip_status(launch_rope_axes(a, pair_axis, stream), "rope_axes");
+}
+
+int int2kv_read_rows(const int2kv_cache* cache, const int32_t* slot_mapping, int num_tokens, const float* R_k,
+                     const float* R_v, const float* mu, int row_format, void* k_out, void* v_out, hipStream_t stream) {
+  if (int st = check_cache(cache)) return st;
+  if (num_tokens < 0) return fail(INT2KV_EINVAL, "num_tokens must be >= 0");
+  if (row_format != INT2KV_ROWS_BF16 && row_format != INT2KV_ROWS_F32) return fail(INT2KV_EINVAL, "unknown row_format");
+  if (cache->num_kv_heads > 65535) return fail(INT2KV_EUNSUPPORTED, "at most 65535 KV heads");
+  if (mu && !R_k) return fail(INT2KV_EINVAL, "mu needs R_k");
+  if (num_tokens == 0) return ok();
+  if (!slot_mapping || (!k_out && !v_out)) return fail(INT2KV_EINVAL, "NULL pointer argument");
+  const bool f32 = row_format == INT2KV_ROWS_F32;
+  if ((R_k && !aligned(R_k, 16)) || (R_v && !aligned(R_v, 16)) || (mu && !aligned(mu, 4)) || !aligned(slot_mapping, 4) ||
+      (k_out && !aligned(k_out, 16)) || (v_out && !aligned(v_out, 16)))
+    return fail(INT2KV_EINVAL, "R_k, R_v, k_out and v_out must be 16-byte aligned");
+  const int64_t row = (int64_t)cache->num_kv_heads * kHeadDim;
+  if (rows_meet(Rows{k_out, row, cache->num_kv_heads, num_tokens, f32 ? 4 : 2}, Rows{v_out, row, cache->num_kv_heads, num_tokens, f32 ? 4 : 2}))
+    return fail(INT2KV_EINVAL, "k_out and v_out overlap");
+  return hip_status(launch_read_rows(view(cache), slot_mapping, num_tokens, R_k, R_v, mu, f32, k_out, v_out, stream), "read_rows");
+}
+
+size_t int2kv_chunk_attention_workspace_bytes(int batch, int num_q_heads, int num_kv_heads, int total_q, int max_q,
+                                              int max_ctx) {
+  if (batch <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads || total_q < 0 || max_q < 0 || max_ctx < 0)
+    return 0;
+  return make_chunk_plan(batch, num_q_heads, num_kv_heads, total_q, max_q < total_q ? max_q : total_q, max_ctx).total;
+}
+
+int int2kv_chunk_attention(const int2kv_cache* cache, const uint16_t* q, int64_t q_stride, const int32_t* q_starts,
+                           int batch, int total_q, int max_q, int num_q_heads, const int32_t* block_table,
+                           int max_blocks_per_seq, const int32_t* ctx_lens, int max_ctx, const float* R_k, const float* R_v,
+                           const uint16_t* k_new, int64_t k_stride, const uint16_t* v_new, int64_t v_stride, const float* mu,
+                           uint16_t* out, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (int st = check_cache(cache)) return st;
+  const int H = cache->num_kv_heads;
+  if (H > 65535) return fail(INT2KV_EUNSUPPORTED, "at most 65535 KV heads");
+  if (batch <= 0) return fail(INT2KV_EINVAL, "batch must be positive");
+  if (num_q_heads <= 0 || num_q_heads % H) return fail(INT2KV_EINVAL, "num_q_heads must be a multiple of num_kv_heads");
+  if (total_q < 0 || max_q < 0 || max_ctx < 0 || max_blocks_per_seq <= 0)
+    return fail(INT2KV_EINVAL, "bad total_q / max_q / max_ctx / max_blocks_per_seq");
+  if (max_q > total_q) max_q = total_q;
+  if (max_q == 0) return ok();
+  if ((int64_t)total_q * num_q_heads > INT32_MAX || (int64_t)batch > (1 << 24))
+    return fail(INT2KV_EUNSUPPORTED, "total_q * num_q_heads must be below 2^31, batch at most 2^24");
+  if (!q || !q_starts || !block_table || !ctx_lens || !R_k || !R_v || !out) return fail(INT2KV_EINVAL, "NULL pointer argument");
+  if (!k_new != !v_new || !k_new != !mu) return fail(INT2KV_EINVAL, "k_new, v_new and mu go together");
+  if (!valid_stride(q_stride, num_q_heads) || (k_new && (!valid_stride(k_stride, H) || !valid_stride(v_stride, H))))
+    return fail(INT2KV_EINVAL, "strides must be multiples of 8, at least 128 * heads and below 2^31");
+  if (!aligned(q, 16) || !aligned(R_k, 16) || !aligned(R_v, 16) || !aligned(out, 16) || (k_new && (!aligned(k_new, 16) || !aligned(v_new, 16))))
+    return fail(INT2KV_EINVAL, "q, R_k, R_v, k_new, v_new and out must be 16-byte aligned");
+  const Rows ro{out, (int64_t)num_q_heads * kHeadDim, num_q_heads, total_q, 2};
+  if (rows_meet(ro, Rows{q, q_stride, num_q_heads, total_q, 2}) || (k_new && (rows_meet(ro, Rows{k_new, k_stride, H, total_q, 2}) ||
+      rows_meet(ro, Rows{v_new, v_stride, H, total_q, 2}))))
+    return fail(INT2KV_EINVAL, "out overlaps q, k_new or v_new");
+  const ChunkPlan plan = make_chunk_plan(batch, num_q_heads, H, total_q, max_q, max_ctx);
+  if ((int64_t)plan.max_items * H > INT32_MAX) return fail(INT2KV_EUNSUPPORTED, "too many row tiles for one launch");
+  if (!workspace || workspace_bytes < plan.total)
+    return fail(INT2KV_EWORKSPACE, "workspace smaller than int2kv_chunk_attention_workspace_bytes()");
+  if (!aligned(workspace, 256)) return fail(INT2KV_EINVAL, "workspace must be 256-byte aligned");
+  ChunkArgs a{};
+  a.cv = view(cache);
+  a.q = q, a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+  a.starts = q_starts, a.B = batch, a.total_q = total_q, a.max_q = max_q, a.Hq = num_q_heads, a.gq = num_q_heads / H;
+  a.table = block_table, a.max_blocks = max_blocks_per_seq, a.lens = ctx_lens, a.max_ctx = max_ctx;
+  a.R_k = R_k, a.R_v = R_v, a.k_new = k_new, a.v_new = v_new, a.mu = mu, a.out = out;
+  return hip_status(launch_chunk_attention(a, plan, static_cast<uint8_t*>(workspace), stream), "chunk_attention");
+}
+
+}  // extern "C"
+
 // ---- OptR offline calibration
 namespace {
 

@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include "common.h"
+
 namespace int2kv {
 
 struct CacheView {
@@ -163,6 +165,66 @@ struct OutErrArgs {
 // stats: [B, Hq, 4]; dy (may be null): [B, Hq, 2, d_model]; ev0 / ev1 track the scan kernel
 hipError_t launch_output_error(const OutErrArgs& e, const uint16_t* W_o, int d_model, float* stats, float* dy,
                                hipStream_t s, hipEvent_t ev0, hipEvent_t ev1);
+
+// ---- rotary positions with several axes (rope.hip)
+struct RopeAxesArgs {
+  const uint16_t *q, *k;                       // bf16 rows: token t, head h at t * stride + 128 h
+  uint16_t *q_out, *k_out;
+  int64_t q_stride, k_stride, q_out_stride, k_out_stride;
+  int hq, hk, n;
+  const int32_t* positions;                    // [num_axes, n]
+  int num_axes, max_pos;
+  const float* cos_sin;                        // [max_pos, 128]
+  uint32_t axis[8];                            // axis of each rotary pair, four bits each (set by the launcher)
+  int heads_per_block;                         // (set by the launcher)
+};
+hipError_t launch_rope_axes(RopeAxesArgs a, const uint8_t* pair_axis, hipStream_t s);
+
+// ---- rows read back (read.hip). R_k / R_v null: the rows as stored; k_out / v_out null: not wanted
+hipError_t launch_read_rows(CacheView c, const int32_t* slots, int n, const float* R_k, const float* R_v, const float* mu,
+                            bool f32, void* k_out, void* v_out, hipStream_t s);
+
+// ---- attention of a chunk of new tokens (chunk.hip)
+struct ChunkTile {  // a tile of query rows of one sequence (the same for every KV head)
+  int b, row0;        // sequence, first row
+  int start, n, ctx;  // the sequence's first token in q, its new and its cached tokens
+  int units;          // 64-token units of its context
+  int pieces, slot;   // pieces it is cut into, and the first one's partial (-1: one piece, no partial)
+};
+struct ChunkItem {  // a piece: units u0 .. u1 of a tile, its partial's slot (-1: the result itself)
+  int tile, u0, u1, slot;
+};
+constexpr int kChunkPartStride = kHeadDim + 2;  // sums, then m and l
+struct ChunkArgs {
+  CacheView cv;
+  const uint16_t* q;                // bf16, token t, head j at t * q_stride + 128 j
+  int64_t q_stride, k_stride, v_stride;
+  const int32_t* starts;            // [B + 1]
+  int B, total_q, max_q, Hq, gq;
+  const int32_t* table;
+  int max_blocks;
+  const int32_t* lens;
+  int max_ctx;
+  const float *R_k, *R_v;
+  const uint16_t *k_new, *v_new;    // the chunk's own keys and values, or null: the cache holds them
+  const float* mu;
+  uint16_t* out;                    // bf16 [total_q, Hq, 128]
+  // workspace and plan
+  int bm, max_tiles, max_items, max_slots, target, min_units, rot_blocks;
+  int32_t *counts, *tile_start;
+  ChunkTile* tiles;
+  ChunkItem* items;
+  uint16_t* qrot;                   // fp16 [H, total_q * gq, 128], in operand order
+  float2* qscale;                   // [H, total_q * gq]: score factor of the fp16 row; q mu^T
+  uint16_t* rv;                     // fp16 operands of R_V
+  float* part;
+};
+struct ChunkPlan {
+  int waves, bm, max_tiles, max_items, max_slots, target, min_units, rot_blocks;
+  size_t off_counts, off_start, off_tiles, off_items, off_qrot, off_qscale, off_rv, off_part, total;
+};
+ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx);
+hipError_t launch_chunk_attention(ChunkArgs a, const ChunkPlan& p, uint8_t* ws, hipStream_t s);
 
 // ---- OptR offline calibration (optr.hip): fp64 throughout
 constexpr int kCalMaxLen = 4096;  // tokens per calibration sequence

@@ -34,6 +34,9 @@ INT2KV_WO_FOLDED = 1
 INT2KV_WO_PREPARED = 2
 INT2KV_WO_PREPARED_FOLDED = 3
 
+INT2KV_ROWS_BF16 = 0
+INT2KV_ROWS_F32 = 1
+
 EXPORTED = (
     "int2kv_last_error", "int2kv_version", "int2kv_pool_bytes", "int2kv_record_bytes", "int2kv_prepare_mu_rot",
     "int2kv_fold_wo",
@@ -44,7 +47,8 @@ EXPORTED = (
     "int2kv_set_decode_tuning", "int2kv_set_decode_events", "int2kv_quantize_append_error",
     "int2kv_output_error_workspace_bytes", "int2kv_output_error", "int2kv_quantize_append_rope",
     "int2kv_optr_workspace_bytes", "int2kv_optr_key_mean", "int2kv_optr_key_loss", "int2kv_optr_value_loss",
-    "int2kv_optr_calibrate",
+    "int2kv_optr_calibrate", "int2kv_rope_axes", "int2kv_read_rows", "int2kv_chunk_attention_workspace_bytes",
+    "int2kv_chunk_attention",
 )
 
 
@@ -79,6 +83,7 @@ def load_library(path: str = LIB_PATH):
                            "(there is no CPU fallback)")
     lib = ctypes.CDLL(path)
     P, I, F, S, Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t
+    L = ctypes.c_int64
     sig = {
         "int2kv_last_error": ([], ctypes.c_char_p),
         "int2kv_version": ([], ctypes.c_char_p),
@@ -115,6 +120,11 @@ def load_library(path: str = LIB_PATH):
         "int2kv_output_error": ([ctypes.POINTER(_Cache), P, I, I, P, I, P, I, P, P, P, P, I, P, I, P, P, P, Z, S],
                                 I),
         "int2kv_set_decode_events": ([P, P], I),
+        "int2kv_rope_axes": ([P, I, L, P, I, L, P, I, ctypes.c_char_p, I, P, I, P, L, P, L, S], I),
+        "int2kv_read_rows": ([ctypes.POINTER(_Cache), P, I, P, P, P, I, P, P, S], I),
+        "int2kv_chunk_attention_workspace_bytes": ([I, I, I, I, I, I], Z),
+        "int2kv_chunk_attention": ([ctypes.POINTER(_Cache), P, L, P, I, I, I, I, P, I, P, I, P, P, P, L, P, L, P, P, P,
+                                    Z, S], I),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -500,6 +510,162 @@ def hadamard_rotation(num_heads: int, device="cuda") -> torch.Tensor:
     scale = torch.tensor(1.0 / math.sqrt(HEAD_DIM), dtype=torch.float32)
     H = torch.where(par == 1, -scale, scale)
     return H[None].expand(num_heads, HEAD_DIM, HEAD_DIM).contiguous().to(device)
+
+
+# ---------------------------------------------------------------------------------------------
+# A chunk's rotary positions, rows read back, attention of a chunk
+
+def _here(*tensors) -> None:
+    """Work goes to the current device's current stream: every tensor has to live there."""
+    cur = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.is_cuda and t.device.index != cur:
+            raise ValueError(f"tensor on {t.device}, but the current device is cuda:{cur}")
+
+
+def _head_rows(t: torch.Tensor, heads: Optional[int], name: str):
+    """(pointer, elements between tokens) of bf16 rows [n, heads, 128] whose tokens may lie apart (a view of a fused
+    projection)."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise TypeError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dtype not in _BF16:
+        raise TypeError(f"{name} has dtype {t.dtype}, expected one of {_BF16}")
+    if t.dim() != 3 or t.shape[2] != HEAD_DIM or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} must be [n, {heads if heads is not None else 'heads'}, 128]")
+    st = t.stride()
+    if t.numel() and (st[2] != 1 or (t.shape[1] > 1 and st[1] != HEAD_DIM)):
+        raise ValueError(f"{name}: the heads of a token must be contiguous")
+    return t.data_ptr(), st[0] if t.shape[0] > 1 else t.shape[1] * HEAD_DIM
+
+
+def rope_axis_table(counts, interleaved: bool = False):
+    """pair_axis of int2kv_rope_axes: counts[a] of the 64 rotary pairs on axis a, the axes one after another, or
+    (interleaved) in turn, each while it has pairs left."""
+    counts = [int(c) for c in counts]
+    if sum(counts) != HEAD_DIM // 2 or min(counts) < 0:
+        raise ValueError("counts must be non-negative and sum to 64")
+    if not interleaved:
+        return bytes(a for a, c in enumerate(counts) for _ in range(c))
+    left, table = counts, []
+    while len(table) < HEAD_DIM // 2:
+        for a in range(len(left)):
+            if left[a]:
+                left[a] -= 1
+                table.append(a)
+    return bytes(table)
+
+
+def int2kv_rope_axes(positions: torch.Tensor, pair_axis, cos_sin: torch.Tensor, q: Optional[torch.Tensor] = None,
+                     k: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                     k_out: Optional[torch.Tensor] = None):
+    """Rotary positions with several axes: positions int32 [axes, n], pair_axis 64 axis numbers (rope_axis_table),
+    cos_sin fp32 [max_pos, 128], q bf16 [n, H_q, 128] and / or k bf16 [n, H_kv, 128] (tokens may lie apart). Returns
+    (q_out, k_out); pass q_out=q to turn in place. A token with a position outside the table keeps its output rows."""
+    if positions.dim() != 2:
+        raise ValueError("positions must be [axes, n]")
+    axes, n = positions.shape
+    pair_axis = bytes(pair_axis)
+    if len(pair_axis) != HEAD_DIM // 2:
+        raise ValueError("pair_axis must hold 64 axes")
+    if cos_sin.dim() != 2 or cos_sin.shape[1] != HEAD_DIM:
+        raise ValueError("cos_sin must be [max_pos, 128]")
+    _here(positions, cos_sin, q, k, q_out, k_out)
+    args = []
+    for x, out, name in ((q, q_out, "q"), (k, k_out, "k")):
+        if x is None:
+            args.append((None, 0, 0, None, 0, None))
+            continue
+        if x.dim() != 3 or x.shape[0] != n:
+            raise ValueError(f"{name} must be [n, heads, 128]")
+        if out is None:
+            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        if out.shape != x.shape:
+            raise ValueError(f"{name}_out must have the shape of {name}")
+        heads = x.shape[1]
+        args.append((*_head_rows(x, heads, name), heads, *_head_rows(out, heads, name + "_out"), out))
+    (qp, qs, hq, qop, qos, q_out), (kp, ks, hk, kop, kos, k_out) = args
+    st = load_library().int2kv_rope_axes(qp, hq, qs, kp, hk, ks, _ptr(positions, _I32, "positions"), axes, pair_axis, n,
+                                         _ptr(cos_sin, _F32, "cos_sin"), cos_sin.shape[0], qop, qos, kop, kos, _stream())
+    _check(st, "int2kv_rope_axes")
+    return q_out, k_out
+
+
+def int2kv_read_rows(cache: Int2KVCache, slot_mapping: torch.Tensor, R_k: Optional[torch.Tensor] = None,
+                     R_v: Optional[torch.Tensor] = None, mu: Optional[torch.Tensor] = None,
+                     k_out: Optional[torch.Tensor] = None, v_out: Optional[torch.Tensor] = None,
+                     dtype: torch.dtype = torch.bfloat16):
+    """Rows of the given slots, (k_out, v_out) [n, H, 128]: in the model's basis with R_k, R_v (and mu), as stored
+    without. Without outputs both are made in `dtype` (zeros where a slot is skipped); with one of them, it alone is
+    written. bf16 or fp32, by the outputs' type."""
+    n, H = slot_mapping.numel(), cache.num_kv_heads
+    if k_out is None and v_out is None:
+        k_out, v_out = torch.zeros((2, n, H, HEAD_DIM), dtype=dtype, device=slot_mapping.device)
+    outs = [t for t in (k_out, v_out) if t is not None]
+    if any(t.shape != (n, H, HEAD_DIM) for t in outs):
+        raise ValueError("k_out / v_out must be [n, num_kv_heads, 128]")
+    if any(t.dtype != outs[0].dtype for t in outs):
+        raise TypeError("k_out and v_out must have one type")
+    for t, name in ((R_k, "R_k"), (R_v, "R_v")):
+        if t is not None and t.shape != (H, HEAD_DIM, HEAD_DIM):
+            raise ValueError(f"{name} must be [num_kv_heads, 128, 128]")
+    if mu is not None and mu.shape != (H, HEAD_DIM):
+        raise ValueError("mu must be [num_kv_heads, 128]")
+    _here(cache.pool, slot_mapping, R_k, R_v, mu, k_out, v_out)
+    f32 = outs[0].dtype == torch.float32
+    kinds = _F32 if f32 else _BF16
+    st = load_library().int2kv_read_rows(
+        cache.desc, _ptr(slot_mapping, _I32, "slot_mapping"), n, _ptr(R_k, _F32, "R_k"), _ptr(R_v, _F32, "R_v"),
+        _ptr(mu, _F32, "mu"), INT2KV_ROWS_F32 if f32 else INT2KV_ROWS_BF16, _ptr(k_out, kinds, "k_out"),
+        _ptr(v_out, kinds, "v_out"), _stream())
+    _check(st, "int2kv_read_rows")
+    return k_out, v_out
+
+
+def int2kv_chunk_attention_workspace_bytes(batch: int, num_q_heads: int, num_kv_heads: int, total_q: int, max_q: int,
+                                           max_ctx: int) -> int:
+    return load_library().int2kv_chunk_attention_workspace_bytes(batch, num_q_heads, num_kv_heads, total_q, max_q, max_ctx)
+
+
+def int2kv_chunk_attention(cache: Int2KVCache, q: torch.Tensor, q_starts: torch.Tensor, max_q: int,
+                           block_table: torch.Tensor, ctx_lens: torch.Tensor, max_ctx: int, R_k: torch.Tensor,
+                           R_v: torch.Tensor, k_new: Optional[torch.Tensor] = None, v_new: Optional[torch.Tensor] = None,
+                           mu: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                           workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the new tokens q bf16 [total, H_q, 128] (sequence b: rows q_starts[b] .. q_starts[b + 1]) over the
+    cache's ctx_lens[b] tokens and, with k_new, v_new (bf16 [total, H_kv, 128]) and mu, the chunk's own tokens so far;
+    without them the cache holds the chunk too. q, k_new, v_new may be views whose tokens lie apart. Returns bf16
+    [total, H_q, 128] (a new `out` is zero in rows outside every sequence)."""
+    total, Hq, H, B = q.shape[0], q.shape[1], cache.num_kv_heads, ctx_lens.numel()
+    if q_starts.numel() != B + 1:
+        raise ValueError("q_starts must hold batch + 1 offsets")
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [batch, max_blocks]")
+    for t, name in ((R_k, "R_k"), (R_v, "R_v")):
+        if t.shape != (H, HEAD_DIM, HEAD_DIM):
+            raise ValueError(f"{name} must be [num_kv_heads, 128, 128]")
+    if mu is not None and mu.shape != (H, HEAD_DIM):
+        raise ValueError("mu must be [num_kv_heads, 128]")
+    _here(cache.pool, q, q_starts, block_table, ctx_lens, R_k, R_v, k_new, v_new, mu, out, workspace)
+    qp, qs = _head_rows(q, Hq, "q")
+    kp, ks = (None, 0) if k_new is None else _head_rows(k_new, H, "k_new")
+    vp, vs = (None, 0) if v_new is None else _head_rows(v_new, H, "v_new")
+    for t, name in ((k_new, "k_new"), (v_new, "v_new")):
+        if t is not None and t.shape[0] != total:
+            raise ValueError(f"{name} must hold the tokens of q")
+    if out is None:
+        out = torch.zeros((total, Hq, HEAD_DIM), dtype=torch.bfloat16, device=q.device)
+    elif out.shape != (total, Hq, HEAD_DIM):
+        raise ValueError("out must be [total, H_q, 128]")
+    if workspace is None:
+        need = int2kv_chunk_attention_workspace_bytes(B, Hq, H, total, max_q, max_ctx)
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+    st = load_library().int2kv_chunk_attention(
+        cache.desc, qp, qs, _ptr(q_starts, _I32, "q_starts"), B, total, max_q, Hq, _ptr(block_table, _I32, "block_table"),
+        block_table.shape[1], _ptr(ctx_lens, _I32, "ctx_lens"), max_ctx, _ptr(R_k, _F32, "R_k"), _ptr(R_v, _F32, "R_v"),
+        kp, ks, vp, vs, _ptr(mu, _F32, "mu"), _ptr(out, _BF16, "out"), _ptr(workspace, (torch.uint8,), "workspace"),
+        workspace.numel(), _stream())
+    _check(st, "int2kv_chunk_attention")
+    return out
 
 
 # ---------------------------------------------------------------------------------------------
