@@ -165,7 +165,8 @@ __device__ void layout_rv(const ChunkArgs& a, int h, int part, int parts) {
 __device__ __forceinline__ int pos_channel(int pos) { return code_channel(pos >> 4, (pos >> 3) & 1, pos & 7); }
 
 // Query rotation: q'^T = R_K^T q^T on the matrix cores, R_K in two bf16 terms (q is exact), a wave per 32 positions, row
-// tiles of 32. q' is held in fp16 times a power of two that brings |q|, which bounds every |q'_c|, to [2^11, 2^12).
+// tiles of 32. q' is held in fp16 with log2(e) / sqrt(128) folded in: what a small q' loses among fp16's subnormals
+// (2^-25 an element) is nothing in a score.
 __device__ void rotate_queries(const ChunkArgs& a, int h, int part, int parts) {
   const int l = threadIdx.x & 63, wave = threadIdx.x >> 6, n = l & 31, hh = l >> 5;
   const float* R = a.R_k + (size_t)h * kHeadDim * kHeadDim;
@@ -192,13 +193,11 @@ __device__ void rotate_queries(const ChunkArgs& a, int h, int part, int parts) {
     cd_f16_t d;
 #pragma unroll
     for (int r = 0; r < 16; ++r) d[r] = 0.0f;
-    float norm = 0.0f, off = 0.0f;
+    float off = 0.0f;
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) {
       d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo[kk], x[kk], d, 0, 0, 0);
       d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi[kk], x[kk], d, 0, 0, 0);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) norm = __builtin_fmaf((float)x[kk][j], (float)x[kk][j], norm);
     }
     if (a.mu && wave == 0) {
       const float* mu = a.mu + (size_t)h * kHeadDim + 8 * hh;
@@ -207,22 +206,17 @@ __device__ void rotate_queries(const ChunkArgs& a, int h, int part, int parts) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) off = __builtin_fmaf((float)x[kk][j], mu[16 * kk + j], off);
     }
-    norm += __shfl_xor(norm, 32);
     off += __shfl_xor(off, 32);
-    // 2^e <= |q| < 2^(e + 1); zero, infinite and NaN rows are left as they are
-    const int e = (int)((__float_as_uint(sqrtf(norm)) >> 23) & 255) - 127;
-    const bool plain = !(norm > 0x1p-100f) || !(norm < 0x1p100f);
-    const float up = plain ? 1.0f : __uint_as_float((uint32_t)(127 + 11 - e) << 23), down = plain ? 1.0f : __uint_as_float((uint32_t)(127 - 11 + e) << 23);
     if (row < rows) {
       uint16_t* o = a.qrot + ((size_t)h * rows + row) * kHeadDim + 32 * wave + 8 * hh;
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         cd_h8_t y;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) y[r] = (_Float16)(d[8 * u + r] * up);
+        for (int r = 0; r < 8; ++r) y[r] = (_Float16)(d[8 * u + r] * kLogit2);
         *reinterpret_cast<cd_h8_t*>(o + 16 * u) = y;
       }
-      if (wave == 0 && hh == 0) a.qscale[(size_t)h * rows + row] = make_float2(down * kLogit2, off * kLogit2);
+      if (wave == 0 && hh == 0) a.qoff[(size_t)h * rows + row] = off * kLogit2;
     }
   }
 }
@@ -241,22 +235,398 @@ __global__ __launch_bounds__(kPrepThreads) void chunk_prep_kernel(ChunkArgs a) {
 
 namespace {
 
-// What RW waves share: a unit's K and V^T operands, two units of them
+constexpr float kMove = kBias + kLazy;
+
+// What the waves share: operands of K (two units) and V^T (three: a unit's values are read after the next unit's barrier)
 struct ChunkLds {
-  cd_h8_t k[2][16][64];  // [buffer][half tm, operand kk][lane]
-  cd_h8_t v[2][16][64];  // [buffer][page, tile][lane]
-  uint32_t bad[2][8];    // per building wave: a value of the unit is not finite (units that need masks)
+  cd_h8_t k[2][16][64];  // [slot][32-token half, operand kk][lane]
+  cd_h8_t v[3][16][64];  // [slot][page, tile][lane]
+};
+
+// Running state of a lane's row. Scores arrive with m taken off (the products start at base = kBias - m); thr is the score
+// that moves m: any score for a row that has seen nothing.
+struct RowState {
+  cd_f16_t O[4];
+  float m, sum, thr;
+};
+
+__device__ __forceinline__ cd_f16_t splat16(float x) {
+  cd_f16_t v;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) v[r] = x;
+  return v;
+}
+// max / sum over a lane and its partner (lane ^ 32)
+__device__ __forceinline__ float pair_max(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float pair_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// fp16 operands: INT2 units. The rotated queries carry log2(e) / sqrt(128), so scores are base-2 logarithms as they are.
+struct HalfOps {
+  typedef cd_h8_t vec;
+  static __device__ __forceinline__ cd_f16_t mfma(const cd_h8_t& a, const vec& b, const cd_f16_t& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ float start(float base) { return base; }
+  static __device__ __forceinline__ float score(float s, float) { return s; }
+  static __device__ __forceinline__ uint32_t pack(float a, float b, float& sum) {
+    typedef float f2 __attribute__((ext_vector_type(2)));
+    const cd_h2_t p = __builtin_convertvector((f2{a, b}), cd_h2_t);
+    sum = __builtin_amdgcn_fdot2(p, cd_h2_t{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+    return __builtin_bit_cast(uint32_t, p);
+  }
+  // the halves of a pair that are not finite
+  static __device__ __forceinline__ uint32_t odd(uint32_t x) {
+    return ((x & 0x7C00u) == 0x7C00u ? 0xFFFFu : 0u) | ((x & 0x7C000000u) == 0x7C000000u ? 0xFFFF0000u : 0u);
+  }
+};
+// bf16 operands: the chunk's own units, whose scores are scaled in fp32
+struct BfOps {
+  typedef cd_b8_t vec;
+  static __device__ __forceinline__ cd_f16_t mfma(const cd_h8_t& a, const vec& b, const cd_f16_t& c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(cd_b8_t, a), b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ float start(float) { return 0.0f; }
+  static __device__ __forceinline__ float score(float s, float base) { return __builtin_fmaf(s, kLogit2, base); }
+  static __device__ __forceinline__ uint32_t pack(float a, float b, float& sum) {
+    sum += a + b;
+    return pack_bf16(a, b);
+  }
+  static __device__ __forceinline__ uint32_t odd(uint32_t x) {
+    return ((x & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
+  }
+};
+
+// The units u0 .. u1 of one kind. Src fetches a unit's rows into registers, makes operands of them (its share of the
+// work-group's), and says which scores count. Steps are 32 tokens: while the matrix cores form the next step's scores the
+// vector ALU turns this step's into probabilities, and while they add this step's values it takes the next step's maximum
+// and makes the operands of the next unit.
+template <class Ops, class Src>
+__device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, const typename Ops::vec (&Q)[8], float off, int u0,
+                                       int u1) {
+  const int l = threadIdx.x & 63;
+  cd_f16_t S, T;
+  float base = kBias - st.m - off;
+  // scores of half tm of the unit in slot kb
+  auto scores = [&](cd_f16_t& X, int kb, int tm) {
+    X = splat16(Ops::start(base));
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) X = Ops::mfma(lds.k[kb][8 * tm + kk][l], Q[kk], X);
+  };
+  // hides what a row does not see and moves m where a score exceeds it by 2^kLazy
+  auto settle = [&](cd_f16_t& X, int u, int tm) {
+    if (src.masked(u)) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) X[i] = src.sees(u, 32 * tm + 8 * (i >> 2) + (i & 3)) ? X[i] : -INFINITY;
+    }
+    float a = fmaxf(X[0], X[1]);
+#pragma unroll
+    for (int i = 2; i < 16; i += 2) a = fmaxf(fmaxf(a, X[i]), X[i + 1]);
+    const float top = Ops::score(pair_max(a), base);
+    const bool move = top > st.thr;
+    if (__any(move)) {
+      const float d = move ? top - kBias : 0.0f;
+      const float f = !move ? 1.0f : st.thr < 0.0f ? 0.0f : __builtin_amdgcn_exp2f(-d);
+      st.m += d;
+      base -= d;
+      st.sum *= f;
+      st.thr = move ? kMove : st.thr;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) st.O[i] *= f;
+      X -= splat16(Ops::start(d));
+    }
+  };
+  // probabilities of a step as operands: page pg of the half takes registers 8 pg .. 8 pg + 7
+  auto soften = [&](const cd_f16_t& X, cd_u4_t (&P)[2]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      P[i >> 2][i & 3] = Ops::pack(__builtin_amdgcn_exp2f(Ops::score(X[2 * i], base)),
+                                   __builtin_amdgcn_exp2f(Ops::score(X[2 * i + 1], base)), st.sum);
+  };
+  auto add = [&](const cd_u4_t (&P)[2], int vb, int tm) {
+#pragma unroll
+    for (int pg = 0; pg < 2; ++pg)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        st.O[i] = Ops::mfma(lds.v[vb][8 * tm + 4 * pg + i][l], __builtin_bit_cast(typename Ops::vec, P[pg]), st.O[i]);
+  };
+
+  src.fetch(u0);
+  src.template build<false>(u0, lds, 0, 0);
+  if (u0 + 1 < u1) src.fetch(u0 + 1);
+  __syncthreads();
+  scores(S, 0, 0);
+  settle(S, u0, 0);
+  int kb = 0, vb = 0;
+  for (int u = u0; u < u1; ++u) {
+    const bool more = u + 1 < u1;
+    const int vn = vb == 2 ? 0 : vb + 1;
+    cd_u4_t P[2];
+    scores(T, kb, 1);
+    soften(S, P);
+    add(P, vb, 0);
+    settle(T, u, 1);
+    if (more) {
+      src.template build<false>(u + 1, lds, kb ^ 1, vn);
+      if (u + 2 < u1) src.fetch(u + 2);
+    }
+    __syncthreads();
+    if (more) scores(S, kb ^ 1, 0);
+    soften(T, P);
+    add(P, vb, 1);
+    if (more) settle(S, u + 1, 0);
+    kb ^= 1;
+    vb = vn;
+  }
+
+  // Values that are not finite, in units that some row of the tile does not see all of, were left out above, where
+  // 0 * inf would have reached rows that do not see them. They are added here, to the rows that do: a token at a time.
+  __syncthreads();
+  uint32_t* flags = reinterpret_cast<uint32_t*>(&lds.k[0][0][0]);
+  const bool mine = __any(src.found != 0);
+  if (l == 0) flags[threadIdx.x >> 6] = mine;
+  __syncthreads();
+  uint32_t found = 0;
+  for (int w = 0; w < (int)(blockDim.x >> 6); ++w) found |= flags[w];
+  if (__builtin_amdgcn_readfirstlane(found)) {
+    for (int u = u0; u < u1; ++u) {
+      src.refetch(u);
+      if (!src.partial(u)) continue;
+      __syncthreads();
+      src.template build<true>(u, lds, 0, 0);
+      __syncthreads();
+      for (int tm = 0; tm < 2; ++tm) {
+        scores(S, 0, tm);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) S[i] = src.sees(u, 32 * tm + 8 * (i >> 2) + (i & 3)) ? S[i] : -INFINITY;
+        cd_u4_t P[2];
+        const float sum = st.sum;
+        soften(S, P);
+        st.sum = sum;
+        for (int t = 0; t < 32; ++t) {
+          const int pg = t >> 4, j = ((t >> 3) & 1) * 4 + (t & 3);
+          const bool lane_has = (l >> 5) == ((t >> 2) & 1), see = src.sees_token(u, 32 * tm + t);
+          auto only = [&](cd_u4_t x) {
+#pragma unroll
+            for (int y = 0; y < 4; ++y) x[y] = lane_has && y == (j >> 1) ? x[y] & (j & 1 ? 0xFFFF0000u : 0xFFFFu) : 0u;
+            return x;
+          };
+          const cd_u4_t p = only(pg ? P[1] : P[0]);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const cd_u4_t v = only(__builtin_bit_cast(cd_u4_t, lds.v[0][8 * tm + 4 * pg + i][l]));
+            const cd_f16_t d = Ops::mfma(__builtin_bit_cast(cd_h8_t, v), __builtin_bit_cast(typename Ops::vec, p), splat16(0.0f));
+#pragma unroll
+            for (int y = 0; y < 16; ++y) st.O[i][y] += see ? d[y] : 0.0f;
+          }
+        }
+      }
+    }
+  }
+}
+
+// The INT2 units of a sequence. Of a unit's operands wave w of NW makes those of KW words of one half's keys, and TV tiles
+// of one page's values.
+template <int NG, int NW>
+struct Int2Source {
+  using Lay = Rec<NG>;
+  static constexpr int KW = 8 / NW, TV = 16 / NW, GV = NG == 4 ? TV : 1;
+  const ChunkArgs& a;
+  const int32_t* table;
+  int h, ctx, pages, lim, lim_min, lim_tile;  // tokens the lane's row sees; the least of the wave's and of the tile's
+  int l, n, hh, half, word0, page, tile0;
+  uint32_t kw[KW], km[NG];
+  cd_u2_t vc[2], vs[GV][2], vz[GV][2];
+  uint32_t ok, ok_prev;                 // pages of the fetched unit and of the one before
+  int pid, fetched;
+  uint32_t found = 0;                   // not zero: a value that is not finite was left out
+
+  __device__ __forceinline__ Int2Source(const ChunkArgs& args, int head, const ChunkTile& t, int w, int limit, int least, int least_tile)
+      : a(args), table(args.table + (size_t)t.b * args.max_blocks), h(head), ctx(t.ctx), pages((t.ctx + kBlock - 1) / kBlock),
+        lim(limit), lim_min(least), lim_tile(least_tile), l(threadIdx.x & 63), n(l & 31), hh(l >> 5), half(w / (NW / 2)), word0(KW * (w % (NW / 2))),
+        page(w / (NW / 4)), tile0(TV * (w % (NW / 4))), ok(0), ok_prev(0), pid(-1), fetched(-1) {}
+  // lane l: the block of page l % 4 of unit u
+  __device__ __forceinline__ int page_id(int u) const {
+    const int p = kUnitPages * u + (l & 3);
+    return p < pages ? table[p] : -1;
+  }
+  __device__ __forceinline__ void fetch(int u) {
+    const int H = a.cv.num_kv_heads, now = fetched == u - 1 && fetched >= 0 ? pid : page_id(u);
+    const bool good = now >= 0 && now < a.cv.num_blocks;
+    ok_prev = ok;
+    ok = (uint32_t)__ballot(good) & 15u;
+    const int id = good ? now : 0;
+    auto record = [&](int p) { return a.cv.pool + ((size_t)(uint32_t)__builtin_amdgcn_readlane(id, p) * H + h) * Lay::kBytes; };
+    const uint8_t* ra = record(2 * half);
+    const uint8_t* rb = record(2 * half + 1);
+    const uint8_t* rk = n < 16 ? ra : rb;
+    const int t = n & 15;
+    const uint32_t* c = reinterpret_cast<const uint32_t*>(rk + kOffKCodes + 32 * t + 16 * hh) + word0;
+#pragma unroll
+    for (int i = 0; i < KW; ++i) kw[i] = c[i];
+    const uint32_t* m = reinterpret_cast<const uint32_t*>(rk + Lay::kOffKMeta + 4 * NG * t);
+#pragma unroll
+    for (int g = 0; g < NG; ++g) km[g] = m[g];
+    const uint8_t* rv = record(page) + 8 * hh;
+    const uint8_t* rm = rv + (NG == 4 ? 32 * tile0 : 0);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      vc[x] = *reinterpret_cast<const cd_u2_t*>(rv + kOffVCodes + 32 * t + 16 * x);
+#pragma unroll
+      for (int g = 0; g < GV; ++g) {
+        vs[g][x] = *reinterpret_cast<const cd_u2_t*>(rm + Lay::kOffVScale + 32 * g + 16 * x);
+        vz[g][x] = *reinterpret_cast<const cd_u2_t*>(rm + Lay::kOffVZero + 32 * g + 16 * x);
+      }
+    }
+    fetched = u;
+    pid = page_id(u + 1);
+  }
+  __device__ __forceinline__ uint32_t pages_of(int u) const { return u == fetched ? ok : ok_prev; }
+  // ODD: of the values only those that are not finite; else, in partial units, only those that are
+  template <bool ODD>
+  __device__ __forceinline__ void build(int u, ChunkLds& lds, int kb, int vb) {
+    cd_h8_t(*k)[64] = lds.k[kb];
+    cd_h8_t(*v)[64] = lds.v[vb];
+    cd_h2_t s[NG], z[NG];
+#pragma unroll
+    for (int g = 0; g < NG; ++g) s[g] = both_lo(km[g]), z[g] = both_hi(km[g]);
+#pragma unroll
+    for (int i = 0; i < KW; ++i) {
+      cd_h8_t x[2];
+      word_operands<NG>(kw[i], s, z, x);
+      k[8 * half + 2 * (word0 + i)][l] = x[0];
+      k[8 * half + 2 * (word0 + i) + 1][l] = x[1];
+    }
+    // pairs of tokens (4 hh, + 1), (+ 2, + 3), (8 + 4 hh, + 1), (+ 2, + 3); tile i's channel 32 i + 16 ph + (n % 16) lies at
+    // bits 2 (2 i + ph) of each half
+    uint32_t word[4], keep[4] = {~0u, ~0u, ~0u, ~0u};
+#pragma unroll
+    for (int x = 0; x < 4; ++x) word[x] = vc[x >> 1][x & 1] >> (2 * (n >> 4) + 4 * tile0);
+    const bool part = ODD || partial(u);
+    if (part) {
+      // tokens that do not exist: their values must not reach the product, where 0 * inf would be NaN
+      int cnt = ctx - (kUnit * u + kBlock * page);
+      cnt = (ok >> page) & 1 ? cnt : 0;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int tb = 8 * (x >> 1) + 4 * hh + 2 * (x & 1);
+        keep[x] = (tb < cnt ? 0xFFFFu : 0u) | (tb + 1 < cnt ? 0xFFFF0000u : 0u);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < TV; ++i) {
+      cd_u4_t f;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const int g = NG == 4 ? i : 0;
+        // (copies: a bit cast of a vector's element takes element 0)
+        const uint32_t sv = vs[g][x >> 1][x & 1], zv = vz[g][x >> 1][x & 1];
+        const cd_h2_t code = i == 0   ? land_codes<0>(word[x])
+                             : i == 1 ? land_codes<4>(word[x])
+                             : i == 2 ? land_codes<8>(word[x])
+                                      : land_codes<4>(word[x] >> 8);
+        const cd_h2_t y = __builtin_elementwise_fma(code, __builtin_bit_cast(cd_h2_t, sv), __builtin_bit_cast(cd_h2_t, zv));
+        f[x] = __builtin_bit_cast(uint32_t, y) & keep[x];
+      }
+      if (part) {
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const uint32_t odd = HalfOps::odd(f[x]);
+          found |= odd;
+          f[x] &= ODD ? odd : ~odd;
+        }
+      }
+      v[4 * page + tile0 + i][l] = __builtin_bit_cast(cd_h8_t, f);
+    }
+  }
+  __device__ __forceinline__ void refetch(int u) {
+    fetched = -1;
+    fetch(u);
+  }
+  __device__ __forceinline__ bool partial(int u) const { return pages_of(u) != 15u || kUnit * (u + 1) > lim_tile; }
+  __device__ __forceinline__ bool masked(int u) const { return pages_of(u) != 15u || kUnit * (u + 1) > lim_min; }
+  // t: token of the unit without the lane half's 4
+  __device__ __forceinline__ bool sees(int u, int t) const { return sees_token(u, t + 4 * hh); }
+  __device__ __forceinline__ bool sees_token(int u, int t) const { return ((pages_of(u) >> (t >> 4)) & 1) && kUnit * u + t < lim; }
+};
+
+// The chunk's own units: bf16 rows. A wave's K operands are 16-byte pieces of its half's rows; its page's values come two
+// channels a load and are paired over tokens, so that tile 2 e + o holds channels 64 e + 2 m + o.
+template <int NW>
+struct OwnSource {
+  static constexpr int KO = 16 / NW, PV = 8 / NW;  // K operands, pairs of V^T tiles
+  const ChunkArgs& a;
+  int n_tok, tok, tok_min, tok_tile;  // the lane's row's token, the wave's and the tile's first
+  int l, n, hh, half, op0, page, pair0;
+  const uint16_t *kb, *vb;
+  cd_u4_t k[KO];
+  uint32_t v[PV][8];
+  uint32_t found = 0;
+
+  __device__ __forceinline__ OwnSource(const ChunkArgs& args, int h, const ChunkTile& t, int w, int row_tok, int least)
+      : a(args), n_tok(t.n), tok(row_tok), tok_min(least), tok_tile(t.row0 / args.gq), l(threadIdx.x & 63), n(l & 31), hh(l >> 5), half(w / (NW / 2)),
+        op0(KO * (w % (NW / 2))), page(w / (NW / 4)), pair0(PV * (w % (NW / 4))),
+        kb(args.k_new + t.start * args.k_stride + (size_t)h * kHeadDim + 8 * hh + 16 * op0),
+        vb(args.v_new + t.start * args.v_stride + (size_t)h * kHeadDim + 2 * n + 64 * pair0) {}
+  __device__ __forceinline__ void fetch(int u) {
+    const uint16_t* row = kb + min(kUnit * u + 32 * half + n, n_tok - 1) * a.k_stride;
+#pragma unroll
+    for (int i = 0; i < KO; ++i) k[i] = *reinterpret_cast<const cd_u4_t*>(row + 16 * i);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const uint16_t* p = vb + min(kUnit * u + kBlock * page + 8 * (j >> 2) + 4 * hh + (j & 3), n_tok - 1) * a.v_stride;
+#pragma unroll
+      for (int x = 0; x < PV; ++x) v[x][j] = *reinterpret_cast<const uint32_t*>(p + 64 * x);
+    }
+  }
+  template <bool ODD>
+  __device__ __forceinline__ void build(int u, ChunkLds& lds, int kbuf, int vbuf) {
+    cd_h8_t(*ko)[64] = lds.k[kbuf];
+    cd_h8_t(*vo)[64] = lds.v[vbuf];
+#pragma unroll
+    for (int i = 0; i < KO; ++i) ko[8 * half + op0 + i][l] = __builtin_bit_cast(cd_h8_t, k[i]);
+    const bool part = ODD || partial(u);
+#pragma unroll
+    for (int x = 0; x < PV; ++x) {
+      uint32_t y[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = v[x][j];
+      if (part) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          y[j] = kUnit * u + kBlock * page + 8 * (j >> 2) + 4 * hh + (j & 3) < n_tok ? y[j] : 0u;
+          const uint32_t odd = BfOps::odd(y[j]);
+          found |= odd;
+          y[j] &= ODD ? odd : ~odd;
+        }
+      }
+      cd_u4_t e, o;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        e[j] = __builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], 0x05040100u);
+        o[j] = __builtin_amdgcn_perm(y[2 * j + 1], y[2 * j], 0x07060302u);
+      }
+      vo[4 * page + 2 * (pair0 + x)][l] = __builtin_bit_cast(cd_h8_t, e);
+      vo[4 * page + 2 * (pair0 + x) + 1][l] = __builtin_bit_cast(cd_h8_t, o);
+    }
+  }
+  __device__ __forceinline__ void refetch(int u) { fetch(u); }
+  __device__ __forceinline__ bool partial(int u) const { return kUnit * u + kUnit - 1 > tok_tile; }
+  __device__ __forceinline__ bool masked(int u) const { return kUnit * u + kUnit - 1 > tok_min; }
+  __device__ __forceinline__ bool sees(int u, int t) const { return kUnit * u + t + 4 * hh <= tok; }
+  __device__ __forceinline__ bool sees_token(int u, int t) const { return kUnit * u + t <= tok; }
 };
 
 }  // namespace
 
-template <int NG, int RW>
-__global__ __launch_bounds__(64 * RW, RW == 8 ? 2 : RW == 4 ? 2 : 1) void chunk_attn_kernel(ChunkArgs a) {
-  using Lay = Rec<NG>;
-  constexpr int KW = 8 / RW;                  // words of a token's half row that a wave makes operands of
-  constexpr int PV = RW >= 4 ? 1 : 4 / RW;    // pages it makes V^T operands of
-  constexpr int TV = RW == 8 ? 2 : 4;         // and tiles of each
-  constexpr int GV = NG == 4 ? TV : 1;        // groups those tiles lie in
+// Work-group: a piece of a tile of 32 NW rows of one KV head; wave w has rows 32 w .. of it.
+template <int NG, int NW>
+__global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
   __shared__ ChunkLds lds;
   const int H = a.cv.num_kv_heads;
   const int h = (int)(blockIdx.x % H), at = (int)(blockIdx.x / H);
@@ -264,429 +634,70 @@ __global__ __launch_bounds__(64 * RW, RW == 8 ? 2 : RW == 4 ? 2 : 1) void chunk_
   const ChunkItem item = a.items[at];
   const ChunkTile tile = a.tiles[item.tile];
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = l & 31, hh = l >> 5;
-  const int rows = tile.n * a.gq, row_w = tile.row0 + 32 * w;  // the wave's first row
-  const int row = row_w + n, rc = min(row, rows - 1), tok = rc / a.gq, head = h * a.gq + rc - tok * a.gq;
-  const int last_tok = min(tile.row0 + a.bm, rows) - 1;
-  const int nI = int2_units(a, Seq{tile.start, tile.n, tile.ctx}, last_tok / a.gq);
-  const int all_rows = a.total_q * a.gq;
-  const size_t grow = (size_t)h * all_rows + (size_t)tile.start * a.gq + rc;
-  const float2 qs = a.qscale[grow];
+  const int rows = tile.n * a.gq, row_w = tile.row0 + 32 * w, tok_w = min(row_w, rows - 1) / a.gq;
+  const int nI = int2_units(a, Seq{tile.start, tile.n, tile.ctx}, (min(tile.row0 + a.bm, rows) - 1) / a.gq);
+  const int row = row_w + n, rc = min(row, rows - 1), tok = rc / a.gq;
+  const size_t grow = (size_t)h * a.total_q * a.gq + (size_t)tile.start * a.gq + rc;
+  RowState st;
+  st.m = 0.0f, st.sum = 0.0f, st.thr = kNone;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) st.O[i] = splat16(0.0f);
 
-  cd_f16_t O[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) O[i][r] = 0.0f;
-  float m = kNone, sum = 0.0f;
-
-  // ---- scores of a unit (S[tm][r]: token 32 tm + 8 (r / 4) + 4 hh + r % 4) to probabilities, moving m, sum and O
-  auto soften = [&](cd_f16_t (&S)[2], float c, float off) {
-    float mx = S[0][0];
-#pragma unroll
-    for (int tm = 0; tm < 2; ++tm)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, S[tm][r]);
-    mx = fmaxf(mx, __shfl_xor(mx, 32));
-    const float top = __builtin_fmaf(mx, c, -off);
-    const bool move = top > m + kLazy;
-    if (__any(move)) {
-      const float to = move ? top : m, f = __builtin_amdgcn_exp2f(m - to);
-      m = to;
-      sum *= f;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) O[i][r] *= f;
-    }
-    const float base = kBias - off - m;
-#pragma unroll
-    for (int tm = 0; tm < 2; ++tm)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        S[tm][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(S[tm][r], c, base));
-        sum += S[tm][r];
-      }
-  };
-
-  // ==== the INT2 units
   const int i1 = min(item.u1, nI);
   if (item.u0 < i1) {
-    const int lim = a.k_new ? tile.ctx : tile.ctx - tile.n + tok + 1;  // tokens this row sees
-    const int lim_min = a.k_new ? tile.ctx : tile.ctx - tile.n + min(row_w, rows - 1) / a.gq + 1;
+    auto limit = [&](int t) { return a.k_new ? tile.ctx : min(tile.ctx, tile.ctx - tile.n + 1 + t); };
     cd_h8_t Q[8];
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk)
-      Q[kk] = *reinterpret_cast<const cd_h8_t*>(a.qrot + grow * kHeadDim + 16 * kk + 8 * hh);
-    const int tmw = RW == 8 ? w >> 2 : RW == 4 ? w >> 1 : w;   // half whose K operands this wave makes
-    const int word0 = RW == 8 ? w & 3 : RW == 4 ? 2 * (w & 1) : 0;
-    const int page0 = RW == 8 ? w >> 1 : RW == 4 ? w : 2 * w;  // its (first) V page
-    const int tile0 = RW == 8 ? 2 * (w & 1) : 0;
-    struct Raw {
-      uint32_t kw[KW], km[NG];
-      cd_u2_t vc[PV][2], vs[PV][GV][2], vz[PV][GV][2];
-      uint32_t ok;  // pages that exist
-    } raw;
-    const int32_t* table = a.table + (size_t)tile.b * a.max_blocks;
-    const int pages = (tile.ctx + kBlock - 1) / kBlock;
-    auto page_id = [&](int u) {  // lane l: the block of page l % 4 of unit u
-      const int p = kUnitPages * u + (l & 3);
-      return p < pages ? table[p] : -1;
-    };
-    auto fetch = [&](int pid) {
-      const bool good = pid >= 0 && pid < a.cv.num_blocks;
-      raw.ok = (uint32_t)__ballot(good) & 15u;
-      const int id = good ? pid : 0;
-      auto record = [&](int p) {
-        return a.cv.pool + ((size_t)(uint32_t)__builtin_amdgcn_readlane(id, p) * H + h) * Lay::kBytes;
-      };
-      const uint8_t* ra = record(2 * tmw);
-      const uint8_t* rb = record(2 * tmw + 1);
-      const uint8_t* rk = n < 16 ? ra : rb;
-      const int t = n & 15;
-      const uint32_t* kw = reinterpret_cast<const uint32_t*>(rk + kOffKCodes + 32 * t + 16 * hh) + word0;
-#pragma unroll
-      for (int i = 0; i < KW; ++i) raw.kw[i] = kw[i];
-      const uint32_t* km = reinterpret_cast<const uint32_t*>(rk + Lay::kOffKMeta + 4 * NG * t);
-#pragma unroll
-      for (int g = 0; g < NG; ++g) raw.km[g] = km[g];
-#pragma unroll
-      for (int p = 0; p < PV; ++p) {
-        const uint8_t* rv = record(page0 + p);
-        const uint8_t* vc = rv + kOffVCodes + 32 * (n & 15) + 8 * hh;
-        const uint8_t* vm = rv + 8 * hh + (NG == 4 ? 32 * tile0 : 0);
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-          raw.vc[p][x] = *reinterpret_cast<const cd_u2_t*>(vc + 16 * x);
-#pragma unroll
-          for (int g = 0; g < GV; ++g) {
-            raw.vs[p][g][x] = *reinterpret_cast<const cd_u2_t*>(vm + Lay::kOffVScale + 32 * g + 16 * x);
-            raw.vz[p][g][x] = *reinterpret_cast<const cd_u2_t*>(vm + Lay::kOffVZero + 32 * g + 16 * x);
-          }
-        }
-      }
-    };
-    // whether some row of the tile may not see all of unit u (the same for every wave)
-    const int lim_tile = a.k_new ? tile.ctx : tile.ctx - tile.n + tile.row0 / a.gq + 1;
-    auto build = [&](int u, int buf) {
-      cd_h2_t s[NG], z[NG];
-#pragma unroll
-      for (int g = 0; g < NG; ++g) s[g] = both_lo(raw.km[g]), z[g] = both_hi(raw.km[g]);
-#pragma unroll
-      for (int i = 0; i < KW; ++i) {
-        cd_h8_t x[2];
-        word_operands<NG>(raw.kw[i], s, z, x);
-        lds.k[buf][8 * tmw + 2 * (word0 + i)][l] = x[0];
-        lds.k[buf][8 * tmw + 2 * (word0 + i) + 1][l] = x[1];
-      }
-      const bool edge = raw.ok != 15u || kUnit * (u + 1) > tile.ctx, masked = edge || kUnit * (u + 1) > lim_tile;
-      bool bad = false;
-#pragma unroll
-      for (int p = 0; p < PV; ++p) {
-        // pairs of tokens (4 hh, + 1), (+ 2, + 3), (8 + 4 hh, + 1), (+ 2, + 3); tile i's channel 32 i + 16 ph + (n % 16)
-        // lies at bits 2 (2 i + ph) of each half
-        uint32_t word[4], keep[4] = {~0u, ~0u, ~0u, ~0u};
-        const int shift = 2 * (n >> 4) + 4 * tile0;
-#pragma unroll
-        for (int x = 0; x < 4; ++x) word[x] = raw.vc[p][x >> 1][x & 1] >> shift;
-        if (edge) {
-          // tokens that do not exist: their values must not reach the product, where 0 * inf would be NaN
-          int cnt = tile.ctx - (kUnit * u + kBlock * (page0 + p));
-          cnt = (raw.ok >> (page0 + p)) & 1 ? cnt : 0;
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const int tb = 8 * (x >> 1) + 4 * hh + 2 * (x & 1);
-            keep[x] = (tb < cnt ? 0xFFFFu : 0u) | (tb + 1 < cnt ? 0xFFFF0000u : 0u);
-          }
-        }
-        auto one = [&](int i, int x, cd_h2_t code) {
-          const int g = NG == 4 ? i : 0;
-          // (copies: a bit cast of a vector's element takes element 0)
-          const uint32_t sv = raw.vs[p][g][x >> 1][x & 1], zv = raw.vz[p][g][x >> 1][x & 1];
-          const cd_h2_t y = __builtin_elementwise_fma(code, __builtin_bit_cast(cd_h2_t, sv), __builtin_bit_cast(cd_h2_t, zv));
-          return __builtin_bit_cast(uint32_t, y) & keep[x];
-        };
-#pragma unroll
-        for (int i = 0; i < TV; ++i) {
-          cd_u4_t f;
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            const cd_h2_t code = i == 0   ? land_codes<0>(word[x])
-                                 : i == 1 ? land_codes<4>(word[x])
-                                 : i == 2 ? land_codes<8>(word[x])
-                                          : land_codes<4>(word[x] >> 8);
-            f[x] = one(i, x, code);
-          }
-          if (masked) {
-#pragma unroll
-            for (int x = 0; x < 4; ++x)
-              bad = bad || (f[x] & 0x7C00u) == 0x7C00u || (f[x] & 0x7C000000u) == 0x7C000000u;
-          }
-          lds.v[buf][4 * (page0 + p) + tile0 + i][l] = __builtin_bit_cast(cd_h8_t, f);
-        }
-      }
-      if (masked) {
-        const bool any = __any(bad);
-        if (l == 0) lds.bad[buf][w] = any;
-      }
-    };
-
-    int u = item.u0;
-    int pid = page_id(u);
-    fetch(pid);
-    pid = page_id(u + 1);
-    build(u, 0);
-    uint32_t ok = raw.ok;
-    int buf = 0;
-    for (; u < i1; ++u, buf ^= 1) {
-      const bool more = u + 1 < i1;
-      if (more) {
-        fetch(pid);
-        pid = page_id(u + 2);
-      }
-      __syncthreads();
-      cd_f16_t S[2];
-#pragma unroll
-      for (int tm = 0; tm < 2; ++tm) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) S[tm][r] = 0.0f;
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk)
-          S[tm] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds.k[buf][8 * tm + kk][l], Q[kk], S[tm], 0, 0, 0);
-      }
-      const bool masked = ok != 15u || kUnit * (u + 1) > lim_min;
-      if (masked) {
-#pragma unroll
-        for (int tm = 0; tm < 2; ++tm)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int t = 32 * tm + 8 * (r >> 2) + 4 * hh + (r & 3);
-            const bool see = ((ok >> (2 * tm + (r >> 3))) & 1) && kUnit * u + t < lim && kUnit * u + t < tile.ctx;
-            S[tm][r] = see ? S[tm][r] : -INFINITY;
-          }
-      }
-      soften(S, qs.x, 0.0f);
-      cd_h8_t P[4];
-#pragma unroll
-      for (int pg = 0; pg < 4; ++pg)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) P[pg][j] = (_Float16)S[pg >> 1][8 * (pg & 1) + j];
-      uint32_t bad = 0;
-      if (ok != 15u || kUnit * (u + 1) > lim_tile) {
-#pragma unroll
-        for (int x = 0; x < RW; ++x) bad |= lds.bad[buf][x];
-      }
-      if (__builtin_amdgcn_readfirstlane(bad)) {
-        // a value that is not finite must not reach rows that do not see its token: one token at a time
-        for (int t = 0; t < kUnit; ++t) {
-          const int pg = t >> 4, j = ((t >> 3) & 1) * 4 + (t & 3), th = (t >> 2) & 1;
-          const bool see = ((ok >> pg) & 1) && kUnit * u + t < lim && kUnit * u + t < tile.ctx;
-          cd_h8_t p1 = P[0];
-#pragma unroll
-          for (int x = 1; x < 4; ++x) p1 = pg == x ? P[x] : p1;
-#pragma unroll
-          for (int x = 0; x < 8; ++x) p1[x] = x == j && hh == th ? p1[x] : (_Float16)0.0f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            cd_h8_t v1 = lds.v[buf][4 * pg + i][l];
-#pragma unroll
-            for (int x = 0; x < 8; ++x) v1[x] = x == j && hh == th ? v1[x] : (_Float16)0.0f;
-            cd_f16_t d;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) d[r] = 0.0f;
-            d = __builtin_amdgcn_mfma_f32_32x32x16_f16(v1, p1, d, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) O[i][r] += see ? d[r] : 0.0f;
-          }
-        }
-      } else {
-#pragma unroll
-        for (int pg = 0; pg < 4; ++pg)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            O[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(lds.v[buf][4 * pg + i][l], P[pg], O[i], 0, 0, 0);
-      }
-      if (more) build(u + 1, buf ^ 1);
-      ok = raw.ok;
-    }
+    for (int kk = 0; kk < 8; ++kk) Q[kk] = *reinterpret_cast<const cd_h8_t*>(a.qrot + grow * kHeadDim + 16 * kk + 8 * hh);
+    Int2Source<NG, NW> src(a, h, tile, w, limit(tok), limit(tok_w), limit(tile.row0 / a.gq));
+    attend<HalfOps>(src, st, lds, Q, 0.0f, item.u0, i1);
 
     // ---- un-rotate: O^T <- R_V O^T, on the normalized sums (within fp16's range, being averages of the values)
     __syncthreads();
     cd_h8_t* rv = &lds.k[0][0][0];
-    const cd_h8_t* src = reinterpret_cast<const cd_h8_t*>(a.rv) + (size_t)h * 2048;
-    for (int x = threadIdx.x; x < 2048; x += 64 * RW) rv[x] = src[x];
+    const cd_h8_t* from = reinterpret_cast<const cd_h8_t*>(a.rv) + (size_t)h * 2048;
+#pragma unroll
+    for (int x = 0; x < 2048 / (64 * NW); ++x) rv[threadIdx.x + 64 * NW * x] = from[threadIdx.x + 64 * NW * x];
     __syncthreads();
-    const float all = sum + __shfl_xor(sum, 32), inv = all == 0.0f ? 0.0f : 1.0f / all;
+    const float all = pair_sum(st.sum), inv = all == 0.0f ? 0.0f : 1.0f / all;
     cd_h8_t B[8];
 #pragma unroll
     for (int op = 0; op < 8; ++op)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) B[op][j] = (_Float16)(O[op >> 1][8 * (op & 1) + j] * inv);
+      for (int j = 0; j < 8; ++j) B[op][j] = (_Float16)(st.O[op >> 1][8 * (op & 1) + j] * inv);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
-      cd_f16_t d;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) d[r] = 0.0f;
+      cd_f16_t d = splat16(0.0f);
 #pragma unroll
       for (int op = 0; op < 8; ++op) d = __builtin_amdgcn_mfma_f32_32x32x16_f16(rv[512 * t + 64 * op + l], B[op], d, 0, 0, 0);
-#pragma unroll
-      for (int r = 0; r < 16; ++r) O[t][r] = d[r] * all;
+      st.O[t] = d * all;
     }
     __syncthreads();
   }
 
-  // ==== the chunk's own tokens, bf16
   const int c0 = max(item.u0 - nI, 0), c1 = item.u1 - nI;
   if (c0 < c1) {
-    constexpr int PP = TV / 2;  // tile pairs: one load of two neighbouring channels serves two tiles
     cd_b8_t Q[8];
-    const uint16_t* qp = a.q + (tile.start + tok) * a.q_stride + (size_t)head * kHeadDim + 8 * hh;
+    const uint16_t* q = a.q + (tile.start + tok) * a.q_stride + (size_t)(h * a.gq + rc - tok * a.gq) * kHeadDim + 8 * hh;
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) Q[kk] = *reinterpret_cast<const cd_b8_t*>(qp + 16 * kk);
-    const int tmw = RW == 8 ? w >> 2 : RW == 4 ? w >> 1 : w;
-    const int op0 = RW == 8 ? 2 * (w & 3) : RW == 4 ? 4 * (w & 1) : 0;
-    const int page0 = RW == 8 ? w >> 1 : RW == 4 ? w : 2 * w;
-    const int pair0 = RW == 8 ? w & 1 : 0;
-    struct Raw {
-      cd_u4_t k[2 * KW];
-      uint32_t v[PV][PP][8];
-    } raw;
-    const uint16_t* kb = a.k_new + tile.start * a.k_stride + (size_t)h * kHeadDim + 8 * hh;
-    const uint16_t* vb = a.v_new + tile.start * a.v_stride + (size_t)h * kHeadDim + 2 * n;
-    auto fetch = [&](int u) {
-      const int t = min(kUnit * u + 32 * tmw + n, tile.n - 1);
-      const uint16_t* kr = kb + t * a.k_stride;
-#pragma unroll
-      for (int i = 0; i < 2 * KW; ++i) raw.k[i] = *reinterpret_cast<const cd_u4_t*>(kr + 16 * (op0 + i));
-#pragma unroll
-      for (int p = 0; p < PV; ++p)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const int tv = min(kUnit * u + kBlock * (page0 + p) + 8 * (j >> 2) + 4 * hh + (j & 3), tile.n - 1);
-          const uint16_t* vr = vb + tv * a.v_stride;
-#pragma unroll
-          for (int x = 0; x < PP; ++x) raw.v[p][x][j] = *reinterpret_cast<const uint32_t*>(vr + 64 * (pair0 + x));
-        }
-    };
-    const int tok_tile = tile.row0 / a.gq, tok_w = min(row_w, rows - 1) / a.gq;  // first tokens of the tile and the wave
-    auto build = [&](int u, int buf) {
-#pragma unroll
-      for (int i = 0; i < 2 * KW; ++i) lds.k[buf][8 * tmw + op0 + i][l] = __builtin_bit_cast(cd_h8_t, raw.k[i]);
-      const bool masked = kUnit * u + kUnit - 1 > tok_tile;
-      bool bad = false;
-#pragma unroll
-      for (int p = 0; p < PV; ++p) {
-        if (masked) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int tv = kUnit * u + kBlock * (page0 + p) + 8 * (j >> 2) + 4 * hh + (j & 3);
-#pragma unroll
-            for (int x = 0; x < PP; ++x) {
-              uint32_t& y = raw.v[p][x][j];
-              y = tv < tile.n ? y : 0u;
-              bad = bad || (y & 0x7F80u) == 0x7F80u || (y & 0x7F800000u) == 0x7F800000u;
-            }
-          }
-        }
-#pragma unroll
-        for (int x = 0; x < PP; ++x) {
-          cd_u4_t e, o;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            e[j] = __builtin_amdgcn_perm(raw.v[p][x][2 * j + 1], raw.v[p][x][2 * j], 0x05040100u);
-            o[j] = __builtin_amdgcn_perm(raw.v[p][x][2 * j + 1], raw.v[p][x][2 * j], 0x07060302u);
-          }
-          lds.v[buf][4 * (page0 + p) + 2 * (pair0 + x)][l] = __builtin_bit_cast(cd_h8_t, e);
-          lds.v[buf][4 * (page0 + p) + 2 * (pair0 + x) + 1][l] = __builtin_bit_cast(cd_h8_t, o);
-        }
-      }
-      if (masked) {
-        const bool any = __any(bad);
-        if (l == 0) lds.bad[buf][w] = any;
-      }
-    };
-    auto operand = [](const cd_h8_t& x) { return __builtin_bit_cast(cd_b8_t, x); };
-    int u = c0, buf = 0;
-    fetch(u);
-    build(u, 0);
-    for (; u < c1; ++u, buf ^= 1) {
-      const bool more = u + 1 < c1;
-      if (more) fetch(u + 1);
-      __syncthreads();
-      cd_f16_t S[2];
-#pragma unroll
-      for (int tm = 0; tm < 2; ++tm) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) S[tm][r] = 0.0f;
-#pragma unroll
-        for (int kk = 0; kk < 8; ++kk)
-          S[tm] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(lds.k[buf][8 * tm + kk][l]), Q[kk], S[tm], 0, 0, 0);
-      }
-      if (kUnit * u + kUnit - 1 > tok_w) {
-#pragma unroll
-        for (int tm = 0; tm < 2; ++tm)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int t = kUnit * u + 32 * tm + 8 * (r >> 2) + 4 * hh + (r & 3);
-            S[tm][r] = t <= tok ? S[tm][r] : -INFINITY;
-          }
-      }
-      soften(S, kLogit2, qs.y);
-      cd_b8_t P[4];
-#pragma unroll
-      for (int pg = 0; pg < 4; ++pg)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) P[pg][j] = (__bf16)S[pg >> 1][8 * (pg & 1) + j];
-      uint32_t bad = 0;
-      if (kUnit * u + kUnit - 1 > tok_tile) {
-#pragma unroll
-        for (int x = 0; x < RW; ++x) bad |= lds.bad[buf][x];
-      }
-      if (__builtin_amdgcn_readfirstlane(bad)) {
-        for (int t = 0; t < kUnit; ++t) {
-          const int pg = t >> 4, j = ((t >> 3) & 1) * 4 + (t & 3), th = (t >> 2) & 1;
-          const bool see = kUnit * u + t <= tok;
-          cd_b8_t p1 = P[0];
-#pragma unroll
-          for (int x = 1; x < 4; ++x) p1 = pg == x ? P[x] : p1;
-#pragma unroll
-          for (int x = 0; x < 8; ++x) p1[x] = x == j && hh == th ? p1[x] : (__bf16)0.0f;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            cd_b8_t v1 = operand(lds.v[buf][4 * pg + i][l]);
-#pragma unroll
-            for (int x = 0; x < 8; ++x) v1[x] = x == j && hh == th ? v1[x] : (__bf16)0.0f;
-            cd_f16_t d;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) d[r] = 0.0f;
-            d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v1, p1, d, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) O[i][r] += see ? d[r] : 0.0f;
-          }
-        }
-      } else {
-#pragma unroll
-        for (int pg = 0; pg < 4; ++pg)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            O[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(operand(lds.v[buf][4 * pg + i][l]), P[pg], O[i], 0, 0, 0);
-      }
-      if (more) build(u + 1, buf ^ 1);
-    }
+    for (int kk = 0; kk < 8; ++kk) Q[kk] = *reinterpret_cast<const cd_b8_t*>(q + 16 * kk);
+    OwnSource<NW> src(a, h, tile, w, tok, tok_w);
+    attend<BfOps>(src, st, lds, Q, a.qoff[grow], c0, c1);
   }
 
-  // ---- results: register 4 u + v of tile 2 a + e is channel 64 a + 16 u + 8 hh + 2 v + e
-  const float all = sum + __shfl_xor(sum, 32);
+  // ---- results: register 4 u + v of tile 2 e + o is channel 64 e + 16 u + 8 hh + 2 v + o
+  const float all = pair_sum(st.sum);
   if (row >= rows) return;
   if (item.slot < 0) {
     const float inv = all == 0.0f ? 0.0f : 1.0f / all;
-    uint16_t* o = a.out + ((size_t)(tile.start + tok) * a.Hq + head) * kHeadDim + 8 * hh;
+    uint16_t* o = a.out + ((size_t)(tile.start + tok) * a.Hq + h * a.gq + row - tok * a.gq) * kHeadDim + 8 * hh;
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         uint32_t y[4];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) y[v] = pack_bf16(O[2 * x][4 * q + v] * inv, O[2 * x + 1][4 * q + v] * inv);
+        for (int v = 0; v < 4; ++v) y[v] = pack_bf16(st.O[2 * x][4 * q + v] * inv, st.O[2 * x + 1][4 * q + v] * inv);
         *reinterpret_cast<uint4*>(o + 64 * x + 16 * q) = make_uint4(y[0], y[1], y[2], y[3]);
       }
   } else {
@@ -699,10 +710,11 @@ __global__ __launch_bounds__(64 * RW, RW == 8 ? 2 : RW == 4 ? 2 : 1) void chunk_
 #pragma unroll
       for (int q = 0; q < 4; ++q) {
         float4* d = reinterpret_cast<float4*>(o + 64 * x + 16 * q);
-        d[0] = make_float4(O[2 * x][4 * q], O[2 * x + 1][4 * q], O[2 * x][4 * q + 1], O[2 * x + 1][4 * q + 1]);
-        d[1] = make_float4(O[2 * x][4 * q + 2], O[2 * x + 1][4 * q + 2], O[2 * x][4 * q + 3], O[2 * x + 1][4 * q + 3]);
+        const cd_f16_t &e = st.O[2 * x], &f = st.O[2 * x + 1];
+        d[0] = make_float4(e[4 * q], f[4 * q], e[4 * q + 1], f[4 * q + 1]);
+        d[1] = make_float4(e[4 * q + 2], f[4 * q + 2], e[4 * q + 3], f[4 * q + 3]);
       }
-    if (hh == 0) reinterpret_cast<float2*>(part + (size_t)a.bm * kHeadDim)[rt] = make_float2(m, all);
+    if (hh == 0) reinterpret_cast<float2*>(part + (size_t)a.bm * kHeadDim)[rt] = make_float2(st.thr < 0.0f ? kNone : st.m, all);
   }
 }
 
@@ -742,14 +754,14 @@ ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_
   ChunkPlan p{};
   const int gq = Hq / H;
   const long long seq_rows = (long long)max_q * gq, rows = (long long)total_q * gq;
-  p.waves = seq_rows <= 64 ? 2 : seq_rows <= 128 ? 4 : 8;
+  p.waves = seq_rows <= 128 ? 4 : 8;
   p.bm = 32 * p.waves;
   const long long per_seq = (seq_rows + p.bm - 1) / p.bm;
   long long tiles = B * per_seq, by_rows = rows / p.bm + B;
   tiles = tiles < by_rows ? tiles : by_rows;
   p.max_tiles = (int)(tiles < 1 ? 1 : tiles);
-  // pieces of all heads: two rounds of the resident work-groups (an eight-wave group per unit, or as many smaller ones)
-  const long long resident = (long long)num_cus() * (8 / p.waves);
+  // pieces of all heads: two rounds of the resident work-groups
+  const long long resident = (long long)num_cus() * (p.waves == 4 ? 2 : 1);
   p.target = 2 * resident;
   p.min_units = 4;
   const long long extra = p.target / H + 1;
@@ -765,7 +777,7 @@ ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_
   p.off_tiles = off, off = up(off + (size_t)p.max_tiles * sizeof(ChunkTile));
   p.off_items = off, off = up(off + (size_t)p.max_items * sizeof(ChunkItem));
   p.off_qrot = off, off = up(off + (size_t)H * rows * kHeadDim * sizeof(uint16_t));
-  p.off_qscale = off, off = up(off + (size_t)H * rows * sizeof(float2));
+  p.off_qoff = off, off = up(off + (size_t)H * rows * sizeof(float));
   p.off_rv = off, off = up(off + (size_t)H * kHeadDim * kHeadDim * sizeof(uint16_t));
   p.off_part = off, off = up(off + (size_t)p.max_slots * H * p.bm * kChunkPartStride * sizeof(float));
   p.total = off;
@@ -774,10 +786,10 @@ ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_
 
 namespace {
 
-template <int NG, int RW>
+template <int NG, int NW>
 hipError_t launch_attn(const ChunkArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((chunk_attn_kernel<NG, RW>), dim3((unsigned)((long long)a.max_items * a.cv.num_kv_heads)), dim3(64 * RW),
-                     0, s, a);
+  hipLaunchKernelGGL((chunk_attn_kernel<NG, NW>), dim3((unsigned)((long long)a.max_items * a.cv.num_kv_heads)), dim3(64 * NW), 0,
+                     s, a);
   return hipGetLastError();
 }
 
@@ -796,7 +808,7 @@ hipError_t launch_chunk_attention(ChunkArgs a, const ChunkPlan& p, uint8_t* ws, 
   a.tiles = reinterpret_cast<ChunkTile*>(ws + p.off_tiles);
   a.items = reinterpret_cast<ChunkItem*>(ws + p.off_items);
   a.qrot = reinterpret_cast<uint16_t*>(ws + p.off_qrot);
-  a.qscale = reinterpret_cast<float2*>(ws + p.off_qscale);
+  a.qoff = reinterpret_cast<float*>(ws + p.off_qoff);
   a.rv = reinterpret_cast<uint16_t*>(ws + p.off_rv);
   a.part = reinterpret_cast<float*>(ws + p.off_part);
   const int H = a.cv.num_kv_heads;
@@ -804,9 +816,9 @@ hipError_t launch_chunk_attention(ChunkArgs a, const ChunkPlan& p, uint8_t* ws, 
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (a.cv.groups == 4)
-    e = p.waves == 8 ? launch_attn<4, 8>(a, s) : p.waves == 4 ? launch_attn<4, 4>(a, s) : launch_attn<4, 2>(a, s);
+    e = p.waves == 8 ? launch_attn<4, 8>(a, s) : launch_attn<4, 4>(a, s);
   else
-    e = p.waves == 8 ? launch_attn<1, 8>(a, s) : p.waves == 4 ? launch_attn<1, 4>(a, s) : launch_attn<1, 2>(a, s);
+    e = p.waves == 8 ? launch_attn<1, 8>(a, s) : launch_attn<1, 4>(a, s);
   if (e != hipSuccess) return e;
   if (p.max_slots > 1) {
     hipLaunchKernelGGL(chunk_merge_kernel, dim3(p.max_tiles, H, p.bm / 16), dim3(256), 0, s, a);

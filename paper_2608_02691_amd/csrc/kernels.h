@@ -215,13 +215,13 @@ struct ChunkArgs {
   ChunkTile* tiles;
   ChunkItem* items;
   uint16_t* qrot;                   // fp16 [H, total_q * gq, 128], in operand order
-  float2* qscale;                   // [H, total_q * gq]: score factor of the fp16 row; q mu^T
+  float* qoff;                      // [H, total_q * gq]: q mu^T in the scores' unit
   uint16_t* rv;                     // fp16 operands of R_V
   float* part;
 };
 struct ChunkPlan {
   int waves, bm, max_tiles, max_items, max_slots, target, min_units, rot_blocks;
-  size_t off_counts, off_start, off_tiles, off_items, off_qrot, off_qscale, off_rv, off_part, total;
+  size_t off_counts, off_start, off_tiles, off_items, off_qrot, off_qoff, off_rv, off_part, total;
 };
 ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx);
 hipError_t launch_chunk_attention(ChunkArgs a, const ChunkPlan& p, uint8_t* ws, hipStream_t s);
