@@ -14,41 +14,13 @@
 // lane-local but for one exchange of halves, the rescaling is one factor per lane, and the probabilities are the second
 // product's B operand as they lie (its k order is the order of S^T's rows in a lane; V^T is laid out to match). INT2 codes
 // become fp16 operands once per work-group and unit and are shared through LDS in operand order.
-#include "codes.h"
-#include "common.h"
-#include "kernels.h"
+#include "chunk_core.h"
 
 namespace int2kv {
 
 namespace {
 
-constexpr int kUnit = 64;                     // tokens of a unit: two 32-token halves, four pages
-constexpr int kUnitPages = kUnit / kBlock;
-constexpr float kLogit2 = 1.4426950408889634f * 0.08838834764831845f;  // log2(e) / sqrt(128)
-constexpr float kLazy = 8.0f;   // the running maximum moves when a score exceeds it by 2^8
-constexpr float kBias = 7.0f;   // probabilities are held times 2^7: the largest is below 2^15, and fp16's normal range
-                                // reaches 2^-21 below the maximum
-constexpr float kNone = -1.0e30f;  // running maximum of a row that has seen nothing
 constexpr int kPrepThreads = 256;
-
-struct Seq {
-  int start, n, ctx;
-};
-__device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int b) {
-  Seq s;
-  s.start = min(max(a.starts[b], 0), a.total_q);
-  const int end = min(max(a.starts[b + 1], 0), a.total_q);
-  s.n = min(max(end - s.start, 0), a.max_q);
-  const long long room = (long long)a.max_blocks * kBlock;
-  s.ctx = min(max(a.lens[b], 0), (int)(room < a.max_ctx ? room : a.max_ctx));
-  return s;
-}
-// Units of a tile whose last new token is i: INT2 units, then units of the chunk's own tokens
-__device__ __forceinline__ int int2_units(const ChunkArgs& a, const Seq& s, int i) {
-  const int lim = a.k_new ? s.ctx : min(s.ctx, max(0, s.ctx - s.n + i + 1));
-  return (lim + kUnit - 1) / kUnit;
-}
-__device__ __forceinline__ int own_units(const ChunkArgs& a, int i) { return a.k_new ? i / kUnit + 1 : 0; }
 
 // Inclusive sum over the block; total to every thread. tmp: a word per wave and one more.
 __device__ __forceinline__ int block_scan(int x, int* tmp, int& total) {
@@ -235,8 +207,6 @@ __global__ __launch_bounds__(kPrepThreads) void chunk_prep_kernel(ChunkArgs a) {
 
 namespace {
 
-constexpr float kMove = kBias + kLazy;
-
 // What the waves share: operands of K (two units) and V^T (three: a unit's values are read after the next unit's barrier)
 struct ChunkLds {
   cd_h8_t k[2][16][64];  // [slot][32-token half, operand kk][lane]
@@ -248,58 +218,6 @@ struct ChunkLds {
 struct RowState {
   cd_f16_t O[4];
   float m, sum, thr;
-};
-
-__device__ __forceinline__ cd_f16_t splat16(float x) {
-  cd_f16_t v;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) v[r] = x;
-  return v;
-}
-// max / sum over a lane and its partner (lane ^ 32)
-__device__ __forceinline__ float pair_max(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
-__device__ __forceinline__ float pair_sum(float x) {
-  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
-}
-
-// fp16 operands: INT2 units. The rotated queries carry log2(e) / sqrt(128), so scores are base-2 logarithms as they are.
-struct HalfOps {
-  typedef cd_h8_t vec;
-  static __device__ __forceinline__ cd_f16_t mfma(const cd_h8_t& a, const vec& b, const cd_f16_t& c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
-  }
-  static __device__ __forceinline__ float start(float base) { return base; }
-  static __device__ __forceinline__ float score(float s, float) { return s; }
-  static __device__ __forceinline__ uint32_t pack(float a, float b, float& sum) {
-    typedef float f2 __attribute__((ext_vector_type(2)));
-    const cd_h2_t p = __builtin_convertvector((f2{a, b}), cd_h2_t);
-    sum = __builtin_amdgcn_fdot2(p, cd_h2_t{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
-    return __builtin_bit_cast(uint32_t, p);
-  }
-  // the halves of a pair that are not finite
-  static __device__ __forceinline__ uint32_t odd(uint32_t x) {
-    return ((x & 0x7C00u) == 0x7C00u ? 0xFFFFu : 0u) | ((x & 0x7C000000u) == 0x7C000000u ? 0xFFFF0000u : 0u);
-  }
-};
-// bf16 operands: the chunk's own units, whose scores are scaled in fp32
-struct BfOps {
-  typedef cd_b8_t vec;
-  static __device__ __forceinline__ cd_f16_t mfma(const cd_h8_t& a, const vec& b, const cd_f16_t& c) {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(cd_b8_t, a), b, c, 0, 0, 0);
-  }
-  static __device__ __forceinline__ float start(float) { return 0.0f; }
-  static __device__ __forceinline__ float score(float s, float base) { return __builtin_fmaf(s, kLogit2, base); }
-  static __device__ __forceinline__ uint32_t pack(float a, float b, float& sum) {
-    sum += a + b;
-    return pack_bf16(a, b);
-  }
-  static __device__ __forceinline__ uint32_t odd(uint32_t x) {
-    return ((x & 0x7F80u) == 0x7F80u ? 0xFFFFu : 0u) | ((x & 0x7F800000u) == 0x7F800000u ? 0xFFFF0000u : 0u);
-  }
 };
 
 // The units u0 .. u1 of one kind. Src fetches a unit's rows into registers, makes operands of them (its share of the
@@ -318,35 +236,13 @@ __device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, co
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) X = Ops::mfma(lds.k[kb][8 * tm + kk][l], Q[kk], X);
   };
-  // hides what a row does not see and moves m where a score exceeds it by 2^kLazy
-  auto settle = [&](cd_f16_t& X, int u, int tm) {
+  // hides what a row does not see
+  auto rest = [&](cd_f16_t& X, int u, int tm) {
     if (src.masked(u)) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) X[i] = src.sees(u, 32 * tm + 8 * (i >> 2) + (i & 3)) ? X[i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) X[i] = src.sees(u, 32 * tm + reg_token(i)) ? X[i] : -INFINITY;
     }
-    float a = fmaxf(X[0], X[1]);
-#pragma unroll
-    for (int i = 2; i < 16; i += 2) a = fmaxf(fmaxf(a, X[i]), X[i + 1]);
-    const float top = Ops::score(pair_max(a), base);
-    const bool move = top > st.thr;
-    if (__any(move)) {
-      const float d = move ? top - kBias : 0.0f;
-      const float f = !move ? 1.0f : st.thr < 0.0f ? 0.0f : __builtin_amdgcn_exp2f(-d);
-      st.m += d;
-      base -= d;
-      st.sum *= f;
-      st.thr = move ? kMove : st.thr;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) st.O[i] *= f;
-      X -= splat16(Ops::start(d));
-    }
-  };
-  // probabilities of a step as operands: page pg of the half takes registers 8 pg .. 8 pg + 7
-  auto soften = [&](const cd_f16_t& X, cd_u4_t (&P)[2]) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      P[i >> 2][i & 3] = Ops::pack(__builtin_amdgcn_exp2f(Ops::score(X[2 * i], base)),
-                                   __builtin_amdgcn_exp2f(Ops::score(X[2 * i + 1], base)), st.sum);
+    settle<Ops>(X, base, st.m, st.sum, st.thr, st.O);
   };
   auto add = [&](const cd_u4_t (&P)[2], int vb, int tm) {
 #pragma unroll
@@ -361,25 +257,25 @@ __device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, co
   if (u0 + 1 < u1) src.fetch(u0 + 1);
   __syncthreads();
   scores(S, 0, 0);
-  settle(S, u0, 0);
+  rest(S, u0, 0);
   int kb = 0, vb = 0;
   for (int u = u0; u < u1; ++u) {
     const bool more = u + 1 < u1;
     const int vn = vb == 2 ? 0 : vb + 1;
     cd_u4_t P[2];
     scores(T, kb, 1);
-    soften(S, P);
+    soften<Ops>(S, base, st.sum, P);
     add(P, vb, 0);
-    settle(T, u, 1);
+    rest(T, u, 1);
     if (more) {
       src.template build<false>(u + 1, lds, kb ^ 1, vn);
       if (u + 2 < u1) src.fetch(u + 2);
     }
     __syncthreads();
     if (more) scores(S, kb ^ 1, 0);
-    soften(T, P);
+    soften<Ops>(T, base, st.sum, P);
     add(P, vb, 1);
-    if (more) settle(S, u + 1, 0);
+    if (more) rest(S, u + 1, 0);
     kb ^= 1;
     vb = vn;
   }
@@ -403,23 +299,17 @@ __device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, co
       for (int tm = 0; tm < 2; ++tm) {
         scores(S, 0, tm);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) S[i] = src.sees(u, 32 * tm + 8 * (i >> 2) + (i & 3)) ? S[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) S[i] = src.sees(u, 32 * tm + reg_token(i)) ? S[i] : -INFINITY;
         cd_u4_t P[2];
-        const float sum = st.sum;
-        soften(S, P);
-        st.sum = sum;
+        float sum = 0.0f;  // already counted
+        soften<Ops>(S, base, sum, P);
         for (int t = 0; t < 32; ++t) {
-          const int pg = t >> 4, j = ((t >> 3) & 1) * 4 + (t & 3);
-          const bool lane_has = (l >> 5) == ((t >> 2) & 1), see = src.sees_token(u, 32 * tm + t);
-          auto only = [&](cd_u4_t x) {
-#pragma unroll
-            for (int y = 0; y < 4; ++y) x[y] = lane_has && y == (j >> 1) ? x[y] & (j & 1 ? 0xFFFF0000u : 0xFFFFu) : 0u;
-            return x;
-          };
-          const cd_u4_t p = only(pg ? P[1] : P[0]);
+          const int pg = t >> 4;
+          const bool see = src.sees_token(u, 32 * tm + t);
+          const cd_u4_t p = only_token(pg ? P[1] : P[0], t);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            const cd_u4_t v = only(__builtin_bit_cast(cd_u4_t, lds.v[0][8 * tm + 4 * pg + i][l]));
+            const cd_u4_t v = only_token(__builtin_bit_cast(cd_u4_t, lds.v[0][8 * tm + 4 * pg + i][l]), t);
             const cd_f16_t d = Ops::mfma(__builtin_bit_cast(cd_h8_t, v), __builtin_bit_cast(typename Ops::vec, p), splat16(0.0f));
 #pragma unroll
             for (int y = 0; y < 16; ++y) st.O[i][y] += see ? d[y] : 0.0f;
@@ -441,7 +331,7 @@ struct Int2Source {
   int h, ctx, pages, lim, lim_min, lim_tile;  // tokens the lane's row sees; the least of the wave's and of the tile's
   int l, n, hh, half, word0, page, tile0;
   uint32_t kw[KW], km[NG];
-  cd_u2_t vc[2], vs[GV][2], vz[GV][2];
+  cd_u4_t vc, vs[GV], vz[GV];
   uint32_t ok, ok_prev;                 // pages of the fetched unit and of the one before
   int pid, fetched;
   uint32_t found = 0;                   // not zero: a value that is not finite was left out
@@ -465,23 +355,20 @@ struct Int2Source {
     const uint8_t* ra = record(2 * half);
     const uint8_t* rb = record(2 * half + 1);
     const uint8_t* rk = n < 16 ? ra : rb;
-    const int t = n & 15;
+    const int t = row_token(n & 15);
     const uint32_t* c = reinterpret_cast<const uint32_t*>(rk + kOffKCodes + 32 * t + 16 * hh) + word0;
 #pragma unroll
     for (int i = 0; i < KW; ++i) kw[i] = c[i];
     const uint32_t* m = reinterpret_cast<const uint32_t*>(rk + Lay::kOffKMeta + 4 * NG * t);
 #pragma unroll
     for (int g = 0; g < NG; ++g) km[g] = m[g];
-    const uint8_t* rv = record(page) + 8 * hh;
+    const uint8_t* rv = record(page) + 16 * hh;
     const uint8_t* rm = rv + (NG == 4 ? 32 * tile0 : 0);
+    vc = *reinterpret_cast<const cd_u4_t*>(rv + kOffVCodes + 32 * (n & 15));
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      vc[x] = *reinterpret_cast<const cd_u2_t*>(rv + kOffVCodes + 32 * t + 16 * x);
-#pragma unroll
-      for (int g = 0; g < GV; ++g) {
-        vs[g][x] = *reinterpret_cast<const cd_u2_t*>(rm + Lay::kOffVScale + 32 * g + 16 * x);
-        vz[g][x] = *reinterpret_cast<const cd_u2_t*>(rm + Lay::kOffVZero + 32 * g + 16 * x);
-      }
+    for (int g = 0; g < GV; ++g) {
+      vs[g] = *reinterpret_cast<const cd_u4_t*>(rm + Lay::kOffVScale + 32 * g);
+      vz[g] = *reinterpret_cast<const cd_u4_t*>(rm + Lay::kOffVZero + 32 * g);
     }
     fetched = u;
     pid = page_id(u + 1);
@@ -502,11 +389,10 @@ struct Int2Source {
       k[8 * half + 2 * (word0 + i)][l] = x[0];
       k[8 * half + 2 * (word0 + i) + 1][l] = x[1];
     }
-    // pairs of tokens (4 hh, + 1), (+ 2, + 3), (8 + 4 hh, + 1), (+ 2, + 3); tile i's channel 32 i + 16 ph + (n % 16) lies at
-    // bits 2 (2 i + ph) of each half
+    // pairs of tokens 8 hh + 2 x, + 1; tile i's channel 32 i + 16 ph + (n % 16) lies at bits 2 (2 i + ph) of each half
     uint32_t word[4], keep[4] = {~0u, ~0u, ~0u, ~0u};
 #pragma unroll
-    for (int x = 0; x < 4; ++x) word[x] = vc[x >> 1][x & 1] >> (2 * (n >> 4) + 4 * tile0);
+    for (int x = 0; x < 4; ++x) word[x] = vc[x] >> (2 * (n >> 4) + 4 * tile0);
     const bool part = ODD || partial(u);
     if (part) {
       // tokens that do not exist: their values must not reach the product, where 0 * inf would be NaN
@@ -514,7 +400,7 @@ struct Int2Source {
       cnt = (ok >> page) & 1 ? cnt : 0;
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        const int tb = 8 * (x >> 1) + 4 * hh + 2 * (x & 1);
+        const int tb = 8 * hh + 2 * x;
         keep[x] = (tb < cnt ? 0xFFFFu : 0u) | (tb + 1 < cnt ? 0xFFFF0000u : 0u);
       }
     }
@@ -525,7 +411,7 @@ struct Int2Source {
       for (int x = 0; x < 4; ++x) {
         const int g = NG == 4 ? i : 0;
         // (copies: a bit cast of a vector's element takes element 0)
-        const uint32_t sv = vs[g][x >> 1][x & 1], zv = vz[g][x >> 1][x & 1];
+        const uint32_t sv = vs[g][x], zv = vz[g][x];
         const cd_h2_t code = i == 0   ? land_codes<0>(word[x])
                              : i == 1 ? land_codes<4>(word[x])
                              : i == 2 ? land_codes<8>(word[x])
@@ -551,7 +437,7 @@ struct Int2Source {
   __device__ __forceinline__ bool partial(int u) const { return pages_of(u) != 15u || kUnit * (u + 1) > lim_tile; }
   __device__ __forceinline__ bool masked(int u) const { return pages_of(u) != 15u || kUnit * (u + 1) > lim_min; }
   // t: token of the unit without the lane half's 4
-  __device__ __forceinline__ bool sees(int u, int t) const { return sees_token(u, t + 4 * hh); }
+  __device__ __forceinline__ bool sees(int u, int t) const { return sees_token(u, t + 8 * hh); }
   __device__ __forceinline__ bool sees_token(int u, int t) const { return ((pages_of(u) >> (t >> 4)) & 1) && kUnit * u + t < lim; }
 };
 
@@ -574,12 +460,12 @@ struct OwnSource {
         kb(args.k_new + t.start * args.k_stride + (size_t)h * kHeadDim + 8 * hh + 16 * op0),
         vb(args.v_new + t.start * args.v_stride + (size_t)h * kHeadDim + 2 * n + 64 * pair0) {}
   __device__ __forceinline__ void fetch(int u) {
-    const uint16_t* row = kb + min(kUnit * u + 32 * half + n, n_tok - 1) * a.k_stride;
+    const uint16_t* row = kb + min(kUnit * u + 32 * half + (n & 16) + row_token(n & 15), n_tok - 1) * a.k_stride;
 #pragma unroll
     for (int i = 0; i < KO; ++i) k[i] = *reinterpret_cast<const cd_u4_t*>(row + 16 * i);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      const uint16_t* p = vb + min(kUnit * u + kBlock * page + 8 * (j >> 2) + 4 * hh + (j & 3), n_tok - 1) * a.v_stride;
+      const uint16_t* p = vb + min(kUnit * u + kBlock * page + 8 * hh + j, n_tok - 1) * a.v_stride;
 #pragma unroll
       for (int x = 0; x < PV; ++x) v[x][j] = *reinterpret_cast<const uint32_t*>(p + 64 * x);
     }
@@ -599,7 +485,7 @@ struct OwnSource {
       if (part) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          y[j] = kUnit * u + kBlock * page + 8 * (j >> 2) + 4 * hh + (j & 3) < n_tok ? y[j] : 0u;
+          y[j] = kUnit * u + kBlock * page + 8 * hh + j < n_tok ? y[j] : 0u;
           const uint32_t odd = BfOps::odd(y[j]);
           found |= odd;
           y[j] &= ODD ? odd : ~odd;
@@ -618,7 +504,7 @@ struct OwnSource {
   __device__ __forceinline__ void refetch(int u) { fetch(u); }
   __device__ __forceinline__ bool partial(int u) const { return kUnit * u + kUnit - 1 > tok_tile; }
   __device__ __forceinline__ bool masked(int u) const { return kUnit * u + kUnit - 1 > tok_min; }
-  __device__ __forceinline__ bool sees(int u, int t) const { return kUnit * u + t + 4 * hh <= tok; }
+  __device__ __forceinline__ bool sees(int u, int t) const { return kUnit * u + t + 8 * hh <= tok; }
   __device__ __forceinline__ bool sees_token(int u, int t) const { return kUnit * u + t <= tok; }
 };
 
@@ -754,14 +640,14 @@ ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_
   ChunkPlan p{};
   const int gq = Hq / H;
   const long long seq_rows = (long long)max_q * gq, rows = (long long)total_q * gq;
-  p.waves = seq_rows <= 128 ? 4 : 8;
+  p.waves = seq_rows <= 64 ? 1 : seq_rows <= 128 ? 4 : 8;
   p.bm = 32 * p.waves;
   const long long per_seq = (seq_rows + p.bm - 1) / p.bm;
   long long tiles = B * per_seq, by_rows = rows / p.bm + B;
   tiles = tiles < by_rows ? tiles : by_rows;
   p.max_tiles = (int)(tiles < 1 ? 1 : tiles);
   // pieces of all heads: two rounds of the resident work-groups
-  const long long resident = (long long)num_cus() * (p.waves == 4 ? 2 : 1);
+  const long long resident = (long long)num_cus() * (p.waves <= 4 ? 2 : 1);
   p.target = 2 * resident;
   p.min_units = 4;
   const long long extra = p.target / H + 1;
@@ -815,7 +701,9 @@ hipError_t launch_chunk_attention(ChunkArgs a, const ChunkPlan& p, uint8_t* ws, 
   hipLaunchKernelGGL(chunk_prep_kernel, dim3(1 + H + H * p.rot_blocks), dim3(kPrepThreads), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (a.cv.groups == 4)
+  if (p.waves == 1)
+    e = launch_chunk_few(a, s);
+  else if (a.cv.groups == 4)
     e = p.waves == 8 ? launch_attn<4, 8>(a, s) : launch_attn<4, 4>(a, s);
   else
     e = p.waves == 8 ? launch_attn<1, 8>(a, s) : launch_attn<1, 4>(a, s);

@@ -1,0 +1,363 @@
+// Attention of few new tokens per sequence (int2kv_chunk_attention, at most 32 query rows a tile): drafted tokens, short
+// turns. Bound by the cache's bytes and, close behind, by the vector ALU that makes operands of its codes, so nothing is
+// shared and nothing waited for: the four waves of a work-group hold the same 32 rows and take different 32-token steps of
+// the context, each with its own records on their way to LDS (LDS-DMA, kAhead steps ahead) and its own softmax. Codes
+// become matrix operands in the registers they are used from. At the end the four partial results meet in LDS, each wave
+// un-rotates the 32 channels of its tile and adds the chunk's own bf16 tokens to them.
+#include <type_traits>
+
+#include "append_core.h"
+#include "chunk_core.h"
+
+namespace int2kv {
+
+namespace {
+
+constexpr int kFewWaves = 4;
+constexpr int kStep = 32;                 // tokens of a step: two pages
+constexpr int kStages = 4, kAhead = kStages - 1;
+constexpr int kStageBytes = 3072;         // codes of two pages, then 512 bytes each of their parameters
+
+struct FewLds {
+  union {
+    uint8_t stage[kFewWaves][kStages][kStageBytes];
+    float o[kFewWaves][4][16][64];        // [wave][tile][register][lane]
+  };
+  cd_h8_t b[8][64];                       // normalized sums as operands of the un-rotation
+  float ml[kFewWaves][2][32];
+};
+
+}  // namespace
+
+template <int NG>
+__global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs a) {
+  using Lay = Rec<NG>;
+  __shared__ __align__(16) FewLds lds;
+  const int H = a.cv.num_kv_heads;
+  const int h = (int)(blockIdx.x % H), at = (int)(blockIdx.x / H);
+  if (at >= a.counts[0]) return;
+  const ChunkItem item = a.items[at];
+  const ChunkTile tile = a.tiles[item.tile];
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = l & 31, hh = l >> 5;
+  const int rows = tile.n * a.gq, row = tile.row0 + n, rc = min(row, rows - 1), tok = rc / a.gq, tok_tile = tile.row0 / a.gq;
+  const int nI = int2_units(a, Seq{tile.start, tile.n, tile.ctx}, (min(tile.row0 + a.bm, rows) - 1) / a.gq);
+  const size_t grow = (size_t)h * a.total_q * a.gq + (size_t)tile.start * a.gq + rc;
+  auto limit = [&](int t) { return a.k_new ? tile.ctx : min(tile.ctx, tile.ctx - tile.n + 1 + t); };
+  const int lim = limit(tok), lim_tile = limit(tok_tile);  // tokens the row sees, the least of the tile's
+
+  float m = 0.0f, sum = 0.0f, thr = kNone;
+  {
+    cd_f16_t O[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) O[i] = splat16(0.0f);
+    // ---- the wave's steps: a quarter of the piece's
+    const int pages = (tile.ctx + kBlock - 1) / kBlock;
+    const int p0 = kUnitPages * item.u0 / 2, p1 = min(kUnitPages * min(item.u1, nI), (pages + 1) & ~1) / 2;
+    const int steps = max(p1 - p0, 0), s0 = p0 + steps * w / kFewWaves, s1 = p0 + steps * (w + 1) / kFewWaves;
+    if (s0 < s1) {
+      cd_h8_t Q[8];
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) Q[kk] = *reinterpret_cast<const cd_h8_t*>(a.qrot + grow * kHeadDim + 16 * kk + 8 * hh);
+      const int32_t* table = a.table + (size_t)tile.b * a.max_blocks;
+      // lane l: the block of page 2 list0 + l, read for 32 steps at a time
+      int list0 = 0, list = 0;
+      auto load_list = [&](int s) {
+        list0 = s;
+        const int p = 2 * s + l;
+        list = p < pages ? table[p] : -1;
+      };
+      auto good = [&](int id) { return id >= 0 && id < a.cv.num_blocks; };
+      auto block = [&](int s, int x) { return __builtin_amdgcn_readlane(list, 2 * (s - list0) + x); };
+      const uint32_t stage0 = (uint32_t)(uintptr_t)(&lds.stage[w][0][0]);
+      auto issue = [&](int s) {  // the step's two records on their way to its stage
+        const uint8_t* r[2];
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+          const int id = block(s, x);
+          r[x] = a.cv.pool + ((size_t)(uint32_t)(good(id) ? id : 0) * H + h) * Lay::kBytes;
+        }
+        const uint32_t to = stage0 + (uint32_t)(s & (kStages - 1)) * kStageBytes;
+        ap_dma16(r[0] + 16 * l, to);
+        ap_dma16(r[1] + 16 * l, to + 1024);
+        // a page's 128 NG bytes of parameters; lanes past them read the last 16 again
+        ap_dma16((l < 32 ? r[0] : r[1]) + 1024 + min(16 * (l & 31), 128 * NG - 16), to + 2048);
+      };
+      const int tA = row_token(n & 15), pgA = n >> 4;  // the token whose keys this lane's A rows are
+      float base = kBias;
+      uint32_t found = 0;
+      auto whole = [&](int s) { return good(block(s, 0)) && good(block(s, 1)) && kStep * (s + 1) <= lim_tile; };
+      // One step: scores, probabilities, values. PART: some row does not see all of it. SECOND: only the values that are not
+      // finite, for the rows that see them
+      auto take = [&](int s, auto part_c, auto second_c) {
+        constexpr bool part = decltype(part_c)::value, second = decltype(second_c)::value;
+        const uint8_t* st = lds.stage[w][s & (kStages - 1)];
+        const cd_u4_t kc = *reinterpret_cast<const cd_u4_t*>(st + 1024 * pgA + 32 * tA + 16 * hh);
+        uint32_t km[NG];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) km[g] = *reinterpret_cast<const uint32_t*>(st + 2048 + 512 * pgA + 4 * NG * tA + 4 * g);
+        cd_h2_t ks[NG], kz[NG];
+#pragma unroll
+        for (int g = 0; g < NG; ++g) ks[g] = both_lo(km[g]), kz[g] = both_hi(km[g]);
+        cd_f16_t S = splat16(base);
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          cd_h8_t k[2];
+          word_operands<NG>(kc[x], ks, kz, k);
+          S = HalfOps::mfma(k[0], Q[2 * x], S);
+          S = HalfOps::mfma(k[1], Q[2 * x + 1], S);
+        }
+        const uint32_t ok = !part ? 3u : (good(block(s, 0)) ? 1u : 0u) | (good(block(s, 1)) ? 2u : 0u);
+        if constexpr (part) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            S[i] = ((ok >> (i >> 3)) & 1) && kStep * s + reg_token(i) + 8 * hh < lim ? S[i] : -INFINITY;
+        }
+        cd_u4_t P[2];
+        if constexpr (!second) {
+          settle<HalfOps>(S, base, m, sum, thr, O);
+          soften<HalfOps>(S, base, sum, P);
+        } else {
+          float none = 0.0f;
+          soften<HalfOps>(S, base, none, P);
+        }
+#pragma unroll
+        for (int pg = 0; pg < 2; ++pg) {
+          const uint8_t* vm = st + 2048 + 512 * pg + 16 * hh;
+          const cd_u4_t vc = *reinterpret_cast<const cd_u4_t*>(st + 1024 * pg + 512 + 32 * (n & 15) + 16 * hh);
+          uint32_t word[4];
+#pragma unroll
+          for (int x = 0; x < 4; ++x) word[x] = vc[x] >> (2 * (n >> 4));
+          cd_u4_t s4 = *reinterpret_cast<const cd_u4_t*>(vm + 64 * NG), z4 = *reinterpret_cast<const cd_u4_t*>(vm + 96 * NG);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            if (NG == 4 && i > 0) {
+              s4 = *reinterpret_cast<const cd_u4_t*>(vm + 64 * NG + 32 * i);
+              z4 = *reinterpret_cast<const cd_u4_t*>(vm + 96 * NG + 32 * i);
+            }
+            cd_u4_t f;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) {
+              const uint32_t sv = s4[x], zv = z4[x];  // (copies: a bit cast of a vector's element takes element 0)
+              const cd_h2_t code = i == 0   ? land_codes<0>(word[x])
+                                   : i == 1 ? land_codes<4>(word[x])
+                                   : i == 2 ? land_codes<8>(word[x])
+                                            : land_codes<4>(word[x] >> 8);
+              f[x] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(code, __builtin_bit_cast(cd_h2_t, sv), __builtin_bit_cast(cd_h2_t, zv)));
+            }
+            if constexpr (part) {
+              // tokens that do not exist are zero; values that are not finite are left for the second pass
+              int cnt = tile.ctx - (kStep * s + kBlock * pg);
+              cnt = (ok >> pg) & 1 ? cnt : 0;
+#pragma unroll
+              for (int x = 0; x < 4; ++x) {
+                const int tb = 8 * hh + 2 * x;
+                f[x] &= (tb < cnt ? 0xFFFFu : 0u) | (tb + 1 < cnt ? 0xFFFF0000u : 0u);
+                const uint32_t odd = HalfOps::odd(f[x]);
+                found |= odd;
+                f[x] &= second ? odd : ~odd;
+              }
+            }
+            if constexpr (!second) {
+              O[i] = HalfOps::mfma(__builtin_bit_cast(cd_h8_t, f), __builtin_bit_cast(cd_h8_t, P[pg]), O[i]);
+            } else {
+              for (int t = 0; t < 16; ++t) {
+                const bool see = ((ok >> pg) & 1) && kStep * s + kBlock * pg + t < lim;
+                const cd_f16_t d = HalfOps::mfma(__builtin_bit_cast(cd_h8_t, only_token(f, t)), __builtin_bit_cast(cd_h8_t, only_token(P[pg], t)), splat16(0.0f));
+#pragma unroll
+                for (int y = 0; y < 16; ++y) O[i][y] += see ? d[y] : 0.0f;
+              }
+            }
+          }
+        }
+      };
+      // before a step: it has landed when at most the younger steps' loads are on their way; after it: its stage's last
+      // readers are done, the step kAhead on may take it
+      auto before = [&](int s) {
+        if (s + kAhead <= s1)
+          asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * (kAhead - 1)) : "memory");
+        else
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      };
+      auto after = [&](int s) {
+        if (s + kAhead < s1) {
+          if (s + kAhead >= list0 + 32) load_list(s + 1);  // steps still to be taken keep their place in it
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          issue(s + kAhead);
+        }
+      };
+      std::true_type yes;
+      std::false_type no;
+      load_list(s0);
+      for (int s = s0; s < min(s0 + kAhead, s1); ++s) issue(s);
+      int s = s0;
+      for (; s < s1 && whole(s); ++s) {
+        before(s);
+        take(s, no, no);
+        after(s);
+      }
+      for (; s < s1; ++s) {  // the end of the context, or behind a page that does not exist
+        before(s);
+        take(s, yes, no);
+        after(s);
+      }
+      if (__any(found != 0)) {
+        for (s = s0; s < s1; ++s) {
+          load_list(s);
+          if (whole(s)) continue;
+          asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+          issue(s);
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          take(s, yes, yes);
+        }
+      }
+    }
+    // ---- the waves' results meet
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) lds.o[w][i][r][l] = O[i][r];
+    sum = pair_sum(sum);
+    if (hh == 0) {
+      lds.ml[w][0][n] = thr < 0.0f ? kNone : m;
+      lds.ml[w][1][n] = sum;
+    }
+    __syncthreads();
+  }
+  float top = kNone, all = 0.0f, f[kFewWaves];
+#pragma unroll
+  for (int x = 0; x < kFewWaves; ++x) top = fmaxf(top, lds.ml[x][0][n]);
+#pragma unroll
+  for (int x = 0; x < kFewWaves; ++x) {
+    f[x] = __builtin_amdgcn_exp2f(lds.ml[x][0][n] - top);
+    all = __builtin_fmaf(f[x], lds.ml[x][1][n], all);
+  }
+  // wave w has the 32 channels of tile w from here on
+  cd_f16_t O[1] = {splat16(0.0f)};
+  if (item.u0 < nI) {
+    const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      float x = 0.0f;
+#pragma unroll
+      for (int y = 0; y < kFewWaves; ++y) x = __builtin_fmaf(f[y], lds.o[y][w][r][l], x);
+      O[0][r] = x * inv;
+    }
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      cd_h8_t b;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) b[j] = (_Float16)O[0][8 * x + j];
+      lds.b[2 * w + x][l] = b;
+    }
+    __syncthreads();
+    // output row m = 8 u + 4 h + v of the tile: channel 32 w + 16 (u / 2) + 8 h + 4 (u % 2) + v, so that a lane's results
+    // are eight neighbours at a time; the operand's k order is the channel order the sums lie in
+    const int ch = 32 * w + 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
+    const float* R = a.R_v + ((size_t)h * kHeadDim + ch) * kHeadDim + 4 * hh;
+    cd_f16_t d = splat16(0.0f);
+#pragma unroll
+    for (int op = 0; op < 8; ++op) {
+      const float4 u = *reinterpret_cast<const float4*>(R + 16 * op), v = *reinterpret_cast<const float4*>(R + 16 * op + 8);
+      const cd_h8_t A = {(_Float16)u.x, (_Float16)u.y, (_Float16)u.z, (_Float16)u.w,
+                         (_Float16)v.x, (_Float16)v.y, (_Float16)v.z, (_Float16)v.w};
+      d = HalfOps::mfma(A, lds.b[op][l], d);
+    }
+    O[0] = d * all;
+  }
+  m = top == kNone ? 0.0f : top;
+  thr = top == kNone ? kNone : kMove;
+  sum = hh == 0 ? all : 0.0f;  // pair_sum adds the halves again
+
+  // ---- the chunk's own tokens: every wave has all scores and its tile's values
+  const int c0 = max(item.u0 - nI, 0), c1 = item.u1 - nI;
+  if (c0 < c1) {
+    cd_b8_t Q[8];
+    const uint16_t* q = a.q + (tile.start + tok) * a.q_stride + (size_t)(h * a.gq + rc - tok * a.gq) * kHeadDim + 8 * hh;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) Q[kk] = *reinterpret_cast<const cd_b8_t*>(q + 16 * kk);
+    float base = kBias - m - a.qoff[grow];
+    const uint16_t* kb = a.k_new + tile.start * a.k_stride + (size_t)h * kHeadDim + 8 * hh;
+    const int ch = 32 * w + 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
+    const uint16_t* vb = a.v_new + tile.start * a.v_stride + (size_t)h * kHeadDim + ch;
+    const int last = (min(tile.row0 + a.bm, rows) - 1) / a.gq;  // the tile's last token
+    for (int s = c0 * (kUnit / kStep); s < c1 * (kUnit / kStep) && kStep * s <= last; ++s) {
+      const uint16_t* kr = kb + min(kStep * s + (n & 16) + row_token(n & 15), tile.n - 1) * a.k_stride;
+      cd_h8_t k[8];
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) k[kk] = *reinterpret_cast<const cd_h8_t*>(kr + 16 * kk);
+      uint32_t v[2][8];
+#pragma unroll
+      for (int pg = 0; pg < 2; ++pg)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[pg][j] = vb[min(kStep * s + kBlock * pg + 8 * hh + j, tile.n - 1) * a.v_stride];
+      cd_f16_t S = splat16(0.0f);
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) S = BfOps::mfma(k[kk], Q[kk], S);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S[i] = kStep * s + reg_token(i) + 8 * hh <= tok ? S[i] : -INFINITY;
+      settle<BfOps>(S, base, m, sum, thr, O);
+      cd_u4_t P[2];
+      soften<BfOps>(S, base, sum, P);
+      uint32_t found = 0;
+      cd_u4_t y[2], z[2];  // values, and those that are not finite
+#pragma unroll
+      for (int pg = 0; pg < 2; ++pg)
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          const int t = kStep * s + kBlock * pg + 8 * hh + 2 * x;
+          const uint32_t pair = (t < tile.n ? v[pg][2 * x] : 0u) | (t + 1 < tile.n ? v[pg][2 * x + 1] << 16 : 0u), odd = BfOps::odd(pair);
+          found |= odd;
+          y[pg][x] = pair & ~odd;
+          z[pg][x] = pair & odd;
+        }
+#pragma unroll
+      for (int pg = 0; pg < 2; ++pg) O[0] = BfOps::mfma(__builtin_bit_cast(cd_h8_t, y[pg]), __builtin_bit_cast(cd_b8_t, P[pg]), O[0]);
+      if (__any(found != 0)) {
+        for (int t = 0; t < kStep; ++t) {
+          const bool see = kStep * s + t <= tok;
+          const cd_u4_t p = only_token(t < 16 ? P[0] : P[1], t), x = only_token(t < 16 ? z[0] : z[1], t);
+          const cd_f16_t d = BfOps::mfma(__builtin_bit_cast(cd_h8_t, x), __builtin_bit_cast(cd_b8_t, p), splat16(0.0f));
+#pragma unroll
+          for (int i = 0; i < 16; ++i) O[0][i] += see ? d[i] : 0.0f;
+        }
+      }
+    }
+  }
+
+  // ---- results: registers 8 x .. 8 x + 7 are channels 32 w + 16 x + 8 hh ..
+  all = pair_sum(sum);
+  if (row >= rows) return;
+  if (item.slot < 0) {
+    const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+    uint16_t* o = a.out + ((size_t)(tile.start + tok) * a.Hq + h * a.gq + row - tok * a.gq) * kHeadDim + 32 * w + 8 * hh;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      uint32_t y[4];
+#pragma unroll
+      for (int v = 0; v < 4; ++v) y[v] = pack_bf16(O[0][8 * x + 2 * v] * inv, O[0][8 * x + 2 * v + 1] * inv);
+      *reinterpret_cast<uint4*>(o + 16 * x) = make_uint4(y[0], y[1], y[2], y[3]);
+    }
+  } else {
+    float* part = a.part + ((size_t)item.slot * H + h) * a.bm * kChunkPartStride;
+    float* o = part + (size_t)n * kHeadDim + 32 * w + 8 * hh;
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      float4* d = reinterpret_cast<float4*>(o + 16 * x);
+      d[0] = make_float4(O[0][8 * x], O[0][8 * x + 1], O[0][8 * x + 2], O[0][8 * x + 3]);
+      d[1] = make_float4(O[0][8 * x + 4], O[0][8 * x + 5], O[0][8 * x + 6], O[0][8 * x + 7]);
+    }
+    if (w == 0 && hh == 0) reinterpret_cast<float2*>(part + (size_t)a.bm * kHeadDim)[n] = make_float2(thr < 0.0f ? kNone : m, all);
+  }
+}
+
+hipError_t launch_chunk_few(const ChunkArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((long long)a.max_items * a.cv.num_kv_heads));
+  if (a.cv.groups == 4)
+    hipLaunchKernelGGL((chunk_few_kernel<4>), grid, dim3(64 * kFewWaves), 0, s, a);
+  else
+    hipLaunchKernelGGL((chunk_few_kernel<1>), grid, dim3(64 * kFewWaves), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace int2kv

@@ -224,6 +224,7 @@ struct ChunkPlan {
   size_t off_counts, off_start, off_tiles, off_items, off_qrot, off_qoff, off_rv, off_part, total;
 };
 ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx);
+hipError_t launch_chunk_few(const ChunkArgs& a, hipStream_t s);  // (chunk_few.hip) tiles of 32 rows
 hipError_t launch_chunk_attention(ChunkArgs a, const ChunkPlan& p, uint8_t* ws, hipStream_t s);
 
 // ---- OptR offline calibration (optr.hip): fp64 throughout
