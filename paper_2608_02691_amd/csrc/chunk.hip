@@ -4,11 +4,10 @@
 // S = {cached s < limit} and, where the chunk's own keys and values are given in bf16, {new t <= i}:
 //     a_s = c (q R_K) k^_s^T,   a_t = c (q k_t^T - q mu^T)   (both with centered keys; c = 1 / sqrt(128)),
 //     o = (sum_s p_s v^_s) R_V^T + sum_t p_t v_t,   p = softmax over S.
-// Three launches:
-//   chunk_prep_kernel   rotates the queries (q' = q R_K as fp16 operands), lays R_V out as operands, and plans the work;
-//   chunk_attn_kernel   a work-group takes a tile of rows of one KV head over a range of 64-token units of the context:
-//                       the INT2 units first, their sum un-rotated, then the chunk's own bf16 units;
-//   chunk_merge_kernel  joins the pieces of tiles whose context was split.
+// A work-group takes a piece: a tile of rows of one KV head over a range of 64-token units of the context. It finds its
+// piece by itself (chunk_core.h; a planning launch goes before it for large batches), rotates its queries, goes over the
+// INT2 units, un-rotates their sum, and goes over the chunk's own bf16 units. chunk_merge_kernel joins the pieces of tiles
+// that were cut.
 //
 // Products are formed transposed (S^T = K Q^T, O^T = V^T P^T, 32 x 32 x 16): a lane holds one query row, so the softmax is
 // lane-local but for one exchange of halves, the rescaling is one factor per lane, and the probabilities are the second
@@ -20,189 +19,77 @@ namespace int2kv {
 
 namespace {
 
-constexpr int kPrepThreads = 256;
+constexpr int kPlanThreads = 256;
 
-// Inclusive sum over the block; total to every thread. tmp: a word per wave and one more.
+// Inclusive sum over the block; total to every thread
 __device__ __forceinline__ int block_scan(int x, int* tmp, int& total) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
+  const int wave = threadIdx.x >> 6;
+  x = wave_scan(x);
   __syncthreads();
-  if (lane == 63) tmp[wave] = x;
+  if ((threadIdx.x & 63) == 63) tmp[wave] = x;
   __syncthreads();
   int before = 0;
   total = 0;
 #pragma unroll
-  for (int w = 0; w < kPrepThreads / 64; ++w) {
+  for (int w = 0; w < kPlanThreads / 64; ++w) {
     before += w < wave ? tmp[w] : 0;
     total += tmp[w];
   }
   return x + before;
 }
 
-// Plan of the attention launch, by one block: tiles of bm rows in sequence order, cut into pieces of at most L units so
-// that all heads' pieces come to about `target`; the last tiles first, since under a causal mask they are the longest.
-__device__ void plan_work(const ChunkArgs& a) {
-  __shared__ int tmp[kPrepThreads / 64];
-  __shared__ unsigned long long sum;
-  const int tid = threadIdx.x;
-  int carry = 0, total;
-  for (int b0 = 0; b0 < a.B; b0 += kPrepThreads) {
-    const int b = b0 + tid;
-    const int rows = b < a.B ? seq_of(a, b).n * a.gq : 0, mine = (rows + a.bm - 1) / a.bm;
-    const int upto = block_scan(mine, tmp, total);
-    if (b < a.B) a.tile_start[b] = carry + upto - mine;
-    carry = min(carry + total, 1 << 30);
-  }
-  // sequences that overlap can ask for more tiles than there is room for: the rest is left out
-  const int T = min(carry, a.max_tiles);
-  if (tid == 0) sum = 0;
-  __syncthreads();
-  unsigned long long mine = 0;
-  for (int t = tid; t < T; t += kPrepThreads) {
-    int lo = 0, hi = a.B - 1;  // the last sequence that starts at or before t (empty ones start where the next does)
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (a.tile_start[mid] <= t)
-        lo = mid;
-      else
-        hi = mid - 1;
-    }
-    const Seq s = seq_of(a, lo);
-    const int row0 = (t - a.tile_start[lo]) * a.bm, last = min(row0 + a.bm, s.n * a.gq) - 1;
-    const int i = last / a.gq, units = int2_units(a, s, i) + own_units(a, i);
-    ChunkTile& d = a.tiles[t];
-    d.b = lo, d.row0 = row0, d.start = s.start, d.n = s.n, d.ctx = s.ctx, d.units = units;
-    mine += units;
-  }
-  atomicAdd(&sum, mine);
-  __syncthreads();
-  const unsigned long long work = sum * a.cv.num_kv_heads;
-  const int L = (int)max((unsigned long long)a.min_units, (work + a.target - 1) / a.target);
-  int items = 0, slots = 0;
-  for (int r0 = 0; r0 < T; r0 += kPrepThreads) {
-    const int t = T - 1 - (r0 + tid);
-    int units = 0, pieces = 0;
-    if (t >= 0) {
-      units = a.tiles[t].units;
-      pieces = units > L ? (units + L - 1) / L : 1;
-    }
-    int want = pieces > 1 ? pieces : 0;
-    int n_slots, n_items;
-    const int slot_end = slots + block_scan(want, tmp, n_slots);
-    if (want && slot_end > a.max_slots) pieces = 1, want = 0;  // cannot happen within the bounds the host sized for
-    const int item_end = items + block_scan(pieces, tmp, n_items);
-    if (t >= 0) {
-      ChunkTile d = a.tiles[t];
-      d.pieces = pieces, d.slot = want ? slot_end - want : -1;
-      a.tiles[t] = d;
-      for (int p = 0; p < pieces; ++p) {
-        const int at = item_end - pieces + p;
-        if (at >= a.max_items) break;
-        ChunkItem it;
-        it.tile = t;
-        it.u0 = (int)((long long)units * p / pieces);
-        it.u1 = (int)((long long)units * (p + 1) / pieces);
-        it.slot = want ? d.slot + p : -1;
-        a.items[at] = it;
-      }
-    }
-    slots += n_slots;
-    items += n_items;
-  }
-  if (tid == 0) {
-    a.counts[0] = min(items, a.max_items);
-    a.counts[1] = T;
-  }
-}
-
-// R_V of a head as A operands of o = o' R_V^T: tile 2 a + e, row m is output channel 64 a + 2 m + e; operand (i, half)
-// takes the channels 32 i + 16 half + {4 hh .. + 3, 8 + 4 hh .. + 3} a lane half holds of tile i of O^T.
-__device__ void layout_rv(const ChunkArgs& a, int h, int part, int parts) {
-  const float* R = a.R_v + (size_t)h * kHeadDim * kHeadDim;
-  cd_h8_t* dst = reinterpret_cast<cd_h8_t*>(a.rv) + (size_t)h * 2048;
-  for (int x = part * kPrepThreads + threadIdx.x; x < 2048; x += parts * kPrepThreads) {
-    const int l = x & 63, m = l & 31, hh = l >> 5, op = (x >> 6) & 7, t = x >> 9;
-    const float* src = R + (size_t)(64 * (t >> 1) + 2 * m + (t & 1)) * kHeadDim + 16 * op + 4 * hh;
-    const float4 u = *reinterpret_cast<const float4*>(src), v = *reinterpret_cast<const float4*>(src + 8);
-    dst[x] = cd_h8_t{(_Float16)u.x, (_Float16)u.y, (_Float16)u.z, (_Float16)u.w,
-                     (_Float16)v.x, (_Float16)v.y, (_Float16)v.z, (_Float16)v.w};
-  }
-}
-
-// Position (in a query row of the workspace) -> channel: chunk 2 kk + hh of eight is operand kk's piece of lane half hh
-__device__ __forceinline__ int pos_channel(int pos) { return code_channel(pos >> 4, (pos >> 3) & 1, pos & 7); }
-
-// Query rotation: q'^T = R_K^T q^T on the matrix cores, R_K in two bf16 terms (q is exact), a wave per 32 positions, row
-// tiles of 32. q' is held in fp16 with log2(e) / sqrt(128) folded in: what a small q' loses among fp16's subnormals
-// (2^-25 an element) is nothing in a score.
-__device__ void rotate_queries(const ChunkArgs& a, int h, int part, int parts) {
-  const int l = threadIdx.x & 63, wave = threadIdx.x >> 6, n = l & 31, hh = l >> 5;
-  const float* R = a.R_k + (size_t)h * kHeadDim * kHeadDim;
-  // A rows: row m = 8 u + 4 hh + v of the wave's tile is position 32 wave + 16 (u / 2) + 8 hh + 4 (u % 2) + v, so that a
-  // lane's results are eight consecutive positions at a time
-  const int mu_ = n >> 3, mh = (n >> 2) & 1, mv = n & 3;
-  const int col = pos_channel(32 * wave + 16 * (mu_ >> 1) + 8 * mh + 4 * (mu_ & 1) + mv);
-  cd_b8_t hi[8], lo[8];
-#pragma unroll
-  for (int kk = 0; kk < 8; ++kk)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float r = R[(size_t)(16 * kk + 8 * hh + j) * kHeadDim + col];
-      hi[kk][j] = (__bf16)r;
-      lo[kk][j] = (__bf16)(r - (float)hi[kk][j]);
-    }
-  const int rows = a.total_q * a.gq, tiles = (rows + 31) / 32;
-  for (int t = part; t < tiles; t += parts) {
-    const int row = t * 32 + n, rc = min(row, rows - 1), tok = rc / a.gq;
-    const uint16_t* q = a.q + tok * a.q_stride + (size_t)(h * a.gq + rc - tok * a.gq) * kHeadDim + 8 * hh;
-    cd_b8_t x[8];
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) x[kk] = *reinterpret_cast<const cd_b8_t*>(q + 16 * kk);
-    cd_f16_t d;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) d[r] = 0.0f;
-    float off = 0.0f;
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) {
-      d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo[kk], x[kk], d, 0, 0, 0);
-      d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi[kk], x[kk], d, 0, 0, 0);
-    }
-    if (a.mu && wave == 0) {
-      const float* mu = a.mu + (size_t)h * kHeadDim + 8 * hh;
-#pragma unroll
-      for (int kk = 0; kk < 8; ++kk)
-#pragma unroll
-        for (int j = 0; j < 8; ++j) off = __builtin_fmaf((float)x[kk][j], mu[16 * kk + j], off);
-    }
-    off += __shfl_xor(off, 32);
-    if (row < rows) {
-      uint16_t* o = a.qrot + ((size_t)h * rows + row) * kHeadDim + 32 * wave + 8 * hh;
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        cd_h8_t y;
-#pragma unroll
-        for (int r = 0; r < 8; ++r) y[r] = (_Float16)(d[8 * u + r] * kLogit2);
-        *reinterpret_cast<cd_h8_t*>(o + 16 * u) = y;
-      }
-      if (wave == 0 && hh == 0) a.qoff[(size_t)h * rows + row] = off * kLogit2;
-    }
-  }
-}
-
 }  // namespace
 
-// Blocks: 0 plans; then H blocks of R_V; then a.rot_blocks per head of the query rotation.
-__global__ __launch_bounds__(kPrepThreads) void chunk_prep_kernel(ChunkArgs a) {
-  const int H = a.cv.num_kv_heads;
-  int x = blockIdx.x;
-  if (x == 0) return plan_work(a);
-  if (--x < H) return layout_rv(a, x, 0, 1);
-  x -= H;
-  rotate_queries(a, x % H, x / H, a.rot_blocks);
+// The plan of a batch too large for every wave to hold, by one block
+__global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
+  __shared__ int tmp[kPlanThreads / 64], counts[kCuts], longest;
+  __shared__ unsigned long long work;
+  const int tid = threadIdx.x;
+  if (tid < kCuts) counts[tid] = 0;
+  if (tid == 0) longest = 0, work = 0;
+  __syncthreads();
+  int T = 0, total = 0;
+  unsigned long long W = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
+    const Load s = b0 + tid < a.B ? load_of(a, seq_of(a, b0 + tid)) : Load{0, 0};
+    int n;
+    block_scan(s.tiles, tmp, n);
+    T = min(T + n, 1 << 28);
+    atomicMax(&longest, s.units);
+    W += (unsigned long long)s.tiles * s.units;
+  }
+  atomicAdd(&work, W);
+  __syncthreads();
+  const int umax = longest;
+  int mine[kCuts] = {};
+  for (int b = tid; b < a.B; b += kPlanThreads) {
+    const Load s = load_of(a, seq_of(a, b));
+#pragma unroll
+    for (int k = 0; k < kCuts; ++k) mine[k] += s.tiles * pieces_of(s, cut_of(a, k, T, umax));
+  }
+#pragma unroll
+  for (int k = 0; k < kCuts; ++k) atomicAdd(&counts[k], mine[k]);
+  __syncthreads();
+  int pieces[kCuts];
+#pragma unroll
+  for (int k = 0; k < kCuts; ++k) pieces[k] = counts[k];
+  const int L = pick_cut(a, pieces, T, (float)work, umax);
+  T = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
+    const int b = b0 + tid;
+    const Load s = b < a.B ? load_of(a, seq_of(a, b)) : Load{0, 0};
+    const int items = s.tiles * pieces_of(s, L);
+    int n_tiles, n_items;
+    const int t = T + block_scan(s.tiles, tmp, n_tiles) - s.tiles, i = total + block_scan(items, tmp, n_items) - items;
+    if (b < a.B) a.tile_start[b] = t, a.item_start[b] = i;
+    T = min(T + n_tiles, 1 << 28);
+    total = min(total + n_items, 1 << 28);
+  }
+  if (tid == 0) {
+    a.head[0] = min(total, a.max_items);
+    a.head[1] = total > a.max_items || T > a.max_tiles ? 0 : T;
+    a.head[2] = L;
+  }
 }
 
 namespace {
@@ -336,8 +223,8 @@ struct Int2Source {
   int pid, fetched;
   uint32_t found = 0;                   // not zero: a value that is not finite was left out
 
-  __device__ __forceinline__ Int2Source(const ChunkArgs& args, int head, const ChunkTile& t, int w, int limit, int least, int least_tile)
-      : a(args), table(args.table + (size_t)t.b * args.max_blocks), h(head), ctx(t.ctx), pages((t.ctx + kBlock - 1) / kBlock),
+  __device__ __forceinline__ Int2Source(const ChunkArgs& args, int head, int b, int tokens, int w, int limit, int least, int least_tile)
+      : a(args), table(args.table + (size_t)b * args.max_blocks), h(head), ctx(tokens), pages((tokens + kBlock - 1) / kBlock),
         lim(limit), lim_min(least), lim_tile(least_tile), l(threadIdx.x & 63), n(l & 31), hh(l >> 5), half(w / (NW / 2)), word0(KW * (w % (NW / 2))),
         page(w / (NW / 4)), tile0(TV * (w % (NW / 4))), ok(0), ok_prev(0), pid(-1), fetched(-1) {}
   // lane l: the block of page l % 4 of unit u
@@ -454,8 +341,8 @@ struct OwnSource {
   uint32_t v[PV][8];
   uint32_t found = 0;
 
-  __device__ __forceinline__ OwnSource(const ChunkArgs& args, int h, const ChunkTile& t, int w, int row_tok, int least)
-      : a(args), n_tok(t.n), tok(row_tok), tok_min(least), tok_tile(t.row0 / args.gq), l(threadIdx.x & 63), n(l & 31), hh(l >> 5), half(w / (NW / 2)),
+  __device__ __forceinline__ OwnSource(const ChunkArgs& args, int h, const Seq& t, int row0, int w, int row_tok, int least)
+      : a(args), n_tok(t.n), tok(row_tok), tok_min(least), tok_tile(row0 / args.gq), l(threadIdx.x & 63), n(l & 31), hh(l >> 5), half(w / (NW / 2)),
         op0(KO * (w % (NW / 2))), page(w / (NW / 4)), pair0(PV * (w % (NW / 4))),
         kb(args.k_new + t.start * args.k_stride + (size_t)h * kHeadDim + 8 * hh + 16 * op0),
         vb(args.v_new + t.start * args.v_stride + (size_t)h * kHeadDim + 2 * n + 64 * pair0) {}
@@ -508,6 +395,83 @@ struct OwnSource {
   __device__ __forceinline__ bool sees_token(int u, int t) const { return kUnit * u + t <= tok; }
 };
 
+// q' = q R_K of the lane's row as fp16 operands with log2(e) / sqrt(128) folded in (what a small q' loses among fp16's
+// subnormals, 2^-25 an element, is nothing in a score). R_K goes through LDS in two bf16 terms, q is exact.
+template <int NW>
+__device__ __forceinline__ void rotate_query(const float* R, ChunkLds& lds, const cd_b8_t (&x)[8], cd_h8_t (&Q)[8]) {
+  cd_b8_t* hi = reinterpret_cast<cd_b8_t*>(&lds);  // [tile][operand][lane], then the low terms
+  cd_b8_t* lo = hi + 2048;
+  static_assert(sizeof(ChunkLds) >= 4096 * 16, "room for both terms");
+#pragma unroll
+  for (int i = 0; i < 2048 / (64 * NW); ++i) {
+    const int e = threadIdx.x + 64 * NW * i, oct = e >> 7, c = e & 127;  // eight channels 8 oct .. of column c
+    const int m16 = c & 15, p = c >> 4, wd = m16 >> 1;
+    const int pos = (2 * (2 * (wd & 3) + (p >> 2)) + (wd >> 2)) * 8 + 2 * (p & 3) + (m16 & 1);
+    // row_position is its own inverse
+    const int at = ((pos >> 5) * 8 + (oct >> 1)) * 64 + (oct & 1) * 32 + row_position(pos & 31);
+    cd_b8_t a, b;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float r = R[(size_t)(8 * oct + j) * kHeadDim + c];
+      a[j] = (__bf16)r;
+      b[j] = (__bf16)(r - (float)a[j]);
+    }
+    hi[at] = a;
+    lo[at] = b;
+  }
+  __syncthreads();
+  const int l = threadIdx.x & 63;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    cd_f16_t d = splat16(0.0f);
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo[(8 * t + kk) * 64 + l], x[kk], d, 0, 0, 0);
+      d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi[(8 * t + kk) * 64 + l], x[kk], d, 0, 0, 0);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) Q[2 * t + u][j] = (_Float16)(d[8 * u + j] * kLogit2);
+  }
+  __syncthreads();
+}
+
+// O^T <- R_V O^T, on the normalized sums (within fp16's range, being averages of the values). R_V goes through LDS as A
+// operands: tile 2 e + o, row m is output channel 64 e + 2 m + o; operand (i, half) takes the channels 32 i + 16 half +
+// {4 hh .. + 3, 8 + 4 hh .. + 3} that a lane half holds of tile i. Chunk m of operand op lies at m ^ op (its low bits), so
+// that a row's pieces, which differ in operand, spread over the banks.
+template <int NW>
+__device__ __forceinline__ void unrotate(const float* R, ChunkLds& lds, RowState& st) {
+  typedef _Float16 h4 __attribute__((ext_vector_type(4)));
+  h4* rv = reinterpret_cast<h4*>(&lds);
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 4096 / (64 * NW); ++i) {
+    const int e = threadIdx.x + 64 * NW * i, c = e >> 5, x = e & 31, op = x >> 2;
+    const float4 r = *reinterpret_cast<const float4*>(R + (size_t)c * kHeadDim + 4 * x);
+    const int t = 2 * (c >> 6) + (c & 1), m = (c & 63) >> 1;
+    rv[2 * ((t * 8 + op) * 64 + (x & 1) * 32 + (m ^ op)) + ((x >> 1) & 1)] = h4{(_Float16)r.x, (_Float16)r.y, (_Float16)r.z, (_Float16)r.w};
+  }
+  __syncthreads();
+  const int l = threadIdx.x & 63;
+  const float all = pair_sum(st.sum), inv = all == 0.0f ? 0.0f : 1.0f / all;
+  cd_h8_t B[8];
+#pragma unroll
+  for (int op = 0; op < 8; ++op)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) B[op][j] = (_Float16)(st.O[op >> 1][8 * (op & 1) + j] * inv);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    cd_f16_t d = splat16(0.0f);
+#pragma unroll
+    for (int op = 0; op < 8; ++op)
+      d = __builtin_amdgcn_mfma_f32_32x32x16_f16(reinterpret_cast<cd_h8_t*>(rv)[(t * 8 + op) * 64 + (l ^ op)], B[op], d, 0, 0, 0);
+    st.O[t] = d * all;
+  }
+  __syncthreads();
+}
+
 }  // namespace
 
 // Work-group: a piece of a tile of 32 NW rows of one KV head; wave w has rows 32 w .. of it.
@@ -515,68 +479,51 @@ template <int NG, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
   __shared__ ChunkLds lds;
   const int H = a.cv.num_kv_heads;
-  const int h = (int)(blockIdx.x % H), at = (int)(blockIdx.x / H);
-  if (at >= a.counts[0]) return;
-  const ChunkItem item = a.items[at];
-  const ChunkTile tile = a.tiles[item.tile];
+  const int h = (int)(blockIdx.x % H);
+  const Place place = locate(a, (int)(blockIdx.x / H), h);
+  if (!place.valid) return;
+  const Seq seq = place.s;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = l & 31, hh = l >> 5;
-  const int rows = tile.n * a.gq, row_w = tile.row0 + 32 * w, tok_w = min(row_w, rows - 1) / a.gq;
-  const int nI = int2_units(a, Seq{tile.start, tile.n, tile.ctx}, (min(tile.row0 + a.bm, rows) - 1) / a.gq);
+  const int rows = seq.n * a.gq, row_w = place.row0 + 32 * w, tok_w = min(row_w, rows - 1) / a.gq;
+  const int nI = int2_units(a, seq, (min(place.row0 + a.bm, rows) - 1) / a.gq);
   const int row = row_w + n, rc = min(row, rows - 1), tok = rc / a.gq;
-  const size_t grow = (size_t)h * a.total_q * a.gq + (size_t)tile.start * a.gq + rc;
   RowState st;
   st.m = 0.0f, st.sum = 0.0f, st.thr = kNone;
 #pragma unroll
   for (int i = 0; i < 4; ++i) st.O[i] = splat16(0.0f);
 
-  const int i1 = min(item.u1, nI);
-  if (item.u0 < i1) {
-    auto limit = [&](int t) { return a.k_new ? tile.ctx : min(tile.ctx, tile.ctx - tile.n + 1 + t); };
+  // the row's query: channels 16 kk + 8 hh .. of operand kk (read again for the chunk's own units: the registers are worth more)
+  const uint16_t* q = a.q + (seq.start + tok) * a.q_stride + (size_t)(h * a.gq + rc - tok * a.gq) * kHeadDim + 8 * hh;
+  auto query = [&](cd_b8_t (&x)[8]) {
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) x[kk] = *reinterpret_cast<const cd_b8_t*>(q + 16 * kk);
+  };
+  const int i1 = min(place.u1, nI);
+  if (place.u0 < i1) {
+    cd_b8_t x[8];
     cd_h8_t Q[8];
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) Q[kk] = *reinterpret_cast<const cd_h8_t*>(a.qrot + grow * kHeadDim + 16 * kk + 8 * hh);
-    Int2Source<NG, NW> src(a, h, tile, w, limit(tok), limit(tok_w), limit(tile.row0 / a.gq));
-    attend<HalfOps>(src, st, lds, Q, 0.0f, item.u0, i1);
-
-    // ---- un-rotate: O^T <- R_V O^T, on the normalized sums (within fp16's range, being averages of the values)
-    __syncthreads();
-    cd_h8_t* rv = &lds.k[0][0][0];
-    const cd_h8_t* from = reinterpret_cast<const cd_h8_t*>(a.rv) + (size_t)h * 2048;
-#pragma unroll
-    for (int x = 0; x < 2048 / (64 * NW); ++x) rv[threadIdx.x + 64 * NW * x] = from[threadIdx.x + 64 * NW * x];
-    __syncthreads();
-    const float all = pair_sum(st.sum), inv = all == 0.0f ? 0.0f : 1.0f / all;
-    cd_h8_t B[8];
-#pragma unroll
-    for (int op = 0; op < 8; ++op)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) B[op][j] = (_Float16)(st.O[op >> 1][8 * (op & 1) + j] * inv);
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      cd_f16_t d = splat16(0.0f);
-#pragma unroll
-      for (int op = 0; op < 8; ++op) d = __builtin_amdgcn_mfma_f32_32x32x16_f16(rv[512 * t + 64 * op + l], B[op], d, 0, 0, 0);
-      st.O[t] = d * all;
-    }
-    __syncthreads();
+    query(x);
+    rotate_query<NW>(a.R_k + (size_t)h * kHeadDim * kHeadDim, lds, x, Q);
+    auto limit = [&](int t) { return a.k_new ? seq.ctx : min(seq.ctx, seq.ctx - seq.n + 1 + t); };
+    Int2Source<NG, NW> src(a, h, place.b, seq.ctx, w, limit(tok), limit(tok_w), limit(place.row0 / a.gq));
+    attend<HalfOps>(src, st, lds, Q, 0.0f, place.u0, i1);
+    unrotate<NW>(a.R_v + (size_t)h * kHeadDim * kHeadDim, lds, st);
   }
 
-  const int c0 = max(item.u0 - nI, 0), c1 = item.u1 - nI;
+  const int c0 = max(place.u0 - nI, 0), c1 = place.u1 - nI;
   if (c0 < c1) {
     cd_b8_t Q[8];
-    const uint16_t* q = a.q + (tile.start + tok) * a.q_stride + (size_t)(h * a.gq + rc - tok * a.gq) * kHeadDim + 8 * hh;
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) Q[kk] = *reinterpret_cast<const cd_b8_t*>(q + 16 * kk);
-    OwnSource<NW> src(a, h, tile, w, tok, tok_w);
-    attend<BfOps>(src, st, lds, Q, a.qoff[grow], c0, c1);
+    query(Q);
+    OwnSource<NW> src(a, h, seq, place.row0, w, tok, tok_w);
+    attend<BfOps>(src, st, lds, Q, query_mean(Q, a.mu + (size_t)h * kHeadDim, hh), c0, c1);
   }
 
   // ---- results: register 4 u + v of tile 2 e + o is channel 64 e + 16 u + 8 hh + 2 v + o
   const float all = pair_sum(st.sum);
   if (row >= rows) return;
-  if (item.slot < 0) {
+  if (place.slot < 0) {
     const float inv = all == 0.0f ? 0.0f : 1.0f / all;
-    uint16_t* o = a.out + ((size_t)(tile.start + tok) * a.Hq + h * a.gq + row - tok * a.gq) * kHeadDim + 8 * hh;
+    uint16_t* o = a.out + ((size_t)(seq.start + tok) * a.Hq + h * a.gq + row - tok * a.gq) * kHeadDim + 8 * hh;
 #pragma unroll
     for (int x = 0; x < 2; ++x)
 #pragma unroll
@@ -588,8 +535,8 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
       }
   } else {
     // partial: bm rows of 128 sums, then their (m, l)
-    float* part = a.part + ((size_t)item.slot * H + h) * a.bm * kChunkPartStride;
-    const int rt = row - tile.row0;
+    float* part = a.part + ((size_t)place.slot * H + h) * a.bm * kChunkPartStride;
+    const int rt = row - place.row0;
     float* o = part + (size_t)rt * kHeadDim + 8 * hh;
 #pragma unroll
     for (int x = 0; x < 2; ++x)
@@ -607,9 +554,9 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
 // Block (tile, KV head, 16 rows): thread (row, eight channels) sums the tile's pieces in order.
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
   const int t = blockIdx.x, h = blockIdx.y, H = a.cv.num_kv_heads;
-  if (t >= a.counts[1]) return;
+  if (t >= a.head[1]) return;
   const ChunkTile tile = a.tiles[t];
-  if (tile.slot < 0) return;
+  if (tile.pieces <= 1) return;
   const int rt = blockIdx.z * 16 + (threadIdx.x >> 4), c = 8 * (threadIdx.x & 15), row = tile.row0 + rt;
   if (row >= tile.n * a.gq) return;
   const size_t stride = (size_t)H * a.bm * kChunkPartStride;
@@ -642,29 +589,26 @@ ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_
   const long long seq_rows = (long long)max_q * gq, rows = (long long)total_q * gq;
   p.waves = seq_rows <= 64 ? 1 : seq_rows <= 128 ? 4 : 8;
   p.bm = 32 * p.waves;
+  p.resident = num_cus() * (p.waves == 8 ? 1 : 2);
+  p.piece_units = p.waves == 1 ? 10.0f : 3.0f;
+  p.merge_units = p.waves == 1 ? 0.016f : 0.00013f * p.bm;
   const long long per_seq = (seq_rows + p.bm - 1) / p.bm;
   long long tiles = B * per_seq, by_rows = rows / p.bm + B;
   tiles = tiles < by_rows ? tiles : by_rows;
   p.max_tiles = (int)(tiles < 1 ? 1 : tiles);
-  // pieces of all heads: two rounds of the resident work-groups
-  const long long resident = (long long)num_cus() * (p.waves <= 4 ? 2 : 1);
-  p.target = 2 * resident;
-  p.min_units = 4;
-  const long long extra = p.target / H + 1;
-  const long long most = ((long long)max_ctx + 63) / 64 + ((long long)max_q + 63) / 64, cuts = (most + p.min_units - 1) / p.min_units;
-  p.max_items = (int)(p.max_tiles + (extra < tiles * cuts ? extra : tiles * cuts));
-  p.max_slots = (int)(2 * extra < tiles * cuts ? 2 * extra : tiles * cuts);
-  const long long q_tiles = (rows + 31) / 32, want = (2LL * num_cus() + H - 1) / H;
-  p.rot_blocks = (int)(q_tiles < want ? (q_tiles < 1 ? 1 : q_tiles) : want);
+  // pieces a KV head: a place on the chip each while the tiles have one, else up to three; never more than the units allow
+  const long long most = ((long long)max_ctx + 63) / 64 + ((long long)max_q + 63) / 64, cuts = (most + 1) / 2;
+  const long long places = (tiles * H <= p.resident ? 1LL : 3LL) * p.resident / H;
+  long long cut = places < p.max_tiles * cuts ? places : p.max_tiles * cuts;
+  p.max_slots = (int)(cut > 1 ? cut : 1);
+  p.max_items = p.max_tiles > p.max_slots ? p.max_tiles : p.max_slots;
   auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
+  const size_t listed = B > kChunkWaveSeqs ? (size_t)B : 0;
   size_t off = 0;
-  p.off_counts = off, off = up(off + 2 * sizeof(int32_t));
-  p.off_start = off, off = up(off + (size_t)B * sizeof(int32_t));
+  p.off_head = off, off = up(off + 4 * sizeof(int32_t));
+  p.off_items = off, off = up(off + listed * sizeof(int32_t));
+  p.off_starts = off, off = up(off + listed * sizeof(int32_t));
   p.off_tiles = off, off = up(off + (size_t)p.max_tiles * sizeof(ChunkTile));
-  p.off_items = off, off = up(off + (size_t)p.max_items * sizeof(ChunkItem));
-  p.off_qrot = off, off = up(off + (size_t)H * rows * kHeadDim * sizeof(uint16_t));
-  p.off_qoff = off, off = up(off + (size_t)H * rows * sizeof(float));
-  p.off_rv = off, off = up(off + (size_t)H * kHeadDim * kHeadDim * sizeof(uint16_t));
   p.off_part = off, off = up(off + (size_t)p.max_slots * H * p.bm * kChunkPartStride * sizeof(float));
   p.total = off;
   return p;
@@ -683,24 +627,24 @@ hipError_t launch_attn(const ChunkArgs& a, hipStream_t s) {
 
 hipError_t launch_chunk_attention(ChunkArgs a, const ChunkPlan& p, uint8_t* ws, hipStream_t s) {
   a.bm = p.bm;
+  a.resident = p.resident;
   a.max_tiles = p.max_tiles;
   a.max_items = p.max_items;
   a.max_slots = p.max_slots;
-  a.target = p.target;
-  a.min_units = p.min_units;
-  a.rot_blocks = p.rot_blocks;
-  a.counts = reinterpret_cast<int32_t*>(ws + p.off_counts);
-  a.tile_start = reinterpret_cast<int32_t*>(ws + p.off_start);
+  a.piece_units = p.piece_units;
+  a.merge_units = p.merge_units;
+  a.head = reinterpret_cast<int32_t*>(ws + p.off_head);
+  a.item_start = reinterpret_cast<int32_t*>(ws + p.off_items);
+  a.tile_start = reinterpret_cast<int32_t*>(ws + p.off_starts);
   a.tiles = reinterpret_cast<ChunkTile*>(ws + p.off_tiles);
-  a.items = reinterpret_cast<ChunkItem*>(ws + p.off_items);
-  a.qrot = reinterpret_cast<uint16_t*>(ws + p.off_qrot);
-  a.qoff = reinterpret_cast<float*>(ws + p.off_qoff);
-  a.rv = reinterpret_cast<uint16_t*>(ws + p.off_rv);
   a.part = reinterpret_cast<float*>(ws + p.off_part);
   const int H = a.cv.num_kv_heads;
-  hipLaunchKernelGGL(chunk_prep_kernel, dim3(1 + H + H * p.rot_blocks), dim3(kPrepThreads), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  hipError_t e = hipSuccess;
+  if (a.B > kChunkWaveSeqs) {
+    hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   if (p.waves == 1)
     e = launch_chunk_few(a, s);
   else if (a.cv.groups == 4)

@@ -23,6 +23,8 @@ __device__ __forceinline__ int row_token(int m) { return (m & 3) | ((m & 4) << 1
 // The token (of its half) of register i, without the lane half's 8
 __device__ __forceinline__ constexpr int reg_token(int i) { return 16 * (i >> 3) + (i & 7); }
 
+constexpr int kMinPiece = 2;  // units
+
 struct Seq {
   int start, n, ctx;
 };
@@ -41,6 +43,142 @@ __device__ __forceinline__ int int2_units(const ChunkArgs& a, const Seq& s, int 
   return (lim + kUnit - 1) / kUnit;
 }
 __device__ __forceinline__ int own_units(const ChunkArgs& a, int i) { return a.k_new ? i / kUnit + 1 : 0; }
+
+// ---- The plan. A sequence's rows are tiles of bm; every tile of a sequence is cut into the same number of pieces, so that
+// its longest has about L units each, and a work-group takes one piece of one KV head. L comes from an estimate of the time
+// in units of work: while all pieces have a place on the chip at once, the longest; beyond that the average load and half a
+// piece; a piece costs piece_units beside its own units, a partial merge_units.
+struct Load {  // of one sequence: row tiles, and units of the last one
+  int tiles, units;
+};
+__device__ __forceinline__ Load load_of(const ChunkArgs& a, const Seq& s) {
+  const int rows = s.n * a.gq;
+  if (rows == 0) return Load{0, 0};
+  return Load{(rows + a.bm - 1) / a.bm, int2_units(a, s, s.n - 1) + own_units(a, s.n - 1)};
+}
+constexpr int kCuts = 16;
+// Candidate k: units of a piece. The last one fills the chip once.
+__device__ __forceinline__ int cut_of(const ChunkArgs& a, int k, int T, int umax) {
+  int j = k & 1 ? 3 << (k >> 1) >> 1 : 1 << (k >> 1);  // 1, 1, 2, 3, 4, 6, 8, 12 ..
+  if (k == kCuts - 1) j = a.resident / max(1, T * a.cv.num_kv_heads);
+  j = max(j, 1);
+  return max(kMinPiece, (umax + j - 1) / j);
+}
+__device__ __forceinline__ int pieces_of(const Load& s, int L) { return s.tiles == 0 ? 0 : max(1, (s.units + L - 1) / L); }
+// pieces[k]: all sequences' pieces at candidate k; W: their units
+__device__ __forceinline__ int pick_cut(const ChunkArgs& a, const int (&pieces)[kCuts], int T, float W, int umax) {
+  const float H = (float)a.cv.num_kv_heads, res = (float)a.resident;
+  const bool few = T * H <= res;
+  float best = 0.0f;
+  int L = 1;
+#pragma unroll
+  for (int k = 0; k < kCuts; ++k) {
+    const int c = cut_of(a, k, T, umax);
+    const float n = pieces[k] * H, one = (float)min(c, umax) + a.piece_units;
+    float cost = n <= res ? one : fmaxf((W * H + n * a.piece_units) / res, one) + 0.5f * one;
+    if (pieces[k] > T) cost += n * a.merge_units;
+    const bool fits = k == 0 || n <= (few ? res : 3.0f * res);
+    if (k == 0 || (fits && cost < best)) best = cost, L = c;
+  }
+  return L;
+}
+
+__device__ __forceinline__ int wave_sum(int x) {
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d);
+  return x;
+}
+__device__ __forceinline__ int wave_scan(int x) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+
+// A work-group's piece
+struct Place {
+  Seq s;
+  int b, row0;      // sequence, first row of the tile
+  int u0, u1;       // units
+  int slot;         // partial, -1: the result itself
+  bool valid;
+};
+// Piece `at` of the plan, found by every wave for itself. The last tiles come first: under a causal mask they are the
+// longest. Writes the record of a cut tile for the merge (first piece, head 0).
+__device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
+  const int lane = threadIdx.x & 63;
+  Place p;
+  p.valid = false;
+  int total, T, L, b, first, tile0;
+  if (a.B <= kChunkWaveSeqs) {
+    Seq s{0, 0, 0};
+    if (lane < a.B) s = seq_of(a, lane);
+    const Load load = load_of(a, s);
+    const int tiles = wave_scan(load.tiles);
+    T = __builtin_amdgcn_readlane(tiles, 63);
+    int umax = load.units;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) umax = max(umax, __shfl_xor(umax, d));
+    int pieces[kCuts];
+    if (a.B == 1) {
+#pragma unroll
+      for (int k = 0; k < kCuts; ++k) pieces[k] = __builtin_amdgcn_readlane(load.tiles * pieces_of(load, cut_of(a, k, T, umax)), 0);
+    } else {
+#pragma unroll
+      for (int k = 0; k < kCuts; ++k) pieces[k] = wave_sum(load.tiles * pieces_of(load, cut_of(a, k, T, umax)));
+    }
+    float W = (float)load.tiles * (float)load.units;
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) W += __shfl_xor(W, d);
+    L = pick_cut(a, pieces, T, W, umax);
+    const int mine = load.tiles * pieces_of(load, L), upto = wave_scan(mine);
+    total = __builtin_amdgcn_readlane(upto, 63);
+    if (at == 0 && h == 0 && threadIdx.x == 0) a.head[1] = total > a.max_items || T > a.max_tiles ? 0 : T;
+    total = min(total, a.max_items);
+    if (at >= total) return p;
+    const int i = total - 1 - at;
+    b = __popcll(__ballot(upto <= i));
+    first = __builtin_amdgcn_readlane(upto - mine, b);
+    tile0 = __builtin_amdgcn_readlane(tiles - load.tiles, b);
+    p.s = Seq{__builtin_amdgcn_readlane(s.start, b), __builtin_amdgcn_readlane(s.n, b), __builtin_amdgcn_readlane(s.ctx, b)};
+  } else {
+    total = a.head[0];
+    L = a.head[2];
+    if (at >= total) return p;
+    const int i = total - 1 - at;
+    // the last sequence whose pieces start at or before i, 64 probes at a time
+    int lo = 0, len = a.B;
+    while (len > 1) {
+      const int step = (len + 63) / 64, x = lo + lane * step;
+      const int n = __popcll(__ballot(lane * step < len && a.item_start[min(x, a.B - 1)] <= i));
+      lo += (n - 1) * step;
+      len = min(step, len - (n - 1) * step);
+    }
+    b = __builtin_amdgcn_readfirstlane(lo);
+    first = a.item_start[b];
+    tile0 = a.tile_start[b];
+    p.s = seq_of(a, b);
+  }
+  const Load load = load_of(a, p.s);
+  const int pieces = pieces_of(load, L), local = total - 1 - at - first, t = local / pieces, piece = local - t * pieces;
+  p.b = b;
+  p.row0 = t * a.bm;
+  const int i = (min(p.row0 + a.bm, p.s.n * a.gq) - 1) / a.gq, units = int2_units(a, p.s, i) + own_units(a, i);
+  p.u0 = (int)((long long)units * piece / pieces);
+  p.u1 = (int)((long long)units * (piece + 1) / pieces);
+  p.slot = pieces > 1 ? total - 1 - at : -1;
+  p.valid = t < load.tiles && p.slot < a.max_slots;
+  if (piece == 0 && h == 0 && threadIdx.x == 0 && tile0 + t < a.max_tiles)
+    a.tiles[tile0 + t] = ChunkTile{p.row0, p.s.start, p.s.n, pieces, p.slot};
+  // the same in every lane: into scalar registers
+  auto one = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
+  p.s = Seq{one(p.s.start), one(p.s.n), one(p.s.ctx)};
+  p.row0 = one(p.row0), p.u0 = one(p.u0), p.u1 = one(p.u1), p.slot = one(p.slot), p.b = one(p.b);
+  return p;
+}
 
 __device__ __forceinline__ cd_f16_t splat16(float x) {
   cd_f16_t v;
@@ -122,6 +260,25 @@ __device__ __forceinline__ void soften(const cd_f16_t& X, float base, float& sum
     P[i >> 2][i & 3] =
         Ops::pack(__builtin_amdgcn_exp2f(Ops::score(X[2 * i], base)), __builtin_amdgcn_exp2f(Ops::score(X[2 * i + 1], base)), sum);
 }
+// q mu^T of a lane's query row, in the scores' unit
+__device__ __forceinline__ float query_mean(const cd_b8_t (&Q)[8], const float* mu, int hh) {
+  float off = 0.0f;
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) {
+    const float4* x = reinterpret_cast<const float4*>(mu + 16 * kk + 8 * hh);
+    const float4 u = x[0], v = x[1];
+    const float y[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) off = __builtin_fmaf((float)Q[kk][j], y[j], off);
+  }
+  return pair_sum(off) * kLogit2;
+}
+// The query rotation q'^T = R_K^T q^T leaves positions 32 i .. 32 i + 31 of tile i in a lane's registers; position ->
+// channel: eight positions 2 kk + hh make operand kk's piece of lane half hh. Row m = 8 u + 4 h + v of a tile's A operand is
+// position 16 (u / 2) + 8 h + 4 (u % 2) + v, so that registers 8 x .. 8 x + 7 are operand 2 i + x as it is used.
+__device__ __forceinline__ int pos_channel(int pos) { return code_channel(pos >> 4, (pos >> 3) & 1, pos & 7); }
+__device__ __forceinline__ int row_position(int m) { return (m & 3) | ((m & 4) << 1) | ((m & 8) >> 1) | (m & 16); }
+
 // An operand with all but element j of the lanes that hold token t of a page cleared
 __device__ __forceinline__ cd_u4_t only_token(cd_u4_t x, int t) {
   const bool has = ((threadIdx.x >> 5) & 1) == (uint32_t)((t >> 3) & 1);

@@ -34,16 +34,50 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
   using Lay = Rec<NG>;
   __shared__ __align__(16) FewLds lds;
   const int H = a.cv.num_kv_heads;
-  const int h = (int)(blockIdx.x % H), at = (int)(blockIdx.x / H);
-  if (at >= a.counts[0]) return;
-  const ChunkItem item = a.items[at];
-  const ChunkTile tile = a.tiles[item.tile];
+  const int h = (int)(blockIdx.x % H);
+  const Place place = locate(a, (int)(blockIdx.x / H), h);
+  if (!place.valid) return;
+  const Seq seq = place.s;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = l & 31, hh = l >> 5;
-  const int rows = tile.n * a.gq, row = tile.row0 + n, rc = min(row, rows - 1), tok = rc / a.gq, tok_tile = tile.row0 / a.gq;
-  const int nI = int2_units(a, Seq{tile.start, tile.n, tile.ctx}, (min(tile.row0 + a.bm, rows) - 1) / a.gq);
-  const size_t grow = (size_t)h * a.total_q * a.gq + (size_t)tile.start * a.gq + rc;
-  auto limit = [&](int t) { return a.k_new ? tile.ctx : min(tile.ctx, tile.ctx - tile.n + 1 + t); };
+  const int rows = seq.n * a.gq, row = place.row0 + n, rc = min(row, rows - 1), tok = rc / a.gq, tok_tile = place.row0 / a.gq;
+  const int nI = int2_units(a, seq, (min(place.row0 + a.bm, rows) - 1) / a.gq);
+  auto limit = [&](int t) { return a.k_new ? seq.ctx : min(seq.ctx, seq.ctx - seq.n + 1 + t); };
   const int lim = limit(tok), lim_tile = limit(tok_tile);  // tokens the row sees, the least of the tile's
+
+  // the row's query: channels 16 kk + 8 hh .. of operand kk (read again for the chunk's own tokens)
+  const uint16_t* q = a.q + (seq.start + tok) * a.q_stride + (size_t)(h * a.gq + rc - tok * a.gq) * kHeadDim + 8 * hh;
+  auto query = [&](cd_b8_t (&x)[8]) {
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) x[kk] = *reinterpret_cast<const cd_b8_t*>(q + 16 * kk);
+  };
+  const bool cached = place.u0 < min(place.u1, nI);
+  if (cached) {
+    cd_b8_t Qb[8];
+    query(Qb);
+    // q R_K (chunk.hip: rotate_query): wave w forms the 32 positions of its tile, R_K's columns straight from memory
+    const float* R = a.R_k + (size_t)h * kHeadDim * kHeadDim + (size_t)(8 * hh) * kHeadDim + pos_channel(32 * w + row_position(n));
+    cd_f16_t d = splat16(0.0f);
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      cd_b8_t hi, lo;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float r = R[(size_t)(16 * kk + j) * kHeadDim];
+        hi[j] = (__bf16)r;
+        lo[j] = (__bf16)(r - (float)hi[j]);
+      }
+      d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, Qb[kk], d, 0, 0, 0);
+      d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, Qb[kk], d, 0, 0, 0);
+    }
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      cd_h8_t y;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = (_Float16)(d[8 * u + j] * kLogit2);
+      lds.b[2 * w + u][l] = y;
+    }
+    __syncthreads();
+  }
 
   float m = 0.0f, sum = 0.0f, thr = kNone;
   {
@@ -51,14 +85,14 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
 #pragma unroll
     for (int i = 0; i < 4; ++i) O[i] = splat16(0.0f);
     // ---- the wave's steps: a quarter of the piece's
-    const int pages = (tile.ctx + kBlock - 1) / kBlock;
-    const int p0 = kUnitPages * item.u0 / 2, p1 = min(kUnitPages * min(item.u1, nI), (pages + 1) & ~1) / 2;
+    const int pages = (seq.ctx + kBlock - 1) / kBlock;
+    const int p0 = kUnitPages * place.u0 / 2, p1 = min(kUnitPages * min(place.u1, nI), (pages + 1) & ~1) / 2;
     const int steps = max(p1 - p0, 0), s0 = p0 + steps * w / kFewWaves, s1 = p0 + steps * (w + 1) / kFewWaves;
     if (s0 < s1) {
       cd_h8_t Q[8];
 #pragma unroll
-      for (int kk = 0; kk < 8; ++kk) Q[kk] = *reinterpret_cast<const cd_h8_t*>(a.qrot + grow * kHeadDim + 16 * kk + 8 * hh);
-      const int32_t* table = a.table + (size_t)tile.b * a.max_blocks;
+      for (int kk = 0; kk < 8; ++kk) Q[kk] = lds.b[kk][l];
+      const int32_t* table = a.table + (size_t)place.b * a.max_blocks;
       // lane l: the block of page 2 list0 + l, read for 32 steps at a time
       int list0 = 0, list = 0;
       auto load_list = [&](int s) {
@@ -146,7 +180,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
             }
             if constexpr (part) {
               // tokens that do not exist are zero; values that are not finite are left for the second pass
-              int cnt = tile.ctx - (kStep * s + kBlock * pg);
+              int cnt = seq.ctx - (kStep * s + kBlock * pg);
               cnt = (ok >> pg) & 1 ? cnt : 0;
 #pragma unroll
               for (int x = 0; x < 4; ++x) {
@@ -234,7 +268,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
   }
   // wave w has the 32 channels of tile w from here on
   cd_f16_t O[1] = {splat16(0.0f)};
-  if (item.u0 < nI) {
+  if (cached) {
     const float inv = all == 0.0f ? 0.0f : 1.0f / all;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -270,19 +304,17 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
   sum = hh == 0 ? all : 0.0f;  // pair_sum adds the halves again
 
   // ---- the chunk's own tokens: every wave has all scores and its tile's values
-  const int c0 = max(item.u0 - nI, 0), c1 = item.u1 - nI;
+  const int c0 = max(place.u0 - nI, 0), c1 = place.u1 - nI;
   if (c0 < c1) {
-    cd_b8_t Q[8];
-    const uint16_t* q = a.q + (tile.start + tok) * a.q_stride + (size_t)(h * a.gq + rc - tok * a.gq) * kHeadDim + 8 * hh;
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) Q[kk] = *reinterpret_cast<const cd_b8_t*>(q + 16 * kk);
-    float base = kBias - m - a.qoff[grow];
-    const uint16_t* kb = a.k_new + tile.start * a.k_stride + (size_t)h * kHeadDim + 8 * hh;
+    cd_b8_t Qb[8];
+    query(Qb);
+    float base = kBias - m - query_mean(Qb, a.mu + (size_t)h * kHeadDim, hh);
+    const uint16_t* kb = a.k_new + seq.start * a.k_stride + (size_t)h * kHeadDim + 8 * hh;
     const int ch = 32 * w + 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
-    const uint16_t* vb = a.v_new + tile.start * a.v_stride + (size_t)h * kHeadDim + ch;
-    const int last = (min(tile.row0 + a.bm, rows) - 1) / a.gq;  // the tile's last token
+    const uint16_t* vb = a.v_new + seq.start * a.v_stride + (size_t)h * kHeadDim + ch;
+    const int last = (min(place.row0 + a.bm, rows) - 1) / a.gq;  // the tile's last token
     for (int s = c0 * (kUnit / kStep); s < c1 * (kUnit / kStep) && kStep * s <= last; ++s) {
-      const uint16_t* kr = kb + min(kStep * s + (n & 16) + row_token(n & 15), tile.n - 1) * a.k_stride;
+      const uint16_t* kr = kb + min(kStep * s + (n & 16) + row_token(n & 15), seq.n - 1) * a.k_stride;
       cd_h8_t k[8];
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) k[kk] = *reinterpret_cast<const cd_h8_t*>(kr + 16 * kk);
@@ -290,10 +322,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[pg][j] = vb[min(kStep * s + kBlock * pg + 8 * hh + j, tile.n - 1) * a.v_stride];
+        for (int j = 0; j < 8; ++j) v[pg][j] = vb[min(kStep * s + kBlock * pg + 8 * hh + j, seq.n - 1) * a.v_stride];
       cd_f16_t S = splat16(0.0f);
 #pragma unroll
-      for (int kk = 0; kk < 8; ++kk) S = BfOps::mfma(k[kk], Q[kk], S);
+      for (int kk = 0; kk < 8; ++kk) S = BfOps::mfma(k[kk], Qb[kk], S);
 #pragma unroll
       for (int i = 0; i < 16; ++i) S[i] = kStep * s + reg_token(i) + 8 * hh <= tok ? S[i] : -INFINITY;
       settle<BfOps>(S, base, m, sum, thr, O);
@@ -306,7 +338,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const int t = kStep * s + kBlock * pg + 8 * hh + 2 * x;
-          const uint32_t pair = (t < tile.n ? v[pg][2 * x] : 0u) | (t + 1 < tile.n ? v[pg][2 * x + 1] << 16 : 0u), odd = BfOps::odd(pair);
+          const uint32_t pair = (t < seq.n ? v[pg][2 * x] : 0u) | (t + 1 < seq.n ? v[pg][2 * x + 1] << 16 : 0u), odd = BfOps::odd(pair);
           found |= odd;
           y[pg][x] = pair & ~odd;
           z[pg][x] = pair & odd;
@@ -328,9 +360,9 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
   // ---- results: registers 8 x .. 8 x + 7 are channels 32 w + 16 x + 8 hh ..
   all = pair_sum(sum);
   if (row >= rows) return;
-  if (item.slot < 0) {
+  if (place.slot < 0) {
     const float inv = all == 0.0f ? 0.0f : 1.0f / all;
-    uint16_t* o = a.out + ((size_t)(tile.start + tok) * a.Hq + h * a.gq + row - tok * a.gq) * kHeadDim + 32 * w + 8 * hh;
+    uint16_t* o = a.out + ((size_t)(seq.start + tok) * a.Hq + h * a.gq + row - tok * a.gq) * kHeadDim + 32 * w + 8 * hh;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
       uint32_t y[4];
@@ -339,7 +371,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
       *reinterpret_cast<uint4*>(o + 16 * x) = make_uint4(y[0], y[1], y[2], y[3]);
     }
   } else {
-    float* part = a.part + ((size_t)item.slot * H + h) * a.bm * kChunkPartStride;
+    float* part = a.part + ((size_t)place.slot * H + h) * a.bm * kChunkPartStride;
     float* o = part + (size_t)n * kHeadDim + 32 * w + 8 * hh;
 #pragma unroll
     for (int x = 0; x < 2; ++x) {

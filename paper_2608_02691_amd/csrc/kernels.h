@@ -185,16 +185,12 @@ hipError_t launch_read_rows(CacheView c, const int32_t* slots, int n, const floa
                             bool f32, void* k_out, void* v_out, hipStream_t s);
 
 // ---- attention of a chunk of new tokens (chunk.hip)
-struct ChunkTile {  // a tile of query rows of one sequence (the same for every KV head)
-  int b, row0;        // sequence, first row
-  int start, n, ctx;  // the sequence's first token in q, its new and its cached tokens
-  int units;          // 64-token units of its context
-  int pieces, slot;   // pieces it is cut into, and the first one's partial (-1: one piece, no partial)
-};
-struct ChunkItem {  // a piece: units u0 .. u1 of a tile, its partial's slot (-1: the result itself)
-  int tile, u0, u1, slot;
+struct ChunkTile {  // a tile of query rows of one sequence that was cut (the same for every KV head)
+  int row0, start, n;  // its first row; the sequence's first token in q and its new tokens
+  int pieces, slot;    // pieces it is cut into, and the first one's partial
 };
 constexpr int kChunkPartStride = kHeadDim + 2;  // sums, then m and l
+constexpr int kChunkWaveSeqs = 64;              // up to so many sequences every work-group plans by itself
 struct ChunkArgs {
   CacheView cv;
   const uint16_t* q;                // bf16, token t, head j at t * q_stride + 128 j
@@ -209,19 +205,18 @@ struct ChunkArgs {
   const uint16_t *k_new, *v_new;    // the chunk's own keys and values, or null: the cache holds them
   const float* mu;
   uint16_t* out;                    // bf16 [total_q, Hq, 128]
-  // workspace and plan
-  int bm, max_tiles, max_items, max_slots, target, min_units, rot_blocks;
-  int32_t *counts, *tile_start;
-  ChunkTile* tiles;
-  ChunkItem* items;
-  uint16_t* qrot;                   // fp16 [H, total_q * gq, 128], in operand order
-  float* qoff;                      // [H, total_q * gq]: q mu^T in the scores' unit
-  uint16_t* rv;                     // fp16 operands of R_V
-  float* part;
+  // plan and workspace
+  int bm, resident, max_tiles, max_items, max_slots;
+  float piece_units, merge_units;
+  int32_t* head;                    // pieces (per KV head), tiles, units of a piece
+  int32_t *item_start, *tile_start; // [B] (batches above kChunkWaveSeqs)
+  ChunkTile* tiles;                 // [max_tiles]
+  float* part;                      // [max_slots, H, bm * kChunkPartStride]
 };
 struct ChunkPlan {
-  int waves, bm, max_tiles, max_items, max_slots, target, min_units, rot_blocks;
-  size_t off_counts, off_start, off_tiles, off_items, off_qrot, off_qoff, off_rv, off_part, total;
+  int waves, bm, resident, max_tiles, max_items, max_slots;
+  float piece_units, merge_units;
+  size_t off_head, off_items, off_starts, off_tiles, off_part, total;
 };
 ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx);
 hipError_t launch_chunk_few(const ChunkArgs& a, hipStream_t s);  // (chunk_few.hip) tiles of 32 rows
