@@ -65,7 +65,7 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   for (int b = tid; b < a.B; b += kPlanThreads) {
     const Load s = load_of(a, seq_of(a, b));
 #pragma unroll
-    for (int k = 0; k < kCuts; ++k) mine[k] += s.tiles * pieces_of(s, cut_of(a, k, T, umax));
+    for (int k = 0; k < kCuts; ++k) mine[k] += s.tiles * pieces_of(s, cut_of(a, k, (float)work, umax));
   }
 #pragma unroll
   for (int k = 0; k < kCuts; ++k) atomicAdd(&counts[k], mine[k]);
@@ -115,19 +115,19 @@ template <class Ops, class Src>
 __device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, const typename Ops::vec (&Q)[8], float off, int u0,
                                        int u1) {
   const int l = threadIdx.x & 63;
-  cd_f16_t S, T;
+  cd_f16_t S[1], T[1];
   float base = kBias - st.m - off;
   // scores of half tm of the unit in slot kb
-  auto scores = [&](cd_f16_t& X, int kb, int tm) {
-    X = splat16(Ops::start(base));
+  auto scores = [&](cd_f16_t (&X)[1], int kb, int tm) {
+    X[0] = splat16(0.0f);
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) X = Ops::mfma(lds.k[kb][8 * tm + kk][l], Q[kk], X);
+    for (int kk = 0; kk < 8; ++kk) X[0] = Ops::mfma(lds.k[kb][8 * tm + kk][l], Q[kk], X[0]);
   };
   // hides what a row does not see
-  auto rest = [&](cd_f16_t& X, int u, int tm) {
+  auto rest = [&](cd_f16_t (&X)[1], int u, int tm) {
     if (src.masked(u)) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) X[i] = src.sees(u, 32 * tm + reg_token(i)) ? X[i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) X[0][i] = src.sees(u, 32 * tm + reg_token(i)) ? X[0][i] : -INFINITY;
     }
     settle<Ops>(X, base, st.m, st.sum, st.thr, st.O);
   };
@@ -151,7 +151,7 @@ __device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, co
     const int vn = vb == 2 ? 0 : vb + 1;
     cd_u4_t P[2];
     scores(T, kb, 1);
-    soften<Ops>(S, base, st.sum, P);
+    soften<Ops>(S[0], base, st.sum, P);
     add(P, vb, 0);
     rest(T, u, 1);
     if (more) {
@@ -160,7 +160,7 @@ __device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, co
     }
     __syncthreads();
     if (more) scores(S, kb ^ 1, 0);
-    soften<Ops>(T, base, st.sum, P);
+    soften<Ops>(T[0], base, st.sum, P);
     add(P, vb, 1);
     if (more) rest(S, u + 1, 0);
     kb ^= 1;
@@ -186,10 +186,10 @@ __device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, co
       for (int tm = 0; tm < 2; ++tm) {
         scores(S, 0, tm);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) S[i] = src.sees(u, 32 * tm + reg_token(i)) ? S[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) S[0][i] = src.sees(u, 32 * tm + reg_token(i)) ? S[0][i] : -INFINITY;
         cd_u4_t P[2];
         float sum = 0.0f;  // already counted
-        soften<Ops>(S, base, sum, P);
+        soften<Ops>(S[0], base, sum, P);
         for (int t = 0; t < 32; ++t) {
           const int pg = t >> 4;
           const bool see = src.sees_token(u, 32 * tm + t);
@@ -590,6 +590,7 @@ ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_
   p.waves = seq_rows <= 64 ? 1 : seq_rows <= 128 ? 4 : 8;
   p.bm = 32 * p.waves;
   p.resident = num_cus() * (p.waves == 8 ? 1 : 2);
+  p.min_piece = p.waves == 1 ? 4 : 2;  // a unit for each wave of the kernel of few rows
   p.piece_units = p.waves == 1 ? 10.0f : 3.0f;
   p.merge_units = p.waves == 1 ? 0.016f : 0.00013f * p.bm;
   const long long per_seq = (seq_rows + p.bm - 1) / p.bm;
@@ -597,7 +598,7 @@ ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_
   tiles = tiles < by_rows ? tiles : by_rows;
   p.max_tiles = (int)(tiles < 1 ? 1 : tiles);
   // pieces a KV head: a place on the chip each while the tiles have one, else up to three; never more than the units allow
-  const long long most = ((long long)max_ctx + 63) / 64 + ((long long)max_q + 63) / 64, cuts = (most + 1) / 2;
+  const long long most = ((long long)max_ctx + 63) / 64 + ((long long)max_q + 63) / 64, cuts = (most + p.min_piece - 1) / p.min_piece;
   const long long places = (tiles * H <= p.resident ? 1LL : 3LL) * p.resident / H;
   long long cut = places < p.max_tiles * cuts ? places : p.max_tiles * cuts;
   p.max_slots = (int)(cut > 1 ? cut : 1);
@@ -628,6 +629,7 @@ hipError_t launch_attn(const ChunkArgs& a, hipStream_t s) {
 hipError_t launch_chunk_attention(ChunkArgs a, const ChunkPlan& p, uint8_t* ws, hipStream_t s) {
   a.bm = p.bm;
   a.resident = p.resident;
+  a.min_piece = p.min_piece;
   a.max_tiles = p.max_tiles;
   a.max_items = p.max_items;
   a.max_slots = p.max_slots;

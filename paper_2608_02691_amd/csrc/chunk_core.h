@@ -23,8 +23,6 @@ __device__ __forceinline__ int row_token(int m) { return (m & 3) | ((m & 4) << 1
 // The token (of its half) of register i, without the lane half's 8
 __device__ __forceinline__ constexpr int reg_token(int i) { return 16 * (i >> 3) + (i & 7); }
 
-constexpr int kMinPiece = 2;  // units
-
 struct Seq {
   int start, n, ctx;
 };
@@ -56,15 +54,23 @@ __device__ __forceinline__ Load load_of(const ChunkArgs& a, const Seq& s) {
   if (rows == 0) return Load{0, 0};
   return Load{(rows + a.bm - 1) / a.bm, int2_units(a, s, s.n - 1) + own_units(a, s.n - 1)};
 }
-constexpr int kCuts = 16;
-// Candidate k: units of a piece. The last one fills the chip once.
-__device__ __forceinline__ int cut_of(const ChunkArgs& a, int k, int T, int umax) {
-  int j = k & 1 ? 3 << (k >> 1) >> 1 : 1 << (k >> 1);  // 1, 1, 2, 3, 4, 6, 8, 12 ..
-  if (k == kCuts - 1) j = a.resident / max(1, T * a.cv.num_kv_heads);
-  j = max(j, 1);
-  return max(kMinPiece, (umax + j - 1) / j);
+constexpr int kCuts = 12;
+// Candidate k: units of a piece. The first leaves the tiles whole; the others lie above the size that would fill the places
+// on the chip evenly, once or (from 8 on) three times.
+__device__ __forceinline__ int cut_of(const ChunkArgs& a, int k, float W, int umax) {
+  if (k == 0) return max(umax, 1);
+  const float even = W * (float)a.cv.num_kv_heads / (float)a.resident;
+  const float c = k < 8 ? even * (1.0f + 0.15f * (float)(k - 1)) : even * (0.35f + 0.15f * (float)(k - 8));
+  return max(a.min_piece, (int)c + 1);
 }
-__device__ __forceinline__ int pieces_of(const Load& s, int L) { return s.tiles == 0 ? 0 : max(1, (s.units + L - 1) / L); }
+// x / d for 0 <= x < 2^24, 0 < d, without a branch
+__device__ __forceinline__ int quotient(int x, int d) {
+  int q = (int)((float)x * __builtin_amdgcn_rcpf((float)d));
+  const int r = x - q * d;
+  q += r >= d ? 1 : 0;
+  return q - (r < 0 ? 1 : 0);
+}
+__device__ __forceinline__ int pieces_of(const Load& s, int L) { return s.tiles == 0 ? 0 : max(1, quotient(s.units + L - 1, L)); }
 // pieces[k]: all sequences' pieces at candidate k; W: their units
 __device__ __forceinline__ int pick_cut(const ChunkArgs& a, const int (&pieces)[kCuts], int T, float W, int umax) {
   const float H = (float)a.cv.num_kv_heads, res = (float)a.resident;
@@ -73,7 +79,7 @@ __device__ __forceinline__ int pick_cut(const ChunkArgs& a, const int (&pieces)[
   int L = 1;
 #pragma unroll
   for (int k = 0; k < kCuts; ++k) {
-    const int c = cut_of(a, k, T, umax);
+    const int c = cut_of(a, k, W, umax);
     const float n = pieces[k] * H, one = (float)min(c, umax) + a.piece_units;
     float cost = n <= res ? one : fmaxf((W * H + n * a.piece_units) / res, one) + 0.5f * one;
     if (pieces[k] > T) cost += n * a.merge_units;
@@ -83,10 +89,20 @@ __device__ __forceinline__ int pick_cut(const ChunkArgs& a, const int (&pieces)[
   return L;
 }
 
+// Sum and maximum over the wave: rotations inside rows of 16 lanes, then swaps of rows and halves
+template <class F>
+__device__ __forceinline__ int wave_fold(int x, F f) {
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x128, 0xF, 0xF, false));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x124, 0xF, 0xF, false));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x122, 0xF, 0xF, false));
+  x = f(x, __builtin_amdgcn_update_dpp(0, x, 0x121, 0xF, 0xF, false));
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = f((int)r[0], (int)r[1]);
+  const auto h = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return f((int)h[0], (int)h[1]);
+}
 __device__ __forceinline__ int wave_sum(int x) {
-#pragma unroll
-  for (int d = 32; d >= 1; d >>= 1) x += __shfl_xor(x, d);
-  return x;
+  return wave_fold(x, [](int a, int b) { return a + b; });
 }
 __device__ __forceinline__ int wave_scan(int x) {
   const int lane = threadIdx.x & 63;
@@ -119,20 +135,21 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
     const Load load = load_of(a, s);
     const int tiles = wave_scan(load.tiles);
     T = __builtin_amdgcn_readlane(tiles, 63);
-    int umax = load.units;
-#pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) umax = max(umax, __shfl_xor(umax, d));
-    int pieces[kCuts];
-    if (a.B == 1) {
-#pragma unroll
-      for (int k = 0; k < kCuts; ++k) pieces[k] = __builtin_amdgcn_readlane(load.tiles * pieces_of(load, cut_of(a, k, T, umax)), 0);
-    } else {
-#pragma unroll
-      for (int k = 0; k < kCuts; ++k) pieces[k] = wave_sum(load.tiles * pieces_of(load, cut_of(a, k, T, umax)));
-    }
+    const int umax = wave_fold(load.units, [](int a, int b) { return max(a, b); });
     float W = (float)load.tiles * (float)load.units;
+    if (a.B > 1) {
+      // units times tiles in two integers, so that the sum is the same however it is formed
+      const long long w = (long long)load.tiles * load.units;
+      W = (float)wave_sum((int)(w >> 20)) * 1048576.0f + (float)wave_sum((int)(w & 0xFFFFF));
+    } else {
+      W = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(W)));
+    }
+    int pieces[kCuts];
 #pragma unroll
-    for (int d = 32; d >= 1; d >>= 1) W += __shfl_xor(W, d);
+    for (int k = 0; k < kCuts; ++k) {
+      const int n = load.tiles * pieces_of(load, cut_of(a, k, W, umax));
+      pieces[k] = a.B > 1 ? wave_sum(n) : __builtin_amdgcn_readfirstlane(n);
+    }
     L = pick_cut(a, pieces, T, W, umax);
     const int mine = load.tiles * pieces_of(load, L), upto = wave_scan(mine);
     total = __builtin_amdgcn_readlane(upto, 63);
@@ -163,7 +180,7 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
     p.s = seq_of(a, b);
   }
   const Load load = load_of(a, p.s);
-  const int pieces = pieces_of(load, L), local = total - 1 - at - first, t = local / pieces, piece = local - t * pieces;
+  const int pieces = pieces_of(load, L), local = total - 1 - at - first, t = quotient(local, pieces), piece = local - t * pieces;
   p.b = b;
   p.row0 = t * a.bm;
   const int i = (min(p.row0 + a.bm, p.s.n * a.gq) - 1) / a.gq, units = int2_units(a, p.s, i) + own_units(a, i);
@@ -202,8 +219,7 @@ struct HalfOps {
   static __device__ __forceinline__ cd_f16_t mfma(const cd_h8_t& a, const vec& b, const cd_f16_t& c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
-  static __device__ __forceinline__ float start(float base) { return base; }
-  static __device__ __forceinline__ float score(float s, float) { return s; }
+  static __device__ __forceinline__ float score(float s, float base) { return s + base; }
   static __device__ __forceinline__ uint32_t pack(float a, float b, float& sum) {
     typedef float f2 __attribute__((ext_vector_type(2)));
     const cd_h2_t p = __builtin_convertvector((f2{a, b}), cd_h2_t);
@@ -221,7 +237,6 @@ struct BfOps {
   static __device__ __forceinline__ cd_f16_t mfma(const cd_h8_t& a, const vec& b, const cd_f16_t& c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(cd_b8_t, a), b, c, 0, 0, 0);
   }
-  static __device__ __forceinline__ float start(float) { return 0.0f; }
   static __device__ __forceinline__ float score(float s, float base) { return __builtin_fmaf(s, kLogit2, base); }
   static __device__ __forceinline__ uint32_t pack(float a, float b, float& sum) {
     sum += a + b;
@@ -233,11 +248,11 @@ struct BfOps {
 };
 
 // Moves m where a score of the step exceeds it by 2^kLazy (the lane's own scores and its partner's)
-template <class Ops, int TILES>
-__device__ __forceinline__ void settle(cd_f16_t& X, float& base, float& m, float& sum, float& thr, cd_f16_t (&O)[TILES]) {
-  float a = fmaxf(X[0], X[1]);
+template <class Ops, int N, int TILES>
+__device__ __forceinline__ void settle(const cd_f16_t (&X)[N], float& base, float& m, float& sum, float& thr, cd_f16_t (&O)[TILES]) {
+  float a = fmaxf(X[0][0], X[0][1]);
 #pragma unroll
-  for (int i = 2; i < 16; i += 2) a = fmaxf(fmaxf(a, X[i]), X[i + 1]);
+  for (int i = 2; i < 16 * N; i += 2) a = fmaxf(fmaxf(a, X[i >> 4][i & 15]), X[i >> 4][(i & 15) + 1]);
   const float top = Ops::score(pair_max(a), base);
   const bool move = top > thr;
   if (__any(move)) {
@@ -249,7 +264,6 @@ __device__ __forceinline__ void settle(cd_f16_t& X, float& base, float& m, float
     thr = move ? kMove : thr;
 #pragma unroll
     for (int i = 0; i < TILES; ++i) O[i] *= f;
-    X -= splat16(Ops::start(d));
   }
 }
 // Probabilities of a step as operands: page pg of the half takes registers 8 pg .. 8 pg + 7

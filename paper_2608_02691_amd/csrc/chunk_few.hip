@@ -1,7 +1,7 @@
 // Attention of few new tokens per sequence (int2kv_chunk_attention, at most 32 query rows a tile): drafted tokens, short
 // turns. Bound by the cache's bytes and, close behind, by the vector ALU that makes operands of its codes, so nothing is
-// shared and nothing waited for: the four waves of a work-group hold the same 32 rows and take different 32-token steps of
-// the context, each with its own records on their way to LDS (LDS-DMA, kAhead steps ahead) and its own softmax. Codes
+// shared and nothing waited for: the four waves of a work-group hold the same 32 rows and take different 64-token units of
+// the context, each with the next unit's records on their way to LDS (LDS-DMA) and its own softmax. Codes
 // become matrix operands in the registers they are used from. At the end the four partial results meet in LDS, each wave
 // un-rotates the 32 channels of its tile and adds the chunk's own bf16 tokens to them.
 #include <type_traits>
@@ -14,8 +14,8 @@ namespace int2kv {
 namespace {
 
 constexpr int kFewWaves = 4;
-constexpr int kStep = 32;                 // tokens of a step: two pages
-constexpr int kStages = 4, kAhead = kStages - 1;
+constexpr int kStep = 32;                 // tokens of a step over the chunk's own
+constexpr int kStages = 4;                // two units, two stages each
 constexpr int kStageBytes = 3072;         // codes of two pages, then 512 bytes each of their parameters
 
 struct FewLds {
@@ -51,113 +51,134 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
     for (int kk = 0; kk < 8; ++kk) x[kk] = *reinterpret_cast<const cd_b8_t*>(q + 16 * kk);
   };
   const bool cached = place.u0 < min(place.u1, nI);
-  if (cached) {
-    cd_b8_t Qb[8];
-    query(Qb);
-    // q R_K (chunk.hip: rotate_query): wave w forms the 32 positions of its tile, R_K's columns straight from memory
-    const float* R = a.R_k + (size_t)h * kHeadDim * kHeadDim + (size_t)(8 * hh) * kHeadDim + pos_channel(32 * w + row_position(n));
-    cd_f16_t d = splat16(0.0f);
-#pragma unroll
-    for (int kk = 0; kk < 8; ++kk) {
-      cd_b8_t hi, lo;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float r = R[(size_t)(16 * kk + j) * kHeadDim];
-        hi[j] = (__bf16)r;
-        lo[j] = (__bf16)(r - (float)hi[j]);
-      }
-      d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, Qb[kk], d, 0, 0, 0);
-      d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, Qb[kk], d, 0, 0, 0);
-    }
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      cd_h8_t y;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = (_Float16)(d[8 * u + j] * kLogit2);
-      lds.b[2 * w + u][l] = y;
-    }
-    __syncthreads();
-  }
-
   float m = 0.0f, sum = 0.0f, thr = kNone;
   {
     cd_f16_t O[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) O[i] = splat16(0.0f);
-    // ---- the wave's steps: a quarter of the piece's
+    // ---- the wave's units: a quarter of the piece's
     const int pages = (seq.ctx + kBlock - 1) / kBlock;
-    const int p0 = kUnitPages * place.u0 / 2, p1 = min(kUnitPages * min(place.u1, nI), (pages + 1) & ~1) / 2;
-    const int steps = max(p1 - p0, 0), s0 = p0 + steps * w / kFewWaves, s1 = p0 + steps * (w + 1) / kFewWaves;
-    if (s0 < s1) {
-      cd_h8_t Q[8];
+    const int units = max(min(place.u1, nI) - place.u0, 0), s0 = place.u0 + units * w / kFewWaves, s1 = place.u0 + units * (w + 1) / kFewWaves;
+    const int32_t* table = a.table + (size_t)place.b * a.max_blocks;
+    // lane l: the block of page 4 list0 + l, read for 16 units at a time
+    int list0 = 0, list = 0;
+    auto load_list = [&](int s) {
+      list0 = s;
+      const int p = kUnitPages * s + l;
+      list = p < pages ? table[p] : -1;
+      // taken here, so that the wait for it stands here and not, for all loads on their way, before its uses in the loop
+      asm volatile("" : "+v"(list));
+    };
+    auto good = [&](int id) { return id >= 0 && id < a.cv.num_blocks; };
+    auto block = [&](int s, int x) { return __builtin_amdgcn_readlane(list, kUnitPages * (s - list0) + x); };
+    const uint32_t stage0 = (uint32_t)(uintptr_t)(&lds.stage[w][0][0]);
+    // the records of a unit on their way to its two stages, two pages each
+    auto issue = [&](int s) {
 #pragma unroll
-      for (int kk = 0; kk < 8; ++kk) Q[kk] = lds.b[kk][l];
-      const int32_t* table = a.table + (size_t)place.b * a.max_blocks;
-      // lane l: the block of page 2 list0 + l, read for 32 steps at a time
-      int list0 = 0, list = 0;
-      auto load_list = [&](int s) {
-        list0 = s;
-        const int p = 2 * s + l;
-        list = p < pages ? table[p] : -1;
-      };
-      auto good = [&](int id) { return id >= 0 && id < a.cv.num_blocks; };
-      auto block = [&](int s, int x) { return __builtin_amdgcn_readlane(list, 2 * (s - list0) + x); };
-      const uint32_t stage0 = (uint32_t)(uintptr_t)(&lds.stage[w][0][0]);
-      auto issue = [&](int s) {  // the step's two records on their way to its stage
+      for (int half = 0; half < 2; ++half) {
         const uint8_t* r[2];
 #pragma unroll
         for (int x = 0; x < 2; ++x) {
-          const int id = block(s, x);
+          const int id = block(s, 2 * half + x);
           r[x] = a.cv.pool + ((size_t)(uint32_t)(good(id) ? id : 0) * H + h) * Lay::kBytes;
         }
-        const uint32_t to = stage0 + (uint32_t)(s & (kStages - 1)) * kStageBytes;
+        const uint32_t to = stage0 + (uint32_t)(2 * (s & 1) + half) * kStageBytes;
         ap_dma16(r[0] + 16 * l, to);
         ap_dma16(r[1] + 16 * l, to + 1024);
         // a page's 128 NG bytes of parameters; lanes past them read the last 16 again
         ap_dma16((l < 32 ? r[0] : r[1]) + 1024 + min(16 * (l & 31), 128 * NG - 16), to + 2048);
-      };
-      const int tA = row_token(n & 15), pgA = n >> 4;  // the token whose keys this lane's A rows are
+      }
+    };
+    if (s0 < s1) {
+      load_list(s0);
+      issue(s0);
+      if (s0 + 1 < s1) issue(s0 + 1);
+    }
+    if (cached) {
+      // q R_K with log2(e) / sqrt(128): wave w forms the 32 channels 32 w .. of q', R_K's columns straight from memory in
+      // two bf16 terms (q is exact), and puts them where the products take them
+      cd_b8_t Qb[8];
+      query(Qb);
+      const float* R = a.R_k + (size_t)h * kHeadDim * kHeadDim + (size_t)(8 * hh) * kHeadDim + 32 * w + n;
+      cd_f16_t d = splat16(0.0f);
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) {
+        cd_b8_t hi, lo;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float r = R[(size_t)(16 * kk + j) * kHeadDim];
+          hi[j] = (__bf16)r;
+          lo[j] = (__bf16)(r - (float)hi[j]);
+        }
+        d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, Qb[kk], d, 0, 0, 0);
+        d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, Qb[kk], d, 0, 0, 0);
+      }
+      // register r: channel 32 w + c, c = 8 (r / 4) + 4 hh + r % 4; channels 16 p + 2 x, + 1 are elements 2 (p % 4), + 1 of
+      // operand 2 (x % 4) + p / 4 in lane half x / 4
+#pragma unroll
+      for (int r = 0; r < 16; r += 2) {
+        const int p = 2 * w + (r >> 3), x = 4 * ((r >> 2) & 1) + 2 * hh + ((r & 3) >> 1);
+        const cd_h2_t y = {(_Float16)(d[r] * kLogit2), (_Float16)(d[r + 1] * kLogit2)};
+        reinterpret_cast<uint32_t*>(&lds.b[2 * (x & 3) + (p >> 2)][32 * (x >> 2) + n])[p & 3] = __builtin_bit_cast(uint32_t, y);
+      }
+      __syncthreads();
+    }
+    if (s0 < s1) {
+      cd_h8_t Q[8];
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) Q[kk] = lds.b[kk][l];
+      const int tA = row_token(n & 15), pgA = n >> 4;  // the token (of a half) whose keys this lane's A rows are
       float base = kBias;
       uint32_t found = 0;
-      auto whole = [&](int s) { return good(block(s, 0)) && good(block(s, 1)) && kStep * (s + 1) <= lim_tile; };
-      // One step: scores, probabilities, values. PART: some row does not see all of it. SECOND: only the values that are not
+      auto whole = [&](int s) {
+        return good(block(s, 0)) && good(block(s, 1)) && good(block(s, 2)) && good(block(s, 3)) && kUnit * (s + 1) <= lim_tile;
+      };
+      // One unit: scores, probabilities, values. PART: some row does not see all of it. SECOND: only the values that are not
       // finite, for the rows that see them
       auto take = [&](int s, auto part_c, auto second_c) {
         constexpr bool part = decltype(part_c)::value, second = decltype(second_c)::value;
-        const uint8_t* st = lds.stage[w][s & (kStages - 1)];
-        const cd_u4_t kc = *reinterpret_cast<const cd_u4_t*>(st + 1024 * pgA + 32 * tA + 16 * hh);
-        uint32_t km[NG];
-#pragma unroll
-        for (int g = 0; g < NG; ++g) km[g] = *reinterpret_cast<const uint32_t*>(st + 2048 + 512 * pgA + 4 * NG * tA + 4 * g);
-        cd_h2_t ks[NG], kz[NG];
-#pragma unroll
-        for (int g = 0; g < NG; ++g) ks[g] = both_lo(km[g]), kz[g] = both_hi(km[g]);
-        cd_f16_t S = splat16(base);
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          cd_h8_t k[2];
-          word_operands<NG>(kc[x], ks, kz, k);
-          S = HalfOps::mfma(k[0], Q[2 * x], S);
-          S = HalfOps::mfma(k[1], Q[2 * x + 1], S);
-        }
-        const uint32_t ok = !part ? 3u : (good(block(s, 0)) ? 1u : 0u) | (good(block(s, 1)) ? 2u : 0u);
+        const uint8_t* st = lds.stage[w][2 * (s & 1)];
+        uint32_t ok = 15u;
         if constexpr (part) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            S[i] = ((ok >> (i >> 3)) & 1) && kStep * s + reg_token(i) + 8 * hh < lim ? S[i] : -INFINITY;
+          for (int x = 0; x < 4; ++x) ok &= good(block(s, x)) ? 15u : ~(1u << x);
         }
-        cd_u4_t P[2];
-        if constexpr (!second) {
-          settle<HalfOps>(S, base, m, sum, thr, O);
-          soften<HalfOps>(S, base, sum, P);
-        } else {
-          float none = 0.0f;
-          soften<HalfOps>(S, base, none, P);
-        }
+        cd_f16_t S[2];
 #pragma unroll
-        for (int pg = 0; pg < 2; ++pg) {
-          const uint8_t* vm = st + 2048 + 512 * pg + 16 * hh;
-          const cd_u4_t vc = *reinterpret_cast<const cd_u4_t*>(st + 1024 * pg + 512 + 32 * (n & 15) + 16 * hh);
+        for (int tm = 0; tm < 2; ++tm) {
+          const uint8_t* half = st + tm * kStageBytes;
+          const cd_u4_t kc = *reinterpret_cast<const cd_u4_t*>(half + 1024 * pgA + 32 * tA + 16 * hh);
+          uint32_t km[NG];
+#pragma unroll
+          for (int g = 0; g < NG; ++g) km[g] = *reinterpret_cast<const uint32_t*>(half + 2048 + 512 * pgA + 4 * NG * tA + 4 * g);
+          cd_h2_t ks[NG], kz[NG];
+#pragma unroll
+          for (int g = 0; g < NG; ++g) ks[g] = both_lo(km[g]), kz[g] = both_hi(km[g]);
+          S[tm] = splat16(0.0f);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            cd_h8_t k[2];
+            word_operands<NG>(kc[x], ks, kz, k);
+            S[tm] = HalfOps::mfma(k[0], Q[2 * x], S[tm]);
+            S[tm] = HalfOps::mfma(k[1], Q[2 * x + 1], S[tm]);
+          }
+          if constexpr (part) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              S[tm][i] = ((ok >> (2 * tm + (i >> 3))) & 1) && kUnit * s + 32 * tm + reg_token(i) + 8 * hh < lim ? S[tm][i] : -INFINITY;
+          }
+        }
+        cd_u4_t P[2][2];
+        float none = 0.0f;
+        if constexpr (!second) settle<HalfOps>(S, base, m, sum, thr, O);
+#pragma unroll
+        for (int tm = 0; tm < 2; ++tm) soften<HalfOps>(S[tm], base, second ? none : sum, P[tm]);
+#pragma unroll
+        for (int pg = 0; pg < 4; ++pg) {
+          const uint8_t* half = st + (pg >> 1) * kStageBytes;
+          const uint8_t* vm = half + 2048 + 512 * (pg & 1) + 16 * hh;
+          const cd_u4_t vc = *reinterpret_cast<const cd_u4_t*>(half + 1024 * (pg & 1) + 512 + 32 * (n & 15) + 16 * hh);
+          const cd_u4_t p = P[pg >> 1][pg & 1];
           uint32_t word[4];
 #pragma unroll
           for (int x = 0; x < 4; ++x) word[x] = vc[x] >> (2 * (n >> 4));
@@ -180,7 +201,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
             }
             if constexpr (part) {
               // tokens that do not exist are zero; values that are not finite are left for the second pass
-              int cnt = seq.ctx - (kStep * s + kBlock * pg);
+              int cnt = seq.ctx - (kUnit * s + kBlock * pg);
               cnt = (ok >> pg) & 1 ? cnt : 0;
 #pragma unroll
               for (int x = 0; x < 4; ++x) {
@@ -192,11 +213,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
               }
             }
             if constexpr (!second) {
-              O[i] = HalfOps::mfma(__builtin_bit_cast(cd_h8_t, f), __builtin_bit_cast(cd_h8_t, P[pg]), O[i]);
+              O[i] = HalfOps::mfma(__builtin_bit_cast(cd_h8_t, f), __builtin_bit_cast(cd_h8_t, p), O[i]);
             } else {
-              for (int t = 0; t < 16; ++t) {
-                const bool see = ((ok >> pg) & 1) && kStep * s + kBlock * pg + t < lim;
-                const cd_f16_t d = HalfOps::mfma(__builtin_bit_cast(cd_h8_t, only_token(f, t)), __builtin_bit_cast(cd_h8_t, only_token(P[pg], t)), splat16(0.0f));
+              for (int t = 0; t < kBlock; ++t) {
+                const bool see = ((ok >> pg) & 1) && kUnit * s + kBlock * pg + t < lim;
+                const cd_f16_t d = HalfOps::mfma(__builtin_bit_cast(cd_h8_t, only_token(f, t)), __builtin_bit_cast(cd_h8_t, only_token(p, t)), splat16(0.0f));
 #pragma unroll
                 for (int y = 0; y < 16; ++y) O[i][y] += see ? d[y] : 0.0f;
               }
@@ -204,25 +225,23 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
           }
         }
       };
-      // before a step: it has landed when at most the younger steps' loads are on their way; after it: its stage's last
-      // readers are done, the step kAhead on may take it
+      // before a unit: it has landed when at most the next one's six loads are on their way; after it: its stages' last
+      // readers are done, the unit after next may take them
       auto before = [&](int s) {
-        if (s + kAhead <= s1)
-          asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * (kAhead - 1)) : "memory");
+        if (s + 1 < s1)
+          asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
         else
           asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       };
       auto after = [&](int s) {
-        if (s + kAhead < s1) {
-          if (s + kAhead >= list0 + 32) load_list(s + 1);  // steps still to be taken keep their place in it
+        if (s + 2 < s1) {
+          if (s + 2 >= list0 + 16) load_list(s + 1);  // units still to be taken keep their place in it
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-          issue(s + kAhead);
+          issue(s + 2);
         }
       };
       std::true_type yes;
       std::false_type no;
-      load_list(s0);
-      for (int s = s0; s < min(s0 + kAhead, s1); ++s) issue(s);
       int s = s0;
       for (; s < s1 && whole(s); ++s) {
         before(s);
@@ -323,14 +342,14 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
       for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[pg][j] = vb[min(kStep * s + kBlock * pg + 8 * hh + j, seq.n - 1) * a.v_stride];
-      cd_f16_t S = splat16(0.0f);
+      cd_f16_t S[1] = {splat16(0.0f)};
 #pragma unroll
-      for (int kk = 0; kk < 8; ++kk) S = BfOps::mfma(k[kk], Qb[kk], S);
+      for (int kk = 0; kk < 8; ++kk) S[0] = BfOps::mfma(k[kk], Qb[kk], S[0]);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) S[i] = kStep * s + reg_token(i) + 8 * hh <= tok ? S[i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) S[0][i] = kStep * s + reg_token(i) + 8 * hh <= tok ? S[0][i] : -INFINITY;
       settle<BfOps>(S, base, m, sum, thr, O);
       cd_u4_t P[2];
-      soften<BfOps>(S, base, sum, P);
+      soften<BfOps>(S[0], base, sum, P);
       uint32_t found = 0;
       cd_u4_t y[2], z[2];  // values, and those that are not finite
 #pragma unroll

@@ -12,6 +12,16 @@ typedef float cd_f16_t __attribute__((ext_vector_type(16)));
 typedef uint32_t cd_u2_t __attribute__((ext_vector_type(2)));
 typedef uint32_t cd_u4_t __attribute__((ext_vector_type(4)));
 
+// A constant in a vector register: with its mask in a scalar one, AND and OR are one instruction (which takes one scalar)
+__device__ __forceinline__ uint32_t in_vgpr(uint32_t x) {
+  asm("" : "+v"(x));
+  return x;
+}
+__device__ __forceinline__ uint32_t in_sgpr(uint32_t x) {
+  asm("" : "+s"(x));
+  return x;
+}
+
 // The codes at bits X, X + 1 of a word's two 16-bit halves as two fp16 numbers. In an fp16 number of exponent 10 - X
 // mantissa bit X weighs 1, so the code bits joined with 2^(10 - X) make 2^(10 - X) + code, and the subtraction is exact.
 template <int X>
@@ -19,7 +29,7 @@ __device__ __forceinline__ cd_h2_t land_codes(uint32_t w) {
   static_assert(X >= 0 && X <= 8, "the codes have to lie in the ten mantissa bits");
   constexpr uint32_t mask = (3u << X) * 0x10001u, magic = ((25u - X) << 10) * 0x10001u;
   const cd_h2_t base = {(_Float16)(float)(1 << (10 - X)), (_Float16)(float)(1 << (10 - X))};
-  return __builtin_bit_cast(cd_h2_t, (w & mask) | magic) - base;
+  return __builtin_bit_cast(cd_h2_t, (w & in_sgpr(mask)) | in_vgpr(magic)) - base;
 }
 
 // The codes of position p (0..7) of a word's two halves: channels 16 p + m of halves m = 2 w, 2 w + 1. `hi` is w >> 10.

@@ -206,7 +206,7 @@ struct ChunkArgs {
   const float* mu;
   uint16_t* out;                    // bf16 [total_q, Hq, 128]
   // plan and workspace
-  int bm, resident, max_tiles, max_items, max_slots;
+  int bm, resident, min_piece, max_tiles, max_items, max_slots;
   float piece_units, merge_units;
   int32_t* head;                    // pieces (per KV head), tiles, units of a piece
   int32_t *item_start, *tile_start; // [B] (batches above kChunkWaveSeqs)
@@ -214,7 +214,7 @@ struct ChunkArgs {
   float* part;                      // [max_slots, H, bm * kChunkPartStride]
 };
 struct ChunkPlan {
-  int waves, bm, resident, max_tiles, max_items, max_slots;
+  int waves, bm, resident, min_piece, max_tiles, max_items, max_slots;
   float piece_units, merge_units;
   size_t off_head, off_items, off_starts, off_tiles, off_part, total;
 };
