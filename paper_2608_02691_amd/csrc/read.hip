@@ -9,6 +9,10 @@
 // (tile 2 a + e holds channels 64 a + 2 m + e in its rows m). R is converted once per work-group into LDS, in operand
 // order; a work-group then walks over tokens, a wave 32 at a time with the next tile's records on their way.
 //
+// Bound by the rows written (256 or 512 bytes a row; the records are 96, in whole pages where neighbours are wanted too).
+// Rows leave through LDS as whole 256-byte pieces by stores that bypass the caches: 32,768 scattered tokens of 8 heads, keys
+// and values, take 36 us (160 MB, 4.4 TB/s); 32-byte pieces straight from the accumulators took 71.
+//
 // bf16 rows: x^ and R in one fp16 term each, an error of about 3e-4 of the row's root mean square against the output's
 // rounding of 2^-9 of each value. fp32 rows: two fp16 terms each, three products (the fourth is below 2^-22).
 #include "codes.h"
@@ -19,7 +23,7 @@ namespace int2kv {
 
 namespace {
 
-constexpr int kReadThreads = 256;
+constexpr int kReadThreads = 512;
 constexpr int kReadTile = 32;                 // tokens of a wave's step
 constexpr int kFrag = 64;                     // lanes of an operand, 16 bytes each
 
@@ -90,25 +94,36 @@ __global__ __launch_bounds__(kReadThreads, 2) void read_rows_kernel(CacheView cv
                                                                     void* __restrict__ v_out, int z0) {
   constexpr int kTerms = F32 ? 2 : 1;
   __shared__ __align__(16) uint32_t frag[kTerms][4][8][kFrag][4];  // [term][tile][operand][lane][8 fp16]
-  __shared__ float off[kHeadDim];
+  __shared__ __align__(16) uint4 rows[kReadThreads / 64][kReadTile * 16];  // results on their way out
+  __shared__ __align__(16) float off[kHeadDim];
   const int tid = threadIdx.x, l = tid & 63, wave = tid >> 6, m = l & 31, hh = l >> 5;
   const int h = blockIdx.y, kv = blockIdx.z + z0, H = cv.num_kv_heads;
   void* out = kv ? v_out : k_out;
-  // ---- R into LDS. A thread takes two neighbouring channels of one row; lane chunk m of operand kk lies at m ^ kk, so
-  // that a row's 64 pairs, which differ in operand and place but not in m, spread over the banks
+  // ---- R into LDS. A thread takes four neighbouring channels of one row; lane chunk m of operand kk lies at m ^ kk, so that
+  // a row's pieces, which differ in operand and place but not in m, spread over the banks
   const float* R = (kv ? R_v : R_k) + (size_t)h * kHeadDim * kHeadDim;
-  for (int i = tid; i < kHeadDim * kHeadDim / 2; i += kReadThreads) {
-    const int row = i >> 6, c2 = i & 63, p = c2 >> 3, w = c2 & 7, kk = 2 * (w & 3) + (p >> 2);
-    const float2 r = *reinterpret_cast<const float2*>(R + row * kHeadDim + 2 * c2);
-    const int tile = 2 * (row >> 6) + (row & 1), at = (w >> 2) * 32 + (((row & 63) >> 1) ^ kk);
-    const cd_h2_t hi = {(_Float16)r.x, (_Float16)r.y};
-    frag[0][tile][kk][at][p & 3] = __builtin_bit_cast(uint32_t, hi);
-    if constexpr (F32) {
-      const cd_h2_t lo = {(_Float16)(r.x - (float)hi.x), (_Float16)(r.y - (float)hi.y)};
-      frag[kTerms - 1][tile][kk][at][p & 3] = __builtin_bit_cast(uint32_t, lo);
+  constexpr int kLoads = kHeadDim * kHeadDim / 4 / kReadThreads;
+  float4 r4[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) r4[i] = reinterpret_cast<const float4*>(R)[tid + kReadThreads * i];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    const int e = tid + kReadThreads * i, row = e >> 5, c4 = e & 31, p = c4 >> 2;
+    const int tile = 2 * (row >> 6) + (row & 1);
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {  // channels 16 p + 2 w, + 1
+      const int w = 2 * (c4 & 3) + x, kk = 2 * (w & 3) + (p >> 2), at = (w >> 2) * 32 + (((row & 63) >> 1) ^ kk);
+      const float u = x ? r4[i].z : r4[i].x, v = x ? r4[i].w : r4[i].y;
+      const cd_h2_t hi = {(_Float16)u, (_Float16)v};
+      frag[0][tile][kk][at][p & 3] = __builtin_bit_cast(uint32_t, hi);
+      if constexpr (F32) {
+        const cd_h2_t lo = {(_Float16)(u - (float)hi.x), (_Float16)(v - (float)hi.y)};
+        frag[kTerms - 1][tile][kk][at][p & 3] = __builtin_bit_cast(uint32_t, lo);
+      }
     }
   }
-  if (tid < kHeadDim) off[tid] = kv == 0 && mu ? mu[(size_t)h * kHeadDim + tid] : 0.0f;
+  const bool centered = kv == 0 && mu;
+  if (centered && tid < kHeadDim) off[tid] = mu[(size_t)h * kHeadDim + tid];
   __syncthreads();
 
   const int tiles = (n + kReadTile - 1) / kReadTile, hop = gridDim.x * (kReadThreads / 64);
@@ -163,71 +178,98 @@ __global__ __launch_bounds__(kReadThreads, 2) void read_rows_kernel(CacheView cv
             acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_f16(A(0, i, 2 * w + o), x[o], acc[i], 0, 0, 0);
       }
     }
-    if (cur.ok) {
-      // register 4 u + v of tile 2 a + e: channel 64 a + 16 u + 8 hh + 2 v + e
-      const size_t at = ((size_t)(tile * kReadTile + m) * H + h) * kHeadDim + 8 * hh;
+    // The next tile's loads are waited for here: behind the stores, which count in the same order, the wait would be for them
 #pragma unroll
-      for (int a = 0; a < 2; ++a)
+    for (int i = 0; i < 4; ++i) asm volatile("" : "+v"(raw.w[i]));
+#pragma unroll
+    for (int g = 0; g < NG; ++g) asm volatile("" : "+v"(raw.s[g]), "+v"(raw.z[g]));
+    asm volatile("" : "+v"(slot_next));
+    // (the stores bypass the caches: with them, 32,768 tokens of 8 heads took 46 us where they take 36)
+    // register 4 u + v of tile 2 a + e: channel 64 a + 16 u + 8 hh + 2 v + e. Through the wave's own piece of LDS, 256 bytes a
+    // token at a time (chunk x of token m at x ^ m), so that a store writes four whole pieces of rows
+    const unsigned long long live = __ballot(cur.ok);
+    uint4* box = rows[wave];
+#pragma unroll
+    for (int part = 0; part < (F32 ? 2 : 1); ++part) {
+#pragma unroll
+      for (int a = F32 ? part : 0; a < (F32 ? part + 1 : 2); ++a)
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-          const int c = 64 * a + 16 * u;
           float y[8];
 #pragma unroll
-          for (int v = 0; v < 8; ++v) y[v] = acc[2 * a + (v & 1)][4 * u + (v >> 1)] + off[c + 8 * hh + v];
+          for (int v = 0; v < 8; ++v) y[v] = acc[2 * a + (v & 1)][4 * u + (v >> 1)];
+          if (centered) {
+            const float4* mu4 = reinterpret_cast<const float4*>(off + 64 * a + 16 * u + 8 * hh);
+            const float4 m0 = mu4[0], m1 = mu4[1];
+            y[0] += m0.x, y[1] += m0.y, y[2] += m0.z, y[3] += m0.w, y[4] += m1.x, y[5] += m1.y, y[6] += m1.z, y[7] += m1.w;
+          }
           if constexpr (F32) {
-            float4* o = reinterpret_cast<float4*>(static_cast<float*>(out) + at + c);
-            o[0] = make_float4(y[0], y[1], y[2], y[3]);
-            o[1] = make_float4(y[4], y[5], y[6], y[7]);
+            const int x = 4 * u + 2 * hh;
+            box[16 * m + (x ^ (m & 15))] = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
+            box[16 * m + ((x + 1) ^ (m & 15))] = make_uint4(__float_as_uint(y[4]), __float_as_uint(y[5]), __float_as_uint(y[6]), __float_as_uint(y[7]));
           } else {
-            *reinterpret_cast<uint4*>(static_cast<uint16_t*>(out) + at + c) =
+            box[16 * m + ((8 * a + 2 * u + hh) ^ (m & 15))] =
                 make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
           }
         }
+      __builtin_amdgcn_wave_barrier();
+      uint8_t* o = static_cast<uint8_t*>(out) + ((size_t)tile * kReadTile * H + h) * (kHeadDim * (F32 ? 4 : 2)) + 256 * part + 16 * (l & 15);
+#pragma unroll
+      for (int r = 0; r < kReadTile; r += 4) {
+        const int t = r + (l >> 4);
+        const uint4 y = box[16 * t + ((l & 15) ^ (t & 15))];
+        if ((live >> t) & 1) __builtin_nontemporal_store(cd_u4_t{y.x, y.y, y.z, y.w}, reinterpret_cast<cd_u4_t*>(o + (size_t)t * H * (kHeadDim * (F32 ? 4 : 2))));
+      }
+      __builtin_amdgcn_wave_barrier();
     }
   }
 }
 
-// Rows as stored: thread (token, KV head, word w) has channels 16 p + 2 w and + 1. Exact before the output's rounding.
+// Rows as stored: thread (token, KV head, position p, half x) has the eight channels 16 p + 8 x .., which are bits 2 p of
+// halves 8 x .. 8 x + 7. Exact before the output's rounding.
 template <int NG, bool F32>
 __global__ __launch_bounds__(256) void read_rotated_kernel(CacheView cv, const int32_t* __restrict__ slots, int n,
                                                            void* __restrict__ k_out, void* __restrict__ v_out, int z0) {
   using Lay = Rec<NG>;
   const int H = cv.num_kv_heads, kv = blockIdx.y + z0;
-  const long long i = (long long)blockIdx.x * 256 + threadIdx.x, row = i >> 3;
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x, row = i >> 4;
   if (row >= (long long)n * H) return;
-  const int w = (int)(i & 7), h = (int)(row % H), slot = slots[row / H];
+  const int x = (int)(i & 1), p = (int)(i >> 1) & 7, g = p * NG / 8, h = (int)(row % H), slot = slots[row / H];
   if (slot < 0 || slot >= cv.num_blocks * kBlock) return;
   const int t = slot & 15;
   const uint8_t* rec = cv.pool + ((size_t)(slot >> 4) * H + h) * Lay::kBytes;
-  uint32_t word;
-  float s[NG], z[NG];
+  uint32_t w[4];
+  float s, z;
   if (kv == 0) {
-    word = *reinterpret_cast<const uint32_t*>(rec + kOffKCodes + 32 * t + 4 * w);
+    const cd_u4_t c = *reinterpret_cast<const cd_u4_t*>(rec + kOffKCodes + 32 * t + 16 * x);
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      const uint32_t m = *reinterpret_cast<const uint32_t*>(rec + Lay::kOffKMeta + 4 * NG * t + 4 * g);
-      s[g] = f16_bits_to_f32(m & 0xFFFFu);
-      z[g] = f16_bits_to_f32(m >> 16);
-    }
+    for (int j = 0; j < 4; ++j) w[j] = c[j];
+    const uint32_t m = *reinterpret_cast<const uint32_t*>(rec + Lay::kOffKMeta + 4 * NG * t + 4 * g);
+    s = f16_bits_to_f32(m & 0xFFFFu);
+    z = f16_bits_to_f32(m >> 16);
   } else {
-    const uint16_t* c = reinterpret_cast<const uint16_t*>(rec + kOffVCodes) + 32 * w + t;
-    word = (uint32_t)c[0] | ((uint32_t)c[16] << 16);
+    // a lane of the row loads one half; the halves 8 x .. come from the lanes that have them
+    const int l = threadIdx.x & 63;
+    const int half = *reinterpret_cast<const uint16_t*>(rec + kOffVCodes + 32 * (l & 15) + 2 * t);
+    const int pair = half | (__builtin_amdgcn_update_dpp(0, half, 0xB1, 0xF, 0xF, false) << 16);  // (even lanes)
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      s[g] = f16_bits_to_f32(*reinterpret_cast<const uint16_t*>(rec + Lay::kOffVScale + 32 * g + 2 * t));
-      z[g] = f16_bits_to_f32(*reinterpret_cast<const uint16_t*>(rec + Lay::kOffVZero + 32 * g + 2 * t));
-    }
+    for (int j = 0; j < 4; ++j) w[j] = (uint32_t)__builtin_amdgcn_ds_bpermute(4 * ((l & 48) + 8 * x + 2 * j), pair);
+    s = f16_bits_to_f32(*reinterpret_cast<const uint16_t*>(rec + Lay::kOffVScale + 32 * g + 2 * t));
+    z = f16_bits_to_f32(*reinterpret_cast<const uint16_t*>(rec + Lay::kOffVZero + 32 * g + 2 * t));
   }
-  void* out = kv ? v_out : k_out;
+  float y[8];
 #pragma unroll
-  for (int p = 0; p < 8; ++p) {
-    const float a = __builtin_fmaf((float)((word >> (2 * p)) & 3u), s[p * NG / 8], z[p * NG / 8]);
-    const float b = __builtin_fmaf((float)((word >> (16 + 2 * p)) & 3u), s[p * NG / 8], z[p * NG / 8]);
-    const size_t at = (size_t)row * kHeadDim + 16 * p + 2 * w;
-    if constexpr (F32)
-      *reinterpret_cast<float2*>(static_cast<float*>(out) + at) = make_float2(a, b);
-    else
-      *reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(out) + at) = pack_bf16(a, b);
+  for (int j = 0; j < 8; ++j) y[j] = __builtin_fmaf((float)((w[j >> 1] >> (16 * (j & 1) + 2 * p)) & 3u), s, z);
+  void* out = kv ? v_out : k_out;
+  const size_t at = (size_t)row * kHeadDim + 16 * p + 8 * x;
+  if constexpr (F32) {
+    typedef float f4 __attribute__((ext_vector_type(4)));
+    f4* o = reinterpret_cast<f4*>(static_cast<float*>(out) + at);
+    __builtin_nontemporal_store(f4{y[0], y[1], y[2], y[3]}, o);
+    __builtin_nontemporal_store(f4{y[4], y[5], y[6], y[7]}, o + 1);
+  } else {
+    __builtin_nontemporal_store(cd_u4_t{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7])},
+                                reinterpret_cast<cd_u4_t*>(static_cast<uint16_t*>(out) + at));
   }
 }
 
@@ -239,12 +281,12 @@ hipError_t launch_read(CacheView c, const int32_t* slots, int n, const float* R_
   const int H = c.num_kv_heads;
   // keys, values or both in one launch where they take the same kernel
   auto rotated = [&](int z0, int nz) {
-    const long long blocks = ((long long)n * H * 8 + 255) / 256;
+    const long long blocks = ((long long)n * H * 16 + 255) / 256;
     hipLaunchKernelGGL((read_rotated_kernel<NG, F32>), dim3((unsigned)blocks, nz), dim3(256), 0, s, c, slots, n, k_out, v_out, z0);
   };
   auto turned = [&](int z0, int nz) {
     const int tiles = (n + kReadTile - 1) / kReadTile, waves = kReadThreads / 64;
-    int nb = (2 * num_cus() + nz * H - 1) / (nz * H);  // two work-groups a compute unit share R's conversion
+    int nb = (num_cus() + nz * H - 1) / (nz * H);  // a work-group a compute unit
     nb = nb < 1 ? 1 : nb;
     const int most = (tiles + waves - 1) / waves;
     hipLaunchKernelGGL((read_rows_kernel<NG, F32>), dim3(nb < most ? nb : most, H, nz), dim3(kReadThreads), 0, s, c, slots, n,
