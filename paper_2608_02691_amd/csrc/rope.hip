@@ -7,7 +7,8 @@
 //
 // Bound by the rows it moves, 512 bytes a (token, head). A token's table rows and positions are read once per thread and
 // used for all the heads the thread takes: thread (token, piece j) holds the eight pairs 8 j .. 8 j + 7 of its token and
-// walks over heads, four threads of the token abreast, so a wave's loads are whole 128-byte half rows.
+// walks over heads, four threads of the token abreast, so a wave's loads are whole 128-byte half rows. The stores bypass the
+// caches: 24,576 tokens of 32 + 8 heads take 97 us (516 MB, 5.3 TB/s), 101 with ordinary stores.
 #include "append_core.h"
 #include "common.h"
 #include "kernels.h"
@@ -73,8 +74,8 @@ __global__ __launch_bounds__(kRopeThreads) void rope_axes_kernel(RopeAxesArgs a)
     for (int u = 0; u < kRopeAhead; ++u) {
       if (dst[u]) {
         rope_pairs(x0[u], x1[u], cs);
-        *reinterpret_cast<ap_u4_t*>(dst[u]) = x0[u];
-        *reinterpret_cast<ap_u4_t*>(dst[u] + 64) = x1[u];
+        __builtin_nontemporal_store(x0[u], reinterpret_cast<ap_u4_t*>(dst[u]));
+        __builtin_nontemporal_store(x1[u], reinterpret_cast<ap_u4_t*>(dst[u] + 64));
       }
     }
   }
