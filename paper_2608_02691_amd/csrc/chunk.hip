@@ -13,6 +13,8 @@
 // lane-local but for one exchange of halves, the rescaling is one factor per lane, and the probabilities are the second
 // product's B operand as they lie (its k order is the order of S^T's rows in a lane; V^T is laid out to match). INT2 codes
 // become fp16 operands once per work-group and unit and are shared through LDS in operand order.
+#include <type_traits>
+
 #include "chunk_core.h"
 
 namespace int2kv {
@@ -117,11 +119,11 @@ __device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, co
   const int l = threadIdx.x & 63;
   cd_f16_t S[1], T[1];
   float base = kBias - st.m - off;
+  cd_f16_t start = splat16(Ops::kBased ? base : 0.0f);
   // scores of half tm of the unit in slot kb
   auto scores = [&](cd_f16_t (&X)[1], int kb, int tm) {
-    X[0] = splat16(0.0f);
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) X[0] = Ops::mfma(lds.k[kb][8 * tm + kk][l], Q[kk], X[0]);
+    for (int kk = 0; kk < 8; ++kk) X[0] = Ops::mfma(lds.k[kb][8 * tm + kk][l], Q[kk], kk == 0 ? start : X[0]);
   };
   // hides what a row does not see
   auto rest = [&](cd_f16_t (&X)[1], int u, int tm) {
@@ -129,7 +131,7 @@ __device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, co
 #pragma unroll
       for (int i = 0; i < 16; ++i) X[0][i] = src.sees(u, 32 * tm + reg_token(i)) ? X[0][i] : -INFINITY;
     }
-    settle<Ops>(X, base, st.m, st.sum, st.thr, st.O);
+    settle<Ops>(X, base, st.m, st.sum, st.thr, st.O, &start);
   };
   auto add = [&](const cd_u4_t (&P)[2], int vb, int tm) {
 #pragma unroll
@@ -139,8 +141,9 @@ __device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, co
         st.O[i] = Ops::mfma(lds.v[vb][8 * tm + 4 * pg + i][l], __builtin_bit_cast(typename Ops::vec, P[pg]), st.O[i]);
   };
 
-  src.fetch(u0);
-  src.template build<false>(u0, lds, 0, 0);
+  // of the two waves of a SIMD (w and w + 4) one goes first, so that they come to lie half a step apart
+  if (__builtin_amdgcn_readfirstlane(threadIdx.x >> 8)) __builtin_amdgcn_s_setprio(1);
+  src.template build<false>(u0, lds, 0, 0);  // (fetched by the caller)
   if (u0 + 1 < u1) src.fetch(u0 + 1);
   __syncthreads();
   scores(S, 0, 0);
@@ -395,44 +398,47 @@ struct OwnSource {
   __device__ __forceinline__ bool sees_token(int u, int t) const { return kUnit * u + t <= tok; }
 };
 
-// q' = q R_K of the lane's row as fp16 operands with log2(e) / sqrt(128) folded in (what a small q' loses among fp16's
-// subnormals, 2^-25 an element, is nothing in a score). R_K goes through LDS in two bf16 terms, q is exact.
+// R_K's elements that a thread brings into LDS: eight channels 8 oct .. of a column at a time
 template <int NW>
-__device__ __forceinline__ void rotate_query(const float* R, ChunkLds& lds, const cd_b8_t (&x)[8], cd_h8_t (&Q)[8]) {
-  cd_b8_t* hi = reinterpret_cast<cd_b8_t*>(&lds);  // [tile][operand][lane], then the low terms
-  cd_b8_t* lo = hi + 2048;
-  static_assert(sizeof(ChunkLds) >= 4096 * 16, "room for both terms");
+struct KeyRotation {
+  static constexpr int N = 2048 / (64 * NW);
+  float r[N][8];
+  __device__ __forceinline__ void load(const float* R) {
 #pragma unroll
-  for (int i = 0; i < 2048 / (64 * NW); ++i) {
-    const int e = threadIdx.x + 64 * NW * i, oct = e >> 7, c = e & 127;  // eight channels 8 oct .. of column c
+    for (int i = 0; i < N; ++i) {
+      const int e = threadIdx.x + 64 * NW * i, oct = e >> 7, c = e & 127;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) r[i][j] = R[(size_t)(8 * oct + j) * kHeadDim + c];
+    }
+  }
+};
+// q' = q R_K of the lane's row as fp16 operands with log2(e) / sqrt(128) folded in (what a small q' loses among fp16's
+// subnormals, 2^-25 an element, is nothing in a score). q is exact in fp16, R_K's elements are rounded to it: 2^-12 of each,
+// as the result's own rounding.
+template <int NW>
+__device__ __forceinline__ void rotate_query(const KeyRotation<NW>& R, ChunkLds& lds, const cd_b8_t (&x)[8], cd_h8_t (&Q)[8]) {
+  cd_h8_t* rk = reinterpret_cast<cd_h8_t*>(&lds);  // [tile][operand][lane]
+#pragma unroll
+  for (int i = 0; i < KeyRotation<NW>::N; ++i) {
+    const int e = threadIdx.x + 64 * NW * i, oct = e >> 7, c = e & 127;
     const int m16 = c & 15, p = c >> 4, wd = m16 >> 1;
     const int pos = (2 * (2 * (wd & 3) + (p >> 2)) + (wd >> 2)) * 8 + 2 * (p & 3) + (m16 & 1);
     // row_position is its own inverse
-    const int at = ((pos >> 5) * 8 + (oct >> 1)) * 64 + (oct & 1) * 32 + row_position(pos & 31);
-    cd_b8_t a, b;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const float r = R[(size_t)(8 * oct + j) * kHeadDim + c];
-      a[j] = (__bf16)r;
-      b[j] = (__bf16)(r - (float)a[j]);
-    }
-    hi[at] = a;
-    lo[at] = b;
+    rk[((pos >> 5) * 8 + (oct >> 1)) * 64 + (oct & 1) * 32 + row_position(pos & 31)] = pack_half8(R.r[i]);
   }
   __syncthreads();
   const int l = threadIdx.x & 63;
+  cd_h8_t q[8];
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) q[kk] = half_of(x[kk]);
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
     cd_f16_t d = splat16(0.0f);
 #pragma unroll
-    for (int kk = 0; kk < 8; ++kk) {
-      d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo[(8 * t + kk) * 64 + l], x[kk], d, 0, 0, 0);
-      d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi[(8 * t + kk) * 64 + l], x[kk], d, 0, 0, 0);
-    }
+    for (int kk = 0; kk < 8; ++kk) d = __builtin_amdgcn_mfma_f32_32x32x16_f16(rk[(8 * t + kk) * 64 + l], q[kk], d, 0, 0, 0);
+    d *= kLogit2;
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) Q[2 * t + u][j] = (_Float16)(d[8 * u + j] * kLogit2);
+    for (int u = 0; u < 2; ++u) Q[2 * t + u] = pack_half8(reinterpret_cast<const float*>(&d) + 8 * u);
   }
   __syncthreads();
 }
@@ -458,9 +464,11 @@ __device__ __forceinline__ void unrotate(const float* R, ChunkLds& lds, RowState
   const float all = pair_sum(st.sum), inv = all == 0.0f ? 0.0f : 1.0f / all;
   cd_h8_t B[8];
 #pragma unroll
-  for (int op = 0; op < 8; ++op)
+  for (int t = 0; t < 4; ++t) {
+    const cd_f16_t o = st.O[t] * inv;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) B[op][j] = (_Float16)(st.O[op >> 1][8 * (op & 1) + j] * inv);
+    for (int u = 0; u < 2; ++u) B[2 * t + u] = pack_half8(reinterpret_cast<const float*>(&o) + 8 * u);
+  }
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
     cd_f16_t d = splat16(0.0f);
@@ -480,6 +488,8 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
   __shared__ ChunkLds lds;
   const int H = a.cv.num_kv_heads;
   const int h = (int)(blockIdx.x % H);
+  KeyRotation<NW> R;
+  if (a.max_ctx > 0) R.load(a.R_k + (size_t)h * kHeadDim * kHeadDim);
   const Place place = locate(a, (int)(blockIdx.x / H), h);
   if (!place.valid) return;
   const Seq seq = place.s;
@@ -503,10 +513,12 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
     cd_b8_t x[8];
     cd_h8_t Q[8];
     query(x);
-    rotate_query<NW>(a.R_k + (size_t)h * kHeadDim * kHeadDim, lds, x, Q);
     auto limit = [&](int t) { return a.k_new ? seq.ctx : min(seq.ctx, seq.ctx - seq.n + 1 + t); };
     Int2Source<NG, NW> src(a, h, place.b, seq.ctx, w, limit(tok), limit(tok_w), limit(place.row0 / a.gq));
-    attend<HalfOps>(src, st, lds, Q, 0.0f, place.u0, i1);
+    src.fetch(place.u0);
+    rotate_query<NW>(R, lds, x, Q);
+    // (the narrow work-group has no registers to spare)
+    attend<typename std::conditional<NW == 8, BasedOps, HalfOps>::type>(src, st, lds, Q, 0.0f, place.u0, i1);
     unrotate<NW>(a.R_v + (size_t)h * kHeadDim * kHeadDim, lds, st);
   }
 
@@ -515,6 +527,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
     cd_b8_t Q[8];
     query(Q);
     OwnSource<NW> src(a, h, seq, place.row0, w, tok, tok_w);
+    src.fetch(c0);
     attend<BfOps>(src, st, lds, Q, query_mean(Q, a.mu + (size_t)h * kHeadDim, hh), c0, c1);
   }
 

@@ -219,6 +219,7 @@ struct HalfOps {
   static __device__ __forceinline__ cd_f16_t mfma(const cd_h8_t& a, const vec& b, const cd_f16_t& c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
   }
+  static constexpr bool kBased = false;
   static __device__ __forceinline__ float score(float s, float base) { return s + base; }
   static __device__ __forceinline__ uint32_t pack(float a, float b, float& sum) {
     typedef float f2 __attribute__((ext_vector_type(2)));
@@ -231,12 +232,18 @@ struct HalfOps {
     return ((x & 0x7C00u) == 0x7C00u ? 0xFFFFu : 0u) | ((x & 0x7C000000u) == 0x7C000000u ? 0xFFFF0000u : 0u);
   }
 };
+// the same with products that start at base: one addition a score less, for 16 registers that hold it
+struct BasedOps : HalfOps {
+  static constexpr bool kBased = true;
+  static __device__ __forceinline__ float score(float s, float) { return s; }
+};
 // bf16 operands: the chunk's own units, whose scores are scaled in fp32
 struct BfOps {
   typedef cd_b8_t vec;
   static __device__ __forceinline__ cd_f16_t mfma(const cd_h8_t& a, const vec& b, const cd_f16_t& c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(cd_b8_t, a), b, c, 0, 0, 0);
   }
+  static constexpr bool kBased = false;
   static __device__ __forceinline__ float score(float s, float base) { return __builtin_fmaf(s, kLogit2, base); }
   static __device__ __forceinline__ uint32_t pack(float a, float b, float& sum) {
     sum += a + b;
@@ -249,7 +256,8 @@ struct BfOps {
 
 // Moves m where a score of the step exceeds it by 2^kLazy (the lane's own scores and its partner's)
 template <class Ops, int N, int TILES>
-__device__ __forceinline__ void settle(const cd_f16_t (&X)[N], float& base, float& m, float& sum, float& thr, cd_f16_t (&O)[TILES]) {
+__device__ __forceinline__ void settle(cd_f16_t (&X)[N], float& base, float& m, float& sum, float& thr, cd_f16_t (&O)[TILES],
+                                       cd_f16_t* start = nullptr) {
   float a = fmaxf(X[0][0], X[0][1]);
 #pragma unroll
   for (int i = 2; i < 16 * N; i += 2) a = fmaxf(fmaxf(a, X[i >> 4][i & 15]), X[i >> 4][(i & 15) + 1]);
@@ -260,6 +268,11 @@ __device__ __forceinline__ void settle(const cd_f16_t (&X)[N], float& base, floa
     const float f = !move ? 1.0f : thr < 0.0f ? 0.0f : __builtin_amdgcn_exp2f(-d);
     m += d;
     base -= d;
+    if constexpr (Ops::kBased) {
+      *start -= d;
+#pragma unroll
+      for (int i = 0; i < N; ++i) X[i] -= d;
+    }
     sum *= f;
     thr = move ? kMove : thr;
 #pragma unroll

@@ -16,7 +16,7 @@ namespace {
 constexpr int kFewWaves = 4;
 constexpr int kStep = 32;                 // tokens of a step over the chunk's own
 constexpr int kStages = 4;                // two units, two stages each
-constexpr int kStageBytes = 3072;         // codes of two pages, then 512 bytes each of their parameters
+constexpr int kStageBytes = 2 * (1024 + 512);         // codes of two pages, then 512 bytes each of their parameters
 
 struct FewLds {
   union {

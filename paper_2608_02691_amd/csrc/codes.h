@@ -67,6 +67,24 @@ __host__ __device__ __forceinline__ int code_channel(int kk, int hh, int j) {
   return 16 * (4 * (kk & 1) + (j >> 1)) + 2 * (4 * hh + (kk >> 1)) + (j & 1);
 }
 
+// Eight numbers rounded to fp16; bf16 numbers as fp16 ones (exact within fp16's normal range)
+__device__ __forceinline__ cd_h8_t pack_half8(const float* x) {
+  typedef float f2 __attribute__((ext_vector_type(2)));
+  cd_h8_t y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const cd_h2_t p = __builtin_convertvector((f2{x[2 * i], x[2 * i + 1]}), cd_h2_t);
+    y[2 * i] = p.x, y[2 * i + 1] = p.y;
+  }
+  return y;
+}
+__device__ __forceinline__ cd_h8_t half_of(const cd_b8_t& x) {
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = (float)x[i];
+  return pack_half8(y);
+}
+
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   typedef float f2 __attribute__((ext_vector_type(2)));
   typedef __bf16 b2 __attribute__((ext_vector_type(2)));
