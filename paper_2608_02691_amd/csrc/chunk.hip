@@ -44,10 +44,12 @@ __device__ __forceinline__ int block_scan(int x, int* tmp, int& total) {
 
 // The plan of a batch too large for every wave to hold, by one block
 __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
-  __shared__ int tmp[kPlanThreads / 64], counts[kCuts], longest;
+  constexpr int kClasses = 64;
+  __shared__ int tmp[kPlanThreads / 64], counts[kCuts], classes[kClasses], longest;
   __shared__ unsigned long long work;
   const int tid = threadIdx.x;
   if (tid < kCuts) counts[tid] = 0;
+  if (tid < kClasses) classes[tid] = 0;
   if (tid == 0) longest = 0, work = 0;
   __syncthreads();
   int T = 0, total = 0;
@@ -63,28 +65,55 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   atomicAdd(&work, W);
   __syncthreads();
   const int umax = longest;
+  const float places = places_of(a), even = (float)work * __builtin_amdgcn_rcpf(places);
   int mine[kCuts] = {};
   for (int b = tid; b < a.B; b += kPlanThreads) {
     const Load s = load_of(a, seq_of(a, b));
 #pragma unroll
-    for (int k = 0; k < kCuts; ++k) mine[k] += s.tiles * pieces_of(s, cut_of(a, k, (float)work, umax));
+    for (int k = 0; k < kCuts; ++k) mine[k] += s.tiles * pieces_of(s, cut_of(a, k, even, umax));
   }
 #pragma unroll
   for (int k = 0; k < kCuts; ++k) atomicAdd(&counts[k], mine[k]);
   __syncthreads();
-  int pieces[kCuts];
-#pragma unroll
-  for (int k = 0; k < kCuts; ++k) pieces[k] = counts[k];
-  const int L = pick_cut(a, pieces, T, (float)work, umax);
+  float best = 0.0f;
+  int L = 1;
+  for (int k = 0; k < kCuts; ++k) {
+    const int c = cut_of(a, k, even, umax);
+    const float cost = cost_of(a, c, counts[k], T, even, places, umax);
+    if (k == 0 || (fits(counts[k], T, places) && cost < best)) best = cost, L = c;
+  }
+  // sequences by classes of their pieces' length; within a class in any order, which changes no result
+  auto class_of = [&](const Load& s) {
+    const int n = pieces_of(s, L);
+    return n == 0 ? kClasses - 1 : (int)((float)(kClasses - 1) * (1.0f - (float)quotient(s.units + n - 1, n) / (float)max(umax, 1)));
+  };
   T = 0;
   for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
     const int b = b0 + tid;
     const Load s = b < a.B ? load_of(a, seq_of(a, b)) : Load{0, 0};
-    const int items = s.tiles * pieces_of(s, L);
-    int n_tiles, n_items;
-    const int t = T + block_scan(s.tiles, tmp, n_tiles) - s.tiles, i = total + block_scan(items, tmp, n_items) - items;
-    if (b < a.B) a.tile_start[b] = t, a.item_start[b] = i;
+    int n_tiles;
+    const int t = T + block_scan(s.tiles, tmp, n_tiles) - s.tiles;
+    if (b < a.B) {
+      a.tile_start[b] = t;
+      atomicAdd(&classes[class_of(s)], 1);
+    }
     T = min(T + n_tiles, 1 << 28);
+  }
+  __syncthreads();
+  if (tid < kClasses) {
+    const int x = classes[tid];
+    classes[tid] = wave_scan(x) - x;
+  }
+  __syncthreads();
+  for (int b = tid; b < a.B; b += kPlanThreads) a.order[atomicAdd(&classes[class_of(load_of(a, seq_of(a, b)))], 1)] = b;
+  __syncthreads();
+  for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
+    const int x = b0 + tid;
+    const Load s = x < a.B ? load_of(a, seq_of(a, a.order[x])) : Load{0, 0};
+    const int items = s.tiles * pieces_of(s, L);
+    int n_items;
+    const int i = total + block_scan(items, tmp, n_items) - items;
+    if (x < a.B) a.item_start[x] = i;
     total = min(total + n_items, 1 << 28);
   }
   if (tid == 0) {
@@ -345,7 +374,7 @@ struct OwnSource {
   uint32_t found = 0;
 
   __device__ __forceinline__ OwnSource(const ChunkArgs& args, int h, const Seq& t, int row0, int w, int row_tok, int least)
-      : a(args), n_tok(t.n), tok(row_tok), tok_min(least), tok_tile(row0 / args.gq), l(threadIdx.x & 63), n(l & 31), hh(l >> 5), half(w / (NW / 2)),
+      : a(args), n_tok(t.n), tok(row_tok), tok_min(least), tok_tile(quotient(row0, args.gq)), l(threadIdx.x & 63), n(l & 31), hh(l >> 5), half(w / (NW / 2)),
         op0(KO * (w % (NW / 2))), page(w / (NW / 4)), pair0(PV * (w % (NW / 4))),
         kb(args.k_new + t.start * args.k_stride + (size_t)h * kHeadDim + 8 * hh + 16 * op0),
         vb(args.v_new + t.start * args.v_stride + (size_t)h * kHeadDim + 2 * n + 64 * pair0) {}
@@ -487,16 +516,16 @@ template <int NG, int NW>
 __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
   __shared__ ChunkLds lds;
   const int H = a.cv.num_kv_heads;
-  const int h = (int)(blockIdx.x % H);
+  const int at = quotient((int)blockIdx.x, H), h = (int)blockIdx.x - at * H;
   KeyRotation<NW> R;
-  if (a.max_ctx > 0) R.load(a.R_k + (size_t)h * kHeadDim * kHeadDim);
-  const Place place = locate(a, (int)(blockIdx.x / H), h);
+  if (a.max_ctx > 0) R.load(a.R_k + (size_t)h * kHeadDim * kHeadDim);  // on its way while the work-group finds its piece
+  const Place place = locate(a, at, h);
   if (!place.valid) return;
   const Seq seq = place.s;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = l & 31, hh = l >> 5;
-  const int rows = seq.n * a.gq, row_w = place.row0 + 32 * w, tok_w = min(row_w, rows - 1) / a.gq;
-  const int nI = int2_units(a, seq, (min(place.row0 + a.bm, rows) - 1) / a.gq);
-  const int row = row_w + n, rc = min(row, rows - 1), tok = rc / a.gq;
+  const int rows = seq.n * a.gq, row_w = place.row0 + 32 * w, tok_w = quotient(min(row_w, rows - 1), a.gq);
+  const int nI = int2_units(a, seq, quotient(min(place.row0 + a.bm, rows) - 1, a.gq));
+  const int row = row_w + n, rc = min(row, rows - 1), tok = quotient(rc, a.gq);
   RowState st;
   st.m = 0.0f, st.sum = 0.0f, st.thr = kNone;
 #pragma unroll
@@ -514,7 +543,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
     cd_h8_t Q[8];
     query(x);
     auto limit = [&](int t) { return a.k_new ? seq.ctx : min(seq.ctx, seq.ctx - seq.n + 1 + t); };
-    Int2Source<NG, NW> src(a, h, place.b, seq.ctx, w, limit(tok), limit(tok_w), limit(place.row0 / a.gq));
+    Int2Source<NG, NW> src(a, h, place.b, seq.ctx, w, limit(tok), limit(tok_w), limit(quotient(place.row0, a.gq)));
     src.fetch(place.u0);
     rotate_query<NW>(R, lds, x, Q);
     // (the narrow work-group has no registers to spare)
@@ -590,7 +619,7 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
     o[6] = __builtin_fmaf(v.z, f, o[6]), o[7] = __builtin_fmaf(v.w, f, o[7]);
   }
   const float inv = all == 0.0f ? 0.0f : 1.0f / all;
-  const int tok = row / a.gq;
+  const int tok = quotient(row, a.gq);
   uint16_t* out = a.out + ((size_t)(tile.start + tok) * a.Hq + h * a.gq + row - tok * a.gq) * kHeadDim + c;
   *reinterpret_cast<uint4*>(out) = make_uint4(pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv),
                                               pack_bf16(o[4] * inv, o[5] * inv), pack_bf16(o[6] * inv, o[7] * inv));
@@ -620,6 +649,7 @@ ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_
   const size_t listed = B > kChunkWaveSeqs ? (size_t)B : 0;
   size_t off = 0;
   p.off_head = off, off = up(off + 4 * sizeof(int32_t));
+  p.off_order = off, off = up(off + listed * sizeof(int32_t));
   p.off_items = off, off = up(off + listed * sizeof(int32_t));
   p.off_starts = off, off = up(off + listed * sizeof(int32_t));
   p.off_tiles = off, off = up(off + (size_t)p.max_tiles * sizeof(ChunkTile));
@@ -642,6 +672,7 @@ hipError_t launch_attn(const ChunkArgs& a, hipStream_t s) {
 hipError_t launch_chunk_attention(ChunkArgs a, const ChunkPlan& p, uint8_t* ws, hipStream_t s) {
   a.bm = p.bm;
   a.resident = p.resident;
+  a.per_cu = p.waves == 8 ? 1 : 2;
   a.min_piece = p.min_piece;
   a.max_tiles = p.max_tiles;
   a.max_items = p.max_items;
@@ -649,6 +680,7 @@ hipError_t launch_chunk_attention(ChunkArgs a, const ChunkPlan& p, uint8_t* ws, 
   a.piece_units = p.piece_units;
   a.merge_units = p.merge_units;
   a.head = reinterpret_cast<int32_t*>(ws + p.off_head);
+  a.order = reinterpret_cast<int32_t*>(ws + p.off_order);
   a.item_start = reinterpret_cast<int32_t*>(ws + p.off_items);
   a.tile_start = reinterpret_cast<int32_t*>(ws + p.off_starts);
   a.tiles = reinterpret_cast<ChunkTile*>(ws + p.off_tiles);

@@ -23,6 +23,19 @@ __device__ __forceinline__ int row_token(int m) { return (m & 3) | ((m & 4) << 1
 // The token (of its half) of register i, without the lane half's 8
 __device__ __forceinline__ constexpr int reg_token(int i) { return 16 * (i >> 3) + (i & 7); }
 
+// x / d for x >= 0, d > 0, without the long way of integer division: a float quotient is off by at most x / d * 2^-22, its
+// remainder's by less than one
+__device__ __forceinline__ int quotient(int x, int d) {
+  const float inv = __builtin_amdgcn_rcpf((float)d);
+  int q = (int)((float)x * inv);
+  int r = x - q * d;
+  const int more = (int)((float)r * inv);
+  q += more;
+  r -= more * d;
+  q += r >= d ? 1 : 0;
+  return q - (r < 0 ? 1 : 0);
+}
+
 struct Seq {
   int start, n, ctx;
 };
@@ -52,42 +65,30 @@ struct Load {  // of one sequence: row tiles, and units of the last one
 __device__ __forceinline__ Load load_of(const ChunkArgs& a, const Seq& s) {
   const int rows = s.n * a.gq;
   if (rows == 0) return Load{0, 0};
-  return Load{(rows + a.bm - 1) / a.bm, int2_units(a, s, s.n - 1) + own_units(a, s.n - 1)};
+  return Load{quotient(rows + a.bm - 1, a.bm), int2_units(a, s, s.n - 1) + own_units(a, s.n - 1)};
 }
 constexpr int kCuts = 12;
 // Candidate k: units of a piece. The first leaves the tiles whole; the others lie above the size that would fill the places
-// on the chip evenly, once or (from 8 on) three times.
-__device__ __forceinline__ int cut_of(const ChunkArgs& a, int k, float W, int umax) {
+// on the chip evenly, once or (from 8 on) three times. even: units of a place
+__device__ __forceinline__ int cut_of(const ChunkArgs& a, int k, float even, int umax) {
   if (k == 0) return max(umax, 1);
-  const float even = W * (float)a.cv.num_kv_heads / (float)a.resident;
-  const float c = k < 8 ? even * (1.0f + 0.15f * (float)(k - 1)) : even * (0.35f + 0.15f * (float)(k - 8));
-  return max(a.min_piece, (int)c + 1);
-}
-// x / d for 0 <= x < 2^24, 0 < d, without a branch
-__device__ __forceinline__ int quotient(int x, int d) {
-  int q = (int)((float)x * __builtin_amdgcn_rcpf((float)d));
-  const int r = x - q * d;
-  q += r >= d ? 1 : 0;
-  return q - (r < 0 ? 1 : 0);
+  return max(a.min_piece, (int)(even * (k < 8 ? 0.85f + 0.15f * (float)k : 0.35f + 0.15f * (float)(k - 8))) + 1);
 }
 __device__ __forceinline__ int pieces_of(const Load& s, int L) { return s.tiles == 0 ? 0 : max(1, quotient(s.units + L - 1, L)); }
-// pieces[k]: all sequences' pieces at candidate k; W: their units
-__device__ __forceinline__ int pick_cut(const ChunkArgs& a, const int (&pieces)[kCuts], int T, float W, int umax) {
-  const float H = (float)a.cv.num_kv_heads, res = (float)a.resident;
-  const bool few = T * H <= res;
-  float best = 0.0f;
-  int L = 1;
-#pragma unroll
-  for (int k = 0; k < kCuts; ++k) {
-    const int c = cut_of(a, k, W, umax);
-    const float n = pieces[k] * H, one = (float)min(c, umax) + a.piece_units;
-    float cost = n <= res ? one : fmaxf((W * H + n * a.piece_units) / res, one) + 0.5f * one;
-    if (pieces[k] > T) cost += n * a.merge_units;
-    const bool fits = k == 0 || n <= (few ? res : 3.0f * res);
-    if (k == 0 || (fits && cost < best)) best = cost, L = c;
-  }
-  return L;
+// The time in units with pieces of at most c units, n of them a KV head; places: a KV head's part of the chip
+__device__ __forceinline__ float cost_of(const ChunkArgs& a, int c, int n, int T, float even, float places, int umax) {
+  const float one = (float)min(c, umax) + a.piece_units, fn = (float)n;
+  const float load = even + fn * a.piece_units * __builtin_amdgcn_rcpf(places);
+  // Two work-groups of a compute unit share it: one alone takes 0.6 of the time, the fullest pair lies between the average
+  // and two of the longest. Beyond one round the longest may come last, by half.
+  const float round = a.per_cu == 2 ? fmaxf(0.6f * one, 0.5f * (one + load)) : one;
+  return (fn <= places ? round : fmaxf(load, one) + 0.5f * one) + (n > T ? fn * (float)a.cv.num_kv_heads * a.merge_units : 0.0f);
 }
+__device__ __forceinline__ float places_of(const ChunkArgs& a) {
+  return (float)a.resident * __builtin_amdgcn_rcpf((float)a.cv.num_kv_heads);
+}
+// whether n pieces may be: while the tiles have a place each, so must the pieces; never more than three rounds
+__device__ __forceinline__ bool fits(int n, int T, float places) { return (float)n <= ((float)T <= places ? places : 3.0f * places); }
 
 // Sum and maximum over the wave: rotations inside rows of 16 lanes, then swaps of rows and halves
 template <class F>
@@ -104,13 +105,14 @@ __device__ __forceinline__ int wave_fold(int x, F f) {
 __device__ __forceinline__ int wave_sum(int x) {
   return wave_fold(x, [](int a, int b) { return a + b; });
 }
+// Inclusive sum over the wave: shifts inside rows of 16 lanes, then the rows' and the halves' last lanes onto those behind
 __device__ __forceinline__ int wave_scan(int x) {
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
   return x;
 }
 
@@ -122,13 +124,19 @@ struct Place {
   int slot;         // partial, -1: the result itself
   bool valid;
 };
-// Piece `at` of the plan, found by every wave for itself. The last tiles come first: under a causal mask they are the
-// longest. Writes the record of a cut tile for the merge (first piece, head 0).
+// The piece, longest first, of a KV head's work-group `at`. Where two work-groups share a compute unit and all have a place,
+// the second ones (those from `half` on) come in the opposite order, the shortest beside the longest.
+__device__ __forceinline__ int rank_of(const ChunkArgs& a, int at, int total) {
+  const int half = quotient(a.resident >> 1, a.cv.num_kv_heads);
+  return a.per_cu == 2 && at >= half && total * a.cv.num_kv_heads <= a.resident ? total - 1 - (at - half) : at;
+}
+// The piece of work-group `at`, found by every wave for itself: the sequences with the longest pieces come first, and of a
+// sequence the last tiles, under a causal mask its longest. Writes the record of a cut tile for the merge (first piece, head 0).
 __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
   const int lane = threadIdx.x & 63;
   Place p;
   p.valid = false;
-  int total, T, L, b, first, tile0;
+  int total, T, L, b, first, tile0, local;
   if (a.B <= kChunkWaveSeqs) {
     Seq s{0, 0, 0};
     if (lane < a.B) s = seq_of(a, lane);
@@ -144,20 +152,31 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
     } else {
       W = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(W)));
     }
-    int pieces[kCuts];
+    const float places = places_of(a), even = W * __builtin_amdgcn_rcpf(places);
+    float best = 0.0f;
+    L = 1;
 #pragma unroll
     for (int k = 0; k < kCuts; ++k) {
-      const int n = load.tiles * pieces_of(load, cut_of(a, k, W, umax));
-      pieces[k] = a.B > 1 ? wave_sum(n) : __builtin_amdgcn_readfirstlane(n);
+      const int c = cut_of(a, k, even, umax), n = wave_sum(load.tiles * pieces_of(load, c));
+      const float cost = cost_of(a, c, n, T, even, places, umax);
+      if (k == 0 || (fits(n, T, places) && cost < best)) best = cost, L = c;
     }
-    L = pick_cut(a, pieces, T, W, umax);
-    const int mine = load.tiles * pieces_of(load, L), upto = wave_scan(mine);
+    const int pieces_b = pieces_of(load, L), mine = load.tiles * pieces_b, upto = wave_scan(mine);
     total = __builtin_amdgcn_readlane(upto, 63);
     if (at == 0 && h == 0 && threadIdx.x == 0) a.head[1] = total > a.max_items || T > a.max_tiles ? 0 : T;
     total = min(total, a.max_items);
     if (at >= total) return p;
-    const int i = total - 1 - at;
-    b = __popcll(__ballot(upto <= i));
+    const int r = rank_of(a, at, total), size = mine > 0 ? quotient(load.units + pieces_b - 1, pieces_b) : -1;
+    // the length of piece r: the greatest that more than r pieces have
+    int lo = 0, hi = umax, above = 0;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1, n = wave_sum(size >= mid ? mine : 0);
+      if (n > r) lo = mid;
+      else hi = mid - 1, above = n;
+    }
+    const int same = size == lo ? mine : 0, past = wave_scan(same);
+    b = min(__ffsll(__ballot(past > r - above)) - 1, a.B - 1);
+    local = r - above - __builtin_amdgcn_readlane(past - same, b);
     first = __builtin_amdgcn_readlane(upto - mine, b);
     tile0 = __builtin_amdgcn_readlane(tiles - load.tiles, b);
     p.s = Seq{__builtin_amdgcn_readlane(s.start, b), __builtin_amdgcn_readlane(s.n, b), __builtin_amdgcn_readlane(s.ctx, b)};
@@ -165,30 +184,32 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
     total = a.head[0];
     L = a.head[2];
     if (at >= total) return p;
-    const int i = total - 1 - at;
-    // the last sequence whose pieces start at or before i, 64 probes at a time
+    const int r = rank_of(a, at, total);
+    // the last sequence, in the order of their pieces' lengths, whose pieces start at or before r, 64 probes at a time
     int lo = 0, len = a.B;
     while (len > 1) {
       const int step = (len + 63) / 64, x = lo + lane * step;
-      const int n = __popcll(__ballot(lane * step < len && a.item_start[min(x, a.B - 1)] <= i));
+      const int n = __popcll(__ballot(lane * step < len && a.item_start[min(x, a.B - 1)] <= r));
       lo += (n - 1) * step;
       len = min(step, len - (n - 1) * step);
     }
-    b = __builtin_amdgcn_readfirstlane(lo);
-    first = a.item_start[b];
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    b = a.order[lo];
+    first = a.item_start[lo];
+    local = r - first;
     tile0 = a.tile_start[b];
     p.s = seq_of(a, b);
   }
   const Load load = load_of(a, p.s);
-  const int pieces = pieces_of(load, L), local = total - 1 - at - first, t = quotient(local, pieces), piece = local - t * pieces;
+  const int pieces = pieces_of(load, L), back = quotient(local, pieces), t = load.tiles - 1 - back, piece = local - back * pieces;
   p.b = b;
   p.row0 = t * a.bm;
-  const int i = (min(p.row0 + a.bm, p.s.n * a.gq) - 1) / a.gq, units = int2_units(a, p.s, i) + own_units(a, i);
+  const int i = quotient(min(p.row0 + a.bm, p.s.n * a.gq) - 1, a.gq), units = int2_units(a, p.s, i) + own_units(a, i);
   p.u0 = (int)((long long)units * piece / pieces);
   p.u1 = (int)((long long)units * (piece + 1) / pieces);
-  p.slot = pieces > 1 ? total - 1 - at : -1;
-  p.valid = t < load.tiles && p.slot < a.max_slots;
-  if (piece == 0 && h == 0 && threadIdx.x == 0 && tile0 + t < a.max_tiles)
+  p.slot = pieces > 1 ? first + local : -1;
+  p.valid = t >= 0 && p.slot < a.max_slots;
+  if (piece == 0 && h == 0 && threadIdx.x == 0 && t >= 0 && tile0 + t < a.max_tiles)
     a.tiles[tile0 + t] = ChunkTile{p.row0, p.s.start, p.s.n, pieces, p.slot};
   // the same in every lane: into scalar registers
   auto one = [](int x) { return __builtin_amdgcn_readfirstlane(x); };

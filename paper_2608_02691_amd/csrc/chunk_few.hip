@@ -16,7 +16,7 @@ namespace {
 constexpr int kFewWaves = 4;
 constexpr int kStep = 32;                 // tokens of a step over the chunk's own
 constexpr int kStages = 4;                // two units, two stages each
-constexpr int kStageBytes = 2 * (1024 + 512);         // codes of two pages, then 512 bytes each of their parameters
+constexpr int kStageBytes = 2 * (1024 + 512);  // codes of two pages, then 512 bytes each of their parameters
 
 struct FewLds {
   union {
@@ -34,13 +34,21 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
   using Lay = Rec<NG>;
   __shared__ __align__(16) FewLds lds;
   const int H = a.cv.num_kv_heads;
-  const int h = (int)(blockIdx.x % H);
-  const Place place = locate(a, (int)(blockIdx.x / H), h);
+  const int at = quotient((int)blockIdx.x, H), h = (int)blockIdx.x - at * H;
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = l & 31, hh = l >> 5;
+  float rk[8][8];  // the wave's columns of R_K: rows 16 kk + 8 hh .. of column 32 w + n
+  if (a.max_ctx > 0) {  // on their way while the work-group finds its piece
+    const float* R = a.R_k + (size_t)h * kHeadDim * kHeadDim + (size_t)(8 * hh) * kHeadDim + 32 * w + n;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) rk[kk][j] = R[(size_t)(16 * kk + j) * kHeadDim];
+  }
+  const Place place = locate(a, at, h);
   if (!place.valid) return;
   const Seq seq = place.s;
-  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = l & 31, hh = l >> 5;
-  const int rows = seq.n * a.gq, row = place.row0 + n, rc = min(row, rows - 1), tok = rc / a.gq, tok_tile = place.row0 / a.gq;
-  const int nI = int2_units(a, seq, (min(place.row0 + a.bm, rows) - 1) / a.gq);
+  const int rows = seq.n * a.gq, row = place.row0 + n, rc = min(row, rows - 1), tok = quotient(rc, a.gq), tok_tile = quotient(place.row0, a.gq);
+  const int nI = int2_units(a, seq, quotient(min(place.row0 + a.bm, rows) - 1, a.gq));
   auto limit = [&](int t) { return a.k_new ? seq.ctx : min(seq.ctx, seq.ctx - seq.n + 1 + t); };
   const int lim = limit(tok), lim_tile = limit(tok_tile);  // tokens the row sees, the least of the tile's
 
@@ -52,6 +60,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
   };
   const bool cached = place.u0 < min(place.u1, nI);
   float m = 0.0f, sum = 0.0f, thr = kNone;
+  // Behind the un-rotation row m = 8 u + 4 h + v of a wave's tile is channel 32 w + 16 (u / 2) + 8 h + 4 (u % 2) + v, so that a
+  // lane's results are eight neighbours at a time; the operand's k order is the channel order the sums lie in
+  const int ch = 32 * w + 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
+  float4 rv[8][2];  // its row of R_V
   {
     cd_f16_t O[4];
 #pragma unroll
@@ -95,24 +107,13 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
       if (s0 + 1 < s1) issue(s0 + 1);
     }
     if (cached) {
-      // q R_K with log2(e) / sqrt(128): wave w forms the 32 channels 32 w .. of q', R_K's columns straight from memory in
-      // two bf16 terms (q is exact), and puts them where the products take them
+      // q R_K with log2(e) / sqrt(128): wave w forms the 32 channels 32 w .. of q' (q is exact in fp16, R_K's elements are
+      // rounded to it, 2^-12 of each) and puts them where the products take them
       cd_b8_t Qb[8];
       query(Qb);
-      const float* R = a.R_k + (size_t)h * kHeadDim * kHeadDim + (size_t)(8 * hh) * kHeadDim + 32 * w + n;
       cd_f16_t d = splat16(0.0f);
 #pragma unroll
-      for (int kk = 0; kk < 8; ++kk) {
-        cd_b8_t hi, lo;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const float r = R[(size_t)(16 * kk + j) * kHeadDim];
-          hi[j] = (__bf16)r;
-          lo[j] = (__bf16)(r - (float)hi[j]);
-        }
-        d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo, Qb[kk], d, 0, 0, 0);
-        d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi, Qb[kk], d, 0, 0, 0);
-      }
+      for (int kk = 0; kk < 8; ++kk) d = HalfOps::mfma(pack_half8(rk[kk]), half_of(Qb[kk]), d);
       // register r: channel 32 w + c, c = 8 (r / 4) + 4 hh + r % 4; channels 16 p + 2 x, + 1 are elements 2 (p % 4), + 1 of
       // operand 2 (x % 4) + p / 4 in lane half x / 4
 #pragma unroll
@@ -264,6 +265,11 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
         }
       }
     }
+    if (cached) {
+      const float* R = a.R_v + ((size_t)h * kHeadDim + ch) * kHeadDim + 4 * hh;
+#pragma unroll
+      for (int op = 0; op < 8; ++op) rv[op][0] = *reinterpret_cast<const float4*>(R + 16 * op), rv[op][1] = *reinterpret_cast<const float4*>(R + 16 * op + 8);
+    }
     // ---- the waves' results meet
     __syncthreads();
 #pragma unroll
@@ -304,17 +310,12 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
       lds.b[2 * w + x][l] = b;
     }
     __syncthreads();
-    // output row m = 8 u + 4 h + v of the tile: channel 32 w + 16 (u / 2) + 8 h + 4 (u % 2) + v, so that a lane's results
-    // are eight neighbours at a time; the operand's k order is the channel order the sums lie in
-    const int ch = 32 * w + 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
-    const float* R = a.R_v + ((size_t)h * kHeadDim + ch) * kHeadDim + 4 * hh;
     cd_f16_t d = splat16(0.0f);
 #pragma unroll
     for (int op = 0; op < 8; ++op) {
-      const float4 u = *reinterpret_cast<const float4*>(R + 16 * op), v = *reinterpret_cast<const float4*>(R + 16 * op + 8);
-      const cd_h8_t A = {(_Float16)u.x, (_Float16)u.y, (_Float16)u.z, (_Float16)u.w,
-                         (_Float16)v.x, (_Float16)v.y, (_Float16)v.z, (_Float16)v.w};
-      d = HalfOps::mfma(A, lds.b[op][l], d);
+      const float4 u = rv[op][0], v = rv[op][1];
+      const float x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+      d = HalfOps::mfma(pack_half8(x), lds.b[op][l], d);
     }
     O[0] = d * all;
   }
@@ -329,9 +330,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
     query(Qb);
     float base = kBias - m - query_mean(Qb, a.mu + (size_t)h * kHeadDim, hh);
     const uint16_t* kb = a.k_new + seq.start * a.k_stride + (size_t)h * kHeadDim + 8 * hh;
-    const int ch = 32 * w + 16 * (n >> 4) + 8 * ((n >> 2) & 1) + 4 * ((n >> 3) & 1) + (n & 3);
     const uint16_t* vb = a.v_new + seq.start * a.v_stride + (size_t)h * kHeadDim + ch;
-    const int last = (min(place.row0 + a.bm, rows) - 1) / a.gq;  // the tile's last token
+    const int last = quotient(min(place.row0 + a.bm, rows) - 1, a.gq);  // the tile's last token
     for (int s = c0 * (kUnit / kStep); s < c1 * (kUnit / kStep) && kStep * s <= last; ++s) {
       const uint16_t* kr = kb + min(kStep * s + (n & 16) + row_token(n & 15), seq.n - 1) * a.k_stride;
       cd_h8_t k[8];

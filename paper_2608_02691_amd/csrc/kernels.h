@@ -206,17 +206,18 @@ struct ChunkArgs {
   const float* mu;
   uint16_t* out;                    // bf16 [total_q, Hq, 128]
   // plan and workspace
-  int bm, resident, min_piece, max_tiles, max_items, max_slots;
+  int bm, resident, per_cu, min_piece, max_tiles, max_items, max_slots;
   float piece_units, merge_units;
   int32_t* head;                    // pieces (per KV head), tiles, units of a piece
-  int32_t *item_start, *tile_start; // [B] (batches above kChunkWaveSeqs)
+  int32_t *order, *item_start;      // [B] (batches above kChunkWaveSeqs) sequences by their pieces' length, their first pieces
+  int32_t* tile_start;              // [B] (the same) the sequences' first tiles
   ChunkTile* tiles;                 // [max_tiles]
   float* part;                      // [max_slots, H, bm * kChunkPartStride]
 };
 struct ChunkPlan {
   int waves, bm, resident, min_piece, max_tiles, max_items, max_slots;
   float piece_units, merge_units;
-  size_t off_head, off_items, off_starts, off_tiles, off_part, total;
+  size_t off_head, off_order, off_items, off_starts, off_tiles, off_part, total;
 };
 ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx);
 hipError_t launch_chunk_few(const ChunkArgs& a, hipStream_t s);  // (chunk_few.hip) tiles of 32 rows
