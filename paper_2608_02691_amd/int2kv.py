@@ -140,7 +140,13 @@ def _check(status: int, name: str) -> None:
         raise RuntimeError(f"{name} failed with status {status}: {msg}")
 
 
+# The current stream's handle without a Stream object around it (2.6 us less a call), where this torch has the function
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
 def _stream() -> int:
+    if _raw_stream is not None:
+        return _raw_stream(torch.cuda.current_device())
     return torch.cuda.current_stream().cuda_stream
 
 
@@ -530,12 +536,14 @@ def _head_rows(t: torch.Tensor, heads: Optional[int], name: str):
         raise TypeError(f"{name} must be a CUDA (HIP) tensor")
     if t.dtype not in _BF16:
         raise TypeError(f"{name} has dtype {t.dtype}, expected one of {_BF16}")
-    if t.dim() != 3 or t.shape[2] != HEAD_DIM or (heads is not None and t.shape[1] != heads):
+    shape = t.shape
+    if len(shape) != 3 or shape[2] != HEAD_DIM or (heads is not None and shape[1] != heads):
         raise ValueError(f"{name} must be [n, {heads if heads is not None else 'heads'}, 128]")
+    n, h, _ = shape
     st = t.stride()
-    if t.numel() and (st[2] != 1 or (t.shape[1] > 1 and st[1] != HEAD_DIM)):
+    if n and h and (st[2] != 1 or (h > 1 and st[1] != HEAD_DIM)):
         raise ValueError(f"{name}: the heads of a token must be contiguous")
-    return t.data_ptr(), st[0] if t.shape[0] > 1 else t.shape[1] * HEAD_DIM
+    return t.data_ptr(), st[0] if n > 1 else h * HEAD_DIM
 
 
 def rope_axis_table(counts, interleaved: bool = False):
