@@ -336,7 +336,8 @@ int int2kv_output_error(const int2kv_cache* cache, const uint16_t* q, int batch,
  *   num_axes     : 1 .. 8;  pair_axis: HOST uint8 [64], the axis of each pair
  *   cos_sin      : fp32 [max_pos, 128], as in int2kv_quantize_append_rope; 16-byte aligned
  *   q_out, k_out : bf16 rows as q, k with strides of their own; may be q, k themselves (same stride),
- *                  otherwise no output row may overlap an input's or the other output's rows */
+ *                  otherwise no output row may overlap an input's or the other output's rows
+ *   num_tokens   : below 2^27 */
 int int2kv_rope_axes(const uint16_t* q, int num_q_heads, int64_t q_stride, const uint16_t* k, int num_kv_heads,
                      int64_t k_stride, const int32_t* positions, int num_axes, const uint8_t* pair_axis,
                      int num_tokens, const float* cos_sin, int max_pos, uint16_t* q_out, int64_t q_out_stride,
@@ -353,7 +354,7 @@ enum {
  *     k_out[i] = k^ R_K^T + mu,   v_out[i] = v^ R_V^T,   k^, v^ = code * s + z of slot slot_mapping[i];
  * without R_k (R_v) the row as stored, k^ (v^), in the rotated basis.
  *   slot_mapping : int32 [num_tokens], in any order, repeats allowed; a slot outside the cache (also a
- *                  negative one) leaves its output rows as they were
+ *                  negative one) leaves its output rows as they were; num_tokens * H_kv below 2^28
  *   R_k, R_v     : fp32 [H_kv, 128, 128], 16-byte aligned, or NULL;  mu: fp32 [H_kv, 128] or NULL (keys
  *                  stay centered); mu needs R_k
  *   row_format   : INT2KV_ROWS_BF16 or INT2KV_ROWS_F32
@@ -391,9 +392,10 @@ int int2kv_read_rows(const int2kv_cache* cache, const int32_t* slot_mapping, int
  *   out          : bf16 [total_q, H_q, 128], 16-byte aligned, model basis; must not overlap q, k_new, v_new
  *   workspace    : int2kv_chunk_attention_workspace_bytes(...) bytes, 256-byte aligned; nothing in it
  *                  needs to be kept or cleared between calls, calls that overlap need one each
- * Products run on the matrix cores with fp32 sums: rotated queries, dequantized rows and the
- * probabilities over the INT2 tokens in fp16, those over the chunk's own tokens in bf16, each rounded
- * once; softmax statistics in fp32. Dequantized values have to lie within fp16's range (|x| <= 65504).
+ * Products run on the matrix cores with fp32 sums: queries and rotations, rotated queries, dequantized
+ * rows and the probabilities over the INT2 tokens in fp16, the chunk's own rows and the probabilities
+ * over them in bf16, each rounded once; softmax statistics in fp32. Queries (where the cache holds
+ * anything), rotations and dequantized values have to lie within fp16's range (|x| <= 65504).
  * A non-finite key or value reaches only the tokens that see it. Deterministic; no atomics on results. */
 size_t int2kv_chunk_attention_workspace_bytes(int batch, int num_q_heads, int num_kv_heads, int total_q, int max_q,
                                               int max_ctx);

@@ -661,6 +661,7 @@ int int2kv_rope_axes(const uint16_t* q, int num_q_heads, int64_t q_stride, const
   if (!pair_axis) return fail(INT2KV_EINVAL, "NULL pointer argument");
   for (int i = 0; i < kHeadDim / 2; ++i)
     if (pair_axis[i] >= num_axes) return fail(INT2KV_EINVAL, "pair_axis names an axis outside [0, num_axes)");
+  if (num_tokens >= 1 << 27) return fail(INT2KV_EUNSUPPORTED, "num_tokens must be below 2^27");
   if (num_tokens == 0 || num_q_heads + num_kv_heads == 0) return ok();
   if (!positions || !cos_sin || (num_q_heads && (!q || !q_out)) || (num_kv_heads && (!k || !k_out)))
     return fail(INT2KV_EINVAL, "NULL pointer argument");
@@ -694,6 +695,8 @@ int int2kv_read_rows(const int2kv_cache* cache, const int32_t* slot_mapping, int
   if (row_format != INT2KV_ROWS_BF16 && row_format != INT2KV_ROWS_F32) return fail(INT2KV_EINVAL, "unknown row_format");
   if (cache->num_kv_heads > 65535) return fail(INT2KV_EUNSUPPORTED, "at most 65535 KV heads");
   if (mu && !R_k) return fail(INT2KV_EINVAL, "mu needs R_k");
+  if ((int64_t)num_tokens * cache->num_kv_heads >= 1 << 28)
+    return fail(INT2KV_EUNSUPPORTED, "num_tokens * num_kv_heads must be below 2^28");
   if (num_tokens == 0) return ok();
   if (!slot_mapping || (!k_out && !v_out)) return fail(INT2KV_EINVAL, "NULL pointer argument");
   const bool f32 = row_format == INT2KV_ROWS_F32;
@@ -740,7 +743,8 @@ int int2kv_chunk_attention(const int2kv_cache* cache, const uint16_t* q, int64_t
       rows_meet(ro, Rows{v_new, v_stride, H, total_q, 2}))))
     return fail(INT2KV_EINVAL, "out overlaps q, k_new or v_new");
   const ChunkPlan plan = make_chunk_plan(batch, num_q_heads, H, total_q, max_q, max_ctx);
-  if ((int64_t)plan.max_items * H > INT32_MAX) return fail(INT2KV_EUNSUPPORTED, "too many row tiles for one launch");
+  // a launch holds 2^32 - 1 threads
+  if ((int64_t)plan.max_items * H > UINT32_MAX / (plan.waves == 8 ? 512 : 256)) return fail(INT2KV_EUNSUPPORTED, "too many row tiles for one launch");
   if (!workspace || workspace_bytes < plan.total)
     return fail(INT2KV_EWORKSPACE, "workspace smaller than int2kv_chunk_attention_workspace_bytes()");
   if (!aligned(workspace, 256)) return fail(INT2KV_EINVAL, "workspace must be 256-byte aligned");

@@ -80,7 +80,7 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   for (int k = 0; k < kCuts; ++k) {
     const int c = cut_of(a, k, even, umax);
     const float cost = cost_of(a, c, counts[k], T, even, places, umax);
-    if (k == 0 || (fits(counts[k], T, places) && cost < best)) best = cost, L = c;
+    if (k == 0 || (fits(a, counts[k], T, places) && cost < best)) best = cost, L = c;
   }
   // sequences by classes of their pieces' length; within a class in any order, which changes no result
   auto class_of = [&](const Load& s) {

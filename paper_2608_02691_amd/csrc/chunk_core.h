@@ -72,7 +72,7 @@ constexpr int kCuts = 12;
 // on the chip evenly, once or (from 8 on) three times. even: units of a place
 __device__ __forceinline__ int cut_of(const ChunkArgs& a, int k, float even, int umax) {
   if (k == 0) return max(umax, 1);
-  return max(a.min_piece, (int)(even * (k < 8 ? 0.85f + 0.15f * (float)k : 0.35f + 0.15f * (float)(k - 8))) + 1);
+  return max(a.min_piece, (int)fminf(even * (k < 8 ? 0.85f + 0.15f * (float)k : 0.35f + 0.15f * (float)(k - 8)), 1.0e9f) + 1);
 }
 __device__ __forceinline__ int pieces_of(const Load& s, int L) { return s.tiles == 0 ? 0 : max(1, quotient(s.units + L - 1, L)); }
 // The time in units with pieces of at most c units, n of them a KV head; places: a KV head's part of the chip
@@ -87,8 +87,10 @@ __device__ __forceinline__ float cost_of(const ChunkArgs& a, int c, int n, int T
 __device__ __forceinline__ float places_of(const ChunkArgs& a) {
   return (float)a.resident * __builtin_amdgcn_rcpf((float)a.cv.num_kv_heads);
 }
-// whether n pieces may be: while the tiles have a place each, so must the pieces; never more than three rounds
-__device__ __forceinline__ bool fits(int n, int T, float places) { return (float)n <= ((float)T <= places ? places : 3.0f * places); }
+// whether n pieces may be: they have room, and a place each while the tiles have one
+__device__ __forceinline__ bool fits(const ChunkArgs& a, int n, int T, float places) {
+  return n <= a.max_slots && ((float)T > places || (float)n <= places);
+}
 
 // Sum and maximum over the wave: rotations inside rows of 16 lanes, then swaps of rows and halves
 template <class F>
@@ -159,7 +161,7 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
     for (int k = 0; k < kCuts; ++k) {
       const int c = cut_of(a, k, even, umax), n = wave_sum(load.tiles * pieces_of(load, c));
       const float cost = cost_of(a, c, n, T, even, places, umax);
-      if (k == 0 || (fits(n, T, places) && cost < best)) best = cost, L = c;
+      if (k == 0 || (fits(a, n, T, places) && cost < best)) best = cost, L = c;
     }
     const int pieces_b = pieces_of(load, L), mine = load.tiles * pieces_b, upto = wave_scan(mine);
     total = __builtin_amdgcn_readlane(upto, 63);

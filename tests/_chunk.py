@@ -51,16 +51,20 @@ def stored_rows(pool, block_row, length):
 
 
 class Chunk:
-    """One call's inputs. seqs: (new tokens, cached tokens) each; cached: the cache holds the new tokens too."""
+    """One call's inputs. seqs: (new tokens, cached tokens) each; cached: the cache holds the new tokens too; blocks: the
+    sequences draw their pages from so many, with repetition, instead of having their own."""
 
     def __init__(self, seqs, heads, gq, group=32, cached=False, seed=0, k_scale=1.0, v_scale=1.0, pad=0, fused=False,
-                 spare=3):
+                 spare=3, blocks=None):
         rng = np.random.default_rng(seed)
         self.seqs, self.H, self.gq, self.group, self.cached = seqs, heads, gq, group, cached
         self.Hq, self.total = heads * gq, sum(n for n, _ in seqs) + pad
         pages = [-(-c // PAGE) for _, c in seqs]
-        blocks = sum(pages) + spare
-        perm = rng.permutation(blocks).astype(np.int32)
+        if blocks is None:
+            blocks = sum(pages) + spare
+            perm = rng.permutation(blocks).astype(np.int32)
+        else:
+            perm = rng.integers(0, blocks, sum(pages)).astype(np.int32)
         self.table = np.full((len(seqs), max(1, max(pages)) + 1), -1, np.int32)
         at = 0
         for b, m in enumerate(pages):

@@ -35,6 +35,8 @@ def test_rope_axes_refusals(kw, word):
 def test_rope_axes_with_nothing_to_do():
     assert _rope(n=0)[0] == K.INT2KV_OK
     assert _rope(hq=0, hk=0)[0] == K.INT2KV_OK
+    st, msg = _rope(n=1 << 27)  # more than a launch holds
+    assert st == K.INT2KV_EUNSUPPORTED and b"num_tokens" in msg
 
 
 def test_axis_tables():
@@ -64,6 +66,8 @@ def test_read_rows_refusals(kw, word):
 
 def test_read_rows_of_nothing_and_bad_caches():
     assert _read(n=0)[0] == K.INT2KV_OK
+    st, msg = _read(n=1 << 27)  # two heads: more than a launch holds
+    assert st == K.INT2KV_EUNSUPPORTED and b"num_tokens" in msg
     assert _read(cache=K._Cache(16, 4, 2, 16, 128, 64))[0] == K.INT2KV_EUNSUPPORTED
     assert _read(cache=K._Cache(16, 4, 2, 8, 128, 32))[0] == K.INT2KV_EUNSUPPORTED
 
@@ -102,6 +106,9 @@ def test_chunk_attention_workspace():
     assert st == K.INT2KV_EWORKSPACE and b"workspace" in msg
     assert _chunk(ws=None)[0] == K.INT2KV_EWORKSPACE
     assert _chunk(total=1 << 30, max_q=1)[0] == K.INT2KV_EUNSUPPORTED
+    # 2^23 sequences of a token: as many work-groups a KV head as a launch of two holds, and one more
+    assert _chunk(total=(1 << 23) - 1, B=(1 << 23) - 1, max_q=1, q=1 << 40, k=2 << 40, v=3 << 40, out=4 << 40, wb=0)[0] == K.INT2KV_EWORKSPACE
+    assert _chunk(total=1 << 23, B=1 << 23, max_q=1, q=1 << 40, k=2 << 40, v=3 << 40, out=4 << 40)[0] == K.INT2KV_EUNSUPPORTED
     assert _chunk(max_q=0)[0] == K.INT2KV_OK and _chunk(total=0)[0] == K.INT2KV_OK
     for bad in ((0, 4, 2, 8, 8, 64), (2, 3, 2, 8, 8, 64), (2, 4, 2, -1, 8, 64), (2, 4, 2, 8, 8, -1)):
         assert lib.int2kv_chunk_attention_workspace_bytes(*bad) == 0
