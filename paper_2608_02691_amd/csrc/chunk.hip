@@ -75,7 +75,7 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   for (int b = tid; b < a.B; b += kPlanThreads) {
     const Load s = load_of(a, seq_of(a, b));
 #pragma unroll
-    for (int k = 0; k < kCuts; ++k) mine[k] += s.tiles * pieces_of(s, cut_of(a, k, even, umax));
+    for (int k = 0; k < kCuts; ++k) mine[k] += s.tiles * pieces_of(s.units, cut_of(a, k, even, umax));
   }
 #pragma unroll
   for (int k = 0; k < kCuts; ++k) atomicAdd(&counts[k], mine[k]);
@@ -89,8 +89,8 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   }
   // sequences by classes of their pieces' length; within a class in any order, which changes no result
   auto class_of = [&](const Load& s) {
-    const int n = pieces_of(s, L);
-    return n == 0 ? kClasses - 1 : (int)((float)(kClasses - 1) * (1.0f - (float)quotient(s.units + n - 1, n) / (float)max(umax, 1)));
+    const int n = pieces_of(s.units, L);
+    return s.tiles == 0 ? kClasses - 1 : (int)((float)(kClasses - 1) * (1.0f - (float)quotient(s.units + n - 1, n) / (float)max(umax, 1)));
   };
   T = 0;
   for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
     const int x = b0 + tid;
     const Load s = x < a.B ? load_of(a, seq_of(a, a.order[x])) : Load{0, 0};
-    const int items = s.tiles * pieces_of(s, L);
+    const int items = s.tiles * pieces_of(s.units, L);
     int n_items;
     const int i = total + block_scan(items, tmp, n_items) - items;
     if (x < a.B) a.item_start[x] = i;

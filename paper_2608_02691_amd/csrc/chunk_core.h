@@ -67,14 +67,15 @@ __device__ __forceinline__ Load load_of(const ChunkArgs& a, const Seq& s) {
   if (rows == 0) return Load{0, 0};
   return Load{quotient(rows + a.bm - 1, a.bm), int2_units(a, s, s.n - 1) + own_units(a, s.n - 1)};
 }
-constexpr int kCuts = 12;
+constexpr int kCuts = 16;
 // Candidate k: units of a piece. The first leaves the tiles whole; the others lie above the size that would fill the places
-// on the chip evenly, once or (from 8 on) three times. even: units of a place
+// on the chip evenly, once or (from 10 on) up to three times. even: units of a place
 __device__ __forceinline__ int cut_of(const ChunkArgs& a, int k, float even, int umax) {
   if (k == 0) return max(umax, 1);
-  return max(a.min_piece, (int)fminf(even * (k < 8 ? 0.85f + 0.15f * (float)k : 0.35f + 0.15f * (float)(k - 8)), 1.0e9f) + 1);
+  return max(a.min_piece, (int)fminf(even * (k < 10 ? 0.85f + 0.15f * (float)k : 0.32f + 0.12f * (float)(k - 10)), 1.0e9f) + 1);
 }
-__device__ __forceinline__ int pieces_of(const Load& s, int L) { return s.tiles == 0 ? 0 : max(1, quotient(s.units + L - 1, L)); }
+// Pieces of a tile of so many units
+__device__ __forceinline__ int pieces_of(int units, int L) { return max(1, quotient(units + L - 1, L)); }
 // The time in units with pieces of at most c units, n of them a KV head; places: a KV head's part of the chip
 __device__ __forceinline__ float cost_of(const ChunkArgs& a, int c, int n, int T, float even, float places, int umax) {
   const float one = (float)min(c, umax) + a.piece_units, fn = (float)n;
@@ -107,6 +108,16 @@ __device__ __forceinline__ int wave_fold(int x, F f) {
 __device__ __forceinline__ int wave_sum(int x) {
   return wave_fold(x, [](int a, int b) { return a + b; });
 }
+__device__ __forceinline__ float wave_sum(float x) {  // the same order, so the same sum, in every wave
+  return __int_as_float(wave_fold(__float_as_int(x), [](int a, int b) { return __float_as_int(__int_as_float(a) + __int_as_float(b)); }));
+}
+// Sum over the lanes l % 16
+__device__ __forceinline__ int quarters_sum(int x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = (int)r[0] + (int)r[1];
+  const auto h = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return (int)h[0] + (int)h[1];
+}
 // Inclusive sum over the wave: shifts inside rows of 16 lanes, then the rows' and the halves' last lanes onto those behind
 __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);
@@ -138,39 +149,33 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
   const int lane = threadIdx.x & 63;
   Place p;
   p.valid = false;
-  int total, T, L, b, first, tile0, local;
+  Load load;
+  int total, T, b, first, tile0, local, pieces;
   if (a.B <= kChunkWaveSeqs) {
     Seq s{0, 0, 0};
     if (lane < a.B) s = seq_of(a, lane);
-    const Load load = load_of(a, s);
+    load = load_of(a, s);
     const int tiles = wave_scan(load.tiles);
     T = __builtin_amdgcn_readlane(tiles, 63);
-    const int umax = wave_fold(load.units, [](int a, int b) { return max(a, b); });
-    float W = (float)load.tiles * (float)load.units;
-    if (a.B > 1) {
-      // units times tiles in two integers, so that the sum is the same however it is formed
-      const long long w = (long long)load.tiles * load.units;
-      W = (float)wave_sum((int)(w >> 20)) * 1048576.0f + (float)wave_sum((int)(w & 0xFFFFF));
-    } else {
-      W = __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(W)));
-    }
-    const float places = places_of(a), even = W * __builtin_amdgcn_rcpf(places);
-    float best = 0.0f;
-    L = 1;
-#pragma unroll
-    for (int k = 0; k < kCuts; ++k) {
-      const int c = cut_of(a, k, even, umax), n = wave_sum(load.tiles * pieces_of(load, c));
-      const float cost = cost_of(a, c, n, T, even, places, umax);
-      if (k == 0 || (fits(a, n, T, places) && cost < best)) best = cost, L = c;
-    }
-    const int pieces_b = pieces_of(load, L), mine = load.tiles * pieces_b, upto = wave_scan(mine);
+    const int umax = wave_fold(load.units, [](int x, int y) { return max(x, y); });
+    const float W = wave_sum((float)load.tiles * (float)load.units), places = places_of(a), even = W * __builtin_amdgcn_rcpf(places);
+    // A candidate per lane (of sixteen), a quarter of the sequences per sixteen lanes
+    const int c = cut_of(a, lane & 15, even, umax);
+    int n = 0;
+    for (int i = lane >> 4; i < ((a.B + 3) & ~3); i += 4) n += __shfl(load.tiles, i) * pieces_of(__shfl(load.units, i), c);
+    n = quarters_sum(n);
+    const bool may = (lane & 15) == 0 || fits(a, n, T, places);
+    const int cost = __float_as_int(may ? cost_of(a, c, n, T, even, places, umax) : INFINITY);  // (positive: ordered as integers)
+    const int best = wave_fold(cost, [](int x, int y) { return min(x, y); });
+    const int L = __builtin_amdgcn_readlane(c, __ffsll(__ballot(cost == best)) - 1);
+    const int mine_k = load.tiles > 0 ? pieces_of(load.units, L) : 0, mine = load.tiles * mine_k, upto = wave_scan(mine);
     total = __builtin_amdgcn_readlane(upto, 63);
     if (at == 0 && h == 0 && threadIdx.x == 0) a.head[1] = total > a.max_items || T > a.max_tiles ? 0 : T;
     total = min(total, a.max_items);
     if (at >= total) return p;
-    const int r = rank_of(a, at, total), size = mine > 0 ? quotient(load.units + pieces_b - 1, pieces_b) : -1;
+    const int r = rank_of(a, at, total), size = mine > 0 ? quotient(load.units + mine_k - 1, mine_k) : -1;
     // the length of piece r: the greatest that more than r pieces have
-    int lo = 0, hi = umax, above = 0;
+    int hi = wave_fold(size, [](int x, int y) { return max(x, y); }), lo = a.B == 1 ? hi : 0, above = 0;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1, n = wave_sum(size >= mid ? mine : 0);
       if (n > r) lo = mid;
@@ -181,10 +186,11 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
     local = r - above - __builtin_amdgcn_readlane(past - same, b);
     first = __builtin_amdgcn_readlane(upto - mine, b);
     tile0 = __builtin_amdgcn_readlane(tiles - load.tiles, b);
+    pieces = __builtin_amdgcn_readlane(mine_k, b);
+    load.tiles = __builtin_amdgcn_readlane(load.tiles, b);
     p.s = Seq{__builtin_amdgcn_readlane(s.start, b), __builtin_amdgcn_readlane(s.n, b), __builtin_amdgcn_readlane(s.ctx, b)};
   } else {
     total = a.head[0];
-    L = a.head[2];
     if (at >= total) return p;
     const int r = rank_of(a, at, total);
     // the last sequence, in the order of their pieces' lengths, whose pieces start at or before r, 64 probes at a time
@@ -201,14 +207,16 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
     local = r - first;
     tile0 = a.tile_start[b];
     p.s = seq_of(a, b);
+    load = load_of(a, p.s);
+    pieces = pieces_of(load.units, a.head[2]);
   }
-  const Load load = load_of(a, p.s);
-  const int pieces = pieces_of(load, L), back = quotient(local, pieces), t = load.tiles - 1 - back, piece = local - back * pieces;
+  const int back = quotient(local, pieces), t = load.tiles - 1 - back, piece = local - back * pieces;
   p.b = b;
   p.row0 = t * a.bm;
   const int i = quotient(min(p.row0 + a.bm, p.s.n * a.gq) - 1, a.gq), units = int2_units(a, p.s, i) + own_units(a, i);
-  p.u0 = (int)((long long)units * piece / pieces);
-  p.u1 = (int)((long long)units * (piece + 1) / pieces);
+  const int each = quotient(units, pieces), more = units - each * pieces;  // the first `more` pieces have one more
+  p.u0 = each * piece + min(piece, more);
+  p.u1 = p.u0 + each + (piece < more ? 1 : 0);
   p.slot = pieces > 1 ? first + local : -1;
   p.valid = t >= 0 && p.slot < a.max_slots;
   if (piece == 0 && h == 0 && threadIdx.x == 0 && t >= 0 && tile0 + t < a.max_tiles)
