@@ -50,10 +50,10 @@ __device__ __forceinline__ int block_scan(int x, int* tmp, int& total) {
 // The plan of a batch too large for every wave to hold, by one block
 __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   constexpr int kClasses = 64;
-  __shared__ int tmp[kPlanThreads / 64], counts[kCuts], classes[kClasses], longest;
+  __shared__ int tmp[kPlanThreads / 64], counts[kCuts], parts[kCuts], classes[kClasses], longest;
   __shared__ unsigned long long work;
   const int tid = threadIdx.x;
-  if (tid < kCuts) counts[tid] = 0;
+  if (tid < kCuts) counts[tid] = 0, parts[tid] = 0;
   if (tid < kClasses) classes[tid] = 0;
   if (tid == 0) longest = 0, work = 0;
   __syncthreads();
@@ -71,20 +71,24 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   __syncthreads();
   const int umax = longest;
   const float places = places_of(a), even = (float)work * __builtin_amdgcn_rcpf(places);
-  int mine[kCuts] = {};
+  int mine[kCuts] = {}, cut[kCuts] = {};
   for (int b = tid; b < a.B; b += kPlanThreads) {
     const Load s = load_of(a, seq_of(a, b));
 #pragma unroll
-    for (int k = 0; k < kCuts; ++k) mine[k] += s.tiles * pieces_of(s.units, cut_of(a, k, even, umax));
+    for (int k = 0; k < kCuts; ++k) {
+      const int n = pieces_of(s.units, cut_of(a, k, even, umax));
+      mine[k] += s.tiles * n;
+      cut[k] += n > 1 ? s.tiles * n : 0;
+    }
   }
 #pragma unroll
-  for (int k = 0; k < kCuts; ++k) atomicAdd(&counts[k], mine[k]);
+  for (int k = 0; k < kCuts; ++k) atomicAdd(&counts[k], mine[k]), atomicAdd(&parts[k], cut[k]);
   __syncthreads();
   float best = 0.0f;
   int L = 1;
   for (int k = 0; k < kCuts; ++k) {
     const int c = cut_of(a, k, even, umax);
-    const float cost = cost_of(a, c, counts[k], T, even, places, umax);
+    const float cost = cost_of(a, c, counts[k], parts[k], even, places, umax);
     if (k == 0 || (fits(a, counts[k], T, places) && cost < best)) best = cost, L = c;
   }
   // sequences by classes of their pieces' length; within a class in any order, which changes no result
@@ -638,13 +642,14 @@ ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_
   p.bm = 32 * p.waves;
   p.resident = num_cus() * (p.waves == 8 ? 1 : 2);
   p.min_piece = p.waves == 1 ? 4 : 2;  // a unit for each wave of the kernel of few rows
-  p.piece_units = p.waves == 1 ? 10.0f : 3.0f;
-  p.merge_units = p.waves == 1 ? 0.016f : 0.00013f * p.bm;
+  p.piece_units = p.waves == 1 ? 10.0f : 4.0f;
+  p.merge_units = p.waves == 1 ? 0.016f : 0.00009f * p.bm;
   const long long per_seq = (seq_rows + p.bm - 1) / p.bm;
   long long tiles = B * per_seq, by_rows = rows / p.bm + B;
   tiles = tiles < by_rows ? tiles : by_rows;
   p.max_tiles = (int)(tiles < 1 ? 1 : tiles);
-  // pieces a KV head: a place on the chip each while the tiles have one, else up to three; never more than the units allow
+  // pieces a KV head where tiles are cut: a place on the chip each while the tiles have one, else up to three; never more than
+  // the units allow
   const long long most = ((long long)max_ctx + 63) / 64 + ((long long)max_q + 63) / 64, cuts = (most + p.min_piece - 1) / p.min_piece;
   const long long places = (tiles * H <= p.resident ? 1LL : 3LL) * p.resident / H;
   long long cut = places < p.max_tiles * cuts ? places : p.max_tiles * cuts;

@@ -55,17 +55,23 @@ __device__ __forceinline__ int int2_units(const ChunkArgs& a, const Seq& s, int 
 }
 __device__ __forceinline__ int own_units(const ChunkArgs& a, int i) { return a.k_new ? i / kUnit + 1 : 0; }
 
-// ---- The plan. A sequence's rows are tiles of bm; every tile of a sequence is cut into the same number of pieces, so that
-// its longest has about L units each, and a work-group takes one piece of one KV head. L comes from an estimate of the time
-// in units of work: while all pieces have a place on the chip at once, the longest; beyond that the average load and half a
-// piece; a piece costs piece_units beside its own units, a partial merge_units.
-struct Load {  // of one sequence: row tiles, and units of the last one
+// ---- The plan. A sequence's rows are tiles of bm; a tile is cut into equal pieces of at most about L units, by its own units
+// where the tiles leave places on the chip free (up to 64 of them), else all tiles of a sequence like its longest; a
+// work-group takes one piece of one KV head. L comes from an estimate of the time in units of work: while all pieces have a
+// place on the chip at once, the longest; beyond that the average load and half a piece; a piece costs piece_units beside its
+// own units, a partial merge_units.
+struct Load {  // of one sequence: row tiles, and units of the last one; or of one tile
   int tiles, units;
 };
 __device__ __forceinline__ Load load_of(const ChunkArgs& a, const Seq& s) {
   const int rows = s.n * a.gq;
   if (rows == 0) return Load{0, 0};
   return Load{quotient(rows + a.bm - 1, a.bm), int2_units(a, s, s.n - 1) + own_units(a, s.n - 1)};
+}
+// Units of the tile of rows row0 ..
+__device__ __forceinline__ int tile_units(const ChunkArgs& a, const Seq& s, int row0) {
+  const int i = quotient(max(min(row0 + a.bm, s.n * a.gq) - 1, 0), a.gq);
+  return int2_units(a, s, i) + own_units(a, i);
 }
 constexpr int kCuts = 16;
 // Candidate k: units of a piece. The first leaves the tiles whole; the others lie above the size that would fill the places
@@ -76,23 +82,25 @@ __device__ __forceinline__ int cut_of(const ChunkArgs& a, int k, float even, int
 }
 // Pieces of a tile of so many units
 __device__ __forceinline__ int pieces_of(int units, int L) { return max(1, quotient(units + L - 1, L)); }
-// The time in units with pieces of at most c units, n of them a KV head; places: a KV head's part of the chip
-__device__ __forceinline__ float cost_of(const ChunkArgs& a, int c, int n, int T, float even, float places, int umax) {
+// The time in units with pieces of at most c units, n of them a KV head, `parts` of them of tiles that are cut; places: a KV
+// head's part of the chip
+__device__ __forceinline__ float cost_of(const ChunkArgs& a, int c, int n, int parts, float even, float places, int umax) {
   const float one = (float)min(c, umax) + a.piece_units, fn = (float)n;
   const float load = even + fn * a.piece_units * __builtin_amdgcn_rcpf(places);
   // Two work-groups of a compute unit share it: one alone takes 0.6 of the time, the fullest pair lies between the average
   // and two of the longest. Beyond one round the longest may come last, by half.
   const float round = a.per_cu == 2 ? fmaxf(0.6f * one, 0.5f * (one + load)) : one;
-  return (fn <= places ? round : fmaxf(load, one) + 0.5f * one) + (n > T ? fn * (float)a.cv.num_kv_heads * a.merge_units : 0.0f);
+  const float time = fn <= places ? round : fmaxf(load, one) + 0.5f * one;
+  return time + (float)parts * (float)a.cv.num_kv_heads * a.merge_units;
+}
+// whether n pieces may be: they have room, and a place each while the tiles have one (a second round of pieces never paid: the
+// chip slows down as its places fill)
+__device__ __forceinline__ bool fits(const ChunkArgs& a, int n, int T, float places) {
+  return n <= a.max_slots && ((float)T > places || (float)n <= places);
 }
 __device__ __forceinline__ float places_of(const ChunkArgs& a) {
   return (float)a.resident * __builtin_amdgcn_rcpf((float)a.cv.num_kv_heads);
 }
-// whether n pieces may be: they have room, and a place each while the tiles have one
-__device__ __forceinline__ bool fits(const ChunkArgs& a, int n, int T, float places) {
-  return n <= a.max_slots && ((float)T > places || (float)n <= places);
-}
-
 // Sum and maximum over the wave: rotations inside rows of 16 lanes, then swaps of rows and halves
 template <class F>
 __device__ __forceinline__ int wave_fold(int x, F f) {
@@ -150,22 +158,41 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
   Place p;
   p.valid = false;
   Load load;
-  int total, T, b, first, tile0, local, pieces;
+  int total, b, first, tile0, local, pieces, row = 0;
   if (a.B <= kChunkWaveSeqs) {
     Seq s{0, 0, 0};
     if (lane < a.B) s = seq_of(a, lane);
     load = load_of(a, s);
-    const int tiles = wave_scan(load.tiles);
-    T = __builtin_amdgcn_readlane(tiles, 63);
+    int tiles = wave_scan(load.tiles), lane_b = lane, lane_row = 0;
+    const int T = __builtin_amdgcn_readlane(tiles, 63);
+    const float places = places_of(a);
+    const bool by_tile = T <= 64 && (float)T < places && __ballot(load.tiles > 1) != 0;
+    if (by_tile) {  // a tile per lane: only those that are longer than others need be cut
+      if (a.B > 1) {
+        lane_b = 0;
+#pragma unroll
+        for (int step = 32; step > 0; step >>= 1) lane_b += __shfl(tiles, lane_b + step - 1) <= lane ? step : 0;
+      } else {
+        lane_b = 0;
+      }
+      const Seq q{0, __shfl(s.n, lane_b), __shfl(s.ctx, lane_b)};
+      lane_row = (lane - __shfl(tiles - load.tiles, lane_b)) * a.bm;
+      load = lane < T ? Load{1, tile_units(a, q, lane_row)} : Load{0, 0};
+      tiles = min(lane + 1, T);
+    }
     const int umax = wave_fold(load.units, [](int x, int y) { return max(x, y); });
-    const float W = wave_sum((float)load.tiles * (float)load.units), places = places_of(a), even = W * __builtin_amdgcn_rcpf(places);
-    // A candidate per lane (of sixteen), a quarter of the sequences per sixteen lanes
-    const int c = cut_of(a, lane & 15, even, umax);
-    int n = 0;
-    for (int i = lane >> 4; i < ((a.B + 3) & ~3); i += 4) n += __shfl(load.tiles, i) * pieces_of(__shfl(load.units, i), c);
-    n = quarters_sum(n);
+    const float W = wave_sum((float)load.tiles * (float)load.units), even = W * __builtin_amdgcn_rcpf(places);
+    // A candidate per lane (of sixteen), a quarter of the sequences or tiles per sixteen lanes
+    const int c = cut_of(a, lane & 15, even, umax), lanes = ((T <= 64 ? max(a.B, T) : a.B) + 3) & ~3;
+    int n = 0, parts = 0;
+    for (int i = lane >> 4; i < lanes; i += 4) {
+      const int k = pieces_of(__shfl(load.units, i), c), x = __shfl(load.tiles, i) * k;
+      n += x;
+      parts += k > 1 ? x : 0;
+    }
+    n = quarters_sum(n), parts = quarters_sum(parts);
     const bool may = (lane & 15) == 0 || fits(a, n, T, places);
-    const int cost = __float_as_int(may ? cost_of(a, c, n, T, even, places, umax) : INFINITY);  // (positive: ordered as integers)
+    const int cost = __float_as_int(may ? cost_of(a, c, n, parts, even, places, umax) : INFINITY);  // (positive: ordered as integers)
     const int best = wave_fold(cost, [](int x, int y) { return min(x, y); });
     const int L = __builtin_amdgcn_readlane(c, __ffsll(__ballot(cost == best)) - 1);
     const int mine_k = load.tiles > 0 ? pieces_of(load.units, L) : 0, mine = load.tiles * mine_k, upto = wave_scan(mine);
@@ -175,19 +202,21 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
     if (at >= total) return p;
     const int r = rank_of(a, at, total), size = mine > 0 ? quotient(load.units + mine_k - 1, mine_k) : -1;
     // the length of piece r: the greatest that more than r pieces have
-    int hi = wave_fold(size, [](int x, int y) { return max(x, y); }), lo = a.B == 1 ? hi : 0, above = 0;
+    int hi = wave_fold(size, [](int x, int y) { return max(x, y); }), lo = a.B == 1 && !by_tile ? hi : 0, above = 0;
     while (lo < hi) {
       const int mid = (lo + hi + 1) >> 1, n = wave_sum(size >= mid ? mine : 0);
       if (n > r) lo = mid;
       else hi = mid - 1, above = n;
     }
     const int same = size == lo ? mine : 0, past = wave_scan(same);
-    b = min(__ffsll(__ballot(past > r - above)) - 1, a.B - 1);
-    local = r - above - __builtin_amdgcn_readlane(past - same, b);
-    first = __builtin_amdgcn_readlane(upto - mine, b);
-    tile0 = __builtin_amdgcn_readlane(tiles - load.tiles, b);
-    pieces = __builtin_amdgcn_readlane(mine_k, b);
-    load.tiles = __builtin_amdgcn_readlane(load.tiles, b);
+    const int x = max(__ffsll(__ballot(past > r - above)) - 1, 0);
+    local = r - above - __builtin_amdgcn_readlane(past - same, x);
+    first = __builtin_amdgcn_readlane(upto - mine, x);
+    tile0 = __builtin_amdgcn_readlane(tiles - load.tiles, x);
+    pieces = __builtin_amdgcn_readlane(mine_k, x);
+    load.tiles = __builtin_amdgcn_readlane(load.tiles, x);
+    row = __builtin_amdgcn_readlane(lane_row, x);
+    b = min(__builtin_amdgcn_readlane(lane_b, x), a.B - 1);
     p.s = Seq{__builtin_amdgcn_readlane(s.start, b), __builtin_amdgcn_readlane(s.n, b), __builtin_amdgcn_readlane(s.ctx, b)};
   } else {
     total = a.head[0];
@@ -212,8 +241,8 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
   }
   const int back = quotient(local, pieces), t = load.tiles - 1 - back, piece = local - back * pieces;
   p.b = b;
-  p.row0 = t * a.bm;
-  const int i = quotient(min(p.row0 + a.bm, p.s.n * a.gq) - 1, a.gq), units = int2_units(a, p.s, i) + own_units(a, i);
+  p.row0 = row + t * a.bm;
+  const int units = tile_units(a, p.s, p.row0);
   const int each = quotient(units, pieces), more = units - each * pieces;  // the first `more` pieces have one more
   p.u0 = each * piece + min(piece, more);
   p.u1 = p.u0 + each + (piece < more ? 1 : 0);
