@@ -27,6 +27,8 @@ PLANS = {
     "narrow": (_ragged(20, (17, 33), (0, 900), 5), 8, 4),
     "narrow, cut": ([(24, 4000), (30, 10)], 2, 4),
     "narrow, listed": (_ragged(80, (10, 30), (0, 300), 6), 2, 4),
+    "narrow, nothing cached": ([(700, 0), (33, 0)], 8, 4),
+    "wide, nothing cached": (_ragged(40, (50, 130), (0, 1), 9), 8, 4),
     "wide, cut": ([(100, 6000)], 1, 4),
     "wide, cut over the chunk's own tokens": ([(700, 100)], 1, 2),
     "wide, more tiles than places": (_ragged(40, (50, 130), (0, 700), 7), 8, 4),
