@@ -88,12 +88,12 @@ __device__ __forceinline__ float cost_of(const ChunkArgs& a, int c, int n, int p
   const float one = (float)min(c, umax) + a.piece_units, fn = (float)n;
   const float load = even + fn * a.piece_units * __builtin_amdgcn_rcpf(places);
   // Two work-groups of a compute unit share it: one alone takes 0.6 of the time, the fullest pair lies between the average
-  // and two of the longest. Beyond one round the longest may come last, by half.
-  const float round = a.per_cu == 2 ? fmaxf(0.6f * one, 0.5f * (one + load)) : one;
-  const float time = fn <= places ? round : fmaxf(load, one) + 0.5f * one;
+  // and two of the longest. Where there are more pieces than places the longest may come last, by half.
+  const float at_once = a.per_cu == 2 ? fmaxf(0.6f * one, 0.5f * (one + load)) : one;
+  const float time = fn <= places ? at_once : fmaxf(load, one) + 0.5f * one;
   return time + (float)parts * (float)a.cv.num_kv_heads * a.merge_units;
 }
-// whether n pieces may be: they have room, and a place each while the tiles have one (a second round of pieces never paid: the
+// whether n pieces may be: they have room, and a place each while the tiles have one (more pieces than that never paid: the
 // chip slows down as its places fill)
 __device__ __forceinline__ bool fits(const ChunkArgs& a, int n, int T, float places) {
   return n <= a.max_slots && ((float)T > places || (float)n <= places);

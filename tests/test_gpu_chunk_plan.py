@@ -1,5 +1,6 @@
-"""How the attention of a chunk is laid out over the chip: every kernel of it with whole and cut tiles, in one round and in
-several, batches planned by every work-group and by a launch of their own; workspaces to the byte, streams, strides."""
+"""How the attention of a chunk is laid out over the chip: every kernel of it with whole and cut tiles, all on the chip at
+once and one after another, batches planned by every work-group and by a launch of their own;
+workspaces to the byte, streams, strides."""
 import numpy as np
 import pytest
 import torch
@@ -28,12 +29,16 @@ PLANS = {
     "narrow, cut": ([(24, 4000), (30, 10)], 2, 4),
     "narrow, listed": (_ragged(80, (10, 30), (0, 300), 6), 2, 4),
     "narrow, nothing cached": ([(700, 0), (33, 0)], 8, 4),
-    "wide, nothing cached": (_ragged(40, (50, 130), (0, 1), 9), 8, 4),
+    "narrow, more tiles than places": (_ragged(40, (50, 130), (0, 700), 7), 8, 4),
+    "narrow, nothing cached, more tiles than places": (_ragged(40, (50, 130), (0, 1), 9), 8, 4),
+    "narrow, listed, ragged": (_ragged(66, (0, 140), (0, 500), 8), 2, 4),
+    "narrow, one long sequence among many": ([(3, 50)] * 70 + [(120, 3000)], 2, 4),
+    "wide, nothing cached": (_ragged(20, (180, 300), (0, 1), 10), 8, 4),
     "wide, cut": ([(100, 6000)], 1, 4),
     "wide, cut over the chunk's own tokens": ([(700, 100)], 1, 2),
-    "wide, more tiles than places": (_ragged(40, (50, 130), (0, 700), 7), 8, 4),
-    "wide, listed": (_ragged(66, (0, 140), (0, 500), 8), 2, 4),
-    "wide, one long sequence among many": ([(3, 50)] * 70 + [(120, 3000)], 2, 4),
+    "wide, more tiles than places": (_ragged(20, (180, 300), (0, 700), 11), 8, 4),
+    "wide, tiles by their own length": ([(250, 900), (64, 20), (130, 300), (190, 2500)], 8, 4),
+    "wide, listed": (_ragged(66, (150, 250), (0, 500), 12), 1, 4),
 }
 
 
