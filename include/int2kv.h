@@ -390,8 +390,9 @@ int int2kv_read_rows(const int2kv_cache* cache, const int32_t* slot_mapping, int
  *   k_new, v_new : bf16 rows as q with H_kv heads and strides of their own (raw post-RoPE keys, not
  *                  centered; values), with mu: fp32 [H_kv, 128]; or NULL, NULL, NULL
  *   out          : bf16 [total_q, H_q, 128], 16-byte aligned, model basis; must not overlap q, k_new, v_new
- *   workspace    : int2kv_chunk_attention_workspace_bytes(...) bytes, 256-byte aligned; nothing in it
- *                  needs to be kept or cleared between calls, calls that overlap need one each
+ *   workspace    : int2kv_chunk_attention_workspace_bytes(...) bytes, 256-byte aligned; enough for every
+ *                  call within the same bounds; nothing in it needs to be kept or cleared between calls,
+ *                  calls that overlap need one each
  * Products run on the matrix cores with fp32 sums: queries and rotations, rotated queries, dequantized
  * rows and the probabilities over the INT2 tokens in fp16, the chunk's own rows and the probabilities
  * over them in bf16, each rounded once; softmax statistics in fp32. Queries (where the cache holds

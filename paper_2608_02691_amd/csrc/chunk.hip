@@ -634,20 +634,12 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
                                               pack_bf16(o[4] * inv, o[5] * inv), pack_bf16(o[6] * inv, o[7] * inv));
 }
 
-ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx) {
+namespace {
+
+// The plan with kernel `waves` (1: few rows)
+ChunkPlan plan_with(int waves, int B, int H, long long seq_rows, long long rows, int max_q, int max_ctx) {
   ChunkPlan p{};
-  const int gq = Hq / H;
-  const long long seq_rows = (long long)max_q * gq, rows = (long long)total_q * gq;
-  // Four waves do the work of eight in 1.1 of the time, but on tiles of half the rows. They take what eight would leave more
-  // than that empty: rows a sequence filled up to whole tiles, or half a tile more where the lengths differ. 16 chunks of 17
-  // to 100 tokens (32 + 8 heads) over up to 8,000: 112 us, with eight waves 129; of 128 over 2,000: 118 and 106. And prompts with
-  // nothing cached (no operands made twice) whose smaller tiles all have a place, since a causal tile's length varies and two
-  // share a compute unit, the shortest beside the longest: 500 and 2,011 tokens 23 and 70 us, with eight waves 27 and 75;
-  // 4,000, twice what the chip holds at once, 187 and 166.
-  auto filled = [&](long long tile) { return rows == seq_rows * B ? (seq_rows + tile - 1) / tile * tile : rows / B + tile / 2; };
-  const long long tiles4 = B * ((seq_rows + 127) / 128), rows4 = rows / 128 + B;
-  const bool placed = (tiles4 < rows4 ? tiles4 : rows4) * H <= 2LL * num_cus();
-  p.waves = seq_rows <= 64 ? 1 : seq_rows <= 128 || 11 * filled(128) < 10 * filled(256) || (max_ctx == 0 && placed) ? 4 : 8;
+  p.waves = waves;
   p.bm = 32 * p.waves;
   p.resident = num_cus() * (p.waves == 8 ? 1 : 2);
   p.min_piece = p.waves == 1 ? 4 : 2;  // a unit for each wave of the kernel of few rows
@@ -674,6 +666,34 @@ ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_
   p.off_tiles = off, off = up(off + (size_t)p.max_tiles * sizeof(ChunkTile));
   p.off_part = off, off = up(off + (size_t)p.max_slots * H * p.bm * kChunkPartStride * sizeof(float));
   p.total = off;
+  return p;
+}
+
+}  // namespace
+
+ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx) {
+  const int gq = Hq / H;
+  const long long seq_rows = (long long)max_q * gq, rows = (long long)total_q * gq;
+  // The kernel of few rows makes the operands again for every 32 rows, which takes 1.5 of the four waves' time a row. It takes
+  // what they would leave more than that empty: 24 sequences of 2 to 20 tokens (32 + 8 heads) over 512 to 16,384: 88 us, with
+  // four waves 135; of 2 to 38 161 and 179; 100 of 1 to 40 over up to 2,000 193 and 184.
+  // Four waves do the work of eight in 1.1 of the time, but on tiles of half the rows. They take what eight would leave more
+  // than that empty: rows a sequence filled up to whole tiles, or half a tile more where the lengths differ. 16 chunks of 17
+  // to 100 tokens (32 + 8 heads) over up to 8,000: 112 us, with eight waves 129; of 128 over 2,000: 118 and 106. And prompts with
+  // nothing cached (no operands made twice) whose smaller tiles all have a place, since a causal tile's length varies and two
+  // share a compute unit, the shortest beside the longest: 500 and 2,011 tokens 23 and 70 us, with eight waves 27 and 75;
+  // 4,000, twice what the chip holds at once, 187 and 166.
+  auto filled = [&](long long tile) { return rows == seq_rows * B ? (seq_rows + tile - 1) / tile * tile : rows / B + tile / 2; };
+  const long long tiles4 = B * ((seq_rows + 127) / 128), rows4 = rows / 128 + B;
+  const bool placed = (tiles4 < rows4 ? tiles4 : rows4) * H <= 2LL * num_cus();
+  const int waves = seq_rows <= 64 || 3 * filled(32) < 2 * filled(128) ? 1 : seq_rows <= 128 || 11 * filled(128) < 10 * filled(256) || (max_ctx == 0 && placed) ? 4 : 8;
+  ChunkPlan p = plan_with(waves, B, H, seq_rows, rows, max_q, max_ctx);
+  // a workspace for these bounds is enough for every call within them, whichever kernel that takes
+  for (int other : {1, 4, 8})
+    if (other == 1 || seq_rows > 16 * other) {
+      const size_t need = plan_with(other, B, H, seq_rows, rows, max_q, max_ctx).total;
+      p.total = p.total < need ? need : p.total;
+    }
   return p;
 }
 

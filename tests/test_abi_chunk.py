@@ -1,6 +1,7 @@
 """Refusals of the chunk operators, before any launch (CPU only)."""
 import ctypes
 
+import numpy as np
 import pytest
 
 from paper_2608_02691_amd import int2kv as K
@@ -116,3 +117,16 @@ def test_chunk_attention_workspace():
     assert K.int2kv_chunk_attention_workspace_bytes(2, 4, 2, 8, 999, 64) == need
     grow = [K.int2kv_chunk_attention_workspace_bytes(1, 32, 8, n, n, 4096) for n in (1, 64, 2048, 16384)]
     assert grow == sorted(grow)
+
+
+def test_chunk_attention_workspace_serves_every_smaller_call():
+    """One workspace, sized for the largest batch, is enough for every call within its bounds."""
+    rng = np.random.default_rng(0)
+    for hq, h in ((32, 8), (40, 8), (8, 8), (64, 1)):
+        for _ in range(400):
+            big = [int(x) for x in np.exp(rng.uniform(0, [6, 9, 8, 11]))]                # batch, total_q, max_q, max_ctx
+            small = [int(x * rng.uniform(0, 1) ** 0.5) for x in big]
+            small[0] = max(1, small[0])
+            b, t, m, c = big
+            assert (K.int2kv_chunk_attention_workspace_bytes(b, hq, h, t, m, c)
+                    >= K.int2kv_chunk_attention_workspace_bytes(small[0], hq, h, *small[1:])), (hq, h, big, small)

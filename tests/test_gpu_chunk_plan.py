@@ -25,14 +25,15 @@ PLANS = {
     "few, more tiles than places": (_ragged(60, (1, 8), (1500, 5500), 2), 12, 5),
     "few, listed and cut": (_ragged(70, (1, 4), (0, 5000), 3), 1, 4),
     "few, listed, long steps": (_ragged(66, (1, 3), (4500, 5000), 4), 8, 1),
+    "few, one long sequence among many": ([(3, 50)] * 70 + [(120, 3000)], 2, 4),
+    "few, one prompt among single tokens": ([(1, 700)] * 30 + [(300, 0)], 2, 4),
     "narrow": (_ragged(20, (17, 33), (0, 900), 5), 8, 4),
     "narrow, cut": ([(24, 4000), (30, 10)], 2, 4),
-    "narrow, listed": (_ragged(80, (10, 30), (0, 300), 6), 2, 4),
+    "narrow, listed": (_ragged(80, (12, 33), (0, 300), 6), 2, 4),
     "narrow, nothing cached": ([(700, 0), (33, 0)], 8, 4),
     "narrow, more tiles than places": (_ragged(40, (50, 130), (0, 700), 7), 8, 4),
     "narrow, nothing cached, more tiles than places": (_ragged(40, (50, 130), (0, 1), 9), 8, 4),
     "narrow, listed, ragged": (_ragged(66, (0, 140), (0, 500), 8), 2, 4),
-    "narrow, one long sequence among many": ([(3, 50)] * 70 + [(120, 3000)], 2, 4),
     "wide, nothing cached": (_ragged(20, (180, 300), (0, 1), 10), 8, 4),
     "wide, cut": ([(100, 6000)], 1, 4),
     "wide, cut over the chunk's own tokens": ([(700, 100)], 1, 2),
