@@ -153,7 +153,7 @@ struct RowState {
 // and makes the operands of the next unit.
 template <class Ops, class Src>
 __device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, const typename Ops::vec (&Q)[8], float off, int u0,
-                                       int u1) {
+                                       int u1, bool live) {
   const int l = threadIdx.x & 63;
   cd_f16_t S[1], T[1];
   float base = kBias - st.m - off;
@@ -184,28 +184,42 @@ __device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, co
   src.template build<false>(u0, lds, 0, 0);  // (fetched by the caller)
   if (u0 + 1 < u1) src.fetch(u0 + 1);
   __syncthreads();
-  scores(S, 0, 0);
-  rest(S, u0, 0);
   int kb = 0, vb = 0;
-  for (int u = u0; u < u1; ++u) {
-    const bool more = u + 1 < u1;
-    const int vn = vb == 2 ? 0 : vb + 1;
-    cd_u4_t P[2];
-    scores(T, kb, 1);
-    soften<Ops>(S[0], base, st.sum, P);
-    add(P, vb, 0);
-    rest(T, u, 1);
-    if (more) {
-      src.template build<false>(u + 1, lds, kb ^ 1, vn);
-      if (u + 2 < u1) src.fetch(u + 2);
+  if (live) {
+    scores(S, 0, 0);
+    rest(S, u0, 0);
+    for (int u = u0; u < u1; ++u) {
+      const bool more = u + 1 < u1;
+      const int vn = vb == 2 ? 0 : vb + 1;
+      cd_u4_t P[2];
+      scores(T, kb, 1);
+      soften<Ops>(S[0], base, st.sum, P);
+      add(P, vb, 0);
+      rest(T, u, 1);
+      if (more) {
+        src.template build<false>(u + 1, lds, kb ^ 1, vn);
+        if (u + 2 < u1) src.fetch(u + 2);
+      }
+      __syncthreads();
+      if (more) scores(S, kb ^ 1, 0);
+      soften<Ops>(T[0], base, st.sum, P);
+      add(P, vb, 1);
+      if (more) rest(S, u + 1, 0);
+      kb ^= 1;
+      vb = vn;
     }
-    __syncthreads();
-    if (more) scores(S, kb ^ 1, 0);
-    soften<Ops>(T[0], base, st.sum, P);
-    add(P, vb, 1);
-    if (more) rest(S, u + 1, 0);
-    kb ^= 1;
-    vb = vn;
+  } else {  // a wave without rows (the last tile's): its share of the operands, the same barriers
+    for (int u = u0; u < u1; ++u) {
+      const bool more = u + 1 < u1;
+      const int vn = vb == 2 ? 0 : vb + 1;
+      if (more) {
+        src.template build<false>(u + 1, lds, kb ^ 1, vn);
+        if (u + 2 < u1) src.fetch(u + 2);
+      }
+      __syncthreads();
+      kb ^= 1;
+      vb = vn;
+    }
   }
 
   // Values that are not finite, in units that some row of the tile does not see all of, were left out above, where
@@ -224,7 +238,7 @@ __device__ __forceinline__ void attend(Src& src, RowState& st, ChunkLds& lds, co
       __syncthreads();
       src.template build<true>(u, lds, 0, 0);
       __syncthreads();
-      for (int tm = 0; tm < 2; ++tm) {
+      for (int tm = 0; live && tm < 2; ++tm) {
         scores(S, 0, tm);
 #pragma unroll
         for (int i = 0; i < 16; ++i) S[0][i] = src.sees(u, 32 * tm + reg_token(i)) ? S[0][i] : -INFINITY;
@@ -535,6 +549,9 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
   const int rows = seq.n * a.gq, row_w = place.row0 + 32 * w, tok_w = quotient(min(row_w, rows - 1), a.gq);
   const int nI = int2_units(a, seq, quotient(min(place.row0 + a.bm, rows) - 1, a.gq));
   const int row = row_w + n, rc = min(row, rows - 1), tok = quotient(rc, a.gq);
+  // Four waves: one without rows only brings its share of the operands (64 chunks of 2 to 44 tokens over up to 4,000: 144 us,
+  // 153 without). Eight: always taken for one with rows, since the second loop costs long chunks 1.5 %.
+  const bool live = NW == 8 || row_w < rows;
   RowState st;
   st.m = 0.0f, st.sum = 0.0f, st.thr = kNone;
 #pragma unroll
@@ -556,7 +573,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
     src.fetch(place.u0);
     rotate_query<NW>(R, lds, x, Q);
     // (the narrow work-group has no registers to spare)
-    attend<typename std::conditional<NW == 8, BasedOps, HalfOps>::type>(src, st, lds, Q, 0.0f, place.u0, i1);
+    attend<typename std::conditional<NW == 8, BasedOps, HalfOps>::type>(src, st, lds, Q, 0.0f, place.u0, i1, live);
     unrotate<NW>(a.R_v + (size_t)h * kHeadDim * kHeadDim, lds, st);
   }
 
@@ -566,7 +583,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
     query(Q);
     OwnSource<NW> src(a, h, seq, place.row0, w, tok, tok_w);
     src.fetch(c0);
-    attend<BfOps>(src, st, lds, Q, query_mean(Q, a.mu + (size_t)h * kHeadDim, hh), c0, c1);
+    attend<BfOps>(src, st, lds, Q, query_mean(Q, a.mu + (size_t)h * kHeadDim, hh), c0, c1, live);
   }
 
   // ---- results: register 4 u + v of tile 2 e + o is channel 64 e + 16 u + 8 hh + 2 v + o
