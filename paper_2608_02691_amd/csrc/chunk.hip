@@ -14,10 +14,10 @@
 // product's B operand as they lie (its k order is the order of S^T's rows in a lane; V^T is laid out to match). INT2 codes
 // become fp16 operands once per work-group and unit and are shared through LDS in operand order.
 //
-// Bound by power on long chunks: 4 x 2,048 tokens of 32 heads after 8,192 cached ones take 1.32 ms (950 TFLOP/s, where an
-// 8,192^3 product reaches 1,270) at 2.0 GHz, with the matrix pipe busy half of the cycles, the vector ALU two thirds and LDS
-// half. Eight waves share a unit's operands (256 rows a work-group): four waves do the same in 1.50 ms, their operands being
-// made twice as often; they serve sequences of 65 to 128 rows, whose tiles eight would leave half empty.
+// Bound by the clock, 2.0 of 2.4 GHz under this load, and by what two waves a SIMD hide of their waits (a third of their
+// cycles): 4 x 2,048 tokens of 32 heads after 8,192 cached ones take 1.32 ms (950 TFLOP/s, where an 8,192^3 product reaches
+// 1,270), with the matrix pipe busy 45 % of the cycles and the vector ALU 57 %. Eight waves share a unit's operands (256 rows a
+// work-group); four waves do the same in 1.50 ms, their operands being made twice as often, and serve shorter sequences.
 #include <type_traits>
 
 #include "chunk_core.h"

@@ -11,7 +11,7 @@
 //
 // Bound by the rows written (256 or 512 bytes a row; the records are 96, in whole pages where neighbours are wanted too).
 // Rows leave through LDS as whole 256-byte pieces by stores that bypass the caches: 32,768 scattered tokens of 8 heads, keys
-// and values, take 36 us (160 MB, 4.4 TB/s); 32-byte pieces straight from the accumulators took 71.
+// and values, take 32 us (160 MB, 5.0 TB/s); 32-byte pieces straight from the accumulators took 71.
 //
 // bf16 rows: x^ and R in one fp16 term each, an error of about 3e-4 of the row's root mean square against the output's
 // rounding of 2^-9 of each value. fp32 rows: two fp16 terms each, three products (the fourth is below 2^-22).
@@ -184,7 +184,7 @@ __global__ __launch_bounds__(kReadThreads, 2) void read_rows_kernel(CacheView cv
 #pragma unroll
     for (int g = 0; g < NG; ++g) asm volatile("" : "+v"(raw.s[g]), "+v"(raw.z[g]));
     asm volatile("" : "+v"(slot_next));
-    // (the stores bypass the caches: with them, 32,768 tokens of 8 heads took 46 us where they take 36)
+    // (the stores bypass the caches: through them they take a quarter longer)
     // register 4 u + v of tile 2 a + e: channel 64 a + 16 u + 8 hh + 2 v + e. Through the wave's own piece of LDS, 256 bytes a
     // token at a time (chunk x of token m at x ^ m), so that a store writes four whole pieces of rows
     const unsigned long long live = __ballot(cur.ok);
