@@ -568,7 +568,8 @@ def int2kv_rope_axes(positions: torch.Tensor, pair_axis, cos_sin: torch.Tensor, 
                      k_out: Optional[torch.Tensor] = None):
     """Rotary positions with several axes: positions int32 [axes, n], pair_axis 64 axis numbers (rope_axis_table),
     cos_sin fp32 [max_pos, 128], q bf16 [n, H_q, 128] and / or k bf16 [n, H_kv, 128] (tokens may lie apart). Returns
-    (q_out, k_out); pass q_out=q to turn in place. A token with a position outside the table keeps its output rows."""
+    (q_out, k_out); pass q_out=q to turn in place. A token with a position outside the table keeps its output rows (new
+    outputs are zero there)."""
     if positions.dim() != 2:
         raise ValueError("positions must be [axes, n]")
     axes, n = positions.shape
@@ -586,7 +587,7 @@ def int2kv_rope_axes(positions: torch.Tensor, pair_axis, cos_sin: torch.Tensor, 
         if x.dim() != 3 or x.shape[0] != n:
             raise ValueError(f"{name} must be [n, heads, 128]")
         if out is None:
-            out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+            out = torch.zeros(x.shape, dtype=x.dtype, device=x.device)
         if out.shape != x.shape:
             raise ValueError(f"{name}_out must have the shape of {name}")
         heads = x.shape[1]

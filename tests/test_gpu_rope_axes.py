@@ -126,3 +126,17 @@ def test_zeros_infinities_and_graphs():
         assert not fine[2, 1, 5] and not fine[2, 1, 69] and not fine[3, 2, 70] and not fine[3, 2, 6]
         assert int((~fine).sum()) == 4
         torch.cuda.synchronize()
+
+
+def test_new_outputs_are_zero_where_a_token_is_skipped():
+    """The padding of a batch (position -1), in memory that held something else before."""
+    rng = np.random.default_rng(5)
+    cs = torch.from_numpy(_table()).cuda()
+    q, k = (torch.from_numpy(rng.standard_normal((40, h, 128)).astype(np.float32)).to(torch.bfloat16).cuda() for h in (4, 2))
+    pos = torch.arange(40, dtype=torch.int32, device="cuda")[None].contiguous()
+    pos[0, 25:] = -1
+    for _ in range(3):
+        junk = [torch.full((40, h, 128), float("nan"), dtype=torch.bfloat16, device="cuda") for h in (4, 2)]
+        del junk
+        for x in K.int2kv_rope_axes(pos, K.rope_axis_table([64]), cs, q, k):
+            assert bool((x[25:] == 0).all()) and bool(torch.isfinite(x.float()).all())
