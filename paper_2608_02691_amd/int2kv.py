@@ -525,7 +525,7 @@ def _here(*tensors) -> None:
     """Work goes to the current device's current stream: every tensor has to live there."""
     cur = torch.cuda.current_device()
     for t in tensors:
-        if t is not None and t.is_cuda and t.device.index != cur:
+        if t is not None and t.get_device() not in (cur, -1):  # (-1: host memory, refused by name later)
             raise ValueError(f"tensor on {t.device}, but the current device is cuda:{cur}")
 
 
@@ -584,13 +584,14 @@ def int2kv_rope_axes(positions: torch.Tensor, pair_axis, cos_sin: torch.Tensor, 
         if x is None:
             args.append((None, 0, 0, None, 0, None))
             continue
-        if x.dim() != 3 or x.shape[0] != n:
+        shape = x.shape
+        if len(shape) != 3 or shape[0] != n:
             raise ValueError(f"{name} must be [n, heads, 128]")
         if out is None:
-            out = torch.zeros(x.shape, dtype=x.dtype, device=x.device)
-        if out.shape != x.shape:
+            out = torch.zeros(shape, dtype=x.dtype, device=x.device)
+        elif out.shape != shape:
             raise ValueError(f"{name}_out must have the shape of {name}")
-        heads = x.shape[1]
+        heads = shape[1]
         args.append((*_head_rows(x, heads, name), heads, *_head_rows(out, heads, name + "_out"), out))
     (qp, qs, hq, qop, qos, q_out), (kp, ks, hk, kop, kos, k_out) = args
     st = load_library().int2kv_rope_axes(qp, hq, qs, kp, hk, ks, _ptr(positions, _I32, "positions"), axes, pair_axis, n,
