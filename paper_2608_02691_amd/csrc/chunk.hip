@@ -619,30 +619,46 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
   }
 }
 
-// Block (tile, KV head, 16 rows): thread (row, eight channels) sums the tile's pieces in order.
+// Block (tile, KV head, 16 rows): thread (row, eight channels) joins the tile's pieces in order, in one pass with the running
+// maximum. Bound by latency, so nothing waits for what it need not: the tile is read beside the number of tiles (its place
+// exists whether or not it was cut), and four pieces at a time are on their way.
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
-  const int t = blockIdx.x, h = blockIdx.y, H = a.cv.num_kv_heads;
-  if (t >= a.head[1]) return;
+  const int t = blockIdx.x, h = blockIdx.y, H = a.cv.num_kv_heads, T = a.head[1];
   const ChunkTile tile = a.tiles[t];
-  if (tile.pieces <= 1) return;
+  if (t >= T || tile.pieces <= 1) return;
   const int rt = blockIdx.z * 16 + (threadIdx.x >> 4), c = 8 * (threadIdx.x & 15), row = tile.row0 + rt;
   if (row >= tile.n * a.gq) return;
-  const size_t stride = (size_t)H * a.bm * kChunkPartStride;
+  const size_t stride = (size_t)H * a.bm * kChunkPartStride, ml_at = (size_t)a.bm * kHeadDim;
   const float* part = a.part + ((size_t)tile.slot * H + h) * a.bm * kChunkPartStride;
-  float top = kNone;
-  for (int p = 0; p < tile.pieces; ++p) top = fmaxf(top, reinterpret_cast<const float2*>(part + p * stride + (size_t)a.bm * kHeadDim)[rt].x);
-  float o[8] = {}, all = 0.0f;
-  for (int p = 0; p < tile.pieces; ++p) {
-    const float* x = part + p * stride;
-    const float2 ml = reinterpret_cast<const float2*>(x + (size_t)a.bm * kHeadDim)[rt];
-    const float4* d = reinterpret_cast<const float4*>(x + (size_t)rt * kHeadDim + c);
-    const float4 u = d[0], v = d[1];
-    const float f = __builtin_amdgcn_exp2f(ml.x - top);
-    all = __builtin_fmaf(ml.y, f, all);
-    o[0] = __builtin_fmaf(u.x, f, o[0]), o[1] = __builtin_fmaf(u.y, f, o[1]);
-    o[2] = __builtin_fmaf(u.z, f, o[2]), o[3] = __builtin_fmaf(u.w, f, o[3]);
-    o[4] = __builtin_fmaf(v.x, f, o[4]), o[5] = __builtin_fmaf(v.y, f, o[5]);
-    o[6] = __builtin_fmaf(v.z, f, o[6]), o[7] = __builtin_fmaf(v.w, f, o[7]);
+  float o[8] = {}, all = 0.0f, top = kNone;
+  for (int p0 = 0; p0 < tile.pieces; p0 += 4) {
+    float2 ml[4];
+    float4 u[4], v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float* x = part + (size_t)min(p0 + i, tile.pieces - 1) * stride;
+      ml[i] = reinterpret_cast<const float2*>(x + ml_at)[rt];
+      const float4* d = reinterpret_cast<const float4*>(x + (size_t)rt * kHeadDim + c);
+      u[i] = d[0], v[i] = d[1];
+    }
+    float next = top;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) next = fmaxf(next, ml[i].x);
+    const float old = __builtin_amdgcn_exp2f(top - next);
+    top = next;
+    all *= old;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] *= old;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (p0 + i >= tile.pieces) continue;
+      const float f = __builtin_amdgcn_exp2f(ml[i].x - top);
+      all = __builtin_fmaf(ml[i].y, f, all);
+      o[0] = __builtin_fmaf(u[i].x, f, o[0]), o[1] = __builtin_fmaf(u[i].y, f, o[1]);
+      o[2] = __builtin_fmaf(u[i].z, f, o[2]), o[3] = __builtin_fmaf(u[i].w, f, o[3]);
+      o[4] = __builtin_fmaf(v[i].x, f, o[4]), o[5] = __builtin_fmaf(v[i].y, f, o[5]);
+      o[6] = __builtin_fmaf(v[i].z, f, o[6]), o[7] = __builtin_fmaf(v[i].w, f, o[7]);
+    }
   }
   const float inv = all == 0.0f ? 0.0f : 1.0f / all;
   const int tok = quotient(row, a.gq);
