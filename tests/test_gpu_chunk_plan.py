@@ -101,3 +101,32 @@ def test_values_beyond_fp16_reach_only_the_tokens_that_see_them(gq):
     v[c.table[0, tok // 16], :, 0, :, tok % 16] = 60000.0
     got = c.call().float().cpu().numpy()
     assert_chunk_close(got[:at], ref[:at], spread[:at])
+
+
+@pytest.mark.parametrize("batch", [20, 70])
+def test_a_captured_call_plans_by_the_lengths_of_its_replay(batch):
+    """Lengths that change in place between replays, an eager call beside each: every work-group's own plan, and the launch's."""
+    c = Chunk(_ragged(batch, (1, 30), (0, 1500), 23), 2, 4, seed=23, blocks=60)
+    dev = lambda x: torch.from_numpy(x).cuda()  # noqa: E731
+    cache = K.Int2KVCache(c.pool.shape[0], 2, pool=dev(c.pool))
+    q, k, v, starts, lens = c.q.cuda(), c.k.cuda(), c.v.cuda(), dev(c.starts), dev(c.lens)
+    rest = (dev(c.R_k), dev(c.R_v), k, v, dev(c.mu))
+    table = dev(np.where(c.table >= 0, c.table, 0).astype(np.int32))
+    need = K.int2kv_chunk_attention_workspace_bytes(batch, 8, 2, c.total, c.max_q, 1600)
+    ws = [torch.full((need,), 0xFF, dtype=torch.uint8, device="cuda") for _ in range(2)]
+    outs = [torch.zeros((c.total, 8, 128), dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    call = lambda i: K.int2kv_chunk_attention(cache, q, starts, c.max_q, table, lens, 1600, *rest, out=outs[i], workspace=ws[i])  # noqa: E731
+    call(1)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call(0)
+    rng = np.random.default_rng(24)
+    room = table.shape[1] * 16
+    for turn in range(5):
+        new = np.minimum(rng.integers(0, 1500, batch), room) if turn % 2 else np.where(np.arange(batch) == turn, min(1500, room), 3)
+        lens.copy_(dev(new.astype(np.int32)))
+        outs[0].zero_()
+        g.replay()
+        assert torch.equal(call(1), outs[0]), turn
+        torch.cuda.synchronize()
