@@ -377,7 +377,9 @@ int int2kv_read_rows(const int2kv_cache* cache, const int32_t* slot_mapping, int
  *       o = (sum_s p_s v^_s) R_V^T + sum_t p_t v_t,   one softmax over both;
  *   k_new NULL: the cache holds the new tokens too (appended first, as for int2kv_decode), ctx_lens[b]
  *     counts them: token i sees the cached tokens 0 .. ctx_lens[b] - n_b + i (for n_b = 1 this is
- *     int2kv_decode without W_O, up to rounding).
+ *     int2kv_decode without W_O, up to rounding). n_b and ctx_lens[b] count here as they are given,
+ *     also where max_q cuts the sequence or max_ctx or the table its context: a token's place does not
+ *     move, it sees those of its tokens that are left.
  * A token that sees nothing gets zeros.
  *   q            : bf16, head j of token t at t * q_stride + 128 j (elements); post-RoPE; 16-byte
  *                  aligned; q_stride a multiple of 8, at least 128 * H_q

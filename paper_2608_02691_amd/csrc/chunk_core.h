@@ -38,20 +38,28 @@ __device__ __forceinline__ int quotient(int x, int d) {
 
 struct Seq {
   int start, n, ctx;
+  int past;  // cached tokens before the first new one where the cache holds both, by the whole sequence and its whole length
+             // (n and ctx are cut to max_q, max_ctx and the table); negative where the length does not hold the sequence.
+             // With the chunk's own rows every new token sees all of ctx: no less than ctx
 };
 __device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int b) {
   Seq s;
   s.start = min(max(a.starts[b], 0), a.total_q);
   const int end = min(max(a.starts[b + 1], 0), a.total_q);
-  s.n = min(max(end - s.start, 0), a.max_q);
+  const int count = max(end - s.start, 0), len = max(a.lens[b], 0);
+  s.n = min(count, a.max_q);
   const long long room = (long long)a.max_blocks * kBlock;
-  s.ctx = min(max(a.lens[b], 0), (int)(room < a.max_ctx ? room : a.max_ctx));
+  s.ctx = min(len, (int)(room < a.max_ctx ? room : a.max_ctx));
+  s.past = a.k_new ? INT32_MAX - s.n : len - count;
   return s;
 }
+// Cached tokens that new token i sees (not above zero: none)
+__device__ __forceinline__ int limit_of(const Seq& s, int i) {
+  return min(s.ctx, s.past + i + 1);
+}
 // Units of a tile whose last new token is i: INT2 units, then units of the chunk's own tokens
-__device__ __forceinline__ int int2_units(const ChunkArgs& a, const Seq& s, int i) {
-  const int lim = a.k_new ? s.ctx : min(s.ctx, max(0, s.ctx - s.n + i + 1));
-  return (lim + kUnit - 1) / kUnit;
+__device__ __forceinline__ int int2_units(const Seq& s, int i) {
+  return (max(limit_of(s, i), 0) + kUnit - 1) / kUnit;
 }
 __device__ __forceinline__ int own_units(const ChunkArgs& a, int i) { return a.k_new ? i / kUnit + 1 : 0; }
 
@@ -66,12 +74,12 @@ struct Load {  // of one sequence: row tiles, and units of the last one; or of o
 __device__ __forceinline__ Load load_of(const ChunkArgs& a, const Seq& s) {
   const int rows = s.n * a.gq;
   if (rows == 0) return Load{0, 0};
-  return Load{quotient(rows + a.bm - 1, a.bm), int2_units(a, s, s.n - 1) + own_units(a, s.n - 1)};
+  return Load{quotient(rows + a.bm - 1, a.bm), int2_units(s, s.n - 1) + own_units(a, s.n - 1)};
 }
 // Units of the tile of rows row0 ..
 __device__ __forceinline__ int tile_units(const ChunkArgs& a, const Seq& s, int row0) {
   const int i = quotient(max(min(row0 + a.bm, s.n * a.gq) - 1, 0), a.gq);
-  return int2_units(a, s, i) + own_units(a, i);
+  return int2_units(s, i) + own_units(a, i);
 }
 constexpr int kCuts = 16;
 // Candidate k: units of a piece. The first leaves the tiles whole; the others lie above the size that would fill the places
@@ -160,7 +168,7 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
   Load load;
   int total, b, first, tile0, local, pieces, row = 0;
   if (a.B <= kChunkWaveSeqs) {
-    Seq s{0, 0, 0};
+    Seq s{0, 0, 0, 0};
     if (lane < a.B) s = seq_of(a, lane);
     load = load_of(a, s);
     int tiles = wave_scan(load.tiles), lane_b = lane, lane_row = 0;
@@ -175,7 +183,7 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
       } else {
         lane_b = 0;
       }
-      const Seq q{0, __shfl(s.n, lane_b), __shfl(s.ctx, lane_b)};
+      const Seq q{0, __shfl(s.n, lane_b), __shfl(s.ctx, lane_b), __shfl(s.past, lane_b)};
       lane_row = (lane - __shfl(tiles - load.tiles, lane_b)) * a.bm;
       load = lane < T ? Load{1, tile_units(a, q, lane_row)} : Load{0, 0};
       tiles = min(lane + 1, T);
@@ -217,7 +225,8 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
     load.tiles = __builtin_amdgcn_readlane(load.tiles, x);
     row = __builtin_amdgcn_readlane(lane_row, x);
     b = min(__builtin_amdgcn_readlane(lane_b, x), a.B - 1);
-    p.s = Seq{__builtin_amdgcn_readlane(s.start, b), __builtin_amdgcn_readlane(s.n, b), __builtin_amdgcn_readlane(s.ctx, b)};
+    p.s = Seq{__builtin_amdgcn_readlane(s.start, b), __builtin_amdgcn_readlane(s.n, b), __builtin_amdgcn_readlane(s.ctx, b),
+              __builtin_amdgcn_readlane(s.past, b)};
   } else {
     total = a.head[0];
     if (at >= total) return p;
@@ -252,7 +261,7 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
     a.tiles[tile0 + t] = ChunkTile{p.row0, p.s.start, p.s.n, pieces, p.slot};
   // the same in every lane: into scalar registers
   auto one = [](int x) { return __builtin_amdgcn_readfirstlane(x); };
-  p.s = Seq{one(p.s.start), one(p.s.n), one(p.s.ctx)};
+  p.s = Seq{one(p.s.start), one(p.s.n), one(p.s.ctx), one(p.s.past)};
   p.row0 = one(p.row0), p.u0 = one(p.u0), p.u1 = one(p.u1), p.slot = one(p.slot), p.b = one(p.b);
   return p;
 }
