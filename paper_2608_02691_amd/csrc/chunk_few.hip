@@ -250,15 +250,15 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
         take(s, no, no);
         after(s);
       }
+      const int part0 = s;
       for (; s < s1; ++s) {  // the end of the context, or behind a page that does not exist
         before(s);
         take(s, yes, no);
         after(s);
       }
       if (__any(found != 0)) {
-        for (s = s0; s < s1; ++s) {
+        for (s = part0; s < s1; ++s) {  // (the units before them took such values as they are)
           load_list(s);
-          if (whole(s)) continue;
           asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
           issue(s);
           asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
