@@ -337,7 +337,7 @@ int int2kv_output_error(const int2kv_cache* cache, const uint16_t* q, int batch,
  *   cos_sin      : fp32 [max_pos, 128], as in int2kv_quantize_append_rope; 16-byte aligned
  *   q_out, k_out : bf16 rows as q, k with strides of their own; may be q, k themselves (same stride),
  *                  otherwise no output row may overlap an input's or the other output's rows
- *   num_tokens   : below 2^27 */
+ *   num_tokens   : at most 2^27 - 8 */
 int int2kv_rope_axes(const uint16_t* q, int num_q_heads, int64_t q_stride, const uint16_t* k, int num_kv_heads,
                      int64_t k_stride, const int32_t* positions, int num_axes, const uint8_t* pair_axis,
                      int num_tokens, const float* cos_sin, int max_pos, uint16_t* q_out, int64_t q_out_stride,

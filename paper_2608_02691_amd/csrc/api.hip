@@ -661,7 +661,8 @@ int int2kv_rope_axes(const uint16_t* q, int num_q_heads, int64_t q_stride, const
   if (!pair_axis) return fail(INT2KV_EINVAL, "NULL pointer argument");
   for (int i = 0; i < kHeadDim / 2; ++i)
     if (pair_axis[i] >= num_axes) return fail(INT2KV_EINVAL, "pair_axis names an axis outside [0, num_axes)");
-  if (num_tokens >= 1 << 27) return fail(INT2KV_EUNSUPPORTED, "num_tokens must be below 2^27");
+  // a launch holds 2^32 - 1 threads: 2^24 - 1 blocks of eight tokens
+  if (num_tokens > (1 << 27) - 8) return fail(INT2KV_EUNSUPPORTED, "num_tokens must be at most 2^27 - 8");
   if (num_tokens == 0 || num_q_heads + num_kv_heads == 0) return ok();
   if (!positions || !cos_sin || (num_q_heads && (!q || !q_out)) || (num_kv_heads && (!k || !k_out)))
     return fail(INT2KV_EINVAL, "NULL pointer argument");
