@@ -354,7 +354,7 @@ enum {
  *     k_out[i] = k^ R_K^T + mu,   v_out[i] = v^ R_V^T,   k^, v^ = code * s + z of slot slot_mapping[i];
  * without R_k (R_v) the row as stored, k^ (v^), in the rotated basis.
  *   slot_mapping : int32 [num_tokens], in any order, repeats allowed; a slot outside the cache (also a
- *                  negative one) leaves its output rows as they were; num_tokens * H_kv below 2^28
+ *                  negative one) leaves its output rows as they were; num_tokens * H_kv at most 2^28 - 16
  *   R_k, R_v     : fp32 [H_kv, 128, 128], 16-byte aligned, or NULL;  mu: fp32 [H_kv, 128] or NULL (keys
  *                  stay centered); mu needs R_k
  *   row_format   : INT2KV_ROWS_BF16 or INT2KV_ROWS_F32

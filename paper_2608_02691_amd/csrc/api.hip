@@ -696,8 +696,9 @@ int int2kv_read_rows(const int2kv_cache* cache, const int32_t* slot_mapping, int
   if (row_format != INT2KV_ROWS_BF16 && row_format != INT2KV_ROWS_F32) return fail(INT2KV_EINVAL, "unknown row_format");
   if (cache->num_kv_heads > 65535) return fail(INT2KV_EUNSUPPORTED, "at most 65535 KV heads");
   if (mu && !R_k) return fail(INT2KV_EINVAL, "mu needs R_k");
-  if ((int64_t)num_tokens * cache->num_kv_heads >= 1 << 28)
-    return fail(INT2KV_EUNSUPPORTED, "num_tokens * num_kv_heads must be below 2^28");
+  // a launch holds 2^32 - 1 threads: 2^24 - 1 blocks of sixteen rows as stored
+  if ((int64_t)num_tokens * cache->num_kv_heads > (1 << 28) - 16)
+    return fail(INT2KV_EUNSUPPORTED, "num_tokens * num_kv_heads must be at most 2^28 - 16");
   if (num_tokens == 0) return ok();
   if (!slot_mapping || (!k_out && !v_out)) return fail(INT2KV_EINVAL, "NULL pointer argument");
   const bool f32 = row_format == INT2KV_ROWS_F32;
