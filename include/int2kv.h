@@ -396,9 +396,10 @@ int int2kv_read_rows(const int2kv_cache* cache, const int32_t* slot_mapping, int
  *                  call within the same bounds; nothing in it needs to be kept or cleared between calls,
  *                  calls that overlap need one each
  * Products run on the matrix cores with fp32 sums: queries and rotations, rotated queries, dequantized
- * rows and the probabilities over the INT2 tokens in fp16, the chunk's own rows and the probabilities
- * over them in bf16, each rounded once; softmax statistics in fp32. Queries (where the cache holds
- * anything), rotations and dequantized values have to lie within fp16's range (|x| <= 65504).
+ * rows, the probabilities over the INT2 tokens and the sums that R_V turns (each row scaled by a power
+ * of two of its own) in fp16, the chunk's own rows and the probabilities over them in bf16, each rounded
+ * once; softmax statistics in fp32. Queries (where the cache holds anything), rotated queries times
+ * log2(e) / sqrt(128), rotations and dequantized values have to lie within fp16's range (|x| <= 65504).
  * A non-finite key or value reaches only the tokens that see it. Deterministic; no atomics on results. */
 size_t int2kv_chunk_attention_workspace_bytes(int batch, int num_q_heads, int num_kv_heads, int total_q, int max_q,
                                               int max_ctx);

@@ -495,7 +495,7 @@ __device__ __forceinline__ void rotate_query(const KeyRotation<NW>& R, ChunkLds&
   __syncthreads();
 }
 
-// O^T <- R_V O^T, on the normalized sums (within fp16's range, being averages of the values). R_V goes through LDS as A
+// O^T <- R_V O^T, each row within fp16's range by a power of two (row_scale). R_V goes through LDS as A
 // operands: tile 2 e + o, row m is output channel 64 e + 2 m + o; operand (i, half) takes the channels 32 i + 16 half +
 // {4 hh .. + 3, 8 + 4 hh .. + 3} that a lane half holds of tile i. Chunk m of operand op lies at m ^ op (its low bits), so
 // that a row's pieces, which differ in operand, spread over the banks.
@@ -513,11 +513,11 @@ __device__ __forceinline__ void unrotate(const float* R, ChunkLds& lds, RowState
   }
   __syncthreads();
   const int l = threadIdx.x & 63;
-  const float all = pair_sum(st.sum), inv = all == 0.0f ? 0.0f : 1.0f / all;
+  const RowScale scale = row_scale(row_top(st.O));
   cd_h8_t B[8];
 #pragma unroll
   for (int t = 0; t < 4; ++t) {
-    const cd_f16_t o = st.O[t] * inv;
+    const cd_f16_t o = st.O[t] * scale.down;
 #pragma unroll
     for (int u = 0; u < 2; ++u) B[2 * t + u] = pack_half8(reinterpret_cast<const float*>(&o) + 8 * u);
   }
@@ -527,7 +527,7 @@ __device__ __forceinline__ void unrotate(const float* R, ChunkLds& lds, RowState
 #pragma unroll
     for (int op = 0; op < 8; ++op)
       d = __builtin_amdgcn_mfma_f32_32x32x16_f16(reinterpret_cast<cd_h8_t*>(rv)[(t * 8 + op) * 64 + (l ^ op)], B[op], d, 0, 0, 0);
-    st.O[t] = d * all;
+    st.O[t] = d * scale.up;
   }
   __syncthreads();
 }

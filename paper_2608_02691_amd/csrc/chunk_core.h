@@ -356,6 +356,25 @@ __device__ __forceinline__ void soften(const cd_f16_t& X, float base, float& sum
     P[i >> 2][i & 3] =
         Ops::pack(__builtin_amdgcn_exp2f(Ops::score(X[2 * i], base)), __builtin_amdgcn_exp2f(Ops::score(X[2 * i + 1], base)), sum);
 }
+// A row's INT2 sums are turned by R_V in fp16. They may be averages of long contexts, far below the values, so the row is
+// brought to 2^12 .. 2^13 by a power of two (`down`, taken out again by `up`) that its largest element `top` names: what lies
+// 2^-26 below that is still in fp16's normal range. (Unscaled, values of 1e-5 over 1,500 tokens came out 5 % off.)
+struct RowScale {
+  float down, up;
+};
+__device__ __forceinline__ RowScale row_scale(float top) {
+  const uint32_t e = min(max(__float_as_uint(top) >> 23, 13u), 253u);  // (zeros: any)
+  return RowScale{__uint_as_float((266u - e) << 23), __uint_as_float((e - 12u) << 23)};
+}
+// The largest element of a lane's registers and its partner's
+__device__ __forceinline__ float row_top(const cd_f16_t (&O)[4]) {
+  float top = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; r += 2) top = fmaxf(fmaxf(top, fabsf(O[i][r])), fabsf(O[i][r + 1]));
+  return pair_max(top);
+}
 // q mu^T of a lane's query row, in the scores' unit
 __device__ __forceinline__ float query_mean(const cd_b8_t (&Q)[8], const float* mu, int hh) {
   float off = 0.0f;

@@ -25,8 +25,8 @@ struct FewLds {
     uint8_t stage[kFewWaves][kStages][kStageBytes];
     float o[kFewWaves][4][16][64];        // [wave][tile][register][lane]
   };
-  cd_h8_t b[8][64];                       // normalized sums as operands of the un-rotation
-  float ml[kFewWaves][2][32];
+  cd_h8_t b[8][64];                       // the rotated queries, then the sums, as operands
+  float ml[kFewWaves][3][32];             // the rows' m, sum and largest element
 };
 
 }  // namespace
@@ -272,6 +272,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
       for (int op = 0; op < 8; ++op) rv[op][0] = *reinterpret_cast<const float4*>(R + 16 * op), rv[op][1] = *reinterpret_cast<const float4*>(R + 16 * op + 8);
     }
     // ---- the waves' results meet
+    const float largest = row_top(O);
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -281,6 +282,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
     if (hh == 0) {
       lds.ml[w][0][n] = thr < 0.0f ? kNone : m;
       lds.ml[w][1][n] = sum;
+      lds.ml[w][2][n] = largest;
     }
     __syncthreads();
   }
@@ -295,13 +297,18 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
   // wave w has the 32 channels of tile w from here on
   cd_f16_t O[1] = {splat16(0.0f)};
   if (cached) {
-    const float inv = all == 0.0f ? 0.0f : 1.0f / all;
+    float bound = 0.0f;  // of the joined row: every wave, having one tile of it, comes to the same scale
+#pragma unroll
+    for (int y = 0; y < kFewWaves; ++y) bound = __builtin_fmaf(f[y], lds.ml[y][2][n], bound);
+    const RowScale scale = row_scale(bound);
+#pragma unroll
+    for (int y = 0; y < kFewWaves; ++y) f[y] *= scale.down;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
       float x = 0.0f;
 #pragma unroll
       for (int y = 0; y < kFewWaves; ++y) x = __builtin_fmaf(f[y], lds.o[y][w][r][l], x);
-      O[0][r] = x * inv;
+      O[0][r] = x;
     }
 #pragma unroll
     for (int x = 0; x < 2; ++x) {
@@ -318,7 +325,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
       const float x[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
       d = HalfOps::mfma(pack_half8(x), lds.b[op][l], d);
     }
-    O[0] = d * all;
+    O[0] = d * scale.up;
   }
   m = top == kNone ? 0.0f : top;
   thr = top == kNone ? kNone : kMove;
