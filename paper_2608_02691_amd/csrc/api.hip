@@ -755,7 +755,7 @@ int int2kv_chunk_attention(const int2kv_cache* cache, const uint16_t* q, int64_t
   a.q = q, a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
   a.starts = q_starts, a.B = batch, a.total_q = total_q, a.max_q = max_q, a.Hq = num_q_heads, a.gq = num_q_heads / H;
   a.table = block_table, a.max_blocks = max_blocks_per_seq, a.lens = ctx_lens, a.max_ctx = max_ctx;
-  a.R_k = R_k, a.R_v = R_v, a.k_new = k_new, a.v_new = v_new, a.mu = mu, a.out = out;
+  a.R_k = R_k, a.R_v = R_v, a.own = k_new != nullptr, a.k_new = k_new, a.v_new = v_new, a.mu = mu, a.out = out;
   return hip_status(launch_chunk_attention(a, plan, static_cast<uint8_t*>(workspace), stream), "chunk_attention");
 }
 

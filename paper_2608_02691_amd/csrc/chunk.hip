@@ -547,7 +547,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
   const Seq seq = place.s;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = l & 31, hh = l >> 5;
   const int rows = seq.n * a.gq, row_w = place.row0 + 32 * w, tok_w = quotient(min(row_w, rows - 1), a.gq);
-  const int nI = int2_units(seq, quotient(min(place.row0 + a.bm, rows) - 1, a.gq));
+  const int nI = int2_units(a, seq, quotient(min(place.row0 + a.bm, rows) - 1, a.gq));
   const int row = row_w + n, rc = min(row, rows - 1), tok = quotient(rc, a.gq);
   // Four waves: one without rows only brings its share of the operands (64 chunks of 2 to 44 tokens over up to 4,000: 144 us,
   // 153 without). Eight: always taken for one with rows, since the second loop costs long chunks 1.5 %.
@@ -568,7 +568,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
     cd_b8_t x[8];
     cd_h8_t Q[8];
     query(x);
-    auto limit = [&](int t) { return limit_of(seq, t); };
+    auto limit = [&](int t) { return limit_of(a, seq, t); };
     Int2Source<NG, NW> src(a, h, place.b, seq.ctx, w, limit(tok), limit(tok_w), limit(quotient(place.row0, a.gq)));
     src.fetch(place.u0);
     rotate_query<NW>(R, lds, x, Q);

@@ -50,8 +50,8 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
   if (!place.valid) return;
   const Seq seq = place.s;
   const int rows = seq.n * a.gq, row = place.row0 + n, rc = min(row, rows - 1), tok = quotient(rc, a.gq), tok_tile = quotient(place.row0, a.gq);
-  const int nI = int2_units(seq, quotient(min(place.row0 + a.bm, rows) - 1, a.gq));
-  const int lim = limit_of(seq, tok), lim_tile = limit_of(seq, tok_tile);  // tokens the row sees, the least of the tile's
+  const int nI = int2_units(a, seq, quotient(min(place.row0 + a.bm, rows) - 1, a.gq));
+  const int lim = limit_of(a, seq, tok), lim_tile = limit_of(a, seq, tok_tile);  // tokens the row sees, the least of the tile's
 
   // the row's query: channels 16 kk + 8 hh .. of operand kk (read again for the chunk's own tokens)
   const uint16_t* q = a.q + (seq.start + tok) * a.q_stride + (size_t)(h * a.gq + rc - tok * a.gq) * kHeadDim + 8 * hh;
