@@ -360,7 +360,8 @@ enum {
  *   row_format   : INT2KV_ROWS_BF16 or INT2KV_ROWS_F32
  *   k_out, v_out : bf16 or fp32 [num_tokens, H_kv, 128], 16-byte aligned; one of them may be NULL; they
  *                  may not overlap
- * Stored rows are exact before the format's one rounding. The un-rotation runs on the matrix cores in
+ * Stored rows are code * s + z in fp32 (exact unless s and z lie more than 2^11 apart), rounded once to
+ * the format. The un-rotation runs on the matrix cores in
  * fp16 terms with fp32 sums: one term each for bf16 rows (about 3e-4 of the row's root mean square,
  * under the rounding of bf16), two for fp32 rows (below 1e-6). Dequantized values and rotations have
  * to lie within fp16's range (|x| <= 65504). */

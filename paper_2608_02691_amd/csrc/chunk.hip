@@ -15,9 +15,9 @@
 // become fp16 operands once per work-group and unit and are shared through LDS in operand order.
 //
 // Bound by the clock, 2.0 of 2.4 GHz under this load, and by what two waves a SIMD hide of their waits (a third of their
-// cycles): 4 x 2,048 tokens of 32 heads after 8,192 cached ones take 1.32 ms (950 TFLOP/s, where an 8,192^3 product reaches
-// 1,270), with the matrix pipe busy 45 % of the cycles and the vector ALU 57 %. Eight waves share a unit's operands (256 rows a
-// work-group); four waves do the same in 1.50 ms, their operands being made twice as often, and serve shorter sequences.
+// cycles): 4 x 2,048 tokens of 32 heads after 8,192 cached ones take 1.33 ms (943 TFLOP/s, where an 8,192^3 product reaches
+// 1,270), with the matrix pipe busy 43 % of the cycles and the vector ALU 54 %. Eight waves share a unit's operands (256 rows a
+// work-group); four waves do the same in 1.51 ms, their operands being made twice as often, and serve shorter sequences.
 #include <type_traits>
 
 #include "chunk_core.h"
@@ -47,7 +47,8 @@ __device__ __forceinline__ int block_scan(int x, int* tmp, int& total) {
 
 }  // namespace
 
-// The plan of a batch too large for every wave to hold, by one block
+// The plan of a batch too large for every wave to hold, by one block: 72 us for 100 as for 256 sequences, which its LDS atomics
+// take: the compiler sums their operands in loops over a wave's lanes
 __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   constexpr int kClasses = 64;
   __shared__ int tmp[kPlanThreads / 64], counts[kCuts], parts[kCuts], classes[kClasses], longest;
@@ -708,14 +709,14 @@ ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_
   const int gq = Hq / H;
   const long long seq_rows = (long long)max_q * gq, rows = (long long)total_q * gq;
   // The kernel of few rows makes the operands again for every 32 rows, which takes 1.5 of the four waves' time a row. It takes
-  // what they would leave more than that empty: 24 sequences of 2 to 20 tokens (32 + 8 heads) over 512 to 16,384: 88 us, with
-  // four waves 135; of 2 to 38 161 and 179; 100 of 1 to 40 over up to 2,000 193 and 184.
+  // what they would leave more than that empty: 24 sequences of 2 to 20 tokens (32 + 8 heads) over 512 to 16,384: 84 us, with
+  // four waves 118; of 2 to 38 157 and 158; 100 of 1 to 40 over up to 2,000 196 and 178.
   // Four waves do the work of eight in 1.1 of the time, but on tiles of half the rows. They take what eight would leave more
   // than that empty: rows a sequence filled up to whole tiles, or half a tile more where the lengths differ. 16 chunks of 17
-  // to 100 tokens (32 + 8 heads) over up to 8,000: 112 us, with eight waves 129; of 128 over 2,000: 118 and 106. And prompts with
+  // to 100 tokens (32 + 8 heads) over up to 8,000: 100 us, with eight waves 121; of 128 over 2,000: 110 and 97. And prompts with
   // nothing cached (no operands made twice) whose smaller tiles all have a place, since a causal tile's length varies and two
-  // share a compute unit, the shortest beside the longest: 500 and 2,011 tokens 23 and 70 us, with eight waves 27 and 75;
-  // 4,000, twice what the chip holds at once, 187 and 166.
+  // share a compute unit, the shortest beside the longest: 500 and 2,011 tokens 23 and 67 us, with eight waves 25 and 71;
+  // 4,000, twice what the chip holds at once, 183 and 163.
   auto filled = [&](long long tile) { return rows == seq_rows * B ? (seq_rows + tile - 1) / tile * tile : rows / B + tile / 2; };
   const long long tiles4 = B * ((seq_rows + 127) / 128), rows4 = rows / 128 + B;
   const bool placed = (tiles4 < rows4 ? tiles4 : rows4) * H <= 2LL * num_cus();

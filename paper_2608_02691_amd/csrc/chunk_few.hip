@@ -1,6 +1,6 @@
 // Attention of few new tokens per sequence (int2kv_chunk_attention): drafted tokens, short turns.
 // Bound by the vector ALU that makes operands of the codes (540 instructions and 32 exponentials a wave and unit, 2,900
-// cycles), at a third more than the time of the cache's bytes, so nothing is shared and nothing waited for: the four waves of
+// cycles; busy 60 % of them all), at a third more than the time of the cache's bytes, so nothing is shared and nothing waited for: the four waves of
 // a work-group hold the same 32 rows and take different 64-token units of the context, each with the next unit's records on
 // their way to LDS (LDS-DMA) and its own softmax. Codes become matrix operands in the registers they are used from. At the
 // end the four partial results meet in LDS, each wave un-rotates the 32 channels of its tile and adds the chunk's own bf16
