@@ -411,6 +411,108 @@ int int2kv_chunk_attention(const int2kv_cache* cache, const uint16_t* q, int64_t
                            int64_t v_stride, const float* mu, uint16_t* out, void* workspace,
                            size_t workspace_bytes, hipStream_t stream);
 
+/* Tokens of a drafted tree at most. */
+#define INT2KV_MAX_TREE 256
+
+/* Attention of the tokens of a drafted tree over the INT2 cache: a target model scoring every drafted
+ * continuation in one pass, or a draft model growing the tree level by level. The tree's keys and
+ * values are the caller's bf16 rows, tree_starts[b] .. tree_starts[b + 1] of k_tree and v_tree for
+ * sequence b, T_b of them; the accepted ones are appended (int2kv_quantize_append, slot -1 for the
+ * others) once they are known. parents[t] is the tree index (0 .. T_b - 1) of the token that token t
+ * follows, a smaller one, or -1 where t follows the last cached token. The queries, n_b rows from
+ * q_starts[b] of q, are the last n_b tokens of the tree: query i is token t = T_b - n_b + i and sees
+ * the ctx_lens[b] cached tokens and its path t, parents[t], .. :
+ *     a_s = (q R_K) k^_s^T / sqrt(d),  a_t = q (k_t - mu)^T / sqrt(d),
+ *     o = (sum_s p_s v^_s) R_V^T + sum_t p_t v_t,   one softmax over both.
+ * A token whose walk to -1 meets a parent outside [-1, own index) is absent, as is one with t < 0 or
+ * t >= max_tree: it sees nothing, not even the cache, and gets zeros (places of a tree of a fixed
+ * shape that stay empty take the parent -2). Rows of k_tree and v_tree on no query's path may hold
+ * anything.
+ *   q, q_starts, total_q, max_q, block_table, max_blocks_per_seq, ctx_lens, max_ctx, R_k, R_v, out :
+ *                  as int2kv_chunk_attention
+ *   tree_starts  : int32 [batch + 1], ascending offsets into 0 .. total_tree; the same as q_starts where
+ *                  every token of the trees is a query
+ *   total_tree, max_tree : rows of k_tree, v_tree and parents; host-side upper bound of T_b, at most
+ *                  INT2KV_MAX_TREE
+ *   k_tree, v_tree, mu : as k_new, v_new and mu of int2kv_chunk_attention
+ *   workspace    : int2kv_tree_attention_workspace_bytes(...) bytes, 256-byte aligned; enough for every
+ *                  call within the same bounds, nothing kept between calls, calls that overlap need one each
+ * Numerics and ranges as int2kv_chunk_attention. Deterministic; no atomics on results. */
+size_t int2kv_tree_attention_workspace_bytes(int batch, int num_q_heads, int num_kv_heads, int total_q, int max_q,
+                                             int max_tree, int max_ctx);
+int int2kv_tree_attention(const int2kv_cache* cache, const uint16_t* q, int64_t q_stride, const int32_t* q_starts,
+                          int batch, int total_q, int max_q, int num_q_heads, const int32_t* tree_starts,
+                          int total_tree, int max_tree, const int32_t* parents, const uint16_t* k_tree,
+                          int64_t k_stride, const uint16_t* v_tree, int64_t v_stride, const float* mu,
+                          const int32_t* block_table, int max_blocks_per_seq, const int32_t* ctx_lens, int max_ctx,
+                          const float* R_k, const float* R_v, uint16_t* out, void* workspace,
+                          size_t workspace_bytes, hipStream_t stream);
+
+/* Attention weight that every cached token receives, added to a running sum: what an eviction goes by.
+ * The cache holds the new tokens too (appended first, as for int2kv_decode): query token i of n_b sees
+ * the cached tokens 0 .. ctx_lens[b] - n_b + i, as the second form of int2kv_chunk_attention. For KV
+ * head h and token s < ctx_lens[b]
+ *     weights_out[b, h, s] = decay weights_in[b, h, s] + sum_i sum_{j in group h} p_ij(s),
+ *     p_ij = softmax over what token i sees of (q_ij R_K) k^_s^T / sqrt(d).
+ * One token a sequence: a decode step; the last tokens of a prompt: their vote on the rest; all of them.
+ *   q .. max_ctx, R_k : as int2kv_chunk_attention (with max_q 0 the sums only decay; q, R_k may be NULL)
+ *   weights_in   : fp32, KV head h of sequence b at (b H_kv + h) weights_stride, or NULL: zeros
+ *   decay        : factor of weights_in, finite
+ *   weights_out  : fp32 as weights_in, which it may be, without otherwise overlapping it. Tokens from
+ *                  min(ctx_lens[b], max_ctx) on are left as they were; tokens in blocks outside the
+ *                  cache receive nothing
+ *   weights_stride : at least max_ctx
+ *   workspace    : int2kv_token_weights_workspace_bytes(...) bytes, 256-byte aligned; enough for every
+ *                  call within the same bounds, nothing kept between calls, calls that overlap need one each
+ * fp32 throughout: products run on the matrix cores in terms that keep fp32's precision, statistics and
+ * sums in fp32 (a weight is off by about 1e-6 of itself and the scores' size times 1e-7). Stored scales
+ * and zeros have to be finite. Deterministic; no atomics on results. */
+size_t int2kv_token_weights_workspace_bytes(int batch, int num_q_heads, int num_kv_heads, int total_q, int max_q,
+                                            int max_ctx);
+int int2kv_token_weights(const int2kv_cache* cache, const uint16_t* q, int64_t q_stride, const int32_t* q_starts,
+                         int batch, int total_q, int max_q, int num_q_heads, const int32_t* block_table,
+                         int max_blocks_per_seq, const int32_t* ctx_lens, int max_ctx, const float* R_k,
+                         const float* weights_in, float decay, float* weights_out, int64_t weights_stride,
+                         void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* The tokens of every sequence and KV head that stay in a cache of `budget` tokens: the first `sink`
+ * and the last `recent` ones, and of the others those of the largest weights (ties: the lower index;
+ * NaN below every number), in ascending order. A sequence of at most `budget` tokens keeps them all.
+ *   weights      : fp32, KV head h of sequence b at (b num_kv_heads + h) weights_stride, tokens
+ *                  s < min(ctx_lens[b], max_ctx) (int2kv_token_weights)
+ *   sink + recent at most budget
+ *   kept         : int32, list of KV head h of sequence b at (b num_kv_heads + h) kept_stride;
+ *                  kept_lens[b] = min(ctx_lens[b], max_ctx, budget) entries are written
+ *   kept_stride  : at least min(budget, max_ctx)
+ *   kept_lens    : int32 [batch] */
+int int2kv_select_tokens(const float* weights, int64_t weights_stride, int batch, int num_kv_heads,
+                         const int32_t* ctx_lens, int max_ctx, int budget, int sink, int recent, int32_t* kept,
+                         int64_t kept_stride, int32_t* kept_lens, hipStream_t stream);
+
+/* The kept tokens' rows, byte for byte, to the front of a sequence: token j < kept_lens[b] of KV head h
+ * becomes the old token kept[b, h, j], whose place in block_table's blocks is written to token j's in
+ * out_table's. Keys are stored after their rotary positions, so the readers see the kept tokens
+ * as they were; the sequence's length is then kept_lens[b]. Lists come from int2kv_select_tokens, or
+ * are the caller's, in any order, with repeats.
+ *   block_table  : int32 [batch, max_blocks_per_seq]
+ *   kept, kept_stride : as int2kv_select_tokens; max_kept: host-side upper bound of kept_lens (larger
+ *                  ones are cut to it), at most kept_stride
+ *   out_table    : int32 [batch, out_max_blocks], at least the pages of max_kept tokens: blocks that no
+ *                  sequence of the call reads and no other writes. NULL (or block_table): in place, through the
+ *                  workspace; no block may then belong to two sequences
+ *   weights      : fp32 (as int2kv_token_weights) or NULL; moved along to out_weights, which in place may
+ *                  be weights itself
+ *   workspace    : in place int2kv_move_tokens_workspace_bytes(...) bytes, 16-byte aligned; else NULL
+ * A row whose old token lies outside the table or in a block outside the cache is left as it was, as
+ * are rows behind the last kept one, pages whose new block lies outside the cache, and weights beyond
+ * a stride. */
+size_t int2kv_move_tokens_workspace_bytes(int batch, int num_kv_heads, int group_size, int max_kept);
+int int2kv_move_tokens(const int2kv_cache* cache, const int32_t* block_table, int max_blocks_per_seq,
+                       const int32_t* kept, int64_t kept_stride, const int32_t* kept_lens, int batch,
+                       int max_kept, const int32_t* out_table, int out_max_blocks, const float* weights,
+                       int64_t weights_stride, float* out_weights, int64_t out_weights_stride, void* workspace,
+                       size_t workspace_bytes, hipStream_t stream);
+
 /* ---- OptR offline calibration (Sec. 4.2 - 4.5; Algorithm 1 of the appendix), fp64 on the GPU.
  * For every KV head h the corrected rotations R = R^0 exp(A - A^T) (eq:OptR_skew) are fitted to
  * calibration traces: first A_K on the key objective (eq:OptR_key_loss)

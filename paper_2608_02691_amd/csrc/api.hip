@@ -646,6 +646,44 @@ bool rows_meet(const Rows& a, const Rows& b) {
 
 bool valid_stride(int64_t stride, int heads) { return stride >= (int64_t)heads * kHeadDim && stride % 8 == 0 && stride <= INT32_MAX; }
 
+// Attention of new tokens over the cache and their own rows: checks, plan and launch. The names of the caller's rows are for
+// messages; own_rows: how many there are.
+int chunk_attention(const int2kv_cache* cache, ChunkArgs a, const char* rows, int own_rows, void* workspace, size_t workspace_bytes,
+                    hipStream_t stream) {
+  if (int st = check_cache(cache)) return st;
+  const int H = cache->num_kv_heads;
+  const std::string names(rows);
+  if (H > 65535) return fail(INT2KV_EUNSUPPORTED, "at most 65535 KV heads");
+  if (a.B <= 0) return fail(INT2KV_EINVAL, "batch must be positive");
+  if (a.Hq <= 0 || a.Hq % H) return fail(INT2KV_EINVAL, "num_q_heads must be a multiple of num_kv_heads");
+  if (a.total_q < 0 || a.max_q < 0 || a.max_ctx < 0 || a.max_blocks <= 0)
+    return fail(INT2KV_EINVAL, "bad total_q / max_q / max_ctx / max_blocks_per_seq");
+  if (a.max_q > a.total_q) a.max_q = a.total_q;
+  if (a.max_q == 0) return ok();
+  if ((int64_t)a.total_q * a.Hq > INT32_MAX || (int64_t)a.B > (1 << 24))
+    return fail(INT2KV_EUNSUPPORTED, "total_q * num_q_heads must be below 2^31, batch at most 2^24");
+  if (!a.q || !a.starts || !a.table || !a.lens || !a.R_k || !a.R_v || !a.out) return fail(INT2KV_EINVAL, "NULL pointer argument");
+  if (!a.k_new != !a.v_new || !a.k_new != !a.mu) return fail(INT2KV_EINVAL, names + " and mu go together");
+  if (!valid_stride(a.q_stride, a.Hq) || (a.k_new && (!valid_stride(a.k_stride, H) || !valid_stride(a.v_stride, H))))
+    return fail(INT2KV_EINVAL, "strides must be multiples of 8, at least 128 * heads and below 2^31");
+  if (!aligned(a.q, 16) || !aligned(a.R_k, 16) || !aligned(a.R_v, 16) || !aligned(a.out, 16) || (a.k_new && (!aligned(a.k_new, 16) || !aligned(a.v_new, 16))))
+    return fail(INT2KV_EINVAL, "q, R_k, R_v, " + names + " and out must be 16-byte aligned");
+  const Rows ro{a.out, (int64_t)a.Hq * kHeadDim, a.Hq, a.total_q, 2};
+  if (rows_meet(ro, Rows{a.q, a.q_stride, a.Hq, a.total_q, 2}) || (a.k_new && own_rows > 0 && (rows_meet(ro, Rows{a.k_new, a.k_stride, H, own_rows, 2}) ||
+      rows_meet(ro, Rows{a.v_new, a.v_stride, H, own_rows, 2}))))
+    return fail(INT2KV_EINVAL, "out overlaps q, " + names);
+  const ChunkPlan plan = make_chunk_plan(a.B, a.Hq, H, a.total_q, a.max_q, a.parents ? a.max_tree : a.max_q, a.max_ctx);
+  // a launch holds 2^32 - 1 threads
+  if ((int64_t)plan.max_items * H > UINT32_MAX / (plan.waves == 8 ? 512 : 256)) return fail(INT2KV_EUNSUPPORTED, "too many row tiles for one launch");
+  const char* name = a.parents ? "tree_attention" : "chunk_attention";
+  if (!workspace || workspace_bytes < plan.total)
+    return fail(INT2KV_EWORKSPACE, std::string("workspace smaller than int2kv_") + name + "_workspace_bytes()");
+  if (!aligned(workspace, 256)) return fail(INT2KV_EINVAL, "workspace must be 256-byte aligned");
+  a.cv = view(cache);
+  a.gq = a.Hq / H;
+  return hip_status(launch_chunk_attention(a, plan, static_cast<uint8_t*>(workspace), stream), name);
+}
+
 }  // namespace
 
 extern "C" {
@@ -715,7 +753,8 @@ size_t int2kv_chunk_attention_workspace_bytes(int batch, int num_q_heads, int nu
                                               int max_ctx) {
   if (batch <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads || total_q < 0 || max_q < 0 || max_ctx < 0)
     return 0;
-  return make_chunk_plan(batch, num_q_heads, num_kv_heads, total_q, max_q < total_q ? max_q : total_q, max_ctx).total;
+  if (max_q > total_q) max_q = total_q;
+  return make_chunk_plan(batch, num_q_heads, num_kv_heads, total_q, max_q, max_q, max_ctx).total;
 }
 
 int int2kv_chunk_attention(const int2kv_cache* cache, const uint16_t* q, int64_t q_stride, const int32_t* q_starts,
@@ -723,6 +762,62 @@ int int2kv_chunk_attention(const int2kv_cache* cache, const uint16_t* q, int64_t
                            int max_blocks_per_seq, const int32_t* ctx_lens, int max_ctx, const float* R_k, const float* R_v,
                            const uint16_t* k_new, int64_t k_stride, const uint16_t* v_new, int64_t v_stride, const float* mu,
                            uint16_t* out, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  ChunkArgs a{};
+  a.q = q, a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+  a.starts = q_starts, a.B = batch, a.total_q = total_q, a.max_q = max_q, a.Hq = num_q_heads;
+  a.table = block_table, a.max_blocks = max_blocks_per_seq, a.lens = ctx_lens, a.max_ctx = max_ctx;
+  a.R_k = R_k, a.R_v = R_v, a.own = k_new != nullptr, a.k_new = k_new, a.v_new = v_new, a.mu = mu, a.out = out;
+  return chunk_attention(cache, a, "k_new, v_new", total_q, workspace, workspace_bytes, stream);
+}
+
+size_t int2kv_tree_attention_workspace_bytes(int batch, int num_q_heads, int num_kv_heads, int total_q, int max_q,
+                                             int max_tree, int max_ctx) {
+  if (batch <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads || total_q < 0 || max_q < 0 ||
+      max_tree < 0 || max_tree > INT2KV_MAX_TREE || max_ctx < 0)
+    return 0;
+  if (max_q > total_q) max_q = total_q;
+  return make_chunk_plan(batch, num_q_heads, num_kv_heads, total_q, max_q, max_tree, max_ctx).total;
+}
+
+int int2kv_tree_attention(const int2kv_cache* cache, const uint16_t* q, int64_t q_stride, const int32_t* q_starts,
+                          int batch, int total_q, int max_q, int num_q_heads, const int32_t* tree_starts,
+                          int total_tree, int max_tree, const int32_t* parents, const uint16_t* k_tree,
+                          int64_t k_stride, const uint16_t* v_tree, int64_t v_stride, const float* mu,
+                          const int32_t* block_table, int max_blocks_per_seq, const int32_t* ctx_lens, int max_ctx,
+                          const float* R_k, const float* R_v, uint16_t* out, void* workspace, size_t workspace_bytes,
+                          hipStream_t stream) {
+  if (int st = check_cache(cache)) return st;
+  if (total_tree < 0 || max_tree < 0) return fail(INT2KV_EINVAL, "bad total_tree / max_tree");
+  if (max_tree > INT2KV_MAX_TREE) return fail(INT2KV_EUNSUPPORTED, "max_tree must be at most 256");
+  if ((int64_t)total_tree * cache->num_kv_heads > INT32_MAX)
+    return fail(INT2KV_EUNSUPPORTED, "total_tree * num_kv_heads must be below 2^31");
+  if (max_q > 0 && total_q > 0) {
+    if (!tree_starts || !aligned(tree_starts, 4)) return fail(INT2KV_EINVAL, "NULL pointer argument: tree_starts");
+    if (!parents || !k_tree || !v_tree || !mu) return fail(INT2KV_EINVAL, "NULL pointer argument: parents, k_tree, v_tree and mu");
+    if (!aligned(parents, 4)) return fail(INT2KV_EINVAL, "parents must be 4-byte aligned");
+  }
+  ChunkArgs a{};
+  a.q = q, a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
+  a.starts = q_starts, a.B = batch, a.total_q = total_q, a.max_q = max_q, a.Hq = num_q_heads;
+  a.table = block_table, a.max_blocks = max_blocks_per_seq, a.lens = ctx_lens, a.max_ctx = max_ctx;
+  a.R_k = R_k, a.R_v = R_v, a.own = true, a.k_new = k_tree, a.v_new = v_tree, a.mu = mu, a.out = out;
+  a.tree_starts = tree_starts, a.parents = parents, a.total_tree = total_tree, a.max_tree = max_tree < total_tree ? max_tree : total_tree;
+  return chunk_attention(cache, a, "k_tree, v_tree", total_tree, workspace, workspace_bytes, stream);
+}
+
+size_t int2kv_token_weights_workspace_bytes(int batch, int num_q_heads, int num_kv_heads, int total_q, int max_q,
+                                            int max_ctx) {
+  if (batch <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads || total_q < 0 || max_q < 0 || max_ctx < 0 ||
+      (int64_t)total_q * num_q_heads > INT32_MAX)
+    return 0;
+  return make_token_weights_plan(batch, num_q_heads, num_kv_heads, total_q, max_q < total_q ? max_q : total_q, max_ctx).total;
+}
+
+int int2kv_token_weights(const int2kv_cache* cache, const uint16_t* q, int64_t q_stride, const int32_t* q_starts,
+                         int batch, int total_q, int max_q, int num_q_heads, const int32_t* block_table,
+                         int max_blocks_per_seq, const int32_t* ctx_lens, int max_ctx, const float* R_k,
+                         const float* weights_in, float decay, float* weights_out, int64_t weights_stride,
+                         void* workspace, size_t workspace_bytes, hipStream_t stream) {
   if (int st = check_cache(cache)) return st;
   const int H = cache->num_kv_heads;
   if (H > 65535) return fail(INT2KV_EUNSUPPORTED, "at most 65535 KV heads");
@@ -730,33 +825,94 @@ int int2kv_chunk_attention(const int2kv_cache* cache, const uint16_t* q, int64_t
   if (num_q_heads <= 0 || num_q_heads % H) return fail(INT2KV_EINVAL, "num_q_heads must be a multiple of num_kv_heads");
   if (total_q < 0 || max_q < 0 || max_ctx < 0 || max_blocks_per_seq <= 0)
     return fail(INT2KV_EINVAL, "bad total_q / max_q / max_ctx / max_blocks_per_seq");
+  if (!(decay == decay) || decay - decay != 0.0f) return fail(INT2KV_EINVAL, "decay must be finite");
+  if (weights_stride < max_ctx) return fail(INT2KV_EINVAL, "weights_stride must be at least max_ctx");
   if (max_q > total_q) max_q = total_q;
-  if (max_q == 0) return ok();
+  if (max_ctx == 0) return ok();
   if ((int64_t)total_q * num_q_heads > INT32_MAX || (int64_t)batch > (1 << 24))
     return fail(INT2KV_EUNSUPPORTED, "total_q * num_q_heads must be below 2^31, batch at most 2^24");
-  if (!q || !q_starts || !block_table || !ctx_lens || !R_k || !R_v || !out) return fail(INT2KV_EINVAL, "NULL pointer argument");
-  if (!k_new != !v_new || !k_new != !mu) return fail(INT2KV_EINVAL, "k_new, v_new and mu go together");
-  if (!valid_stride(q_stride, num_q_heads) || (k_new && (!valid_stride(k_stride, H) || !valid_stride(v_stride, H))))
-    return fail(INT2KV_EINVAL, "strides must be multiples of 8, at least 128 * heads and below 2^31");
-  if (!aligned(q, 16) || !aligned(R_k, 16) || !aligned(R_v, 16) || !aligned(out, 16) || (k_new && (!aligned(k_new, 16) || !aligned(v_new, 16))))
-    return fail(INT2KV_EINVAL, "q, R_k, R_v, k_new, v_new and out must be 16-byte aligned");
-  const Rows ro{out, (int64_t)num_q_heads * kHeadDim, num_q_heads, total_q, 2};
-  if (rows_meet(ro, Rows{q, q_stride, num_q_heads, total_q, 2}) || (k_new && (rows_meet(ro, Rows{k_new, k_stride, H, total_q, 2}) ||
-      rows_meet(ro, Rows{v_new, v_stride, H, total_q, 2}))))
-    return fail(INT2KV_EINVAL, "out overlaps q, k_new or v_new");
-  const ChunkPlan plan = make_chunk_plan(batch, num_q_heads, H, total_q, max_q, max_ctx);
+  if (!q_starts || !block_table || !ctx_lens || !weights_out || (max_q > 0 && (!q || !R_k)))
+    return fail(INT2KV_EINVAL, "NULL pointer argument");
+  if (max_q > 0 && !valid_stride(q_stride, num_q_heads))
+    return fail(INT2KV_EINVAL, "q_stride must be a multiple of 8, at least 128 * H_q and below 2^31");
+  if (!aligned(q, 16) || !aligned(R_k, 16) || !aligned(weights_in, 4) || !aligned(weights_out, 4))
+    return fail(INT2KV_EINVAL, "q and R_k must be 16-byte aligned, the weights 4-byte");
+  if (weights_in && weights_in != weights_out) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(weights_in), y = reinterpret_cast<uintptr_t>(weights_out);
+    const uint64_t len = ((uint64_t)batch * H - 1) * (uint64_t)weights_stride * 4 + (uint64_t)max_ctx * 4;
+    if ((x < y ? y - x : x - y) < len) return fail(INT2KV_EINVAL, "weights_out overlaps weights_in without being it");
+  }
+  const TokenWeightsPlan plan = make_token_weights_plan(batch, num_q_heads, H, total_q, max_q, max_ctx);
   // a launch holds 2^32 - 1 threads
-  if ((int64_t)plan.max_items * H > UINT32_MAX / (plan.waves == 8 ? 512 : 256)) return fail(INT2KV_EUNSUPPORTED, "too many row tiles for one launch");
+  if ((int64_t)batch * H * plan.ranges > UINT32_MAX / 512 / plan.slices || (int64_t)batch * H * plan.seq_tiles > UINT32_MAX / 256)
+    return fail(INT2KV_EUNSUPPORTED, "too many row tiles or token ranges for one launch");
   if (!workspace || workspace_bytes < plan.total)
-    return fail(INT2KV_EWORKSPACE, "workspace smaller than int2kv_chunk_attention_workspace_bytes()");
+    return fail(INT2KV_EWORKSPACE, "workspace smaller than int2kv_token_weights_workspace_bytes()");
   if (!aligned(workspace, 256)) return fail(INT2KV_EINVAL, "workspace must be 256-byte aligned");
-  ChunkArgs a{};
+  TokenWeightsArgs a{};
   a.cv = view(cache);
-  a.q = q, a.q_stride = q_stride, a.k_stride = k_stride, a.v_stride = v_stride;
-  a.starts = q_starts, a.B = batch, a.total_q = total_q, a.max_q = max_q, a.Hq = num_q_heads, a.gq = num_q_heads / H;
+  a.q = q, a.q_stride = q_stride, a.starts = q_starts, a.B = batch, a.total_q = total_q, a.max_q = max_q, a.Hq = num_q_heads, a.gq = num_q_heads / H;
   a.table = block_table, a.max_blocks = max_blocks_per_seq, a.lens = ctx_lens, a.max_ctx = max_ctx;
-  a.R_k = R_k, a.R_v = R_v, a.own = k_new != nullptr, a.k_new = k_new, a.v_new = v_new, a.mu = mu, a.out = out;
-  return hip_status(launch_chunk_attention(a, plan, static_cast<uint8_t*>(workspace), stream), "chunk_attention");
+  a.R_k = R_k, a.w_in = weights_in, a.w_out = weights_out, a.w_stride = weights_stride, a.decay = decay;
+  return hip_status(launch_token_weights(a, plan, static_cast<uint8_t*>(workspace), stream), "token_weights");
+}
+
+int int2kv_select_tokens(const float* weights, int64_t weights_stride, int batch, int num_kv_heads, const int32_t* ctx_lens,
+                         int max_ctx, int budget, int sink, int recent, int32_t* kept, int64_t kept_stride, int32_t* kept_lens,
+                         hipStream_t stream) {
+  if (batch <= 0 || num_kv_heads <= 0) return fail(INT2KV_EINVAL, "batch and num_kv_heads must be positive");
+  if (max_ctx < 0 || weights_stride < max_ctx) return fail(INT2KV_EINVAL, "max_ctx must lie in [0, weights_stride]");
+  if (budget < 0 || sink < 0 || recent < 0 || (int64_t)sink + recent > budget)
+    return fail(INT2KV_EINVAL, "budget must hold sink + recent tokens");
+  if (kept_stride < (budget < max_ctx ? budget : max_ctx)) return fail(INT2KV_EINVAL, "kept_stride must hold min(budget, max_ctx) tokens");
+  if ((int64_t)batch * num_kv_heads > UINT32_MAX / 1024) return fail(INT2KV_EUNSUPPORTED, "too many lists for one launch");
+  if (max_ctx > INT32_MAX - 4096) return fail(INT2KV_EUNSUPPORTED, "max_ctx must be below 2^31 - 4096");
+  if (!ctx_lens || !kept_lens || (max_ctx > 0 && !weights) || (max_ctx > 0 && budget > 0 && !kept)) return fail(INT2KV_EINVAL, "NULL pointer argument");
+  if (!aligned(weights, 4) || !aligned(kept, 4) || !aligned(ctx_lens, 4) || !aligned(kept_lens, 4))
+    return fail(INT2KV_EINVAL, "weights, ctx_lens, kept and kept_lens must be 4-byte aligned");
+  SelectArgs a{weights, weights_stride, ctx_lens, batch, num_kv_heads, max_ctx, budget, sink, recent, kept, kept_stride, kept_lens};
+  return hip_status(launch_select_tokens(a, stream), "select_tokens");
+}
+
+size_t int2kv_move_tokens_workspace_bytes(int batch, int num_kv_heads, int group_size, int max_kept) {
+  if (batch <= 0 || num_kv_heads <= 0 || (group_size != 32 && group_size != 128) || max_kept < 0) return 0;
+  return (size_t)batch * num_kv_heads * (((size_t)max_kept + kBlock - 1) / kBlock) * move_stage_bytes(kHeadDim / group_size);
+}
+
+int int2kv_move_tokens(const int2kv_cache* cache, const int32_t* block_table, int max_blocks_per_seq, const int32_t* kept,
+                       int64_t kept_stride, const int32_t* kept_lens, int batch, int max_kept, const int32_t* out_table,
+                       int out_max_blocks, const float* weights, int64_t weights_stride, float* out_weights,
+                       int64_t out_weights_stride, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (int st = check_cache(cache)) return st;
+  const int H = cache->num_kv_heads;
+  const bool in_place = !out_table || out_table == block_table;
+  if (batch <= 0) return fail(INT2KV_EINVAL, "batch must be positive");
+  if (max_blocks_per_seq <= 0 || max_kept < 0) return fail(INT2KV_EINVAL, "bad max_blocks_per_seq / max_kept");
+  if (in_place) out_table = block_table, out_max_blocks = max_blocks_per_seq;
+  const int pages = (int)(((int64_t)max_kept + kBlock - 1) / kBlock);
+  if (kept_stride < max_kept) return fail(INT2KV_EINVAL, "kept_stride must be at least max_kept");
+  if (out_max_blocks < pages) return fail(INT2KV_EINVAL, "the result's table must hold max_kept tokens");
+  if (!weights != !out_weights) return fail(INT2KV_EINVAL, "weights and out_weights go together");
+  if (weights && (weights_stride <= 0 || out_weights_stride < max_kept))
+    return fail(INT2KV_EINVAL, "weights_stride must be positive, out_weights_stride at least max_kept");
+  if (max_kept == 0) return ok();
+  if ((int64_t)batch * H > UINT32_MAX / 64 / pages) return fail(INT2KV_EUNSUPPORTED, "too many pages for one launch");
+  if (!block_table || !kept || !kept_lens) return fail(INT2KV_EINVAL, "NULL pointer argument");
+  if (!aligned(block_table, 4) || !aligned(kept, 4) || !aligned(kept_lens, 4) || !aligned(out_table, 4) || !aligned(weights, 4) || !aligned(out_weights, 4))
+    return fail(INT2KV_EINVAL, "tables, lists and weights must be 4-byte aligned");
+  if (weights && !in_place) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(weights), y = reinterpret_cast<uintptr_t>(out_weights);
+    const uint64_t lists = (uint64_t)batch * H, xl = lists * weights_stride * 4, yl = (lists - 1) * out_weights_stride * 4 + 4ull * max_kept;
+    if (x < y + yl && y < x + xl) return fail(INT2KV_EINVAL, "out_weights overlaps weights");
+  }
+  if (in_place) {
+    if (!workspace || workspace_bytes < int2kv_move_tokens_workspace_bytes(batch, H, cache->group_size, max_kept))
+      return fail(INT2KV_EWORKSPACE, "workspace smaller than int2kv_move_tokens_workspace_bytes()");
+    if (!aligned(workspace, 16)) return fail(INT2KV_EINVAL, "workspace must be 16-byte aligned");
+  }
+  MoveArgs a{view(cache), block_table, max_blocks_per_seq, kept, kept_stride, kept_lens, batch, max_kept, pages, out_table, out_max_blocks,
+             weights, out_weights, weights_stride, out_weights_stride, static_cast<uint8_t*>(workspace)};
+  return hip_status(launch_move_tokens(a, in_place, stream), "move_tokens");
 }
 
 }  // extern "C"

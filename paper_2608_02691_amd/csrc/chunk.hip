@@ -49,6 +49,7 @@ __device__ __forceinline__ int block_scan(int x, int* tmp, int& total) {
 
 // The plan of a batch too large for every wave to hold, by one block: 72 us for 100 as for 256 sequences, which its LDS atomics
 // take: the compiler sums their operands in loops over a wave's lanes
+template <bool TREE>
 __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   constexpr int kClasses = 64;
   __shared__ int tmp[kPlanThreads / 64], counts[kCuts], parts[kCuts], classes[kClasses], longest;
@@ -61,7 +62,7 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   int T = 0, total = 0;
   unsigned long long W = 0;
   for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
-    const Load s = b0 + tid < a.B ? load_of(a, seq_of(a, b0 + tid)) : Load{0, 0};
+    const Load s = b0 + tid < a.B ? load_of<TREE>(a, seq_of<TREE>(a, b0 + tid)) : Load{0, 0};
     int n;
     block_scan(s.tiles, tmp, n);
     T = min(T + n, 1 << 28);
@@ -74,7 +75,7 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   const float places = places_of(a), even = (float)work * __builtin_amdgcn_rcpf(places);
   int mine[kCuts] = {}, cut[kCuts] = {};
   for (int b = tid; b < a.B; b += kPlanThreads) {
-    const Load s = load_of(a, seq_of(a, b));
+    const Load s = load_of<TREE>(a, seq_of<TREE>(a, b));
 #pragma unroll
     for (int k = 0; k < kCuts; ++k) {
       const int n = pieces_of(s.units, cut_of(a, k, even, umax));
@@ -100,7 +101,7 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
   T = 0;
   for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
     const int b = b0 + tid;
-    const Load s = b < a.B ? load_of(a, seq_of(a, b)) : Load{0, 0};
+    const Load s = b < a.B ? load_of<TREE>(a, seq_of<TREE>(a, b)) : Load{0, 0};
     int n_tiles;
     const int t = T + block_scan(s.tiles, tmp, n_tiles) - s.tiles;
     if (b < a.B) {
@@ -115,11 +116,11 @@ __global__ __launch_bounds__(kPlanThreads) void chunk_plan_kernel(ChunkArgs a) {
     classes[tid] = wave_scan(x) - x;
   }
   __syncthreads();
-  for (int b = tid; b < a.B; b += kPlanThreads) a.order[atomicAdd(&classes[class_of(load_of(a, seq_of(a, b)))], 1)] = b;
+  for (int b = tid; b < a.B; b += kPlanThreads) a.order[atomicAdd(&classes[class_of(load_of<TREE>(a, seq_of<TREE>(a, b)))], 1)] = b;
   __syncthreads();
   for (int b0 = 0; b0 < a.B; b0 += kPlanThreads) {
     const int x = b0 + tid;
-    const Load s = x < a.B ? load_of(a, seq_of(a, a.order[x])) : Load{0, 0};
+    const Load s = x < a.B ? load_of<TREE>(a, seq_of<TREE>(a, a.order[x])) : Load{0, 0};
     const int items = s.tiles * pieces_of(s.units, L);
     int n_items;
     const int i = total + block_scan(items, tmp, n_items) - items;
@@ -386,7 +387,8 @@ struct Int2Source {
 
 // The chunk's own units: bf16 rows. A wave's K operands are 16-byte pieces of its half's rows; its page's values come two
 // channels a load and are paired over tokens, so that tile 2 e + o holds channels 64 e + 2 m + o.
-template <int NW>
+// TREE: a token sees those on its path, and every unit counts as one that some row does not see all of.
+template <int NW, bool TREE>
 struct OwnSource {
   static constexpr int KO = 16 / NW, PV = 8 / NW;  // K operands, pairs of V^T tiles
   const ChunkArgs& a;
@@ -396,12 +398,14 @@ struct OwnSource {
   cd_u4_t k[KO];
   uint32_t v[PV][8];
   uint32_t found = 0;
+  path_t path = 0;
 
-  __device__ __forceinline__ OwnSource(const ChunkArgs& args, int h, const Seq& t, int row0, int w, int row_tok, int least)
-      : a(args), n_tok(t.n), tok(row_tok), tok_min(least), tok_tile(quotient(row0, args.gq)), l(threadIdx.x & 63), n(l & 31), hh(l >> 5), half(w / (NW / 2)),
+  // start, count: the rows in k_new and v_new
+  __device__ __forceinline__ OwnSource(const ChunkArgs& args, int h, int start, int count, int row0, int w, int row_tok, int least)
+      : a(args), n_tok(count), tok(row_tok), tok_min(least), tok_tile(quotient(row0, args.gq)), l(threadIdx.x & 63), n(l & 31), hh(l >> 5), half(w / (NW / 2)),
         op0(KO * (w % (NW / 2))), page(w / (NW / 4)), pair0(PV * (w % (NW / 4))),
-        kb(args.k_new + t.start * args.k_stride + (size_t)h * kHeadDim + 8 * hh + 16 * op0),
-        vb(args.v_new + t.start * args.v_stride + (size_t)h * kHeadDim + 2 * n + 64 * pair0) {}
+        kb(args.k_new + start * args.k_stride + (size_t)h * kHeadDim + 8 * hh + 16 * op0),
+        vb(args.v_new + start * args.v_stride + (size_t)h * kHeadDim + 2 * n + 64 * pair0) {}
   __device__ __forceinline__ void fetch(int u) {
     const uint16_t* row = kb + min(kUnit * u + 32 * half + (n & 16) + row_token(n & 15), n_tok - 1) * a.k_stride;
 #pragma unroll
@@ -445,10 +449,15 @@ struct OwnSource {
     }
   }
   __device__ __forceinline__ void refetch(int u) { fetch(u); }
-  __device__ __forceinline__ bool partial(int u) const { return kUnit * u + kUnit - 1 > tok_tile; }
-  __device__ __forceinline__ bool masked(int u) const { return kUnit * u + kUnit - 1 > tok_min; }
-  __device__ __forceinline__ bool sees(int u, int t) const { return kUnit * u + t + 8 * hh <= tok; }
-  __device__ __forceinline__ bool sees_token(int u, int t) const { return kUnit * u + t <= tok; }
+  __device__ __forceinline__ bool partial(int u) const { return TREE || kUnit * u + kUnit - 1 > tok_tile; }
+  __device__ __forceinline__ bool masked(int u) const { return TREE || kUnit * u + kUnit - 1 > tok_min; }
+  // (the lane half's 8 never crosses a word)
+  __device__ __forceinline__ bool sees(int u, int t) const { return sees_token(u, t + 8 * hh, t); }
+  __device__ __forceinline__ bool sees_token(int u, int t) const { return sees_token(u, t, t); }
+  __device__ __forceinline__ bool sees_token(int u, int t, int t0) const {
+    if constexpr (TREE) return (path_word(path, 2 * u + (t0 >> 5)) >> (t & 31)) & 1;
+    return kUnit * u + t <= tok;
+  }
 };
 
 // R_K's elements that a thread brings into LDS: eight channels 8 oct .. of a column at a time
@@ -536,14 +545,14 @@ __device__ __forceinline__ void unrotate(const float* R, ChunkLds& lds, RowState
 }  // namespace
 
 // Work-group: a piece of a tile of 32 NW rows of one KV head; wave w has rows 32 w .. of it.
-template <int NG, int NW>
+template <int NG, int NW, bool TREE>
 __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
   __shared__ ChunkLds lds;
   const int H = a.cv.num_kv_heads;
   const int at = quotient((int)blockIdx.x, H), h = (int)blockIdx.x - at * H;
   KeyRotation<NW> R;
   if (a.max_ctx > 0) R.load(a.R_k + (size_t)h * kHeadDim * kHeadDim);  // on its way while the work-group finds its piece
-  const Place place = locate(a, at, h);
+  const Place place = locate<TREE>(a, at, h);
   if (!place.valid) return;
   const Seq seq = place.s;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = l & 31, hh = l >> 5;
@@ -579,11 +588,25 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
   }
 
   const int c0 = max(place.u0 - nI, 0), c1 = place.u1 - nI;
+  Tree tree{0, 0};
+  bool absent = false;  // a row of a token without a path sees nothing
+  if constexpr (TREE) {
+    tree = tree_of(a, place.b);
+    absent = seq.past + tok < 0 || seq.past + tok >= min(tree.count, a.max_tree);
+  }
   if (c0 < c1) {
     cd_b8_t Q[8];
     query(Q);
-    OwnSource<NW> src(a, h, seq, place.row0, w, tok, tok_w);
+    OwnSource<NW, TREE> src(a, h, TREE ? tree.start : seq.start, TREE ? min(tree.count, a.max_tree) : seq.n, place.row0, w, tok, tok_w);
     src.fetch(c0);
+    if constexpr (TREE) {
+      int32_t* parents = reinterpret_cast<int32_t*>(&lds);  // (behind unrotate's last barrier nothing is read there)
+      if ((int)threadIdx.x < min(tree.count, a.max_tree)) parents[threadIdx.x] = a.parents[tree.start + threadIdx.x];
+      __syncthreads();
+      src.path = path_of(parents, seq.past + tok, min(tree.count, a.max_tree));
+      absent = absent || !has_path(src.path);
+      __syncthreads();
+    }
     attend<BfOps>(src, st, lds, Q, query_mean(Q, a.mu + (size_t)h * kHeadDim, hh), c0, c1, live);
   }
 
@@ -599,7 +622,10 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
       for (int q = 0; q < 4; ++q) {
         uint32_t y[4];
 #pragma unroll
-        for (int v = 0; v < 4; ++v) y[v] = pack_bf16(st.O[2 * x][4 * q + v] * inv, st.O[2 * x + 1][4 * q + v] * inv);
+        for (int v = 0; v < 4; ++v) {
+          y[v] = pack_bf16(st.O[2 * x][4 * q + v] * inv, st.O[2 * x + 1][4 * q + v] * inv);
+          if (TREE && absent) y[v] = 0;
+        }
         *reinterpret_cast<uint4*>(o + 64 * x + 16 * q) = make_uint4(y[0], y[1], y[2], y[3]);
       }
   } else {
@@ -616,13 +642,14 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
         d[0] = make_float4(e[4 * q], f[4 * q], e[4 * q + 1], f[4 * q + 1]);
         d[1] = make_float4(e[4 * q + 2], f[4 * q + 2], e[4 * q + 3], f[4 * q + 3]);
       }
-    if (hh == 0) reinterpret_cast<float2*>(part + (size_t)a.bm * kHeadDim)[rt] = make_float2(st.thr < 0.0f ? kNone : st.m, all);
+    if (hh == 0) reinterpret_cast<float2*>(part + (size_t)a.bm * kHeadDim)[rt] = make_float2(TREE && absent ? kAbsent : st.thr < 0.0f ? kNone : st.m, all);
   }
 }
 
 // Block (tile, KV head, 16 rows): thread (row, eight channels) joins the tile's pieces in order, in one pass with the running
 // maximum. Bound by latency, so nothing waits for what it need not: the tile is read beside the number of tiles (its place
 // exists whether or not it was cut), and four pieces at a time are on their way.
+template <bool TREE>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
   const int t = blockIdx.x, h = blockIdx.y, H = a.cv.num_kv_heads, T = a.head[1];
   const ChunkTile tile = a.tiles[t];
@@ -661,6 +688,11 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
       o[6] = __builtin_fmaf(v[i].z, f, o[6]), o[7] = __builtin_fmaf(v[i].w, f, o[7]);
     }
   }
+  if (TREE && top >= kAbsent) {  // whatever the other pieces hold
+    all = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) o[j] = 0.0f;
+  }
   const float inv = all == 0.0f ? 0.0f : 1.0f / all;
   const int tok = quotient(row, a.gq);
   uint16_t* out = a.out + ((size_t)(tile.start + tok) * a.Hq + h * a.gq + row - tok * a.gq) * kHeadDim + c;
@@ -671,7 +703,7 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
 namespace {
 
 // The plan with kernel `waves` (1: few rows)
-ChunkPlan plan_with(int waves, int B, int H, long long seq_rows, long long rows, int max_q, int max_ctx) {
+ChunkPlan plan_with(int waves, int B, int H, long long seq_rows, long long rows, int max_own, int max_ctx) {
   ChunkPlan p{};
   p.waves = waves;
   p.bm = 32 * p.waves;
@@ -685,7 +717,7 @@ ChunkPlan plan_with(int waves, int B, int H, long long seq_rows, long long rows,
   p.max_tiles = (int)(tiles < 1 ? 1 : tiles);
   // pieces a KV head where tiles are cut: a place on the chip each while the tiles have one, else up to three; never more than
   // the units allow
-  const long long most = ((long long)max_ctx + 63) / 64 + ((long long)max_q + 63) / 64, cuts = (most + p.min_piece - 1) / p.min_piece;
+  const long long most = ((long long)max_ctx + 63) / 64 + ((long long)max_own + 63) / 64, cuts = (most + p.min_piece - 1) / p.min_piece;
   const long long places = (tiles * H <= p.resident ? 1LL : 3LL) * p.resident / H;
   long long cut = places < p.max_tiles * cuts ? places : p.max_tiles * cuts;
   p.max_slots = (int)(cut > 1 ? cut : 1);
@@ -705,7 +737,7 @@ ChunkPlan plan_with(int waves, int B, int H, long long seq_rows, long long rows,
 
 }  // namespace
 
-ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx) {
+ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_own, int max_ctx) {
   const int gq = Hq / H;
   const long long seq_rows = (long long)max_q * gq, rows = (long long)total_q * gq;
   // The kernel of few rows makes the operands again for every 32 rows, which takes 1.5 of the four waves' time a row. It takes
@@ -721,11 +753,11 @@ ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_
   const long long tiles4 = B * ((seq_rows + 127) / 128), rows4 = rows / 128 + B;
   const bool placed = (tiles4 < rows4 ? tiles4 : rows4) * H <= 2LL * num_cus();
   const int waves = seq_rows <= 64 || 3 * filled(32) < 2 * filled(128) ? 1 : seq_rows <= 128 || 11 * filled(128) < 10 * filled(256) || (max_ctx == 0 && placed) ? 4 : 8;
-  ChunkPlan p = plan_with(waves, B, H, seq_rows, rows, max_q, max_ctx);
+  ChunkPlan p = plan_with(waves, B, H, seq_rows, rows, max_own, max_ctx);
   // a workspace for these bounds is enough for every call within them, whichever kernel that takes
   for (int other : {1, 4, 8})
     if (other == 1 || seq_rows > 16 * other) {
-      const size_t need = plan_with(other, B, H, seq_rows, rows, max_q, max_ctx).total;
+      const size_t need = plan_with(other, B, H, seq_rows, rows, max_own, max_ctx).total;
       p.total = p.total < need ? need : p.total;
     }
   return p;
@@ -733,11 +765,33 @@ ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_
 
 namespace {
 
-template <int NG, int NW>
+template <int NG, int NW, bool TREE>
 hipError_t launch_attn(const ChunkArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((chunk_attn_kernel<NG, NW>), dim3((unsigned)((long long)a.max_items * a.cv.num_kv_heads)), dim3(64 * NW), 0,
+  hipLaunchKernelGGL((chunk_attn_kernel<NG, NW, TREE>), dim3((unsigned)((long long)a.max_items * a.cv.num_kv_heads)), dim3(64 * NW), 0,
                      s, a);
   return hipGetLastError();
+}
+
+template <bool TREE>
+hipError_t launch_pieces(const ChunkArgs& a, const ChunkPlan& p, hipStream_t s) {
+  hipError_t e = hipSuccess;
+  if (a.B > kChunkWaveSeqs) {
+    hipLaunchKernelGGL(chunk_plan_kernel<TREE>, dim3(1), dim3(kPlanThreads), 0, s, a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (p.waves == 1)
+    e = launch_chunk_few(a, s);
+  else if (a.cv.groups == 4)
+    e = p.waves == 8 ? launch_attn<4, 8, TREE>(a, s) : launch_attn<4, 4, TREE>(a, s);
+  else
+    e = p.waves == 8 ? launch_attn<1, 8, TREE>(a, s) : launch_attn<1, 4, TREE>(a, s);
+  if (e != hipSuccess) return e;
+  if (p.max_slots > 1) {
+    hipLaunchKernelGGL(chunk_merge_kernel<TREE>, dim3(p.max_tiles, a.cv.num_kv_heads, p.bm / 16), dim3(256), 0, s, a);
+    e = hipGetLastError();
+  }
+  return e;
 }
 
 }  // namespace
@@ -758,25 +812,7 @@ hipError_t launch_chunk_attention(ChunkArgs a, const ChunkPlan& p, uint8_t* ws, 
   a.tile_start = reinterpret_cast<int32_t*>(ws + p.off_starts);
   a.tiles = reinterpret_cast<ChunkTile*>(ws + p.off_tiles);
   a.part = reinterpret_cast<float*>(ws + p.off_part);
-  const int H = a.cv.num_kv_heads;
-  hipError_t e = hipSuccess;
-  if (a.B > kChunkWaveSeqs) {
-    hipLaunchKernelGGL(chunk_plan_kernel, dim3(1), dim3(kPlanThreads), 0, s, a);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  if (p.waves == 1)
-    e = launch_chunk_few(a, s);
-  else if (a.cv.groups == 4)
-    e = p.waves == 8 ? launch_attn<4, 8>(a, s) : launch_attn<4, 4>(a, s);
-  else
-    e = p.waves == 8 ? launch_attn<1, 8>(a, s) : launch_attn<1, 4>(a, s);
-  if (e != hipSuccess) return e;
-  if (p.max_slots > 1) {
-    hipLaunchKernelGGL(chunk_merge_kernel, dim3(p.max_tiles, H, p.bm / 16), dim3(256), 0, s, a);
-    e = hipGetLastError();
-  }
-  return e;
+  return a.parents ? launch_pieces<true>(a, p, s) : launch_pieces<false>(a, p, s);
 }
 
 }  // namespace int2kv

@@ -39,8 +39,17 @@ __device__ __forceinline__ int quotient(int x, int d) {
 struct Seq {
   int start, n, ctx;
   int past;  // cached tokens before the first new one where the cache holds both, by the whole sequence and its whole length
-             // (n and ctx are cut to max_q, max_ctx and the table); negative where the length does not hold the sequence
+             // (n and ctx are cut to max_q, max_ctx and the table); negative where the length does not hold the sequence.
+             // TREE: the tree's tokens before the first new one, by the same rule
 };
+struct Tree {  // rows of a sequence's tree in k_new and v_new
+  int start, count;
+};
+__device__ __forceinline__ Tree tree_of(const ChunkArgs& a, int b) {
+  const int start = min(max(a.tree_starts[b], 0), a.total_tree), end = min(max(a.tree_starts[b + 1], 0), a.total_tree);
+  return Tree{start, max(end - start, 0)};
+}
+template <bool TREE>
 __device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int b) {
   Seq s;
   s.start = min(max(a.starts[b], 0), a.total_q);
@@ -49,7 +58,7 @@ __device__ __forceinline__ Seq seq_of(const ChunkArgs& a, int b) {
   s.n = min(count, a.max_q);
   const long long room = (long long)a.max_blocks * kBlock;
   s.ctx = min(len, (int)(room < a.max_ctx ? room : a.max_ctx));
-  s.past = len - count;
+  s.past = (TREE ? tree_of(a, b).count : len) - count;
   return s;
 }
 // Cached tokens that new token i sees (not above zero: none)
@@ -59,7 +68,14 @@ __device__ __forceinline__ int int2_units(const ChunkArgs& a, const Seq& s, int 
   const int lim = a.own ? s.ctx : max(0, min(s.ctx, s.past + i + 1));
   return (lim + kUnit - 1) / kUnit;
 }
-__device__ __forceinline__ int own_units(const ChunkArgs& a, int i) { return a.own ? i / kUnit + 1 : 0; }
+template <bool TREE>
+__device__ __forceinline__ int own_units(const ChunkArgs& a, const Seq& s, int i) {
+  if constexpr (TREE) {
+    const int t = min(s.past + i, a.max_tree - 1);
+    return t < 0 ? 0 : t / kUnit + 1;
+  }
+  return a.own ? i / kUnit + 1 : 0;
+}
 
 // ---- The plan. A sequence's rows are tiles of bm; a tile is cut into equal pieces of at most about L units, by its own units
 // where the tiles leave places on the chip free (up to 64 of them), else all tiles of a sequence like its longest; a
@@ -69,15 +85,17 @@ __device__ __forceinline__ int own_units(const ChunkArgs& a, int i) { return a.o
 struct Load {  // of one sequence: row tiles, and units of the last one; or of one tile
   int tiles, units;
 };
+template <bool TREE>
 __device__ __forceinline__ Load load_of(const ChunkArgs& a, const Seq& s) {
   const int rows = s.n * a.gq;
   if (rows == 0) return Load{0, 0};
-  return Load{quotient(rows + a.bm - 1, a.bm), int2_units(a, s, s.n - 1) + own_units(a, s.n - 1)};
+  return Load{quotient(rows + a.bm - 1, a.bm), int2_units(a, s, s.n - 1) + own_units<TREE>(a, s, s.n - 1)};
 }
 // Units of the tile of rows row0 ..
+template <bool TREE>
 __device__ __forceinline__ int tile_units(const ChunkArgs& a, const Seq& s, int row0) {
   const int i = quotient(max(min(row0 + a.bm, s.n * a.gq) - 1, 0), a.gq);
-  return int2_units(a, s, i) + own_units(a, i);
+  return int2_units(a, s, i) + own_units<TREE>(a, s, i);
 }
 constexpr int kCuts = 16;
 // Candidate k: units of a piece. The first leaves the tiles whole; the others lie above the size that would fill the places
@@ -159,6 +177,7 @@ __device__ __forceinline__ int rank_of(const ChunkArgs& a, int at, int total) {
 }
 // The piece of work-group `at`, found by every wave for itself: the sequences with the longest pieces come first, and of a
 // sequence the last tiles, under a causal mask its longest. Writes the record of a cut tile for the merge (first piece, head 0).
+template <bool TREE>
 __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
   const int lane = threadIdx.x & 63;
   Place p;
@@ -168,8 +187,8 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
   // (expected, so that this path's code comes first: behind the other's it cost long chunks 0.6 %)
   if (__builtin_expect(a.B <= kChunkWaveSeqs, 1)) {
     Seq s{0, 0, 0, 0};
-    if (lane < a.B) s = seq_of(a, lane);
-    load = load_of(a, s);
+    if (lane < a.B) s = seq_of<TREE>(a, lane);
+    load = load_of<TREE>(a, s);
     int tiles = wave_scan(load.tiles), lane_b = lane, lane_row = 0;
     const int T = __builtin_amdgcn_readlane(tiles, 63);
     const float places = places_of(a);
@@ -184,7 +203,7 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
       }
       const Seq q{0, __shfl(s.n, lane_b), __shfl(s.ctx, lane_b), __shfl(s.past, lane_b)};
       lane_row = (lane - __shfl(tiles - load.tiles, lane_b)) * a.bm;
-      load = lane < T ? Load{1, tile_units(a, q, lane_row)} : Load{0, 0};
+      load = lane < T ? Load{1, tile_units<TREE>(a, q, lane_row)} : Load{0, 0};
       tiles = min(lane + 1, T);
     }
     const int umax = wave_fold(load.units, [](int x, int y) { return max(x, y); });
@@ -243,14 +262,14 @@ __device__ __forceinline__ Place locate(const ChunkArgs& a, int at, int h) {
     first = a.item_start[lo];
     local = r - first;
     tile0 = a.tile_start[b];
-    p.s = seq_of(a, b);
-    load = load_of(a, p.s);
+    p.s = seq_of<TREE>(a, b);
+    load = load_of<TREE>(a, p.s);
     pieces = pieces_of(load.units, a.head[2]);
   }
   const int back = quotient(local, pieces), t = load.tiles - 1 - back, piece = local - back * pieces;
   p.b = b;
   p.row0 = row + t * a.bm;
-  const int units = tile_units(a, p.s, p.row0);
+  const int units = tile_units<TREE>(a, p.s, p.row0);
   const int each = quotient(units, pieces), more = units - each * pieces;  // the first `more` pieces have one more
   p.u0 = each * piece + min(piece, more);
   p.u1 = p.u0 + each + (piece < more ? 1 : 0);
@@ -396,6 +415,43 @@ __device__ __forceinline__ float query_mean(const cd_b8_t (&Q)[8], const float* 
 // position 16 (u / 2) + 8 h + 4 (u % 2) + v, so that registers 8 x .. 8 x + 7 are operand 2 i + x as it is used.
 __device__ __forceinline__ int pos_channel(int pos) { return code_channel(pos >> 4, (pos >> 3) & 1, pos & 7); }
 __device__ __forceinline__ int row_position(int m) { return (m & 3) | ((m & 4) << 1) | ((m & 8) >> 1) | (m & 16); }
+
+// ---- Trees: a token sees the tokens on its path, itself, its parent and so on to one whose parent is -1
+constexpr float kAbsent = 1.0e30f;  // running maximum of a partial whose row has no path: nothing else counts beside it
+typedef uint32_t path_t __attribute__((ext_vector_type(kTreeMost / 32)));  // bit t % 32 of word t / 32: token t lies on it
+// The path of token t of a tree whose parents lie in LDS; nothing on it for a token that has none. A parent outside [-1, t)
+// ends a walk that way, so each takes at most kTreeMost steps.
+__device__ __forceinline__ path_t path_of(const int32_t* parents, int t, int count) {
+  path_t p = 0;
+  bool any = t >= 0 && t < count;
+  int x = any ? t : -1;
+  while (__any(x >= 0)) {
+    const int next = parents[max(x, 0)];
+#pragma unroll
+    for (int i = 0; i < kTreeMost / 32; ++i) p[i] |= x >> 5 == i ? 1u << (x & 31) : 0u;
+    const bool good = next >= -1 && next < x;
+    any = any && (x < 0 || good);
+    x = good ? next : -1;
+  }
+  const path_t none = 0;
+  return any ? p : none;
+}
+__device__ __forceinline__ bool has_path(const path_t& p) {
+  uint32_t x = 0;
+#pragma unroll
+  for (int i = 0; i < kTreeMost / 32; ++i) x |= p[i];
+  return x != 0;
+}
+// Word i (the same in every lane)
+__device__ __forceinline__ uint32_t path_word(const path_t& p, int i) {
+  uint32_t x = p[0];
+#pragma unroll
+  for (int j = 1; j < kTreeMost / 32; ++j) {
+    const uint32_t y = p[j];
+    x = i == j ? y : x;
+  }
+  return x;
+}
 
 // An operand with all but element j of the lanes that hold token t of a page cleared
 __device__ __forceinline__ cd_u4_t only_token(cd_u4_t x, int t) {

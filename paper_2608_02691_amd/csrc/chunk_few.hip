@@ -28,13 +28,16 @@ struct FewLds {
   cd_h8_t b[8][64];                       // the rotated queries, then the sums, as operands
   float ml[kFewWaves][3][32];             // the rows' m, sum and largest element
 };
+struct TreeLds : FewLds {
+  int32_t parents[kTreeMost];
+};
 
 }  // namespace
 
-template <int NG>
+template <int NG, bool TREE>
 __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs a) {
   using Lay = Rec<NG>;
-  __shared__ __align__(16) FewLds lds;
+  __shared__ __align__(16) typename std::conditional<TREE, TreeLds, FewLds>::type lds;
   const int H = a.cv.num_kv_heads;
   const int at = quotient((int)blockIdx.x, H), h = (int)blockIdx.x - at * H;
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), n = l & 31, hh = l >> 5;
@@ -46,12 +49,23 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
 #pragma unroll
       for (int j = 0; j < 8; ++j) rk[kk][j] = R[(size_t)(16 * kk + j) * kHeadDim];
   }
-  const Place place = locate(a, at, h);
+  const Place place = locate<TREE>(a, at, h);
   if (!place.valid) return;
   const Seq seq = place.s;
   const int rows = seq.n * a.gq, row = place.row0 + n, rc = min(row, rows - 1), tok = quotient(rc, a.gq), tok_tile = quotient(place.row0, a.gq);
   const int nI = int2_units(a, seq, quotient(min(place.row0 + a.bm, rows) - 1, a.gq));
   const int lim = limit_of(a, seq, tok), lim_tile = limit_of(a, seq, tok_tile);  // tokens the row sees, the least of the tile's
+
+  // Trees: the rows of the sequence's tree in k_new, and a row of a token without a path, which sees nothing
+  Tree tree{0, 0};
+  bool absent = false;
+  if constexpr (TREE) {
+    static_assert(kTreeMost == 64 * kFewWaves, "a parent a thread");
+    tree = tree_of(a, place.b);
+    tree.count = min(tree.count, a.max_tree);
+    absent = seq.past + tok < 0 || seq.past + tok >= tree.count;
+    if (place.u1 > nI && (int)threadIdx.x < tree.count) lds.parents[threadIdx.x] = a.parents[tree.start + threadIdx.x];
+  }
 
   // the row's query: channels 16 kk + 8 hh .. of operand kk (read again for the chunk's own tokens)
   const uint16_t* q = a.q + (seq.start + tok) * a.q_stride + (size_t)(h * a.gq + rc - tok * a.gq) * kHeadDim + 8 * hh;
@@ -337,11 +351,19 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
     cd_b8_t Qb[8];
     query(Qb);
     float base = kBias - m - query_mean(Qb, a.mu + (size_t)h * kHeadDim, hh);
-    const uint16_t* kb = a.k_new + seq.start * a.k_stride + (size_t)h * kHeadDim + 8 * hh;
-    const uint16_t* vb = a.v_new + seq.start * a.v_stride + (size_t)h * kHeadDim + ch;
-    const int last = quotient(min(place.row0 + a.bm, rows) - 1, a.gq);  // the tile's last token
+    const int own0 = TREE ? tree.start : seq.start, own_n = TREE ? tree.count : seq.n;
+    const uint16_t* kb = a.k_new + own0 * a.k_stride + (size_t)h * kHeadDim + 8 * hh;
+    const uint16_t* vb = a.v_new + own0 * a.v_stride + (size_t)h * kHeadDim + ch;
+    const int last_row = quotient(min(place.row0 + a.bm, rows) - 1, a.gq);  // the tile's last token
+    const int last = TREE ? min(seq.past + last_row, own_n - 1) : last_row;
+    path_t path = 0;
+    if constexpr (TREE) {
+      path = path_of(lds.parents, seq.past + tok, tree.count);
+      absent = !has_path(path);
+    }
     for (int s = c0 * (kUnit / kStep); s < c1 * (kUnit / kStep) && kStep * s <= last; ++s) {
-      const uint16_t* kr = kb + min(kStep * s + (n & 16) + row_token(n & 15), seq.n - 1) * a.k_stride;
+      const uint32_t seen = TREE ? path_word(path, s) : 0;
+      const uint16_t* kr = kb + min(kStep * s + (n & 16) + row_token(n & 15), own_n - 1) * a.k_stride;
       cd_h8_t k[8];
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) k[kk] = *reinterpret_cast<const cd_h8_t*>(kr + 16 * kk);
@@ -349,12 +371,15 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
 #pragma unroll
       for (int pg = 0; pg < 2; ++pg)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[pg][j] = vb[min(kStep * s + kBlock * pg + 8 * hh + j, seq.n - 1) * a.v_stride];
+        for (int j = 0; j < 8; ++j) v[pg][j] = vb[min(kStep * s + kBlock * pg + 8 * hh + j, own_n - 1) * a.v_stride];
       cd_f16_t S[1] = {splat16(0.0f)};
 #pragma unroll
       for (int kk = 0; kk < 8; ++kk) S[0] = BfOps::mfma(k[kk], Qb[kk], S[0]);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) S[0][i] = kStep * s + reg_token(i) + 8 * hh <= tok ? S[0][i] : -INFINITY;
+      for (int i = 0; i < 16; ++i) {
+        const int t = reg_token(i) + 8 * hh;
+        S[0][i] = (TREE ? (seen >> t) & 1 : kStep * s + t <= tok) ? S[0][i] : -INFINITY;
+      }
       settle<BfOps>(S, base, m, sum, thr, O);
       cd_u4_t P[2];
       soften<BfOps>(S[0], base, sum, P);
@@ -365,7 +390,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
 #pragma unroll
         for (int x = 0; x < 4; ++x) {
           const int t = kStep * s + kBlock * pg + 8 * hh + 2 * x;
-          const uint32_t pair = (t < seq.n ? v[pg][2 * x] : 0u) | (t + 1 < seq.n ? v[pg][2 * x + 1] << 16 : 0u), odd = BfOps::odd(pair);
+          const uint32_t pair = (t < own_n ? v[pg][2 * x] : 0u) | (t + 1 < own_n ? v[pg][2 * x + 1] << 16 : 0u), odd = BfOps::odd(pair);
           found |= odd;
           y[pg][x] = pair & ~odd;
           z[pg][x] = pair & odd;
@@ -374,7 +399,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
       for (int pg = 0; pg < 2; ++pg) O[0] = BfOps::mfma(__builtin_bit_cast(cd_h8_t, y[pg]), __builtin_bit_cast(cd_b8_t, P[pg]), O[0]);
       if (__any(found != 0)) {
         for (int t = 0; t < kStep; ++t) {
-          const bool see = kStep * s + t <= tok;
+          const bool see = TREE ? (seen >> t) & 1 : kStep * s + t <= tok;
           const cd_u4_t p = only_token(t < 16 ? P[0] : P[1], t), x = only_token(t < 16 ? z[0] : z[1], t);
           const cd_f16_t d = BfOps::mfma(__builtin_bit_cast(cd_h8_t, x), __builtin_bit_cast(cd_b8_t, p), splat16(0.0f));
 #pragma unroll
@@ -394,7 +419,10 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
     for (int x = 0; x < 2; ++x) {
       uint32_t y[4];
 #pragma unroll
-      for (int v = 0; v < 4; ++v) y[v] = pack_bf16(O[0][8 * x + 2 * v] * inv, O[0][8 * x + 2 * v + 1] * inv);
+      for (int v = 0; v < 4; ++v) {
+        y[v] = pack_bf16(O[0][8 * x + 2 * v] * inv, O[0][8 * x + 2 * v + 1] * inv);
+        if (TREE && absent) y[v] = 0;
+      }
       *reinterpret_cast<uint4*>(o + 16 * x) = make_uint4(y[0], y[1], y[2], y[3]);
     }
   } else {
@@ -406,17 +434,23 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
       d[0] = make_float4(O[0][8 * x], O[0][8 * x + 1], O[0][8 * x + 2], O[0][8 * x + 3]);
       d[1] = make_float4(O[0][8 * x + 4], O[0][8 * x + 5], O[0][8 * x + 6], O[0][8 * x + 7]);
     }
-    if (w == 0 && hh == 0) reinterpret_cast<float2*>(part + (size_t)a.bm * kHeadDim)[n] = make_float2(thr < 0.0f ? kNone : m, all);
+    if (w == 0 && hh == 0) reinterpret_cast<float2*>(part + (size_t)a.bm * kHeadDim)[n] = make_float2(TREE && absent ? kAbsent : thr < 0.0f ? kNone : m, all);
   }
 }
 
-hipError_t launch_chunk_few(const ChunkArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((long long)a.max_items * a.cv.num_kv_heads));
-  if (a.cv.groups == 4)
-    hipLaunchKernelGGL((chunk_few_kernel<4>), grid, dim3(64 * kFewWaves), 0, s, a);
-  else
-    hipLaunchKernelGGL((chunk_few_kernel<1>), grid, dim3(64 * kFewWaves), 0, s, a);
+namespace {
+
+template <int NG, bool TREE>
+hipError_t launch_few(const ChunkArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((chunk_few_kernel<NG, TREE>), dim3((unsigned)((long long)a.max_items * a.cv.num_kv_heads)), dim3(64 * kFewWaves), 0, s, a);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_chunk_few(const ChunkArgs& a, hipStream_t s) {
+  if (a.parents) return a.cv.groups == 4 ? launch_few<4, true>(a, s) : launch_few<1, true>(a, s);
+  return a.cv.groups == 4 ? launch_few<4, false>(a, s) : launch_few<1, false>(a, s);
 }
 
 }  // namespace int2kv

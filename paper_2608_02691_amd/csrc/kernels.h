@@ -190,6 +190,7 @@ struct ChunkTile {  // a tile of query rows of one sequence that was cut (the sa
   int pieces, slot;    // pieces it is cut into, and the first one's partial
 };
 constexpr int kChunkPartStride = kHeadDim + 2;  // sums, then m and l
+constexpr int kTreeMost = 256;                  // tokens of a drafted tree
 constexpr int kChunkWaveSeqs = 64;              // up to so many sequences every work-group plans by itself
 struct ChunkArgs {
   CacheView cv;
@@ -207,6 +208,8 @@ struct ChunkArgs {
                                     // a prompt of 2,011 tokens 72 us, with the flag 69)
   const uint16_t *k_new, *v_new;
   const float* mu;
+  const int32_t *tree_starts, *parents;  // trees: offsets of their rows in k_new [B + 1], parents [total_tree]; or null
+  int total_tree, max_tree;
   uint16_t* out;                    // bf16 [total_q, Hq, 128]
   // plan and workspace
   int bm, resident, per_cu, min_piece, max_tiles, max_items, max_slots;
@@ -222,9 +225,71 @@ struct ChunkPlan {
   float piece_units, merge_units;
   size_t off_head, off_order, off_items, off_starts, off_tiles, off_part, total;
 };
-ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx);
+// max_own: tokens of a sequence whose keys and values are given beside the cache
+ChunkPlan make_chunk_plan(int B, int Hq, int H, int total_q, int max_q, int max_own, int max_ctx);
 hipError_t launch_chunk_few(const ChunkArgs& a, hipStream_t s);  // (chunk_few.hip) tiles of 32 rows
 hipError_t launch_chunk_attention(ChunkArgs a, const ChunkPlan& p, uint8_t* ws, hipStream_t s);
+
+// ---- attention weight that cached tokens receive (token_weights.hip)
+struct TokenWeightsArgs {
+  CacheView cv;
+  const uint16_t* q;                // bf16, token t, head j at t * q_stride + 128 j
+  int64_t q_stride;
+  const int32_t* starts;            // [B + 1]
+  int B, total_q, max_q, Hq, gq;
+  const int32_t* table;
+  int max_blocks;
+  const int32_t* lens;
+  int max_ctx;
+  const float* R_k;
+  const float* w_in;                // fp32 [B, H, w_stride] or null
+  float* w_out;
+  int64_t w_stride;
+  float decay;
+  // plan and workspace
+  int seq_tiles, ranges, slices, tiles;  // row tiles of a sequence at most; token ranges; slices of a sequence's row tiles; all tiles
+  uint8_t* ops;                     // [tiles, H] row operands
+  float* down;                      // [tiles, H] what brings their scores back to size
+  float2* stats;                    // [ranges, tiles, H, 32] maximum and sum of a row over a range
+  float* lse;                       // [tiles, H, 32]
+  float* part;                      // [slices, B, H, ranges * kRangeTokens] where slices > 1
+};
+struct TokenWeightsPlan {
+  int seq_tiles, ranges, slices, tiles;
+  size_t off_ops, off_down, off_stats, off_lse, off_part, total;
+};
+constexpr int kRangeTokens = 256;
+TokenWeightsPlan make_token_weights_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx);
+hipError_t launch_token_weights(TokenWeightsArgs a, const TokenWeightsPlan& p, uint8_t* ws, hipStream_t s);
+
+// ---- tokens that stay, and their rows' move (evict.hip)
+struct SelectArgs {
+  const float* weights;             // fp32 [B, H, stride]
+  int64_t stride;
+  const int32_t* lens;
+  int B, H, max_ctx, budget, sink, recent;
+  int32_t* kept;                    // [B, H, kept_stride]
+  int64_t kept_stride;
+  int32_t* kept_lens;               // [B]
+};
+hipError_t launch_select_tokens(const SelectArgs& a, hipStream_t s);
+struct MoveArgs {
+  CacheView cv;
+  const int32_t* table;
+  int max_blocks;
+  const int32_t* kept;              // [B, H, kept_stride]
+  int64_t kept_stride;
+  const int32_t* kept_lens;
+  int B, max_kept, pages;           // pages: of max_kept tokens
+  const int32_t* out_table;
+  int out_max_blocks;
+  const float* weights;             // fp32 [B, H, weights_stride] or null
+  float* out_weights;
+  int64_t weights_stride, out_weights_stride;
+  uint8_t* stage;                   // in place: [B, pages, H] records and weights
+};
+size_t move_stage_bytes(int groups);  // of a page of one KV head
+hipError_t launch_move_tokens(const MoveArgs& a, bool in_place, hipStream_t s);
 
 // ---- OptR offline calibration (optr.hip): fp64 throughout
 constexpr int kCalMaxLen = 4096;  // tokens per calibration sequence

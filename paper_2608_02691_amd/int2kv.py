@@ -48,8 +48,12 @@ EXPORTED = (
     "int2kv_output_error_workspace_bytes", "int2kv_output_error", "int2kv_quantize_append_rope",
     "int2kv_optr_workspace_bytes", "int2kv_optr_key_mean", "int2kv_optr_key_loss", "int2kv_optr_value_loss",
     "int2kv_optr_calibrate", "int2kv_rope_axes", "int2kv_read_rows", "int2kv_chunk_attention_workspace_bytes",
-    "int2kv_chunk_attention",
+    "int2kv_chunk_attention", "int2kv_tree_attention_workspace_bytes", "int2kv_tree_attention",
+    "int2kv_token_weights_workspace_bytes", "int2kv_token_weights", "int2kv_select_tokens",
+    "int2kv_move_tokens_workspace_bytes", "int2kv_move_tokens",
 )
+
+MAX_TREE = 256
 
 
 class _Cache(ctypes.Structure):
@@ -125,6 +129,14 @@ def load_library(path: str = LIB_PATH):
         "int2kv_chunk_attention_workspace_bytes": ([I, I, I, I, I, I], Z),
         "int2kv_chunk_attention": ([ctypes.POINTER(_Cache), P, L, P, I, I, I, I, P, I, P, I, P, P, P, L, P, L, P, P, P,
                                     Z, S], I),
+        "int2kv_tree_attention_workspace_bytes": ([I, I, I, I, I, I, I], Z),
+        "int2kv_tree_attention": ([ctypes.POINTER(_Cache), P, L, P, I, I, I, I, P, I, I, P, P, L, P, L, P, P, I, P, I, P, P,
+                                   P, P, Z, S], I),
+        "int2kv_token_weights_workspace_bytes": ([I, I, I, I, I, I], Z),
+        "int2kv_token_weights": ([ctypes.POINTER(_Cache), P, L, P, I, I, I, I, P, I, P, I, P, P, F, P, L, P, Z, S], I),
+        "int2kv_select_tokens": ([P, L, I, I, P, I, I, I, I, P, L, P, S], I),
+        "int2kv_move_tokens_workspace_bytes": ([I, I, I, I], Z),
+        "int2kv_move_tokens": ([ctypes.POINTER(_Cache), P, I, P, L, P, I, I, P, I, P, L, P, L, P, Z, S], I),
     }
     for name, (args, res) in sig.items():
         fn = getattr(lib, name)
@@ -676,6 +688,172 @@ def int2kv_chunk_attention(cache: Int2KVCache, q: torch.Tensor, q_starts: torch.
         workspace.numel(), _stream())
     _check(st, "int2kv_chunk_attention")
     return out
+
+
+def int2kv_tree_attention_workspace_bytes(batch: int, num_q_heads: int, num_kv_heads: int, total_q: int, max_q: int,
+                                          max_tree: int, max_ctx: int) -> int:
+    return load_library().int2kv_tree_attention_workspace_bytes(batch, num_q_heads, num_kv_heads, total_q, max_q, max_tree, max_ctx)
+
+
+def int2kv_tree_attention(cache: Int2KVCache, q: torch.Tensor, q_starts: torch.Tensor, max_q: int, parents: torch.Tensor,
+                          k_tree: torch.Tensor, v_tree: torch.Tensor, mu: torch.Tensor, block_table: torch.Tensor,
+                          ctx_lens: torch.Tensor, max_ctx: int, R_k: torch.Tensor, R_v: torch.Tensor,
+                          tree_starts: Optional[torch.Tensor] = None, max_tree: Optional[int] = None,
+                          out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of drafted trees' tokens over the cache's ctx_lens[b] tokens and their own paths. k_tree, v_tree bf16
+    [total_tree, H_kv, 128] and parents int32 [total_tree] are the trees' tokens (sequence b: rows tree_starts[b] ..
+    tree_starts[b + 1], by default those of q), q bf16 [total, H_q, 128] the last tokens of each tree; parents count within
+    a tree, -1: the token follows the cache, -2: the place is empty. q, k_tree, v_tree may be views whose tokens lie apart.
+    Returns bf16 [total, H_q, 128] (a new `out` is zero in rows outside every sequence)."""
+    total, Hq, H, B = q.shape[0], q.shape[1], cache.num_kv_heads, ctx_lens.numel()
+    if tree_starts is None:
+        tree_starts = q_starts
+        max_tree = max_q if max_tree is None else max_tree
+    elif max_tree is None:
+        raise ValueError("tree_starts needs max_tree")
+    if q_starts.numel() != B + 1 or tree_starts.numel() != B + 1:
+        raise ValueError("q_starts and tree_starts must hold batch + 1 offsets")
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [batch, max_blocks]")
+    for t, name in ((R_k, "R_k"), (R_v, "R_v")):
+        if t.shape != (H, HEAD_DIM, HEAD_DIM):
+            raise ValueError(f"{name} must be [num_kv_heads, 128, 128]")
+    if mu.shape != (H, HEAD_DIM):
+        raise ValueError("mu must be [num_kv_heads, 128]")
+    n_tree = parents.numel()
+    if k_tree.shape[0] != n_tree or v_tree.shape[0] != n_tree:
+        raise ValueError("parents, k_tree and v_tree must hold the same tokens")
+    _here(cache.pool, q, q_starts, tree_starts, parents, block_table, ctx_lens, R_k, R_v, k_tree, v_tree, mu, out, workspace)
+    qp, qs = _head_rows(q, Hq, "q")
+    kp, ks = _head_rows(k_tree, H, "k_tree")
+    vp, vs = _head_rows(v_tree, H, "v_tree")
+    if out is None:
+        out = torch.zeros((total, Hq, HEAD_DIM), dtype=torch.bfloat16, device=q.device)
+    elif out.shape != (total, Hq, HEAD_DIM):
+        raise ValueError("out must be [total, H_q, 128]")
+    if workspace is None:
+        need = int2kv_tree_attention_workspace_bytes(B, Hq, H, total, max_q, max_tree, max_ctx)
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+    st = load_library().int2kv_tree_attention(
+        cache.desc, qp, qs, _ptr(q_starts, _I32, "q_starts"), B, total, max_q, Hq, _ptr(tree_starts, _I32, "tree_starts"), n_tree,
+        max_tree, _ptr(parents, _I32, "parents"), kp, ks, vp, vs, _ptr(mu, _F32, "mu"), _ptr(block_table, _I32, "block_table"),
+        block_table.shape[1], _ptr(ctx_lens, _I32, "ctx_lens"), max_ctx, _ptr(R_k, _F32, "R_k"), _ptr(R_v, _F32, "R_v"),
+        _ptr(out, _BF16, "out"), _ptr(workspace, (torch.uint8,), "workspace"), workspace.numel(), _stream())
+    _check(st, "int2kv_tree_attention")
+    return out
+
+
+# ---------------------------------------------------------------------------------------------
+# Eviction: the weight that tokens receive, those that stay, their move
+def _lists(t: torch.Tensor, dtypes, batch: int, heads: int, least: int, name: str):
+    """(pointer, elements between lists) of [batch, heads, n] lists, n at least `least`."""
+    if t.dim() != 3 or t.shape[0] != batch or t.shape[1] != heads or t.shape[2] < least:
+        raise ValueError(f"{name} must be [batch, num_kv_heads, at least {least}]")
+    return _ptr(t, dtypes, name), t.shape[2]
+
+
+def int2kv_token_weights_workspace_bytes(batch: int, num_q_heads: int, num_kv_heads: int, total_q: int, max_q: int,
+                                         max_ctx: int) -> int:
+    return load_library().int2kv_token_weights_workspace_bytes(batch, num_q_heads, num_kv_heads, total_q, max_q, max_ctx)
+
+
+def int2kv_token_weights(cache: Int2KVCache, q: torch.Tensor, q_starts: torch.Tensor, max_q: int, block_table: torch.Tensor,
+                         ctx_lens: torch.Tensor, max_ctx: int, R_k: torch.Tensor, weights: Optional[torch.Tensor] = None,
+                         decay: float = 1.0, out: Optional[torch.Tensor] = None,
+                         workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """decay * weights plus the attention weight that each cached token receives from the queries q bf16 [total, H_q, 128],
+    the last tokens of every sequence (in the cache already), summed over them and the KV head's query heads. Returns fp32
+    [batch, H_kv, n], n at least max_ctx (a new `out`: max_ctx, or as `weights`; zeros behind the lengths); `out` may be
+    `weights`."""
+    total, Hq, H, B = q.shape[0], q.shape[1], cache.num_kv_heads, ctx_lens.numel()
+    if q_starts.numel() != B + 1:
+        raise ValueError("q_starts must hold batch + 1 offsets")
+    if block_table.dim() != 2 or block_table.shape[0] != B:
+        raise ValueError("block_table must be [batch, max_blocks]")
+    if R_k.shape != (H, HEAD_DIM, HEAD_DIM):
+        raise ValueError("R_k must be [num_kv_heads, 128, 128]")
+    _here(cache.pool, q, q_starts, block_table, ctx_lens, R_k, weights, out, workspace)
+    if out is None:
+        out = torch.zeros((B, H, max_ctx if weights is None else weights.shape[-1]), dtype=torch.float32, device=q.device)
+    op, stride = _lists(out, _F32, B, H, max_ctx, "out")
+    wp = None
+    if weights is not None:
+        wp, w_stride = _lists(weights, _F32, B, H, max_ctx, "weights")
+        if w_stride != stride:
+            raise ValueError("weights and out must have one shape")
+    qp, qs = _head_rows(q, Hq, "q")
+    if workspace is None:
+        need = int2kv_token_weights_workspace_bytes(B, Hq, H, total, max_q, max_ctx)
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=q.device)
+    st = load_library().int2kv_token_weights(
+        cache.desc, qp, qs, _ptr(q_starts, _I32, "q_starts"), B, total, max_q, Hq, _ptr(block_table, _I32, "block_table"),
+        block_table.shape[1], _ptr(ctx_lens, _I32, "ctx_lens"), max_ctx, _ptr(R_k, _F32, "R_k"), wp, decay, op, stride,
+        _ptr(workspace, (torch.uint8,), "workspace"), workspace.numel(), _stream())
+    _check(st, "int2kv_token_weights")
+    return out
+
+
+def int2kv_select_tokens(weights: torch.Tensor, ctx_lens: torch.Tensor, max_ctx: int, budget: int, sink: int = 0, recent: int = 0,
+                         kept: Optional[torch.Tensor] = None, kept_lens: Optional[torch.Tensor] = None):
+    """(kept int32 [batch, H_kv, n], kept_lens int32 [batch]): the tokens of each sequence and KV head that stay, ascending:
+    the first `sink`, the last `recent`, and the largest weights (fp32 [batch, H_kv, at least max_ctx]) of the others, up to
+    `budget`. Entries behind kept_lens[b] are left as they were (-1 in a new `kept`)."""
+    if weights.dim() != 3:
+        raise ValueError("weights must be [batch, num_kv_heads, at least max_ctx]")
+    B, H = weights.shape[0], weights.shape[1]
+    if ctx_lens.numel() != B:
+        raise ValueError("ctx_lens must be [batch]")
+    _here(weights, ctx_lens, kept, kept_lens)
+    wp, ws = _lists(weights, _F32, B, H, max_ctx, "weights")
+    most = max(0, min(budget, max_ctx))
+    if kept is None:
+        kept = torch.full((B, H, most), -1, dtype=torch.int32, device=weights.device)
+    if kept_lens is None:
+        kept_lens = torch.zeros(B, dtype=torch.int32, device=weights.device)
+    elif kept_lens.numel() != B:
+        raise ValueError("kept_lens must be [batch]")
+    kp, ks = _lists(kept, _I32, B, H, most, "kept")
+    st = load_library().int2kv_select_tokens(wp, ws, B, H, _ptr(ctx_lens, _I32, "ctx_lens"), max_ctx, budget, sink, recent, kp, ks,
+                                             _ptr(kept_lens, _I32, "kept_lens"), _stream())
+    _check(st, "int2kv_select_tokens")
+    return kept, kept_lens
+
+
+def int2kv_move_tokens_workspace_bytes(batch: int, num_kv_heads: int, group_size: int, max_kept: int) -> int:
+    return load_library().int2kv_move_tokens_workspace_bytes(batch, num_kv_heads, group_size, max_kept)
+
+
+def int2kv_move_tokens(cache: Int2KVCache, block_table: torch.Tensor, kept: torch.Tensor, kept_lens: torch.Tensor, max_kept: int,
+                       out_table: Optional[torch.Tensor] = None, weights: Optional[torch.Tensor] = None,
+                       out_weights: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Writes the rows of the kept tokens to the front: token j of KV head h becomes the old token kept[b, h, j] (int32
+    [batch, H_kv, at least max_kept]), in the blocks of out_table, or without it in place. With weights fp32 [batch, H_kv, n],
+    theirs to out_weights (in place: by default weights themselves; else new, zeros behind kept_lens). Returns
+    out_weights."""
+    B, H = kept_lens.numel(), cache.num_kv_heads
+    for t, name in ((block_table, "block_table"), (out_table, "out_table")):
+        if t is not None and (t.dim() != 2 or t.shape[0] != B):
+            raise ValueError(f"{name} must be [batch, max_blocks]")
+    if out_weights is not None and weights is None:
+        raise ValueError("out_weights needs weights")
+    in_place = out_table is None or out_table.data_ptr() == block_table.data_ptr()
+    if weights is not None and out_weights is None:
+        out_weights = weights if in_place else torch.zeros((B, H, max_kept), dtype=torch.float32, device=weights.device)
+    _here(cache.pool, block_table, kept, kept_lens, out_table, weights, out_weights, workspace)
+    kp, ks = _lists(kept, _I32, B, H, max_kept, "kept")
+    wp, ws, op, os_ = None, 0, None, 0
+    if weights is not None:
+        wp, ws = _lists(weights, _F32, B, H, 1 if max_kept else 0, "weights")
+        op, os_ = _lists(out_weights, _F32, B, H, max_kept, "out_weights")
+    if in_place and workspace is None:
+        need = int2kv_move_tokens_workspace_bytes(B, H, cache.group_size, max_kept)
+        workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=cache.pool.device)
+    st = load_library().int2kv_move_tokens(
+        cache.desc, _ptr(block_table, _I32, "block_table"), block_table.shape[1], kp, ks, _ptr(kept_lens, _I32, "kept_lens"), B,
+        max_kept, _ptr(out_table, _I32, "out_table"), 0 if out_table is None else out_table.shape[1], wp, ws, op, os_,
+        _ptr(workspace, (torch.uint8,), "workspace"), 0 if workspace is None else workspace.numel(), _stream())
+    _check(st, "int2kv_move_tokens")
+    return out_weights
 
 
 # ---------------------------------------------------------------------------------------------
