@@ -137,7 +137,8 @@ class WeightsCall:
         (base 2), what the terms of its sum come to: a score is off by fewer than 16 roundings of partial sums of at most M,
         2^-24 each, and 2^-22 of the terms for the two-term queries, together below 2^-19 M; its row's log sum by as much and
         some roundings of its own size. A weight is then off by less than ln 2 (2^-18 M + 2^-21 |L|) of itself; sums over
-        rows and the decayed part add a few roundings: 2^-20 of the result's parts."""
+        rows and the decayed part add a few roundings: 2^-20 of the result's parts. fp32's normal numbers end at 2^-126: a
+        weight below that comes out as zero or as a multiple of 2^-149, off by at most 2^-126 a row that sees the token."""
         got, tol = np.zeros(self.shape), np.zeros(self.shape)
         q, ng = self.q.double().numpy(), D // self.group
         for b, (n, ctx) in enumerate(self.seqs):
@@ -170,7 +171,7 @@ class WeightsCall:
                     p = np.exp2(x - L)
                     worst = np.where(see, M, 0).max(1, keepdims=True)
                     got[b, h, :ctx] += p.sum(0)
-                    tol[b, h, :ctx] += (p * (2.0 ** -18 * worst + 2.0 ** -21 * np.abs(L) + 2.0 ** -20)).sum(0)
+                    tol[b, h, :ctx] += (p * (2.0 ** -18 * worst + 2.0 ** -21 * np.abs(L) + 2.0 ** -20)).sum(0) + 2.0 ** -126 * see.sum(0)
         return got, tol
 
     def _zeros(self, b, ctx, h):
