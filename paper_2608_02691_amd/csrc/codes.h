@@ -9,6 +9,7 @@ typedef _Float16 cd_h2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 cd_h8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 cd_b8_t __attribute__((ext_vector_type(8)));
 typedef float cd_f16_t __attribute__((ext_vector_type(16)));
+typedef float cd_f4_t __attribute__((ext_vector_type(4)));
 typedef uint32_t cd_u2_t __attribute__((ext_vector_type(2)));
 typedef uint32_t cd_u4_t __attribute__((ext_vector_type(4)));
 

@@ -253,10 +253,15 @@ struct TokenWeightsArgs {
   float2* stats;                    // [ranges, tiles, H, 32] maximum and sum of a row over a range
   float* lse;                       // [tiles, H, 32]
   float* part;                      // [slices, B, H, ranges * kRangeTokens] where slices > 1
+  // few rows a sequence (stats: [B, H, pieces, 8])
+  int pieces, page_cap, row_cap;    // pieces and pages of a sequence, rows of a KV head, each at most
+  uint8_t* few;                     // [B, H] row operands
+  float* scores;                    // [B, H, page_cap, row_cap, 16]
 };
 struct TokenWeightsPlan {
-  int seq_tiles, ranges, slices, tiles;
-  size_t off_ops, off_down, off_stats, off_lse, off_part, total;
+  bool few;
+  int seq_tiles, ranges, slices, tiles, pieces, page_cap, row_cap;
+  size_t off_ops, off_down, off_stats, off_lse, off_part, off_few, off_few_stats, off_scores, total;
 };
 constexpr int kRangeTokens = 256;
 TokenWeightsPlan make_token_weights_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx);

@@ -352,12 +352,238 @@ __global__ __launch_bounds__(256) void weight_join_kernel(TokenWeightsArgs a) {
   a.w_out[at] = a.w_in ? __builtin_fmaf(a.decay, a.w_in[at], sum) : sum;
 }
 
+// ---- Few rows a sequence (decode steps): up to kFewRows rows of one KV head. The scores are formed once and kept; the second
+// pass goes over them and not over the keys.
+namespace {
+
+constexpr int kFewRows = 8;
+constexpr int kPieceTokens = 512, kPiecePages = kPieceTokens / kBlock / 4;  // of a block; pages of each of its four waves
+constexpr int kJoinTokens = 1024;
+
+// The rows' operands for products of 16 rows x 16 tokens: row 4 j + g of tile t holds group g's channels of query row
+// 4 t + j and zeros elsewhere, so that D's registers are the four groups' sums of one query row and token. A lane's
+// eight channels (lane = 16 quad + 4 j + g): positions 2 g, 2 g + 1 of words 2 quad, 2 quad + 1.
+struct FewOps {
+  cd_h8_t term[2][2][64];  // [tile][high, low]
+  float sum[2][4][4];      // Q_g of [tile][row]
+  float down, pad[3];
+};
+
+__device__ __forceinline__ cd_f4_t product16(const cd_h8_t& x, const cd_h8_t& y, const cd_f4_t& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
+}
+
+}  // namespace
+
+// Block: one (sequence, KV head). Thread: channel c of every other row.
+__global__ __launch_bounds__(256) void weight_few_rows_kernel(TokenWeightsArgs a) {
+  __shared__ float q[kFewRows][kHeadDim], top[4];
+  const int H = a.cv.num_kv_heads, h = blockIdx.x % H, b = blockIdx.x / H, c = threadIdx.x & 127, odd = threadIdx.x >> 7;
+  const Span s = span_of(a, b);
+  const int rows = min(s.n * a.gq, kFewRows);
+  if (rows == 0 || s.ctx == 0) return;
+  for (int i = threadIdx.x; i < kFewRows * kHeadDim; i += 256) {
+    const int r = i >> 7, tok = r / a.gq;
+    q[r][i & 127] = r < rows ? bf16_bits_to_f32(a.q[(s.start + tok) * a.q_stride + (size_t)(h * a.gq + r - tok * a.gq) * kHeadDim + (i & 127)]) : 0.0f;
+  }
+  __syncthreads();
+  float d[kFewRows / 2] = {};
+  const float* R = a.R_k + (size_t)h * kHeadDim * kHeadDim + c;
+#pragma unroll 32
+  for (int k = 0; k < kHeadDim; ++k) {
+    const float x = R[(size_t)k * kHeadDim];
+#pragma unroll
+    for (int i = 0; i < kFewRows / 2; ++i) d[i] = __builtin_fmaf(q[2 * i + odd][k], x, d[i]);
+  }
+  float big = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kFewRows / 2; ++i) {
+    d[i] *= kLogit2;
+    big = fmaxf(big, fabsf(d[i]));
+  }
+#pragma unroll
+  for (int step = 32; step > 0; step >>= 1) big = fmaxf(big, __shfl_xor(big, step));
+  if ((threadIdx.x & 63) == 0) top[threadIdx.x >> 6] = big;
+  __syncthreads();
+  big = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
+  const uint32_t e = min(max(__float_as_uint(big) >> 23, 8u), 254u);
+  const float up = __uint_as_float((261u - e) << 23);
+  FewOps& out = reinterpret_cast<FewOps*>(a.few)[(size_t)b * H + h];
+  const int g = c >> 5, p = (c >> 4) & 1, word = (c & 15) >> 1, element = ((word & 1) << 2) | (p << 1) | (c & 1);
+#pragma unroll
+  for (int i = 0; i < kFewRows / 2; ++i) {
+    const int r = 2 * i + odd, lane = 16 * (word >> 1) + 4 * (r & 3) + g;
+    const float x = d[i] * up;
+    const _Float16 hi = (_Float16)x;
+    reinterpret_cast<_Float16*>(&out.term[r >> 2][0][lane])[element] = hi;
+    reinterpret_cast<_Float16*>(&out.term[r >> 2][1][lane])[element] = (_Float16)(x - (float)hi);
+    float sum = x;  // over the group: 32 lanes
+#pragma unroll
+    for (int step = 16; step > 0; step >>= 1) sum += __shfl_xor(sum, step);
+    if ((c & 31) == 0) out.sum[r >> 2][r & 3][g] = sum;
+  }
+  if (threadIdx.x == 0) out.down = __uint_as_float((e - 7u) << 23);
+}
+
+// Block: 512 tokens of one KV head, a wave eight pages of them; all loads of a wave are on their way at once. Lane: one token
+// of a page and one row of each tile. TILES: of four rows.
+template <int NG, int TILES>
+__global__ __launch_bounds__(256) void weight_few_scores_kernel(TokenWeightsArgs a) {
+  using Lay = Rec<NG>;
+  __shared__ float2 both[4][kFewRows];
+  const int H = a.cv.num_kv_heads, h = blockIdx.x % H, piece = blockIdx.x / H % a.pieces, b = blockIdx.x / H / a.pieces;
+  const Span s = span_of(a, b);
+  if (kPieceTokens * piece >= s.ctx || s.n == 0) return;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, t = l & 15, quad = l >> 4;
+  const int page0 = kPieceTokens / kBlock * piece + kPiecePages * w, pages = (s.ctx + kBlock - 1) / kBlock;
+  int id = -1;
+  if (l < kPiecePages && page0 + l < pages) id = a.table[(size_t)b * a.max_blocks + page0 + l];
+  const uint32_t real = (uint32_t)__ballot(id >= 0 && id < a.cv.num_blocks);
+  cd_u2_t code[kPiecePages];
+  uint32_t meta[kPiecePages][NG];
+#pragma unroll
+  for (int i = 0; i < kPiecePages; ++i) {
+    const int x = __builtin_amdgcn_readlane(id, i);
+    const uint8_t* rec = a.cv.pool + ((size_t)(uint32_t)((real >> i) & 1 ? x : 0) * H + h) * Lay::kBytes;
+    code[i] = *reinterpret_cast<const cd_u2_t*>(rec + kOffKCodes + 32 * t + 8 * quad);
+#pragma unroll
+    for (int g = 0; g < NG; ++g) meta[i][g] = reinterpret_cast<const uint32_t*>(rec + Lay::kOffKMeta + 4 * NG * t)[g];
+  }
+  const FewOps& ops = reinterpret_cast<const FewOps*>(a.few)[(size_t)b * H + h];
+  const float down = ops.down;
+  cd_h8_t A[TILES][2][4];  // [tile][high, low][group]
+  float Q[TILES][4];
+  int lim[TILES];
+  const cd_h8_t none{};
+#pragma unroll
+  for (int k = 0; k < TILES; ++k) {
+#pragma unroll
+    for (int x = 0; x < 2; ++x) {
+      const cd_h8_t y = ops.term[k][x][l];
+#pragma unroll
+      for (int g = 0; g < 4; ++g) A[k][x][g] = (l & 3) == g ? y : none;
+    }
+    const float4 v = *reinterpret_cast<const float4*>(ops.sum[k][quad]);
+    Q[k][0] = v.x * down, Q[k][1] = v.y * down, Q[k][2] = v.z * down, Q[k][3] = v.w * down;
+    const int row = 4 * k + quad;
+    lim[k] = row < s.n * a.gq ? s.limit(row / a.gq) : 0;
+  }
+  float m[TILES], sum[TILES];
+#pragma unroll
+  for (int k = 0; k < TILES; ++k) m[k] = kNone, sum[k] = 0.0f;
+  float* scores = a.scores + ((size_t)b * H + h) * a.page_cap * (kBlock * a.row_cap);
+#pragma unroll
+  for (int i = 0; i < kPiecePages; ++i) {
+    if (page0 + i >= pages) break;
+    cd_h8_t c[4];
+    const uint32_t u = code[i].x, v = code[i].y, uh = u >> 10, vh = v >> 10;
+    auto put = [&](cd_h8_t& y, cd_h2_t p, cd_h2_t q, cd_h2_t r, cd_h2_t z) { y = cd_h8_t{p.x, p.y, q.x, q.y, r.x, r.y, z.x, z.y}; };
+    put(c[0], land_position<0>(u, uh), land_position<1>(u, uh), land_position<0>(v, vh), land_position<1>(v, vh));
+    put(c[1], land_position<2>(u, uh), land_position<3>(u, uh), land_position<2>(v, vh), land_position<3>(v, vh));
+    put(c[2], land_position<4>(u, uh), land_position<5>(u, uh), land_position<4>(v, vh), land_position<5>(v, vh));
+    put(c[3], land_position<6>(u, uh), land_position<7>(u, uh), land_position<6>(v, vh), land_position<7>(v, vh));
+    const int token = kBlock * (page0 + i) + t;
+#pragma unroll
+    for (int k = 0; k < TILES; ++k) {
+      cd_f4_t D = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        D = product16(A[k][0][g], c[g], D);
+        D = product16(A[k][1][g], c[g], D);
+      }
+      float x = 0.0f;
+      if constexpr (NG == 4) {
+        float z = 0.0f;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          x = __builtin_fmaf(f16_bits_to_f32(meta[i][g] & 0xFFFFu), D[g], x);
+          z = __builtin_fmaf(f16_bits_to_f32(meta[i][g] >> 16), Q[k][g], z);
+        }
+        x = __builtin_fmaf(x, down, z);
+      } else {
+        x = __builtin_fmaf(f16_bits_to_f32(meta[i][0] & 0xFFFFu) * down, (D[0] + D[1]) + (D[2] + D[3]),
+                           f16_bits_to_f32(meta[i][0] >> 16) * ((Q[k][0] + Q[k][1]) + (Q[k][2] + Q[k][3])));
+      }
+      x = (real >> i) & 1 && token < lim[k] ? x : -INFINITY;
+      // the reference moves when a score exceeds it by 2^40, which fp32's sums have room for
+      if (__any(x > m[k] + 40.0f)) {
+        const float top = fmaxf(m[k], x);
+        sum[k] *= __builtin_amdgcn_exp2f(m[k] - top);
+        m[k] = top;
+      }
+      sum[k] += __builtin_amdgcn_exp2f(x - m[k]);
+      if (4 * k + quad < a.row_cap) scores[((size_t)(page0 + i) * a.row_cap + 4 * k + quad) * kBlock + t] = x;
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < TILES; ++k) {
+    const float top = row_max16(m[k]);
+    const float all = row_sum16(sum[k] * __builtin_amdgcn_exp2f(m[k] - top));
+    if (t == 0) both[w][4 * k + quad] = make_float2(top, all);
+  }
+  __syncthreads();
+  if (threadIdx.x < 4 * TILES) {
+    float top = kNone, all = 0.0f;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) top = fmaxf(top, both[x][threadIdx.x].x);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) all += both[x][threadIdx.x].y * __builtin_amdgcn_exp2f(both[x][threadIdx.x].x - top);
+    a.stats[(((size_t)b * H + h) * a.pieces + piece) * kFewRows + threadIdx.x] = make_float2(top, all);
+  }
+}
+
+// Block: 1,024 tokens of one KV head, a thread four of them. Each wave joins the pieces of its rows first.
+__global__ __launch_bounds__(256) void weight_few_join_kernel(TokenWeightsArgs a) {
+  __shared__ float lse[kFewRows];
+  const int H = a.cv.num_kv_heads, joins = (a.page_cap * kBlock + kJoinTokens - 1) / kJoinTokens;
+  const int h = blockIdx.x % H, join = blockIdx.x / H % joins, b = blockIdx.x / H / joins, w = threadIdx.x >> 6, l = threadIdx.x & 63;
+  const Span s = span_of(a, b);
+  if (kJoinTokens * join >= s.ctx) return;
+  const int rows = min(s.n * a.gq, a.row_cap), pieces = (s.ctx + kPieceTokens - 1) / kPieceTokens;
+  const float2* stats = a.stats + ((size_t)b * H + h) * a.pieces * kFewRows;
+  for (int r = w; r < rows; r += 4) {
+    float top = kNone, all = 0.0f;
+    for (int x = l; x < pieces; x += 64) {
+      const float2 v = stats[(size_t)x * kFewRows + r];
+      const float next = fmaxf(top, v.x);
+      all = all * __builtin_amdgcn_exp2f(top - next) + v.y * __builtin_amdgcn_exp2f(v.x - next);
+      top = next;
+    }
+    float most = top;
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1) most = fmaxf(most, __shfl_xor(most, step));
+    all *= __builtin_amdgcn_exp2f(top - most);
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1) all += __shfl_xor(all, step);
+    if (l == 0) lse[r] = all == 0.0f ? INFINITY : most + __builtin_amdgcn_logf(all);
+  }
+  __syncthreads();
+  const int t = kJoinTokens * join + 4 * threadIdx.x;
+  if (t >= s.ctx) return;
+  const float* scores = a.scores + (((size_t)b * H + h) * a.page_cap + t / kBlock) * (kBlock * a.row_cap) + (t & 15);
+  float sum[4] = {};
+  for (int r = 0; r < rows; ++r) {
+    const float4 x = *reinterpret_cast<const float4*>(scores + r * kBlock);
+    sum[0] += __builtin_amdgcn_exp2f(x.x - lse[r]), sum[1] += __builtin_amdgcn_exp2f(x.y - lse[r]);
+    sum[2] += __builtin_amdgcn_exp2f(x.z - lse[r]), sum[3] += __builtin_amdgcn_exp2f(x.w - lse[r]);
+  }
+  const size_t at = ((size_t)b * H + h) * a.w_stride + t;
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (t + i < s.ctx) a.w_out[at + i] = a.w_in ? __builtin_fmaf(a.decay, a.w_in[at + i], sum[i]) : sum[i];
+}
+
 TokenWeightsPlan make_token_weights_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx) {
   TokenWeightsPlan p{};
   const int gq = Hq / H;
-  p.seq_tiles = (int)(((long long)max_q * gq + kRows - 1) / kRows);
+  const long long seq_rows = (long long)max_q * gq;
+  p.few = seq_rows > 0 && seq_rows <= kFewRows;
+  p.seq_tiles = (int)((seq_rows + kRows - 1) / kRows);
   p.ranges = (int)(((long long)max_ctx + kRangeTokens - 1) / kRangeTokens);
   if (p.ranges < 1) p.ranges = 1;
+  p.pieces = (int)(((long long)max_ctx + kPieceTokens - 1) / kPieceTokens);
+  p.page_cap = (int)(((long long)max_ctx + kBlock - 1) / kBlock);
+  p.row_cap = (int)(seq_rows < kFewRows ? seq_rows : kFewRows);
   p.tiles = (int)((long long)total_q * gq / kRows + B + 1);
   // slices of the row tiles while the ranges leave places on the chip free
   const long long blocks = (long long)B * H * p.ranges, places = 2LL * num_cus();
@@ -372,10 +598,33 @@ TokenWeightsPlan make_token_weights_plan(int B, int Hq, int H, int total_q, int 
   p.off_lse = off, off = up(off + (size_t)p.tiles * H * kRows * sizeof(float));
   p.off_part = off, off = up(off + (size_t)places * kRangeTokens * sizeof(float));  // (a smaller call may take more slices)
   p.total = off;
+  // few rows: a call within these bounds may have them, whether or not this one does
+  off = 0;
+  p.off_few = off, off = up(off + (size_t)B * H * sizeof(FewOps));
+  p.off_few_stats = off, off = up(off + (size_t)B * H * p.pieces * kFewRows * sizeof(float2));
+  p.off_scores = off, off = up(off + (size_t)B * H * p.page_cap * kBlock * p.row_cap * sizeof(float));
+  p.total = p.total > off ? p.total : off;
   return p;
 }
 
 namespace {
+
+template <int NG>
+hipError_t launch_few(const TokenWeightsArgs& a, hipStream_t s) {
+  const long long H = a.cv.num_kv_heads;
+  hipLaunchKernelGGL(weight_few_rows_kernel, dim3((unsigned)(a.B * H)), dim3(256), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  const dim3 grid((unsigned)(a.B * H * a.pieces));
+  if (a.row_cap <= 4)
+    hipLaunchKernelGGL((weight_few_scores_kernel<NG, 1>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((weight_few_scores_kernel<NG, 2>), grid, dim3(256), 0, s, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  const long long joins = ((long long)a.page_cap * kBlock + kJoinTokens - 1) / kJoinTokens;
+  hipLaunchKernelGGL(weight_few_join_kernel, dim3((unsigned)(a.B * H * joins)), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
 
 template <int NG>
 hipError_t launch_ng(const TokenWeightsArgs& a, hipStream_t s) {
@@ -409,6 +658,13 @@ hipError_t launch_token_weights(TokenWeightsArgs a, const TokenWeightsPlan& p, u
   a.stats = reinterpret_cast<float2*>(ws + p.off_stats);
   a.lse = reinterpret_cast<float*>(ws + p.off_lse);
   a.part = reinterpret_cast<float*>(ws + p.off_part);
+  if (p.few) {
+    a.few = ws + p.off_few;
+    a.stats = reinterpret_cast<float2*>(ws + p.off_few_stats);
+    a.scores = reinterpret_cast<float*>(ws + p.off_scores);
+    a.pieces = p.pieces, a.page_cap = p.page_cap, a.row_cap = p.row_cap;
+    return a.cv.groups == 4 ? launch_few<4>(a, s) : launch_few<1>(a, s);
+  }
   return a.cv.groups == 4 ? launch_ng<4>(a, s) : launch_ng<1>(a, s);
 }
 
