@@ -247,12 +247,11 @@ struct TokenWeightsArgs {
   int64_t w_stride;
   float decay;
   // plan and workspace
-  int seq_tiles, ranges, slices, tiles;  // row tiles of a sequence at most; token ranges; slices of a sequence's row tiles; all tiles
-  uint8_t* ops;                     // [tiles, H] row operands
-  float* down;                      // [tiles, H] what brings their scores back to size
+  int seq_tiles, ranges, tiles;     // row tiles of a sequence at most; token ranges; all row tiles
+  int chunks, chunk_tiles;          // chunks of a sequence's row tiles
+  uint8_t* ops;                     // [tiles, H] row tiles
   float2* stats;                    // [ranges, tiles, H, 32] maximum and sum of a row over a range
-  float* lse;                       // [tiles, H, 32]
-  float* part;                      // [slices, B, H, ranges * kRangeTokens] where slices > 1
+  float* part;                      // [chunks, B, H, ranges * kRangeTokens] where there are several
   // few rows a sequence (stats: [B, H, pieces, 8])
   int pieces, page_cap, row_cap;    // pieces and pages of a sequence, rows of a KV head, each at most
   uint8_t* few;                     // [B, H] row operands
@@ -260,8 +259,8 @@ struct TokenWeightsArgs {
 };
 struct TokenWeightsPlan {
   bool few;
-  int seq_tiles, ranges, slices, tiles, pieces, page_cap, row_cap;
-  size_t off_ops, off_down, off_stats, off_lse, off_part, off_few, off_few_stats, off_scores, total;
+  int seq_tiles, ranges, tiles, chunks, chunk_tiles, pieces, page_cap, row_cap;
+  size_t off_ops, off_stats, off_part, off_few, off_few_stats, off_scores, total;
 };
 constexpr int kRangeTokens = 256;
 TokenWeightsPlan make_token_weights_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx);

@@ -9,6 +9,7 @@
 //     x = sum_g s_g D_g + sum_g z_g Q_g,   D_g = sum_{c in g} q'_c code_c,   Q_g = sum_{c in g} q'_c,
 // where a code is exact in fp16, q' and Q_g are two fp16 terms each (22 bits) and z_g is fp16 as stored, all products are
 // exact in fp32, and s_g enters in fp32.
+#include "append_core.h"
 #include "chunk_core.h"
 
 namespace int2kv {
@@ -16,9 +17,9 @@ namespace int2kv {
 namespace {
 
 constexpr int kRows = 32;                                     // rows of a tile
-constexpr int kOpBytes = 2 * 8 * 64 * 16 + 64 * 16;           // a tile's operands: high terms, low terms, Q_g
-constexpr int kWaves = 8;
-static_assert(kRangeTokens == 32 * kWaves, "a wave takes 32 tokens of a range");
+constexpr int kWaves = 8;                                     // of a block of the first pass
+constexpr int kChunkTiles = 32;                               // row tiles of a block at most
+static_assert(kRangeTokens == 32 * kWaves && kRangeTokens == 64 * 4, "the waves' tokens");
 
 struct Span {
   int start, n, ctx, past;  // as Seq
@@ -94,21 +95,66 @@ struct Token {
   }
 };
 
-// A row tile's operands in LDS
-struct Ops {
-  cd_h8_t hi[8][64], lo[8][64], group[64];
+// A row tile's operands, and beside them what else its readers need
+struct RowTile {
+  cd_h8_t hi[8][64], lo[8][64];
+  cd_h8_t group[32];       // Q_g: high terms, low terms (the other lane half's is zero)
+  float lse[kRows];        // L_r; infinite for rows that see nothing and behind the last one, so that their weights are zero
+  float down, pad[95];     // what brings the scores back to size
 };
-static_assert(sizeof(Ops) == kOpBytes, "as the workspace holds them");
+constexpr int kTileBytes = sizeof(RowTile), kPieces = kTileBytes / 1024;
+static_assert(kTileBytes == 17 * 1024, "pieces of 64 lanes x 16 bytes");
 
 __device__ __forceinline__ cd_f16_t product(const cd_h8_t& x, const cd_h8_t& y, const cd_f16_t& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, c, 0, 0, 0);
 }
 
-// Brings a tile's operands to LDS by all threads of the block
-__device__ __forceinline__ void bring(const uint8_t* from, Ops& to) {
-  const uint4* s = reinterpret_cast<const uint4*>(from);
-  uint4* d = reinterpret_cast<uint4*>(&to);
-  for (int i = threadIdx.x; i < kOpBytes / 16; i += 64 * kWaves) d[i] = s[i];
+// The row tiles t0 .. t1 of one KV head, two on their way to LDS while a third is in use. All waves of the block call it.
+template <int NW, class F>
+__device__ __forceinline__ void for_tiles(const TokenWeightsArgs& a, const uint8_t* tiles, int t0, int t1, RowTile (&lds)[3], F f) {
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const size_t stride = (size_t)a.cv.num_kv_heads * kTileBytes;
+  const uint32_t to = (uint32_t)(uintptr_t)&lds[0];
+  auto issue = [&](int t, int slot) {
+    const uint8_t* from = tiles + t * stride + 16 * l;
+    for (int c = w; c < kPieces; c += NW) ap_dma16(from + 1024 * c, to + (uint32_t)(slot * kTileBytes + 1024 * c));
+  };
+  if (t0 < t1) issue(t0, 0);
+  if (t0 + 1 < t1) issue(t0 + 1, 1);
+  int slot = 0;
+  for (int t = t0; t < t1; ++t) {
+    // this tile has landed when at most the next one's pieces are on their way: 17 / NW of them, the first wave's one more
+    static_assert(NW == 8 || NW == 4, "the counts below");
+    if (t + 1 == t1)
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    else if (w == 0)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPieces / NW + 1) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPieces / NW) : "memory");
+    __syncthreads();  // and every wave is done with the tile before, whose place the one after the next takes
+    if (t + 2 < t1) issue(t + 2, slot == 0 ? 2 : slot - 1);
+    f(t, lds[slot]);
+    slot = slot == 2 ? 0 : slot + 1;
+  }
+}
+
+// A block's share: a range of tokens of one KV head and a chunk of the row tiles that see it
+struct Share {
+  int b, h, bh, range, chunk, first, t0, t1;  // first token; tiles
+};
+__device__ __forceinline__ Share share_of(const TokenWeightsArgs& a, int bh, int range, int chunk, const Span& s) {
+  Share x;
+  x.bh = bh, x.range = range, x.chunk = chunk;
+  x.b = bh / a.cv.num_kv_heads, x.h = bh - x.b * a.cv.num_kv_heads;
+  x.first = kRangeTokens * range;
+  x.t0 = x.t1 = 0;
+  if (x.first < s.ctx) {
+    const int rows = s.n * a.gq, tiles = (rows + kRows - 1) / kRows;
+    // the first row that sees the first token
+    x.t0 = max(a.chunk_tiles * chunk, max(x.first - s.past, 0) * a.gq / kRows);
+    x.t1 = min(tiles, a.chunk_tiles * (chunk + 1));
+  }
+  return x;
 }
 
 }  // namespace
@@ -118,12 +164,13 @@ __device__ __forceinline__ void bring(const uint8_t* from, Ops& to) {
 // the largest element to 2^7 .. 2^8: what the low terms lose, 2^-24, is 2^-31 of it, and a group's sum fits fp16.
 __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, int tiles_per_block) {
   __shared__ float top[4], sums[4][kRows];
+  __shared__ __align__(16) RowTile out;
   const int H = a.cv.num_kv_heads, blocks = (a.seq_tiles + tiles_per_block - 1) / tiles_per_block;
-  const int at = blockIdx.x % blocks, h = blockIdx.x / blocks % H, b = blockIdx.x / blocks / H;
+  const int h = blockIdx.x % H, at = blockIdx.x / H % blocks, b = blockIdx.x / H / blocks;
   const Span s = span_of(a, b);
   const int tiles = (s.n * a.gq + kRows - 1) / kRows;
   const int w = threadIdx.x >> 6, l = threadIdx.x & 63, n = l & 31, hh = l >> 5;
-  if (at * tiles_per_block >= tiles) return;
+  if (at * tiles_per_block >= tiles || s.ctx == 0) return;
   cd_u4_t R[8][3];  // of column 32 w + n, rows 16 kk + 8 hh ..
 #pragma unroll
   for (int kk = 0; kk < 8; ++kk) {
@@ -136,7 +183,7 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
     R[kk][0] = pack_terms(x), R[kk][1] = pack_terms(y), R[kk][2] = pack_terms(z);
   }
   for (int t = at * tiles_per_block; t < min(tiles, (at + 1) * tiles_per_block); ++t) {
-    const int row = kRows * t + n, tok = row / a.gq;
+    const int row = kRows * t + n, tok = quotient(row, a.gq);
     const bool live = row < s.n * a.gq;
     const uint16_t* q = a.q + (s.start + (live ? tok : 0)) * a.q_stride + (size_t)(h * a.gq + (live ? row - tok * a.gq : 0)) * kHeadDim + 8 * hh;
     cd_f16_t d = splat16(0.0f);
@@ -157,14 +204,11 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
     }
 #pragma unroll
     for (int step = 32; step > 0; step >>= 1) big = fmaxf(big, __shfl_xor(big, step));
-    __syncthreads();  // (the tile before is done with them)
     if (l == 0) top[w] = big;
-    __syncthreads();
+    __syncthreads();  // (and the tile before has left)
     big = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
     const uint32_t e = min(max(__float_as_uint(big) >> 23, 8u), 254u);
     const float up = __uint_as_float((261u - e) << 23), down = __uint_as_float((e - 7u) << 23);
-    const size_t tile = ((size_t)(s.tile0 + t) * H + h);
-    Ops& out = *reinterpret_cast<Ops*>(a.ops + tile * kOpBytes);
 #pragma unroll
     for (int r = 0; r < 16; r += 2) {
       const float x = d[r] * up, y = d[r + 1] * up;
@@ -177,37 +221,40 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
     sum = pair_sum(sum);
     if (hh == 0) sums[w][n] = sum;
     __syncthreads();
-    if (w == 0) {
-      cd_h8_t g{};
-      if (hh == 0) {
-        float x[4];
+    uint4* to = reinterpret_cast<uint4*>(a.ops + ((size_t)(s.tile0 + t) * H + h) * kTileBytes);
+    const uint4* from = reinterpret_cast<const uint4*>(&out);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = sums[i][n];
-        if (a.cv.groups == 1) x[0] = (x[0] + x[1]) + (x[2] + x[3]), x[1] = x[2] = x[3] = 0.0f;
+    for (int i = 0; i < 4; ++i) to[threadIdx.x + 256 * i] = from[threadIdx.x + 256 * i];
+    if (threadIdx.x < kRows) {
+      float x[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) g[i] = (_Float16)x[i], g[4 + i] = (_Float16)(x[i] - (float)g[i]);
-      }
-      out.group[l] = g;
-      if (l == 0) a.down[tile] = down;
+      for (int i = 0; i < 4; ++i) x[i] = sums[i][n];
+      if (a.cv.groups == 1) x[0] = (x[0] + x[1]) + (x[2] + x[3]), x[1] = x[2] = x[3] = 0.0f;
+      cd_h8_t g;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) g[i] = (_Float16)x[i], g[4 + i] = (_Float16)(x[i] - (float)g[i]);
+      to[1024 + n] = __builtin_bit_cast(uint4, g);
+      if (n == 0) reinterpret_cast<RowTile*>(to)->down = down;
     }
   }
 }
 
-// ---- Maximum and sum of the rows over a range. Block: 256 tokens of one KV head over a slice of the row tiles, wave w
-// with 32 of them. Products are codes x rows, so that a lane holds a row and the sums are its own.
+// ---- Maximum and sum of the rows over a range. Block: 256 tokens of one KV head, wave w with 32 of them. Products are
+// codes x rows, so that a lane holds a row and the sums are its own.
 template <int NG>
 __global__ __launch_bounds__(64 * kWaves, 2) void weight_stats_kernel(TokenWeightsArgs a) {
-  __shared__ Ops ops;
+  __shared__ __align__(16) RowTile lds[3];
   __shared__ float scales[kWaves][32][NG];
-  __shared__ float2 both[kWaves][kRows];
-  const int H = a.cv.num_kv_heads;
-  const int range = blockIdx.x % a.ranges, slice = blockIdx.x / a.ranges % a.slices, bh = blockIdx.x / a.ranges / a.slices, b = bh / H, h = bh % H;
-  const Span s = span_of(a, b);
-  const int rows = s.n * a.gq, tiles = (rows + kRows - 1) / kRows, per = (tiles + a.slices - 1) / a.slices;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, hh = l >> 5, first = kRangeTokens * range, t0 = first + 32 * w;
-  if (first >= s.ctx) return;
+  __shared__ float2 both[2][kWaves][kRows], stats[kChunkTiles][kRows];
+  const int BH = a.B * a.cv.num_kv_heads, bh = blockIdx.x % BH;
+  const Span s = span_of(a, bh / a.cv.num_kv_heads);
+  const Share me = share_of(a, bh, blockIdx.x / BH % a.ranges, blockIdx.x / BH / a.ranges, s);
+  if (me.t0 >= me.t1) return;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, hh = l >> 5, token0 = me.first + 32 * w;
+  const int rows = s.n * a.gq;
+  const uint8_t* tiles = a.ops + ((size_t)s.tile0 * a.cv.num_kv_heads + me.h) * kTileBytes;
   Token<NG> tok;
-  tok.load(a, b, h, t0 + n, s.ctx, hh);
+  tok.load(a, me.b, me.h, token0 + n, s.ctx, hh);
   if (hh == 0) {
 #pragma unroll
     for (int g = 0; g < NG; ++g) scales[w][n][g] = tok.scale[g];
@@ -219,135 +266,184 @@ __global__ __launch_bounds__(64 * kWaves, 2) void weight_stats_kernel(TokenWeigh
   for (int r = 0; r < 16; ++r)
 #pragma unroll
     for (int g = 0; g < NG; ++g) sc[g][r] = scales[w][8 * (r >> 2) + 4 * hh + (r & 3)][g];
-  for (int t = slice * per; t < min(tiles, (slice + 1) * per); ++t) {
-    if (s.limit(min(kRows * t + kRows - 1, rows - 1) / a.gq) <= first) continue;  // none of its rows sees the range
-    const size_t tile = (size_t)(s.tile0 + t) * H + h;
-    __syncthreads();
-    bring(a.ops + tile * kOpBytes, ops);
-    const float down = a.down[tile];
-    __syncthreads();
-    cd_f16_t S = product(tok.zero, ops.group[l], splat16(0.0f));
+  const int all_from = real == ~0u ? max(token0 + 31 - s.past, 0) * a.gq : rows + kRows;  // rows that see all of the wave's tokens
+  const int some_from = max(token0 - s.past, 0) * a.gq;                                    // rows that see some
+  auto join = [&](int t) {
+    const float2(&x)[kWaves][kRows] = both[t & 1];
+    float top = -INFINITY, all = 0.0f;
 #pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      cd_f16_t D = splat16(0.0f);
+    for (int i = 0; i < kWaves; ++i) top = fmaxf(top, x[i][n].x);
+    const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-      for (int x = 8 / NG * g; x < 8 / NG * (g + 1); ++x) {
-        D = product(tok.code[x], ops.hi[x][l], D);
-        D = product(tok.code[x], ops.lo[x][l], D);
+    for (int i = 0; i < kWaves; ++i) all = __builtin_fmaf(x[i][n].y, __builtin_amdgcn_exp2f(x[i][n].x - base), all);
+    stats[t - me.t0][n] = make_float2(top, all);
+  };
+  for_tiles<kWaves>(a, tiles, me.t0, me.t1, lds, [&](int t, const RowTile& ops) {
+    if (t > me.t0 && w == ((t - 1) & 7)) join(t - 1);
+    float m = -INFINITY, sum = 0.0f;
+    if (kRows * t + kRows > some_from && real != 0) {
+      cd_h8_t group = ops.group[n];
+      if (hh) group = cd_h8_t{};
+      cd_f16_t S = product(tok.zero, group, splat16(0.0f));
+      const float down = ops.down;
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        cd_f16_t D = splat16(0.0f);
+#pragma unroll
+        for (int x = 8 / NG * g; x < 8 / NG * (g + 1); ++x) {
+          D = product(tok.code[x], ops.hi[x][l], D);
+          D = product(tok.code[x], ops.lo[x][l], D);
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) S[r] = __builtin_fmaf(sc[g][r], D[r], S[r]);
       }
+      if (kRows * t < all_from) {
+        const int lim = s.limit(quotient(min(kRows * t + n, rows - 1), a.gq)) - token0;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) S[r] = __builtin_fmaf(sc[g][r], D[r], S[r]);
-    }
-    const int lim = s.limit(min(kRows * t + n, rows - 1) / a.gq) - t0;
-    float m = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int x = 8 * (r >> 2) + 4 * hh + (r & 3);
-      S[r] = x < lim && ((real >> x) & 1) ? S[r] * down : -INFINITY;
-      m = fmaxf(m, S[r]);
-    }
-    m = pair_max(m);
-    const float base = m == -INFINITY ? 0.0f : m;
-    float sum = 0.0f;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(S[r] - base);
-    sum = pair_sum(sum);
-    if (hh == 0) both[w][n] = make_float2(m, sum);
-    __syncthreads();
-    if (threadIdx.x < kRows) {
-      float top = -INFINITY, all = 0.0f;
-#pragma unroll
-      for (int x = 0; x < kWaves; ++x) top = fmaxf(top, both[x][threadIdx.x].x);
-#pragma unroll
-      for (int x = 0; x < kWaves; ++x) {
-        const float2 v = both[x][threadIdx.x];
-        all += v.y == 0.0f ? 0.0f : v.y * __builtin_amdgcn_exp2f(v.x - top);
+        for (int r = 0; r < 16; ++r) {
+          const int x = 8 * (r >> 2) + 4 * hh + (r & 3);
+          S[r] = x < lim && ((real >> x) & 1) ? S[r] : -INFINITY;
+        }
       }
-      a.stats[(((size_t)range * a.tiles + s.tile0 + t) * H + h) * kRows + threadIdx.x] = make_float2(top, all);
+      m = fmaxf(S[0], S[1]);
+#pragma unroll
+      for (int r = 2; r < 16; r += 2) m = fmaxf(fmaxf(m, S[r]), S[r + 1]);
+      m = pair_max(m) * down;
+      const float base = m == -INFINITY ? 0.0f : m;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], down, -base));
+      sum = pair_sum(sum);
     }
-  }
+    if (hh == 0) both[t & 1][w][n] = make_float2(m, sum);
+  });
+  __syncthreads();
+  if (w == ((me.t1 - 1) & 7)) join(me.t1 - 1);
+  __syncthreads();
+  for (int i = threadIdx.x; i < (me.t1 - me.t0) * kRows; i += 64 * kWaves)
+    a.stats[(((size_t)me.range * a.tiles + s.tile0 + me.t0 + i / kRows) * a.cv.num_kv_heads + me.h) * kRows + i % kRows] = stats[i / kRows][i % kRows];
 }
 
-// ---- L_r of every row; infinite for rows that see nothing and behind the last one, so that their weights are zero
+// ---- L_r of every row. Block: a row tile; eight threads a row, each with every eighth range.
 __global__ __launch_bounds__(256) void weight_lse_kernel(TokenWeightsArgs a) {
-  const int H = a.cv.num_kv_heads, n = threadIdx.x & 31;
-  const long long item = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-  if (item >= (long long)a.B * H * a.seq_tiles) return;
-  const int t = (int)(item % a.seq_tiles), h = (int)(item / a.seq_tiles % H), b = (int)(item / a.seq_tiles / H);
+  __shared__ float2 part[8][kRows];
+  const int H = a.cv.num_kv_heads, n = threadIdx.x & 31, k = threadIdx.x >> 5;
+  const int h = blockIdx.x % H, t = blockIdx.x / H % a.seq_tiles, b = blockIdx.x / H / a.seq_tiles;
   const Span s = span_of(a, b);
   const int rows = s.n * a.gq, row = kRows * t + n;
-  if (kRows * t >= rows) return;
+  if (kRows * t >= rows || s.ctx == 0) return;
   const int ranges = row < rows ? (s.limit(row / a.gq) + kRangeTokens - 1) / kRangeTokens : 0;
   float m = -INFINITY, sum = 0.0f;
-  for (int r = 0; r < ranges; ++r) {
+#pragma unroll 4
+  for (int r = k; r < ranges; r += 8) {
     const float2 v = a.stats[(((size_t)r * a.tiles + s.tile0 + t) * H + h) * kRows + n];
     const float top = fmaxf(m, v.x), base = top == -INFINITY ? 0.0f : top;
     sum = sum * __builtin_amdgcn_exp2f(m - base) + v.y * __builtin_amdgcn_exp2f(v.x - base);
     m = top;
   }
-  a.lse[((size_t)(s.tile0 + t) * H + h) * kRows + n] = sum == 0.0f ? INFINITY : m + __builtin_amdgcn_logf(sum);
+  part[k][n] = make_float2(m, sum);
+  __syncthreads();
+  if (k) return;
+#pragma unroll
+  for (int x = 1; x < 8; ++x) m = fmaxf(m, part[x][n].x);
+  const float base = m == -INFINITY ? 0.0f : m;
+  sum = 0.0f;
+#pragma unroll
+  for (int x = 0; x < 8; ++x) sum = __builtin_fmaf(part[x][n].y, __builtin_amdgcn_exp2f(part[x][n].x - base), sum);
+  reinterpret_cast<RowTile*>(a.ops + ((size_t)(s.tile0 + t) * H + h) * kTileBytes)->lse[n] = sum == 0.0f ? INFINITY : m + __builtin_amdgcn_logf(sum);
 }
 
-// ---- The sums over the rows. Products are rows x codes, so that a lane holds a token.
+// ---- The sums over the rows. Products are rows x codes, so that a lane holds a token; a wave has 64 of them.
 template <int NG>
-__global__ __launch_bounds__(64 * kWaves, 2) void weight_sums_kernel(TokenWeightsArgs a) {
-  __shared__ Ops ops;
-  __shared__ float lse[kRows];
-  const int H = a.cv.num_kv_heads;
-  const int range = blockIdx.x % a.ranges, slice = blockIdx.x / a.ranges % a.slices, bh = blockIdx.x / a.ranges / a.slices, b = bh / H, h = bh % H;
-  const Span s = span_of(a, b);
-  const int rows = s.n * a.gq, tiles = (rows + kRows - 1) / kRows, per = (tiles + a.slices - 1) / a.slices;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, hh = l >> 5, first = kRangeTokens * range, t0 = first + 32 * w;
-  if (first >= s.ctx) return;
-  Token<NG> tok;
-  tok.load(a, b, h, t0 + n, s.ctx, hh);
-  float sum = 0.0f;
-  for (int t = slice * per; t < min(tiles, (slice + 1) * per); ++t) {
-    if (s.limit(min(kRows * t + kRows - 1, rows - 1) / a.gq) <= first) continue;
-    const size_t tile = (size_t)(s.tile0 + t) * H + h;
-    __syncthreads();
-    bring(a.ops + tile * kOpBytes, ops);
-    if (threadIdx.x < kRows) lse[threadIdx.x] = a.lse[tile * kRows + threadIdx.x];
-    const float down = a.down[tile];
-    __syncthreads();
-    cd_f16_t S = product(ops.group[l], tok.zero, splat16(0.0f));
+__global__ __launch_bounds__(256, 2) void weight_sums_kernel(TokenWeightsArgs a) {
+  __shared__ __align__(16) RowTile lds[3];
+  const int BH = a.B * a.cv.num_kv_heads, bh = blockIdx.x % BH;
+  const Span s = span_of(a, bh / a.cv.num_kv_heads);
+  const Share me = share_of(a, bh, blockIdx.x / BH % a.ranges, blockIdx.x / BH / a.ranges, s);
+  if (me.t0 >= me.t1 && (a.chunks > 1 || me.first >= s.ctx)) return;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, hh = l >> 5, token0 = me.first + 64 * w;
+  const uint8_t* tiles = a.ops + ((size_t)s.tile0 * a.cv.num_kv_heads + me.h) * kTileBytes;
+  Token<NG> tok[2];
+  float sum[2] = {0.0f, 0.0f};
+  int from[2];  // rows that see the lane's tokens
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    tok[u].load(a, me.b, me.h, token0 + 32 * u + n, s.ctx, hh);
+    from[u] = max(min(token0 + 32 * u + n, s.ctx - 1) - s.past, 0) * a.gq;
+  }
+  const int all_from = max(min(token0 + 63, s.ctx - 1) - s.past, 0) * a.gq, some_from = max(token0 - s.past, 0) * a.gq;
+  for_tiles<4>(a, tiles, me.t0, me.t1, lds, [&](int t, const RowTile& ops) {
+    if (kRows * t + kRows <= some_from || token0 >= s.ctx) return;
+    cd_h8_t group = ops.group[n];
+    if (hh) group = cd_h8_t{};
+    cd_f16_t S[2];
+#pragma unroll
+    for (int u = 0; u < 2; ++u) S[u] = product(group, tok[u].zero, splat16(0.0f));
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
-      cd_f16_t D = splat16(0.0f);
+      cd_f16_t D[2] = {splat16(0.0f), splat16(0.0f)};
 #pragma unroll
       for (int x = 8 / NG * g; x < 8 / NG * (g + 1); ++x) {
-        D = product(ops.hi[x][l], tok.code[x], D);
-        D = product(ops.lo[x][l], tok.code[x], D);
+        const cd_h8_t hi = ops.hi[x][l], lo = ops.lo[x][l];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) D[u] = product(hi, tok[u].code[x], D[u]);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) D[u] = product(lo, tok[u].code[x], D[u]);
       }
 #pragma unroll
-      for (int r = 0; r < 16; ++r) S[r] = __builtin_fmaf(tok.scale[g], D[r], S[r]);
-    }
-    float add = 0.0f;
+      for (int u = 0; u < 2; ++u)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int x = 8 * (r >> 2) + 4 * hh + (r & 3);
-      const bool sees = kRows * t + x < rows && t0 + n < s.limit((kRows * t + x) / a.gq);
-      add += sees ? __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], down, -lse[x])) : 0.0f;
+        for (int r = 0; r < 16; ++r) S[u][r] = __builtin_fmaf(tok[u].scale[g], D[u][r], S[u][r]);
     }
-    sum += add;
-  }
-  sum = pair_sum(sum);
-  if (!tok.real) sum = 0.0f;
-  if (hh || t0 + n >= s.ctx) return;
-  if (a.slices > 1) {
-    a.part[((size_t)slice * a.B * H + bh) * ((size_t)a.ranges * kRangeTokens) + t0 + n] = sum;
-  } else {
-    const size_t at = (size_t)bh * a.w_stride + t0 + n;
-    a.w_out[at] = a.w_in ? __builtin_fmaf(a.decay, a.w_in[at], sum) : sum;
+    const float down = ops.down;
+    float add[2] = {0.0f, 0.0f};
+    const bool whole = kRows * t >= all_from;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float4 v = *reinterpret_cast<const float4*>(&ops.lse[8 * x + 4 * hh]);
+      const float lse[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) S[u][4 * x + y] = __builtin_fmaf(S[u][4 * x + y], down, -lse[y]);
+    }
+    if (!whole) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) S[u][r] = kRows * t + 8 * (r >> 2) + 4 * hh + (r & 3) >= from[u] ? S[u][r] : -INFINITY;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) add[u] += __builtin_amdgcn_exp2f(S[u][r]);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) sum[u] += add[u];
+  });
+#pragma unroll
+  for (int u = 0; u < 2; ++u) {
+    const int t = token0 + 32 * u + n;
+    float x = pair_sum(sum[u]);
+    if (!tok[u].real) x = 0.0f;
+    if (hh || t >= s.ctx) continue;
+    if (a.chunks > 1) {
+      a.part[((size_t)me.chunk * BH + bh) * ((size_t)a.ranges * kRangeTokens) + t] = x;
+    } else {
+      const size_t at = (size_t)bh * a.w_stride + t;
+      a.w_out[at] = a.w_in ? __builtin_fmaf(a.decay, a.w_in[at], x) : x;
+    }
   }
 }
 
+// ---- The chunks' sums, and the running ones
 __global__ __launch_bounds__(256) void weight_join_kernel(TokenWeightsArgs a) {
-  const int H = a.cv.num_kv_heads, range = blockIdx.x % a.ranges, bh = blockIdx.x / a.ranges, t = kRangeTokens * range + threadIdx.x;
-  const Span s = span_of(a, bh / H);
+  const int BH = a.B * a.cv.num_kv_heads, bh = blockIdx.x % BH, range = blockIdx.x / BH, t = kRangeTokens * range + threadIdx.x;
+  const Span s = span_of(a, bh / a.cv.num_kv_heads);
   if (t >= s.ctx) return;
   float sum = 0.0f;
-  for (int x = 0; x < a.slices; ++x) sum += a.part[((size_t)x * a.B * H + bh) * ((size_t)a.ranges * kRangeTokens) + t];
+  for (int x = 0; x < a.chunks; ++x) {
+    const Share share = share_of(a, bh, range, x, s);
+    if (share.t0 < share.t1) sum += a.part[((size_t)x * BH + bh) * ((size_t)a.ranges * kRangeTokens) + t];
+  }
   const size_t at = (size_t)bh * a.w_stride + t;
   a.w_out[at] = a.w_in ? __builtin_fmaf(a.decay, a.w_in[at], sum) : sum;
 }
@@ -585,18 +681,19 @@ TokenWeightsPlan make_token_weights_plan(int B, int Hq, int H, int total_q, int 
   p.page_cap = (int)(((long long)max_ctx + kBlock - 1) / kBlock);
   p.row_cap = (int)(seq_rows < kFewRows ? seq_rows : kFewRows);
   p.tiles = (int)((long long)total_q * gq / kRows + B + 1);
-  // slices of the row tiles while the ranges leave places on the chip free
-  const long long blocks = (long long)B * H * p.ranges, places = 2LL * num_cus();
-  long long slices = places / (blocks < 1 ? 1 : blocks);
-  if (slices > (p.seq_tiles + 3) / 4) slices = (p.seq_tiles + 3) / 4;
-  p.slices = slices < 1 ? 1 : (int)slices;
+  // chunks of the row tiles: shorter ones while there are fewer than four blocks a compute unit
+  const long long ranges = (long long)B * H * p.ranges, places = 4LL * num_cus();
+  auto chunks = [&](int tiles) { return ((long long)p.seq_tiles + tiles - 1) / tiles; };
+  p.chunk_tiles = kChunkTiles;
+  while (p.chunk_tiles > 4 && ranges * chunks(p.chunk_tiles) < places) p.chunk_tiles /= 2;
+  p.chunks = (int)chunks(p.chunk_tiles);
   auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
   size_t off = 0;
-  p.off_ops = off, off = up(off + (size_t)p.tiles * H * kOpBytes);
-  p.off_down = off, off = up(off + (size_t)p.tiles * H * sizeof(float));
+  p.off_ops = off, off = up(off + (size_t)p.tiles * H * kTileBytes);
   p.off_stats = off, off = up(off + (size_t)p.ranges * p.tiles * H * kRows * sizeof(float2));
-  p.off_lse = off, off = up(off + (size_t)p.tiles * H * kRows * sizeof(float));
-  p.off_part = off, off = up(off + (size_t)places * kRangeTokens * sizeof(float));  // (a smaller call may take more slices)
+  // (a smaller call may take shorter chunks: fewer than twice as many as there are places, and one a range)
+  const long long most = ranges * chunks(kChunkTiles), shorter = 2 * places + ranges;
+  p.off_part = off, off = up(off + (size_t)(most > shorter ? most : shorter) * kRangeTokens * sizeof(float));
   p.total = off;
   // few rows: a call within these bounds may have them, whether or not this one does
   off = 0;
@@ -627,23 +724,24 @@ hipError_t launch_few(const TokenWeightsArgs& a, hipStream_t s) {
 }
 
 template <int NG>
-hipError_t launch_ng(const TokenWeightsArgs& a, hipStream_t s) {
-  const long long H = a.cv.num_kv_heads;
+hipError_t launch_many(const TokenWeightsArgs& a, hipStream_t s) {
+  const long long BH = (long long)a.B * a.cv.num_kv_heads;
   hipError_t e = hipSuccess;
   if (a.seq_tiles > 0) {
-    const long long items = a.B * H * a.seq_tiles;
+    const long long items = BH * a.seq_tiles;
     const int per = (int)(items / 1024 < 1 ? 1 : items / 1024 > 8 ? 8 : items / 1024);
-    hipLaunchKernelGGL(weight_rows_kernel, dim3((unsigned)(a.B * H * ((a.seq_tiles + per - 1) / per))), dim3(256), 0, s, a, per);
+    const dim3 shares((unsigned)(BH * a.ranges * a.chunks));
+    hipLaunchKernelGGL(weight_rows_kernel, dim3((unsigned)(BH * ((a.seq_tiles + per - 1) / per))), dim3(256), 0, s, a, per);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(weight_stats_kernel<NG>, dim3((unsigned)(a.B * H * a.slices * a.ranges)), dim3(64 * kWaves), 0, s, a);
+    hipLaunchKernelGGL(weight_stats_kernel<NG>, shares, dim3(64 * kWaves), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(weight_lse_kernel, dim3((unsigned)((items + 7) / 8)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL(weight_lse_kernel, dim3((unsigned)items), dim3(256), 0, s, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipLaunchKernelGGL(weight_sums_kernel<NG>, shares, dim3(256), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  hipLaunchKernelGGL(weight_sums_kernel<NG>, dim3((unsigned)(a.B * H * a.slices * a.ranges)), dim3(64 * kWaves), 0, s, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (a.slices > 1) {
-    hipLaunchKernelGGL(weight_join_kernel, dim3((unsigned)(a.B * H * a.ranges)), dim3(kRangeTokens), 0, s, a);
+  if (a.chunks != 1) {
+    hipLaunchKernelGGL(weight_join_kernel, dim3((unsigned)(BH * a.ranges)), dim3(kRangeTokens), 0, s, a);
     e = hipGetLastError();
   }
   return e;
@@ -652,11 +750,9 @@ hipError_t launch_ng(const TokenWeightsArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_token_weights(TokenWeightsArgs a, const TokenWeightsPlan& p, uint8_t* ws, hipStream_t s) {
-  a.seq_tiles = p.seq_tiles, a.ranges = p.ranges, a.slices = p.slices, a.tiles = p.tiles;
+  a.seq_tiles = p.seq_tiles, a.ranges = p.ranges, a.chunks = p.chunks, a.chunk_tiles = p.chunk_tiles, a.tiles = p.tiles;
   a.ops = ws + p.off_ops;
-  a.down = reinterpret_cast<float*>(ws + p.off_down);
   a.stats = reinterpret_cast<float2*>(ws + p.off_stats);
-  a.lse = reinterpret_cast<float*>(ws + p.off_lse);
   a.part = reinterpret_cast<float*>(ws + p.off_part);
   if (p.few) {
     a.few = ws + p.off_few;
@@ -665,7 +761,7 @@ hipError_t launch_token_weights(TokenWeightsArgs a, const TokenWeightsPlan& p, u
     a.pieces = p.pieces, a.page_cap = p.page_cap, a.row_cap = p.row_cap;
     return a.cv.groups == 4 ? launch_few<4>(a, s) : launch_few<1>(a, s);
   }
-  return a.cv.groups == 4 ? launch_ng<4>(a, s) : launch_ng<1>(a, s);
+  return a.cv.groups == 4 ? launch_many<4>(a, s) : launch_many<1>(a, s);
 }
 
 }  // namespace int2kv
