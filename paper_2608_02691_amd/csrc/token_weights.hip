@@ -17,9 +17,11 @@ namespace int2kv {
 namespace {
 
 constexpr int kRows = 32;                                     // rows of a tile
-constexpr int kWaves = 8;                                     // of a block of the first pass
-constexpr int kChunkTiles = 32;                               // row tiles of a block at most
-static_assert(kRangeTokens == 32 * kWaves && kRangeTokens == 64 * 4, "the waves' tokens");
+#ifndef KCH
+#define KCH 32
+#endif
+constexpr int kChunkTiles = KCH;                               // row tiles of a block at most
+static_assert(kRangeTokens == 4 * 64, "the waves' tokens");
 
 struct Span {
   int start, n, ctx, past;  // as Seq
@@ -62,7 +64,7 @@ __device__ __forceinline__ Spot spot_of(int c) {
 template <int NG>
 struct Token {
   cd_h8_t code[8];
-  float scale[NG];
+  float scale[NG], low[NG];
   cd_h8_t zero;
   bool real;
   __device__ __forceinline__ void load(const TokenWeightsArgs& a, int b, int h, int token, int ctx, int hh) {
@@ -78,6 +80,7 @@ struct Token {
     for (int g = 0; g < NG; ++g) {
       const uint32_t sz = m[g];
       scale[g] = f16_bits_to_f32(sz & 0xFFFFu);
+      low[g] = f16_bits_to_f32(sz >> 16);
       const _Float16 z = __builtin_bit_cast(cd_h2_t, sz).y;
       zero[g] = hh == 0 ? z : (_Float16)0.0f;
       zero[4 + g] = zero[g];
@@ -99,8 +102,11 @@ struct Token {
 struct RowTile {
   cd_h8_t hi[8][64], lo[8][64];
   cd_h8_t group[32];       // Q_g: high terms, low terms (the other lane half's is zero)
+  float ref[kRows];        // near the row's largest score over the first tokens: its sums are formed relative to it
   float lse[kRows];        // L_r; infinite for rows that see nothing and behind the last one, so that their weights are zero
-  float down, pad[95];     // what brings the scores back to size
+  float down;              // what brings the scores back to size
+  uint32_t unsure;         // not zero: some row's ref names no score of its own
+  float pad[62];
 };
 constexpr int kTileBytes = sizeof(RowTile), kPieces = kTileBytes / 1024;
 static_assert(kTileBytes == 17 * 1024, "pieces of 64 lanes x 16 bytes");
@@ -110,8 +116,9 @@ __device__ __forceinline__ cd_f16_t product(const cd_h8_t& x, const cd_h8_t& y, 
 }
 
 // The row tiles t0 .. t1 of one KV head, two on their way to LDS while a third is in use. All waves of the block call it.
-template <int NW, class F>
-__device__ __forceinline__ void for_tiles(const TokenWeightsArgs& a, const uint8_t* tiles, int t0, int t1, RowTile (&lds)[3], F f) {
+// first() runs while the first ones are on their way.
+template <int NW, class First, class F>
+__device__ __forceinline__ void for_tiles(const TokenWeightsArgs& a, const uint8_t* tiles, int t0, int t1, RowTile (&lds)[3], First first, F f) {
   const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const size_t stride = (size_t)a.cv.num_kv_heads * kTileBytes;
   const uint32_t to = (uint32_t)(uintptr_t)&lds[0];
@@ -121,6 +128,7 @@ __device__ __forceinline__ void for_tiles(const TokenWeightsArgs& a, const uint8
   };
   if (t0 < t1) issue(t0, 0);
   if (t0 + 1 < t1) issue(t0 + 1, 1);
+  first();
   int slot = 0;
   for (int t = t0; t < t1; ++t) {
     // this tile has landed when at most the next one's pieces are on their way: 17 / NW of them, the first wave's one more
@@ -161,7 +169,9 @@ __device__ __forceinline__ Share share_of(const TokenWeightsArgs& a, int bh, int
 
 // ---- The rows' operands. Block: row tiles of one KV head, one after the other; wave w forms channels 32 w .. of q R_K on the
 // matrix cores, R_K in three bf16 terms that sum to it exactly. A tile's rows are scaled by one power of two that brings
-// the largest element to 2^7 .. 2^8: what the low terms lose, 2^-24, is 2^-31 of it, and a group's sum fits fp16.
+// the largest element to 2^7 .. 2^8: what the low terms lose, 2^-24, is 2^-31 of it, and a group's sum fits fp16. The
+// last wave forms the rows' scores over the sequence's first 32 tokens, in one fp16 term: their maximum is where the first pass starts.
+template <int NG>
 __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, int tiles_per_block) {
   __shared__ float top[4], sums[4][kRows];
   __shared__ __align__(16) RowTile out;
@@ -181,6 +191,20 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
       x[j] = upper(r), y[j] = upper(r - x[j]), z[j] = r - x[j] - y[j];
     }
     R[kk][0] = pack_terms(x), R[kk][1] = pack_terms(y), R[kk][2] = pack_terms(z);
+  }
+  cd_h8_t keys[8];  // the first tokens' rows, rounded to fp16
+  uint32_t real = 0;
+  if (w == 3) {
+    Token<NG> first;
+    first.load(a, b, h, n, s.ctx, hh);
+    real = (uint32_t)__ballot(first.real);
+#pragma unroll
+    for (int x = 0; x < 8; ++x)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float z = NG == 4 ? first.low[x * NG / 8] : first.low[0];
+        keys[x][j] = (_Float16)__builtin_fmaf((float)first.code[x][j], first.scale[x * NG / 8], z);
+      }
   }
   for (int t = at * tiles_per_block; t < min(tiles, (at + 1) * tiles_per_block); ++t) {
     const int row = kRows * t + n, tok = quotient(row, a.gq);
@@ -222,7 +246,25 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
     if (hh == 0) sums[w][n] = sum;
     __syncthreads();
     uint4* to = reinterpret_cast<uint4*>(a.ops + ((size_t)(s.tile0 + t) * H + h) * kTileBytes);
+    RowTile& tile = *reinterpret_cast<RowTile*>(to);
     const uint4* from = reinterpret_cast<const uint4*>(&out);
+    if (w == 3) {
+      cd_f16_t S = splat16(0.0f);
+#pragma unroll
+      for (int x = 0; x < 8; ++x) S = product(keys[x], out.hi[x][l], S);
+      const int lim = live ? s.limit(tok) : 0;
+      float m = -INFINITY;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int x = 8 * (r >> 2) + 4 * hh + (r & 3);
+        m = fmaxf(m, x < lim && ((real >> x) & 1) ? S[r] : -INFINITY);
+      }
+      m = pair_max(m) * down;
+      const bool good = fabsf(m) < 1.0e30f;
+      if (hh == 0) tile.ref[n] = good ? m : 0.0f;
+      const bool unsure = __any(lim > 0 && !good);
+      if (l == 0) tile.unsure = unsure;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) to[threadIdx.x + 256 * i] = from[threadIdx.x + 256 * i];
     if (threadIdx.x < kRows) {
@@ -234,93 +276,241 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
 #pragma unroll
       for (int i = 0; i < 4; ++i) g[i] = (_Float16)x[i], g[4 + i] = (_Float16)(x[i] - (float)g[i]);
       to[1024 + n] = __builtin_bit_cast(uint4, g);
-      if (n == 0) reinterpret_cast<RowTile*>(to)->down = down;
+      if (n == 0) tile.down = down;
     }
   }
 }
 
-// ---- Maximum and sum of the rows over a range. Block: 256 tokens of one KV head, wave w with 32 of them. Products are
-// codes x rows, so that a lane holds a row and the sums are its own.
-template <int NG>
-__global__ __launch_bounds__(64 * kWaves, 2) void weight_stats_kernel(TokenWeightsArgs a) {
-  __shared__ __align__(16) RowTile lds[3];
-  __shared__ float scales[kWaves][32][NG];
-  __shared__ float2 both[2][kWaves][kRows], stats[kChunkTiles][kRows];
-  const int BH = a.B * a.cv.num_kv_heads, bh = blockIdx.x % BH;
-  const Span s = span_of(a, bh / a.cv.num_kv_heads);
-  const Share me = share_of(a, bh, blockIdx.x / BH % a.ranges, blockIdx.x / BH / a.ranges, s);
-  if (me.t0 >= me.t1) return;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, hh = l >> 5, token0 = me.first + 32 * w;
-  const int rows = s.n * a.gq;
-  const uint8_t* tiles = a.ops + ((size_t)s.tile0 * a.cv.num_kv_heads + me.h) * kTileBytes;
-  Token<NG> tok;
-  tok.load(a, me.b, me.h, token0 + n, s.ctx, hh);
-  if (hh == 0) {
+// ---- The two passes over the keys. Block: 256 tokens of one KV head and a chunk of the row tiles that see them; a wave has
+// 64 tokens. Products are rows x codes, so that a lane holds a token and its scales. PASS 1 sums each row's 2^(x - ref)
+// over the range, PASS 2 each token's 2^(x - L) over the rows.
+namespace {
+
+constexpr float kFar = 100.0f;  // scores above ref by more than this are summed relative to their own maximum
+
+// Sums over the 32 lanes of a half for all sixteen registers: halves of what is left change places, so that a lane ends with the
+// sum of one register, lane_register()
+__device__ __forceinline__ float fold(cd_f16_t v, const bool max_of) {
+  auto f = [&](float x, float y) { return max_of ? fmaxf(x, y) : x + y; };
+  const int l = threadIdx.x;
+  float a[8], b[4], c[2];
 #pragma unroll
-    for (int g = 0; g < NG; ++g) scales[w][n][g] = tok.scale[g];
+  for (int i = 0; i < 8; ++i) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 8]), false, false);
+    a[i] = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
   }
-  const uint32_t real = (uint32_t)__ballot(tok.real);  // (the lane halves hold the same tokens)
-  __syncthreads();
-  float sc[NG][16];
 #pragma unroll
-  for (int r = 0; r < 16; ++r)
+  for (int i = 0; i < 4; ++i) b[i] = f(l & 8 ? a[i + 4] : a[i], dppf<0x128>(l & 8 ? a[i] : a[i + 4]));        // row_ror:8
 #pragma unroll
-    for (int g = 0; g < NG; ++g) sc[g][r] = scales[w][8 * (r >> 2) + 4 * hh + (r & 3)][g];
-  const int all_from = real == ~0u ? max(token0 + 31 - s.past, 0) * a.gq : rows + kRows;  // rows that see all of the wave's tokens
-  const int some_from = max(token0 - s.past, 0) * a.gq;                                    // rows that see some
+  for (int i = 0; i < 2; ++i) c[i] = f(l & 4 ? b[i + 2] : b[i], dppf<0x141>(l & 4 ? b[i] : b[i + 2]));        // row_half_mirror
+  const float d = f(l & 2 ? c[1] : c[0], dppf<0x4E>(l & 2 ? c[0] : c[1]));                                     // quad_perm 2 3 0 1
+  return f(d, dppf<0xB1>(d));                                                                                 // quad_perm 1 0 3 2
+}
+// Of the instructions around: a product, then V of the vector ALU, N times
+template <int N, int V>
+__device__ __forceinline__ void in_turn() {
+  if constexpr (N > 0) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x402, V, 0);
+    in_turn<N - 1, V>();
+  }
+}
+// The row (of its tile) of a lane's fold
+__device__ __forceinline__ int fold_row(int l) {
+  const int r = ((l >> 4) & 1) << 3 | ((l >> 3) & 1) << 2 | ((l >> 2) & 1) << 1 | ((l >> 1) & 1);
+  return 8 * (r >> 2) + 4 * (l >> 5) + (r & 3);
+}
+
+}  // namespace
+
+template <int NG, int PASS>
+__global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a) {
+  __shared__ __align__(16) RowTile lds[3];
+  __shared__ float2 both[2][4][kRows], stats[PASS == 1 ? kChunkTiles : 1][kRows];
+  __shared__ float top_of[4][kRows];
+  // Heads come first, so that the blocks of a head share an XCD's L2, then ranges: the engines of an XCD take
+  // blocks in turn, which by sequences of different lengths leaves some with more to do. Last chunks go first: those that most ranges see
+  const int H = a.cv.num_kv_heads, BH = a.B * H, other = blockIdx.x / H, bh = other / a.ranges % a.B * H + blockIdx.x % H;
+  const Span s = span_of(a, bh / H);
+  const Share me = share_of(a, bh, other % a.ranges, a.chunks - 1 - other / a.ranges / a.B, s);
+  if (me.t0 >= me.t1 && (PASS == 1 || a.chunks > 1 || me.first >= s.ctx)) return;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, hh = l >> 5, token0 = me.first + 64 * w;
+  const uint8_t* tiles = a.ops + ((size_t)s.tile0 * H + me.h) * kTileBytes;
+  Token<NG> tok[2];
+  float sum[2] = {0.0f, 0.0f};
+  int from[2];  // rows that see the lane's tokens, less its half's 4
+  int all_from = 0, some_from = 0;  // tiles from which all of the wave's tokens are seen by every row, some by some
+  auto load = [&] {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      tok[u].load(a, me.b, me.h, token0 + 32 * u + n, s.ctx, hh);
+      from[u] = tok[u].real ? max(token0 + 32 * u + n - s.past, 0) * a.gq - 4 * hh : INT32_MAX;
+    }
+    const bool whole = __all(tok[0].real && tok[1].real), any = __any(tok[0].real || tok[1].real);
+    all_from = PASS == 1 && !whole ? me.t1 : (max(min(token0 + 63, s.ctx - 1) - s.past, 0) * a.gq + kRows - 1) / kRows;
+    some_from = any ? max(token0 - s.past, 0) * a.gq / kRows : me.t1;
+  };
+  // Eight steps a tile (a quarter of the products of one token tile each): while the matrix cores form a step's products the
+  // vector ALU adds the last one's to the scores, in the first two also sums the tile before. X: that tile's
+  // scores less ref (L), then this one's.
+  cd_f16_t X[2] = {splat16(-INFINITY), splat16(-INFINITY)};
+  bool pending = false;
+  auto scores = [&](const RowTile& ops, auto&& beside) {
+    cd_h8_t group = ops.group[n], op[2][2][2];  // [quarter][high, low]
+    if (hh) group = cd_h8_t{};
+    auto read = [&](int q) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) op[q & 1][0][x] = ops.hi[2 * q + x][l], op[q & 1][1][x] = ops.lo[2 * q + x][l];
+    };
+    read(0);
+    cd_f16_t D[2];
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        if (PASS == 2 ? u == 0 && q < 3 : u == 1 && q < 3) read(q + 1);
+        const cd_h8_t(&y)[2][2] = op[q & 1];
+        D[u] = product(y[0][0], tok[u].code[2 * q], NG == 4 || q == 0 ? splat16(0.0f) : D[u]);
+        D[u] = product(y[1][0], tok[u].code[2 * q], D[u]);
+        D[u] = product(y[0][1], tok[u].code[2 * q + 1], D[u]);
+        D[u] = product(y[1][1], tok[u].code[2 * q + 1], D[u]);
+        beside(2 * q + u);
+        if (q == 0) X[u] = product(group, tok[u].zero, splat16(0.0f));
+        if (NG == 4 && q + u > 0) {
+          const int v = u ^ 1, g = u == 1 ? q : q - 1;
+#pragma unroll
+          for (int r = 0; r < 16; ++r) X[v][r] = __builtin_fmaf(tok[v].scale[NG == 4 ? g : 0], D[v][r], X[v][r]);
+        }
+        // products and vector instructions in turn: a wave issues in order, and each product waits for the one before
+        if (q == 0)
+          in_turn<5, 8>();
+        else
+          in_turn<4, 4>();
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    const float* base = PASS == 1 ? ops.ref : ops.lse;
+    const float down = ops.down;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const float4 v = *reinterpret_cast<const float4*>(&base[8 * x + 4 * hh]);
+      const float less[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+      for (int y = 0; y < 4; ++y)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int r = 4 * x + y;
+          if (u == 1 || NG == 1) X[u][r] = __builtin_fmaf(tok[u].scale[NG - 1], D[u][r], X[u][r]);
+          X[u][r] = __builtin_fmaf(X[u][r], down, -less[y]);
+        }
+    }
+  };
+  // A tile's sums from its X: step 0 and 1 the token tiles', step 2, in PASS 1, over the wave's tokens
+  cd_f16_t v;
+  auto sums = [&](int i, int t) {
+    if (i > 2) return;
+    if (i == 2) {
+      if (PASS == 2 || !pending) return;
+      const float all = fold(v, false);
+      if ((l & 1) == 0) both[t & 1][w][fold_row(l)] = make_float2(0.0f, all);
+      return;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float x = __builtin_amdgcn_exp2f(X[i][r]);
+      if constexpr (PASS == 2)
+        sum[i] += x;
+      else
+        v[r] = i == 0 ? x : v[r] + x;
+    }
+  };
+  auto all_sums = [&](int t) {
+    for (int i = 0; i < 3; ++i) sums(i, t);
+    X[0] = X[1] = splat16(-INFINITY);
+    pending = false;
+  };
+  // PASS 1: relative to the rows' maxima, which lie far from ref
+  auto peak_sums = [&](int t) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] = fmaxf(X[0][r], X[1][r]);
+    float top = fold(v, true);
+    top = top == -INFINITY ? 0.0f : top;
+    top_of[w][fold_row(l)] = top;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float m = top_of[w][8 * (r >> 2) + 4 * hh + (r & 3)];
+      v[r] = __builtin_amdgcn_exp2f(X[0][r] - m) + __builtin_amdgcn_exp2f(X[1][r] - m);
+    }
+    const float all = fold(v, false);
+    if ((l & 1) == 0) both[t & 1][w][fold_row(l)] = make_float2(top, all);
+    X[0] = X[1] = splat16(-INFINITY);
+    pending = false;
+  };
+  auto far_off = [&]() {
+    float m = X[0][0];
+#pragma unroll
+    for (int r = 1; r < 32; ++r) m = fmaxf(m, X[r >> 4][r & 15]);
+    return __any(m > kFar);
+  };
+  // PASS 1: the waves' sums of a tile, relative to its ref
   auto join = [&](int t) {
-    const float2(&x)[kWaves][kRows] = both[t & 1];
+    const float2(&x)[4][kRows] = both[t & 1];
     float top = -INFINITY, all = 0.0f;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) top = fmaxf(top, x[i][n].x);
+    for (int i = 0; i < 4; ++i) top = fmaxf(top, x[i][n].y == 0.0f ? -INFINITY : x[i][n].x);
     const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
-    for (int i = 0; i < kWaves; ++i) all = __builtin_fmaf(x[i][n].y, __builtin_amdgcn_exp2f(x[i][n].x - base), all);
-    stats[t - me.t0][n] = make_float2(top, all);
+    for (int i = 0; i < 4; ++i) all = x[i][n].y == 0.0f ? all : __builtin_fmaf(x[i][n].y, __builtin_amdgcn_exp2f(x[i][n].x - base), all);
+    stats[t - me.t0][n] = make_float2(base, all);
   };
-  for_tiles<kWaves>(a, tiles, me.t0, me.t1, lds, [&](int t, const RowTile& ops) {
-    if (t > me.t0 && w == ((t - 1) & 7)) join(t - 1);
-    float m = -INFINITY, sum = 0.0f;
-    if (kRows * t + kRows > some_from && real != 0) {
-      cd_h8_t group = ops.group[n];
-      if (hh) group = cd_h8_t{};
-      cd_f16_t S = product(tok.zero, group, splat16(0.0f));
-      const float down = ops.down;
+  for_tiles<4>(a, tiles, me.t0, me.t1, lds, load, [&](int t, const RowTile& ops) {
+    // (the tile before last is complete in every wave)
+    if (PASS == 1 && t >= me.t0 + 2 && w == (t & 3)) join(t - 2);
+    if (t >= all_from) {
+      scores(ops, [&](int i) { sums(i, t - 1); });
+      pending = true;
+    } else {
+      if (pending) all_sums(t - 1);
+      if (t >= some_from) {
+        scores(ops, [](int) {});
 #pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        cd_f16_t D = splat16(0.0f);
+        for (int u = 0; u < 2; ++u) {
+          const int least = from[u] - kRows * t;  // of the lane's rows, less its half's 4
 #pragma unroll
-        for (int x = 8 / NG * g; x < 8 / NG * (g + 1); ++x) {
-          D = product(tok.code[x], ops.hi[x][l], D);
-          D = product(tok.code[x], ops.lo[x][l], D);
+          for (int r = 0; r < 16; ++r) X[u][r] = 8 * (r >> 2) + (r & 3) >= least ? X[u][r] : -INFINITY;
         }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) S[r] = __builtin_fmaf(sc[g][r], D[r], S[r]);
+        pending = true;
+      } else if (PASS == 1 && l < kRows) {
+        both[t & 1][w][l] = make_float2(0.0f, 0.0f);
       }
-      if (kRows * t < all_from) {
-        const int lim = s.limit(quotient(min(kRows * t + n, rows - 1), a.gq)) - token0;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int x = 8 * (r >> 2) + 4 * hh + (r & 3);
-          S[r] = x < lim && ((real >> x) & 1) ? S[r] : -INFINITY;
-        }
-      }
-      m = fmaxf(S[0], S[1]);
-#pragma unroll
-      for (int r = 2; r < 16; r += 2) m = fmaxf(fmaxf(m, S[r]), S[r + 1]);
-      m = pair_max(m) * down;
-      const float base = m == -INFINITY ? 0.0f : m;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(S[r], down, -base));
-      sum = pair_sum(sum);
     }
-    if (hh == 0) both[t & 1][w][n] = make_float2(m, sum);
+    if (PASS == 1 && pending && (ops.unsure || far_off())) peak_sums(t);
   });
-  __syncthreads();
-  if (w == ((me.t1 - 1) & 7)) join(me.t1 - 1);
-  __syncthreads();
-  for (int i = threadIdx.x; i < (me.t1 - me.t0) * kRows; i += 64 * kWaves)
-    a.stats[(((size_t)me.range * a.tiles + s.tile0 + me.t0 + i / kRows) * a.cv.num_kv_heads + me.h) * kRows + i % kRows] = stats[i / kRows][i % kRows];
+  if (pending) all_sums(me.t1 - 1);
+  if constexpr (PASS == 1) {
+    __syncthreads();
+    for (int t = max(me.t0, me.t1 - 2); t < me.t1; ++t)
+      if (w == (t & 3)) join(t);
+    __syncthreads();
+    for (int i = threadIdx.x; i < (me.t1 - me.t0) * kRows; i += 256) {
+      const size_t tile = (size_t)(s.tile0 + me.t0 + i / kRows) * H + me.h;
+      const float2 v = stats[i / kRows][i % kRows];
+      a.stats[((size_t)me.range * a.tiles * H + tile) * kRows + i % kRows] = make_float2(v.x + reinterpret_cast<const RowTile*>(a.ops + tile * kTileBytes)->ref[i % kRows], v.y);
+    }
+  } else {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int t = token0 + 32 * u + n;
+      float x = pair_sum(sum[u]);
+      if (!tok[u].real) x = 0.0f;
+      if (hh || t >= s.ctx) continue;
+      if (a.chunks > 1) {
+        a.part[((size_t)me.chunk * BH + bh) * ((size_t)a.ranges * kRangeTokens) + t] = x;
+      } else {
+        const size_t at = (size_t)bh * a.w_stride + t;
+        a.w_out[at] = a.w_in ? __builtin_fmaf(a.decay, a.w_in[at], x) : x;
+      }
+    }
+  }
 }
 
 // ---- L_r of every row. Block: a row tile; eight threads a row, each with every eighth range.
@@ -350,88 +540,6 @@ __global__ __launch_bounds__(256) void weight_lse_kernel(TokenWeightsArgs a) {
 #pragma unroll
   for (int x = 0; x < 8; ++x) sum = __builtin_fmaf(part[x][n].y, __builtin_amdgcn_exp2f(part[x][n].x - base), sum);
   reinterpret_cast<RowTile*>(a.ops + ((size_t)(s.tile0 + t) * H + h) * kTileBytes)->lse[n] = sum == 0.0f ? INFINITY : m + __builtin_amdgcn_logf(sum);
-}
-
-// ---- The sums over the rows. Products are rows x codes, so that a lane holds a token; a wave has 64 of them.
-template <int NG>
-__global__ __launch_bounds__(256, 2) void weight_sums_kernel(TokenWeightsArgs a) {
-  __shared__ __align__(16) RowTile lds[3];
-  const int BH = a.B * a.cv.num_kv_heads, bh = blockIdx.x % BH;
-  const Span s = span_of(a, bh / a.cv.num_kv_heads);
-  const Share me = share_of(a, bh, blockIdx.x / BH % a.ranges, blockIdx.x / BH / a.ranges, s);
-  if (me.t0 >= me.t1 && (a.chunks > 1 || me.first >= s.ctx)) return;
-  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, hh = l >> 5, token0 = me.first + 64 * w;
-  const uint8_t* tiles = a.ops + ((size_t)s.tile0 * a.cv.num_kv_heads + me.h) * kTileBytes;
-  Token<NG> tok[2];
-  float sum[2] = {0.0f, 0.0f};
-  int from[2];  // rows that see the lane's tokens
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    tok[u].load(a, me.b, me.h, token0 + 32 * u + n, s.ctx, hh);
-    from[u] = max(min(token0 + 32 * u + n, s.ctx - 1) - s.past, 0) * a.gq;
-  }
-  const int all_from = max(min(token0 + 63, s.ctx - 1) - s.past, 0) * a.gq, some_from = max(token0 - s.past, 0) * a.gq;
-  for_tiles<4>(a, tiles, me.t0, me.t1, lds, [&](int t, const RowTile& ops) {
-    if (kRows * t + kRows <= some_from || token0 >= s.ctx) return;
-    cd_h8_t group = ops.group[n];
-    if (hh) group = cd_h8_t{};
-    cd_f16_t S[2];
-#pragma unroll
-    for (int u = 0; u < 2; ++u) S[u] = product(group, tok[u].zero, splat16(0.0f));
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      cd_f16_t D[2] = {splat16(0.0f), splat16(0.0f)};
-#pragma unroll
-      for (int x = 8 / NG * g; x < 8 / NG * (g + 1); ++x) {
-        const cd_h8_t hi = ops.hi[x][l], lo = ops.lo[x][l];
-#pragma unroll
-        for (int u = 0; u < 2; ++u) D[u] = product(hi, tok[u].code[x], D[u]);
-#pragma unroll
-        for (int u = 0; u < 2; ++u) D[u] = product(lo, tok[u].code[x], D[u]);
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) S[u][r] = __builtin_fmaf(tok[u].scale[g], D[u][r], S[u][r]);
-    }
-    const float down = ops.down;
-    float add[2] = {0.0f, 0.0f};
-    const bool whole = kRows * t >= all_from;
-#pragma unroll
-    for (int x = 0; x < 4; ++x) {
-      const float4 v = *reinterpret_cast<const float4*>(&ops.lse[8 * x + 4 * hh]);
-      const float lse[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-      for (int y = 0; y < 4; ++y)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) S[u][4 * x + y] = __builtin_fmaf(S[u][4 * x + y], down, -lse[y]);
-    }
-    if (!whole) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-#pragma unroll
-        for (int u = 0; u < 2; ++u) S[u][r] = kRows * t + 8 * (r >> 2) + 4 * hh + (r & 3) >= from[u] ? S[u][r] : -INFINITY;
-    }
-#pragma unroll
-    for (int r = 0; r < 16; ++r)
-#pragma unroll
-      for (int u = 0; u < 2; ++u) add[u] += __builtin_amdgcn_exp2f(S[u][r]);
-#pragma unroll
-    for (int u = 0; u < 2; ++u) sum[u] += add[u];
-  });
-#pragma unroll
-  for (int u = 0; u < 2; ++u) {
-    const int t = token0 + 32 * u + n;
-    float x = pair_sum(sum[u]);
-    if (!tok[u].real) x = 0.0f;
-    if (hh || t >= s.ctx) continue;
-    if (a.chunks > 1) {
-      a.part[((size_t)me.chunk * BH + bh) * ((size_t)a.ranges * kRangeTokens) + t] = x;
-    } else {
-      const size_t at = (size_t)bh * a.w_stride + t;
-      a.w_out[at] = a.w_in ? __builtin_fmaf(a.decay, a.w_in[at], x) : x;
-    }
-  }
 }
 
 // ---- The chunks' sums, and the running ones
@@ -731,13 +839,13 @@ hipError_t launch_many(const TokenWeightsArgs& a, hipStream_t s) {
     const long long items = BH * a.seq_tiles;
     const int per = (int)(items / 1024 < 1 ? 1 : items / 1024 > 8 ? 8 : items / 1024);
     const dim3 shares((unsigned)(BH * a.ranges * a.chunks));
-    hipLaunchKernelGGL(weight_rows_kernel, dim3((unsigned)(BH * ((a.seq_tiles + per - 1) / per))), dim3(256), 0, s, a, per);
+    hipLaunchKernelGGL(weight_rows_kernel<NG>, dim3((unsigned)(BH * ((a.seq_tiles + per - 1) / per))), dim3(256), 0, s, a, per);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(weight_stats_kernel<NG>, shares, dim3(64 * kWaves), 0, s, a);
+    hipLaunchKernelGGL((weight_scan_kernel<NG, 1>), shares, dim3(256), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL(weight_lse_kernel, dim3((unsigned)items), dim3(256), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(weight_sums_kernel<NG>, shares, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((weight_scan_kernel<NG, 2>), shares, dim3(256), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (a.chunks != 1) {
