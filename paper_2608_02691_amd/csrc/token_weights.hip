@@ -9,6 +9,8 @@
 //     x = sum_g s_g D_g + sum_g z_g Q_g,   D_g = sum_{c in g} q'_c code_c,   Q_g = sum_{c in g} q'_c,
 // where a code is exact in fp16, q' and Q_g are two fp16 terms each (22 bits) and z_g is fp16 as stored, all products are
 // exact in fp32, and s_g enters in fp32.
+#include <type_traits>
+
 #include "append_core.h"
 #include "chunk_core.h"
 
@@ -17,10 +19,7 @@ namespace int2kv {
 namespace {
 
 constexpr int kRows = 32;                                     // rows of a tile
-#ifndef KCH
-#define KCH 32
-#endif
-constexpr int kChunkTiles = KCH;                               // row tiles of a block at most
+constexpr int kChunkTiles = 32;                               // row tiles of a block at most
 static_assert(kRangeTokens == 4 * 64, "the waves' tokens");
 
 struct Span {
@@ -113,37 +112,6 @@ static_assert(kTileBytes == 17 * 1024, "pieces of 64 lanes x 16 bytes");
 
 __device__ __forceinline__ cd_f16_t product(const cd_h8_t& x, const cd_h8_t& y, const cd_f16_t& c) {
   return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, c, 0, 0, 0);
-}
-
-// The row tiles t0 .. t1 of one KV head, two on their way to LDS while a third is in use. All waves of the block call it.
-// first() runs while the first ones are on their way.
-template <int NW, class First, class F>
-__device__ __forceinline__ void for_tiles(const TokenWeightsArgs& a, const uint8_t* tiles, int t0, int t1, RowTile (&lds)[3], First first, F f) {
-  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const size_t stride = (size_t)a.cv.num_kv_heads * kTileBytes;
-  const uint32_t to = (uint32_t)(uintptr_t)&lds[0];
-  auto issue = [&](int t, int slot) {
-    const uint8_t* from = tiles + t * stride + 16 * l;
-    for (int c = w; c < kPieces; c += NW) ap_dma16(from + 1024 * c, to + (uint32_t)(slot * kTileBytes + 1024 * c));
-  };
-  if (t0 < t1) issue(t0, 0);
-  if (t0 + 1 < t1) issue(t0 + 1, 1);
-  first();
-  int slot = 0;
-  for (int t = t0; t < t1; ++t) {
-    // this tile has landed when at most the next one's pieces are on their way: 17 / NW of them, the first wave's one more
-    static_assert(NW == 8 || NW == 4, "the counts below");
-    if (t + 1 == t1)
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    else if (w == 0)
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPieces / NW + 1) : "memory");
-    else
-      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kPieces / NW) : "memory");
-    __syncthreads();  // and every wave is done with the tile before, whose place the one after the next takes
-    if (t + 2 < t1) issue(t + 2, slot == 0 ? 2 : slot - 1);
-    f(t, lds[slot]);
-    slot = slot == 2 ? 0 : slot + 1;
-  }
 }
 
 // A block's share: a range of tokens of one KV head and a chunk of the row tiles that see it
@@ -286,6 +254,7 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
 // over the range, PASS 2 each token's 2^(x - L) over the rows.
 namespace {
 
+constexpr int kSlots = 4;
 constexpr float kFar = 100.0f;  // scores above ref by more than this are summed relative to their own maximum
 
 // Sums over the 32 lanes of a half for all sixteen registers: halves of what is left change places, so that a lane ends with the
@@ -325,7 +294,7 @@ __device__ __forceinline__ int fold_row(int l) {
 
 template <int NG, int PASS>
 __global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a) {
-  __shared__ __align__(16) RowTile lds[3];
+  __shared__ __align__(16) RowTile lds[kSlots];
   __shared__ float2 both[2][4][kRows], stats[PASS == 1 ? kChunkTiles : 1][kRows];
   __shared__ float top_of[4][kRows];
   // Heads come first, so that the blocks of a head share an XCD's L2, then ranges: the engines of an XCD take
@@ -335,27 +304,50 @@ __global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a)
   const Share me = share_of(a, bh, other % a.ranges, a.chunks - 1 - other / a.ranges / a.B, s);
   if (me.t0 >= me.t1 && (PASS == 1 || a.chunks > 1 || me.first >= s.ctx)) return;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, hh = l >> 5, token0 = me.first + 64 * w;
-  const uint8_t* tiles = a.ops + ((size_t)s.tile0 * H + me.h) * kTileBytes;
+  // ---- Row tiles on their way to LDS, tile t in slot t % kSlots. Half way through a tile (at its start) the next one has landed for every wave
+  // and the one before is done with, so that no wave waits between tiles.
+  const uint8_t* tiles = a.ops + ((size_t)s.tile0 * H + me.h) * kTileBytes + 16 * l;
+  const size_t stride = (size_t)H * kTileBytes;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)&lds[0];
+  auto slot = [&](int t) -> const RowTile& { return lds[t & (kSlots - 1)]; };
+  auto issue = [&](int t) {  // 17 pieces by four waves: the first has one more
+    if (t >= me.t1) return;
+    for (int c = w; c < kPieces; c += 4) ap_dma16(tiles + t * stride + 1024 * c, lds0 + (uint32_t)((t & (kSlots - 1)) * kTileBytes + 1024 * c));
+  };
+  // until tile t has landed, with what came after it, up to `after` tiles, on its way
+  auto landed = [&](int t, auto after) {
+    constexpr int A = decltype(after)::value;
+    if (t + A >= me.t1)
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    else if (w == 0)
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(A * (kPieces / 4 + 1)) : "memory");
+    else
+      asm volatile("s_waitcnt vmcnt(%0)" ::"n"(A * (kPieces / 4)) : "memory");
+    __syncthreads();
+  };
+#pragma unroll
+  for (int t = 0; t < kSlots - 1; ++t) issue(me.t0 + t);
+
   Token<NG> tok[2];
   float sum[2] = {0.0f, 0.0f};
   int from[2];  // rows that see the lane's tokens, less its half's 4
-  int all_from = 0, some_from = 0;  // tiles from which all of the wave's tokens are seen by every row, some by some
-  auto load = [&] {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      tok[u].load(a, me.b, me.h, token0 + 32 * u + n, s.ctx, hh);
-      from[u] = tok[u].real ? max(token0 + 32 * u + n - s.past, 0) * a.gq - 4 * hh : INT32_MAX;
-    }
-    const bool whole = __all(tok[0].real && tok[1].real), any = __any(tok[0].real || tok[1].real);
-    all_from = PASS == 1 && !whole ? me.t1 : (max(min(token0 + 63, s.ctx - 1) - s.past, 0) * a.gq + kRows - 1) / kRows;
-    some_from = any ? max(token0 - s.past, 0) * a.gq / kRows : me.t1;
-  };
+  for (int u = 0; u < 2; ++u) {
+    tok[u].load(a, me.b, me.h, token0 + 32 * u + n, s.ctx, hh);
+    from[u] = tok[u].real ? max(token0 + 32 * u + n - s.past, 0) * a.gq - 4 * hh : INT32_MAX;
+  }
+  const bool whole = __all(tok[0].real && tok[1].real), any = __any(tok[0].real || tok[1].real);
+  // tiles from which all of the wave's tokens are seen by every row, some by some
+  const int all_from = PASS == 1 && !whole ? me.t1 : (max(min(token0 + 63, s.ctx - 1) - s.past, 0) * a.gq + kRows - 1) / kRows;
+  const int some_from = any ? max(token0 - s.past, 0) * a.gq / kRows : me.t1;
+
   // Eight steps a tile (a quarter of the products of one token tile each): while the matrix cores form a step's products the
   // vector ALU adds the last one's to the scores, in the first two also sums the tile before. X: that tile's
   // scores less ref (L), then this one's.
   cd_f16_t X[2] = {splat16(-INFINITY), splat16(-INFINITY)};
   bool pending = false;
-  auto scores = [&](const RowTile& ops, auto&& beside) {
+  auto scores = [&](const RowTile& ops, auto&& beside, auto&& middle) {
+    if constexpr (PASS == 2) middle();  // (in the middle it would cost the second pass registers it does not have)
     cd_h8_t group = ops.group[n], op[2][2][2];  // [quarter][high, low]
     if (hh) group = cd_h8_t{};
     auto read = [&](int q) {
@@ -368,7 +360,8 @@ __global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a)
     for (int q = 0; q < 4; ++q)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        if (PASS == 2 ? u == 0 && q < 3 : u == 1 && q < 3) read(q + 1);
+        if (PASS == 1 && q == 2 && u == 0) middle();
+        if (u == 1 && q < 3) read(q + 1);
         const cd_h8_t(&y)[2][2] = op[q & 1];
         D[u] = product(y[0][0], tok[u].code[2 * q], NG == 4 || q == 0 ? splat16(0.0f) : D[u]);
         D[u] = product(y[1][0], tok[u].code[2 * q], D[u]);
@@ -462,16 +455,21 @@ __global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a)
     for (int i = 0; i < 4; ++i) all = x[i][n].y == 0.0f ? all : __builtin_fmaf(x[i][n].y, __builtin_amdgcn_exp2f(x[i][n].x - base), all);
     stats[t - me.t0][n] = make_float2(base, all);
   };
-  for_tiles<4>(a, tiles, me.t0, me.t1, lds, load, [&](int t, const RowTile& ops) {
-    // (the tile before last is complete in every wave)
-    if (PASS == 1 && t >= me.t0 + 2 && w == (t & 3)) join(t - 2);
+  if (me.t0 < me.t1) landed(me.t0, std::integral_constant<int, 2>());
+  for (int t = me.t0; t < me.t1; ++t) {
+    const RowTile& ops = slot(t);
+    auto middle = [&] {
+      landed(t + 1, std::integral_constant<int, 1>());
+      issue(t + 3);
+      if (PASS == 1 && t > me.t0 && w == (t & 3)) join(t - 1);  // every wave's sums of it are in LDS
+    };
     if (t >= all_from) {
-      scores(ops, [&](int i) { sums(i, t - 1); });
+      scores(ops, [&](int i) { sums(i, t - 1); }, middle);
       pending = true;
     } else {
       if (pending) all_sums(t - 1);
       if (t >= some_from) {
-        scores(ops, [](int) {});
+        scores(ops, [](int) {}, middle);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           const int least = from[u] - kRows * t;  // of the lane's rows, less its half's 4
@@ -479,17 +477,17 @@ __global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a)
           for (int r = 0; r < 16; ++r) X[u][r] = 8 * (r >> 2) + (r & 3) >= least ? X[u][r] : -INFINITY;
         }
         pending = true;
-      } else if (PASS == 1 && l < kRows) {
-        both[t & 1][w][l] = make_float2(0.0f, 0.0f);
+      } else {
+        if (PASS == 1 && l < kRows) both[t & 1][w][l] = make_float2(0.0f, 0.0f);
+        middle();
       }
     }
     if (PASS == 1 && pending && (ops.unsure || far_off())) peak_sums(t);
-  });
+  }
   if (pending) all_sums(me.t1 - 1);
   if constexpr (PASS == 1) {
     __syncthreads();
-    for (int t = max(me.t0, me.t1 - 2); t < me.t1; ++t)
-      if (w == (t & 3)) join(t);
+    if (w == 0) join(me.t1 - 1);
     __syncthreads();
     for (int i = threadIdx.x; i < (me.t1 - me.t0) * kRows; i += 256) {
       const size_t tile = (size_t)(s.tile0 + me.t0 + i / kRows) * H + me.h;
