@@ -142,12 +142,14 @@ __device__ __forceinline__ Share share_of(const TokenWeightsArgs& a, int bh, int
 template <int NG>
 __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, int tiles_per_block) {
   __shared__ float top[4], sums[4][kRows];
+  __shared__ cd_h8_t keys[8][64];  // the first tokens' rows, rounded to fp16: the last wave's
+  __shared__ cd_u4_t in[2][8][64];
   __shared__ __align__(16) RowTile out;
   const int H = a.cv.num_kv_heads, blocks = (a.seq_tiles + tiles_per_block - 1) / tiles_per_block;
   const int h = blockIdx.x % H, at = blockIdx.x / H % blocks, b = blockIdx.x / H / blocks;
   const Span s = span_of(a, b);
   const int tiles = (s.n * a.gq + kRows - 1) / kRows;
-  const int w = threadIdx.x >> 6, l = threadIdx.x & 63, n = l & 31, hh = l >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, hh = l >> 5;
   if (at * tiles_per_block >= tiles || s.ctx == 0) return;
   cd_u4_t R[8][3];  // of column 32 w + n, rows 16 kk + 8 hh ..
 #pragma unroll
@@ -160,29 +162,37 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
     }
     R[kk][0] = pack_terms(x), R[kk][1] = pack_terms(y), R[kk][2] = pack_terms(z);
   }
-  cd_h8_t keys[8];  // the first tokens' rows, rounded to fp16
   uint32_t real = 0;
   if (w == 3) {
     Token<NG> first;
     first.load(a, b, h, n, s.ctx, hh);
     real = (uint32_t)__ballot(first.real);
 #pragma unroll
-    for (int x = 0; x < 8; ++x)
+    for (int x = 0; x < 8; ++x) {
+      cd_h8_t k;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float z = NG == 4 ? first.low[x * NG / 8] : first.low[0];
-        keys[x][j] = (_Float16)__builtin_fmaf((float)first.code[x][j], first.scale[x * NG / 8], z);
-      }
+      for (int j = 0; j < 8; ++j) k[j] = (_Float16)__builtin_fmaf((float)first.code[x][j], first.scale[x * NG / 8], first.low[x * NG / 8]);
+      keys[x][l] = k;
+    }
   }
-  for (int t = at * tiles_per_block; t < min(tiles, (at + 1) * tiles_per_block); ++t) {
-    const int row = kRows * t + n, tok = quotient(row, a.gq);
-    const bool live = row < s.n * a.gq;
-    const uint16_t* q = a.q + (s.start + (live ? tok : 0)) * a.q_stride + (size_t)(h * a.gq + (live ? row - tok * a.gq : 0)) * kHeadDim + 8 * hh;
+  const int t0 = at * tiles_per_block, t1 = min(tiles, t0 + tiles_per_block), rows = s.n * a.gq;
+  // a tile's rows on their way to LDS as the products take them, a quarter by each wave; the last one's again behind the last
+  auto fetch = [&](int t) {
+    const int row = min(kRows * t + n, rows - 1), tok = quotient(row, a.gq);
+    const uint16_t* q = a.q + (s.start + tok) * a.q_stride + (size_t)(h * a.gq + row - tok * a.gq) * kHeadDim + 8 * hh;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) ap_dma16(q + 16 * (2 * w + i), (uint32_t)(uintptr_t)&in[t & 1][2 * w + i][0]);
+  };
+  fetch(t0);
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+  for (int t = t0; t < t1; ++t) {
+    if (t + 1 < t1) fetch(t + 1);
+    const bool live = kRows * t + n < rows;
     cd_f16_t d = splat16(0.0f);
 #pragma unroll
     for (int kk = 0; kk < 8; ++kk) {
-      cd_u4_t x = *reinterpret_cast<const cd_u4_t*>(q + 16 * kk);
-      if (!live) x = cd_u4_t{0, 0, 0, 0};
+      const cd_u4_t x = live ? in[t & 1][kk][l] : cd_u4_t{0, 0, 0, 0};
 #pragma unroll
       for (int i = 0; i < 3; ++i)
         d = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(cd_b8_t, R[kk][i]), __builtin_bit_cast(cd_b8_t, x), d, 0, 0, 0);
@@ -212,6 +222,7 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
     }
     sum = pair_sum(sum);
     if (hh == 0) sums[w][n] = sum;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // the next tile's rows (and the last one's stores)
     __syncthreads();
     uint4* to = reinterpret_cast<uint4*>(a.ops + ((size_t)(s.tile0 + t) * H + h) * kTileBytes);
     RowTile& tile = *reinterpret_cast<RowTile*>(to);
@@ -219,8 +230,8 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
     if (w == 3) {
       cd_f16_t S = splat16(0.0f);
 #pragma unroll
-      for (int x = 0; x < 8; ++x) S = product(keys[x], out.hi[x][l], S);
-      const int lim = live ? s.limit(tok) : 0;
+      for (int x = 0; x < 8; ++x) S = product(keys[x][l], out.hi[x][l], S);
+      const int lim = live ? s.limit(quotient(kRows * t + n, a.gq)) : 0;
       float m = -INFINITY;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
@@ -562,74 +573,92 @@ constexpr int kFewRows = 8;
 constexpr int kPieceTokens = 512, kPiecePages = kPieceTokens / kBlock / 4;  // of a block; pages of each of its four waves
 constexpr int kJoinTokens = 1024;
 
-// The rows' operands for products of 16 rows x 16 tokens: row 4 j + g of tile t holds group g's channels of query row
-// 4 t + j and zeros elsewhere, so that D's registers are the four groups' sums of one query row and token. A lane's
-// eight channels (lane = 16 quad + 4 j + g): positions 2 g, 2 g + 1 of words 2 quad, 2 quad + 1.
+// The rows' operands for products of 16 rows x 16 tokens, with zeros where a row has no part in a group, so that one chain of
+// products forms several groups' sums. Up to four rows: operand row 4 j + g is group g of row j, and D's registers are the four groups of
+// one row. Up to eight: operand row 2 j + g % 2, two D, for g / 2. A lane's eight channels (lane = 16 quad + operand
+// row): positions 2 g, 2 g + 1 of words 2 quad, 2 quad + 1.
+// Codes are used as they lie: as an fp16 number their bits at 2 p are the subnormal code 2^(2 p - 24), which the matrix cores take
+// exactly, and the queries' operands carry 2^(-2 p). So one AND makes two channels.
 struct FewOps {
-  cd_h8_t term[2][2][64];  // [tile][high, low]
-  float sum[2][4][4];      // Q_g of [tile][row]
+  cd_h8_t term[2][2][64];  // [group / 2 (up to eight rows)][high, low]
+  float sum[kFewRows][4];  // of a row's channels of each group
   float down, pad[3];
 };
 
 __device__ __forceinline__ cd_f4_t product16(const cd_h8_t& x, const cd_h8_t& y, const cd_f4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
 }
+// Positions P, P + 1 (both below 5 or not) of two words
+template <int P>
+__device__ __forceinline__ uint32_t bits_at(uint32_t w, uint32_t hi) {
+  return P < 5 ? w & in_sgpr((3u << 2 * P) * 0x10001u) : hi & in_sgpr((3u << (2 * P - 10)) * 0x10001u);
+}
+template <int P>
+__device__ __forceinline__ cd_h8_t bits_of(uint32_t u, uint32_t uh, uint32_t v, uint32_t vh) {
+  return __builtin_bit_cast(cd_h8_t, cd_u4_t{bits_at<P>(u, uh), bits_at<P + 1>(u, uh), bits_at<P>(v, vh), bits_at<P + 1>(v, vh)});
+}
 
 }  // namespace
 
-// Block: one (sequence, KV head). Thread: channel c of every other row.
-__global__ __launch_bounds__(256) void weight_few_rows_kernel(TokenWeightsArgs a) {
-  __shared__ float q[kFewRows][kHeadDim], top[4];
-  const int H = a.cv.num_kv_heads, h = blockIdx.x % H, b = blockIdx.x / H, c = threadIdx.x & 127, odd = threadIdx.x >> 7;
+// Block: one (sequence, KV head). Thread: channel c, a sixteenth of the sum's terms (all loads on their way at once); then one
+// row of it. Bound by the latency of its loads.
+__global__ __launch_bounds__(1024) void weight_few_rows_kernel(TokenWeightsArgs a) {
+  __shared__ float q[kFewRows][kHeadDim], part[8][kFewRows][kHeadDim], top[16];
+  const int H = a.cv.num_kv_heads, h = blockIdx.x % H, b = blockIdx.x / H, c = threadIdx.x & 127, k = threadIdx.x >> 7;
+  const float* R = a.R_k + ((size_t)h * kHeadDim + 16 * k) * kHeadDim + c;
+  float x[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) x[i] = R[(size_t)i * kHeadDim];
   const Span s = span_of(a, b);
   const int rows = min(s.n * a.gq, kFewRows);
   if (rows == 0 || s.ctx == 0) return;
-  for (int i = threadIdx.x; i < kFewRows * kHeadDim; i += 256) {
-    const int r = i >> 7, tok = r / a.gq;
-    q[r][i & 127] = r < rows ? bf16_bits_to_f32(a.q[(s.start + tok) * a.q_stride + (size_t)(h * a.gq + r - tok * a.gq) * kHeadDim + (i & 127)]) : 0.0f;
+  {
+    const int tok = k / a.gq;
+    q[k][c] = k < rows ? bf16_bits_to_f32(a.q[(s.start + tok) * a.q_stride + (size_t)(h * a.gq + k - tok * a.gq) * kHeadDim + c]) : 0.0f;
   }
   __syncthreads();
-  float d[kFewRows / 2] = {};
-  const float* R = a.R_k + (size_t)h * kHeadDim * kHeadDim + c;
-#pragma unroll 32
-  for (int k = 0; k < kHeadDim; ++k) {
-    const float x = R[(size_t)k * kHeadDim];
 #pragma unroll
-    for (int i = 0; i < kFewRows / 2; ++i) d[i] = __builtin_fmaf(q[2 * i + odd][k], x, d[i]);
-  }
-  float big = 0.0f;
+  for (int r = 0; r < kFewRows; ++r) {
+    float d = 0.0f;
 #pragma unroll
-  for (int i = 0; i < kFewRows / 2; ++i) {
-    d[i] *= kLogit2;
-    big = fmaxf(big, fabsf(d[i]));
+    for (int i = 0; i < 16; ++i) d = __builtin_fmaf(q[r][16 * k + i], x[i], d);
+    part[k][r][c] = d;
   }
+  __syncthreads();
+  const int r = k;
+  float d = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) d += part[i][r][c];
+  d *= kLogit2;
+  float big = fabsf(d);
 #pragma unroll
   for (int step = 32; step > 0; step >>= 1) big = fmaxf(big, __shfl_xor(big, step));
   if ((threadIdx.x & 63) == 0) top[threadIdx.x >> 6] = big;
   __syncthreads();
-  big = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
-  const uint32_t e = min(max(__float_as_uint(big) >> 23, 8u), 254u);
-  const float up = __uint_as_float((261u - e) << 23);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) big = fmaxf(big, top[i]);
+  // the largest element to 2^13 .. 2^14
+  const uint32_t e = min(max(__float_as_uint(big) >> 23, 14u), 240u);
   FewOps& out = reinterpret_cast<FewOps*>(a.few)[(size_t)b * H + h];
-  const int g = c >> 5, p = (c >> 4) & 1, word = (c & 15) >> 1, element = ((word & 1) << 2) | (p << 1) | (c & 1);
-#pragma unroll
-  for (int i = 0; i < kFewRows / 2; ++i) {
-    const int r = 2 * i + odd, lane = 16 * (word >> 1) + 4 * (r & 3) + g;
-    const float x = d[i] * up;
-    const _Float16 hi = (_Float16)x;
-    reinterpret_cast<_Float16*>(&out.term[r >> 2][0][lane])[element] = hi;
-    reinterpret_cast<_Float16*>(&out.term[r >> 2][1][lane])[element] = (_Float16)(x - (float)hi);
-    float sum = x;  // over the group: 32 lanes
-#pragma unroll
-    for (int step = 16; step > 0; step >>= 1) sum += __shfl_xor(sum, step);
-    if ((c & 31) == 0) out.sum[r >> 2][r & 3][g] = sum;
+  const int g = c >> 5, pos = c >> 4, word = (c & 15) >> 1, element = ((word & 1) << 2) | ((pos & 1) << 1) | (c & 1);
+  const float y = d * __uint_as_float((267u - e) << 23), z = y * __uint_as_float((127u - 2 * (pos % 5)) << 23);
+  const _Float16 hi = (_Float16)z, lo = (_Float16)(z - (float)hi);
+  const bool narrow = a.row_cap <= 4;
+  if (!narrow || r < 4) {
+    const int at = narrow ? 0 : g >> 1, lane = 16 * (word >> 1) + (narrow ? 4 * r + g : 2 * r + (g & 1));
+    reinterpret_cast<_Float16*>(&out.term[at][0][lane])[element] = hi;
+    reinterpret_cast<_Float16*>(&out.term[at][1][lane])[element] = lo;
   }
-  if (threadIdx.x == 0) out.down = __uint_as_float((e - 7u) << 23);
+  float sum = y;  // over the group: 32 lanes
+#pragma unroll
+  for (int step = 16; step > 0; step >>= 1) sum += __shfl_xor(sum, step);
+  if ((c & 31) == 0) out.sum[r][g] = sum;
+  if (threadIdx.x == 0) out.down = __uint_as_float((e - 13u) << 23);
 }
 
 // Block: 512 tokens of one KV head, a wave eight pages of them; all loads of a wave are on their way at once. Lane: one token
-// of a page and one row of each tile. TILES: of four rows.
-template <int NG, int TILES>
+// of a page and ROWS rows, 1 (up to four of a KV head) or 2.
+template <int NG, int ROWS>
 __global__ __launch_bounds__(256) void weight_few_scores_kernel(TokenWeightsArgs a) {
   using Lay = Rec<NG>;
   __shared__ float2 both[4][kFewRows];
@@ -652,60 +681,63 @@ __global__ __launch_bounds__(256) void weight_few_scores_kernel(TokenWeightsArgs
     for (int g = 0; g < NG; ++g) meta[i][g] = reinterpret_cast<const uint32_t*>(rec + Lay::kOffKMeta + 4 * NG * t)[g];
   }
   const FewOps& ops = reinterpret_cast<const FewOps*>(a.few)[(size_t)b * H + h];
-  const float down = ops.down;
-  cd_h8_t A[TILES][2][4];  // [tile][high, low][group]
-  float Q[TILES][4];
-  int lim[TILES];
+  const float down = ops.down, down24 = down * 0x1p24f;
+  cd_h8_t A[2][4];  // [high, low][group]
+  float Q[ROWS][4];
+  int lim[ROWS];
   const cd_h8_t none{};
 #pragma unroll
-  for (int k = 0; k < TILES; ++k) {
+  for (int x = 0; x < 2; ++x)
 #pragma unroll
-    for (int x = 0; x < 2; ++x) {
-      const cd_h8_t y = ops.term[k][x][l];
-#pragma unroll
-      for (int g = 0; g < 4; ++g) A[k][x][g] = (l & 3) == g ? y : none;
+    for (int g = 0; g < 4; ++g) {
+      if constexpr (ROWS == 1)
+        A[x][g] = (l & 3) == g ? ops.term[0][x][l] : none;
+      else
+        A[x][g] = (l & 1) == (g & 1) ? ops.term[g >> 1][x][l] : none;
     }
-    const float4 v = *reinterpret_cast<const float4*>(ops.sum[k][quad]);
+#pragma unroll
+  for (int k = 0; k < ROWS; ++k) {
+    const int row = ROWS * quad + k;
+    const float4 v = *reinterpret_cast<const float4*>(ops.sum[row]);
     Q[k][0] = v.x * down, Q[k][1] = v.y * down, Q[k][2] = v.z * down, Q[k][3] = v.w * down;
-    const int row = 4 * k + quad;
+    if constexpr (NG == 1) Q[k][0] = (Q[k][0] + Q[k][1]) + (Q[k][2] + Q[k][3]);
     lim[k] = row < s.n * a.gq ? s.limit(row / a.gq) : 0;
   }
-  float m[TILES], sum[TILES];
+  float m[ROWS], sum[ROWS];
 #pragma unroll
-  for (int k = 0; k < TILES; ++k) m[k] = kNone, sum[k] = 0.0f;
+  for (int k = 0; k < ROWS; ++k) m[k] = kNone, sum[k] = 0.0f;
   float* scores = a.scores + ((size_t)b * H + h) * a.page_cap * (kBlock * a.row_cap);
 #pragma unroll
   for (int i = 0; i < kPiecePages; ++i) {
     if (page0 + i >= pages) break;
-    cd_h8_t c[4];
     const uint32_t u = code[i].x, v = code[i].y, uh = u >> 10, vh = v >> 10;
-    auto put = [&](cd_h8_t& y, cd_h2_t p, cd_h2_t q, cd_h2_t r, cd_h2_t z) { y = cd_h8_t{p.x, p.y, q.x, q.y, r.x, r.y, z.x, z.y}; };
-    put(c[0], land_position<0>(u, uh), land_position<1>(u, uh), land_position<0>(v, vh), land_position<1>(v, vh));
-    put(c[1], land_position<2>(u, uh), land_position<3>(u, uh), land_position<2>(v, vh), land_position<3>(v, vh));
-    put(c[2], land_position<4>(u, uh), land_position<5>(u, uh), land_position<4>(v, vh), land_position<5>(v, vh));
-    put(c[3], land_position<6>(u, uh), land_position<7>(u, uh), land_position<6>(v, vh), land_position<7>(v, vh));
+    const cd_h8_t c[4] = {bits_of<0>(u, uh, v, vh), bits_of<2>(u, uh, v, vh), bits_of<4>(u, uh, v, vh), bits_of<6>(u, uh, v, vh)};
     const int token = kBlock * (page0 + i) + t;
+    cd_f4_t D[ROWS];
 #pragma unroll
-    for (int k = 0; k < TILES; ++k) {
-      cd_f4_t D = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int g = 0; g < 4; ++g) {
+      cd_f4_t& d = D[ROWS == 1 ? 0 : g >> 1];
+      if (g == 0 || (ROWS == 2 && g == 2)) d = cd_f4_t{0.0f, 0.0f, 0.0f, 0.0f};
+      d = product16(A[0][g], c[g], d);
+      d = product16(A[1][g], c[g], d);
+    }
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        D = product16(A[k][0][g], c[g], D);
-        D = product16(A[k][1][g], c[g], D);
-      }
-      float x = 0.0f;
+    for (int k = 0; k < ROWS; ++k) {
+      float d[4];  // the row's groups
+#pragma unroll
+      for (int g = 0; g < 4; ++g) d[g] = ROWS == 1 ? D[0][g] : D[g >> 1][2 * k + (g & 1)];
+      float x = 0.0f, z = 0.0f;
       if constexpr (NG == 4) {
-        float z = 0.0f;
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
-          x = __builtin_fmaf(f16_bits_to_f32(meta[i][g] & 0xFFFFu), D[g], x);
+          x = __builtin_fmaf(f16_bits_to_f32(meta[i][g] & 0xFFFFu), d[g], x);
           z = __builtin_fmaf(f16_bits_to_f32(meta[i][g] >> 16), Q[k][g], z);
         }
-        x = __builtin_fmaf(x, down, z);
       } else {
-        x = __builtin_fmaf(f16_bits_to_f32(meta[i][0] & 0xFFFFu) * down, (D[0] + D[1]) + (D[2] + D[3]),
-                           f16_bits_to_f32(meta[i][0] >> 16) * ((Q[k][0] + Q[k][1]) + (Q[k][2] + Q[k][3])));
+        x = f16_bits_to_f32(meta[i][0] & 0xFFFFu) * ((d[0] + d[1]) + (d[2] + d[3]));
+        z = f16_bits_to_f32(meta[i][0] >> 16) * Q[k][0];
       }
+      x = __builtin_fmaf(x, down24, z);
       x = (real >> i) & 1 && token < lim[k] ? x : -INFINITY;
       // the reference moves when a score exceeds it by 2^40, which fp32's sums have room for
       if (__any(x > m[k] + 40.0f)) {
@@ -714,17 +746,17 @@ __global__ __launch_bounds__(256) void weight_few_scores_kernel(TokenWeightsArgs
         m[k] = top;
       }
       sum[k] += __builtin_amdgcn_exp2f(x - m[k]);
-      if (4 * k + quad < a.row_cap) scores[((size_t)(page0 + i) * a.row_cap + 4 * k + quad) * kBlock + t] = x;
+      if (ROWS * quad + k < a.row_cap) scores[((size_t)(page0 + i) * a.row_cap + ROWS * quad + k) * kBlock + t] = x;
     }
   }
 #pragma unroll
-  for (int k = 0; k < TILES; ++k) {
+  for (int k = 0; k < ROWS; ++k) {
     const float top = row_max16(m[k]);
     const float all = row_sum16(sum[k] * __builtin_amdgcn_exp2f(m[k] - top));
-    if (t == 0) both[w][4 * k + quad] = make_float2(top, all);
+    if (t == 0) both[w][ROWS * quad + k] = make_float2(top, all);
   }
   __syncthreads();
-  if (threadIdx.x < 4 * TILES) {
+  if (threadIdx.x < 4 * ROWS) {
     float top = kNone, all = 0.0f;
 #pragma unroll
     for (int x = 0; x < 4; ++x) top = fmaxf(top, both[x][threadIdx.x].x);
@@ -815,7 +847,7 @@ namespace {
 template <int NG>
 hipError_t launch_few(const TokenWeightsArgs& a, hipStream_t s) {
   const long long H = a.cv.num_kv_heads;
-  hipLaunchKernelGGL(weight_few_rows_kernel, dim3((unsigned)(a.B * H)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL(weight_few_rows_kernel, dim3((unsigned)(a.B * H)), dim3(1024), 0, s, a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   const dim3 grid((unsigned)(a.B * H * a.pieces));
