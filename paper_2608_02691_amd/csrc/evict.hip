@@ -1,6 +1,5 @@
 // The tokens of a cache that stay, and their rows' move (int2kv_select_tokens, int2kv_move_tokens).
-#include "common.h"
-#include "kernels.h"
+#include "chunk_core.h"
 
 namespace int2kv {
 
@@ -17,10 +16,27 @@ __device__ __forceinline__ uint32_t order_of(float w) {
 
 }  // namespace
 
-// Block: one (sequence, KV head). The threshold comes byte by byte from histograms of the keys that share the bytes so far.
+namespace {
+
+// Sum of the waves' numbers before this wave, and of all
+__device__ __forceinline__ int2 across(const int* waves) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int x = lane < kSelectWaves ? waves[lane] : 0, upto = wave_scan(x);
+  return make_int2(__builtin_amdgcn_readlane(upto - x, wave), __builtin_amdgcn_readlane(upto, 63));
+}
+
+}  // namespace
+
+// Block: one (sequence, KV head). Thread i has tokens 4 i .. of every 4,096, counted from the 16-byte boundary at or before the
+// list; up to 4,096 J tokens are read once and kept in registers, longer lists a span of so many at a time, again in every
+// pass. The threshold, the need-th largest key, comes in three passes from histograms of 11, 11 and 10 bits of the keys that
+// share the bits so far; then the kept tokens' places are their ranks.
+template <int J>
 __global__ __launch_bounds__(kSelectThreads) void select_tokens_kernel(SelectArgs a) {
-  __shared__ int bins[256], waves[kSelectWaves], found[2];
-  const int b = blockIdx.x / a.H, h = blockIdx.x - b * a.H, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  constexpr int kBins = 2048, kStep = 4 * kSelectThreads, kSpan = J * kStep;
+  static_assert(J * kSelectWaves <= 128, "two counts a lane");
+  __shared__ int bins[kBins], waves[kSelectWaves], found[2], counts[128];
+  const int b = blockIdx.x / a.H, h = blockIdx.x - b * a.H, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int len = min(max(a.lens[b], 0), a.max_ctx), keep = min(len, a.budget);
   const float* w = a.weights + ((size_t)b * a.H + h) * a.stride;
   int32_t* kept = a.kept + ((size_t)b * a.H + h) * a.kept_stride;
@@ -31,52 +47,114 @@ __global__ __launch_bounds__(kSelectThreads) void select_tokens_kernel(SelectArg
   }
   const int lo = min(a.sink, len), hi = max(lo, len - a.recent);  // lo .. hi - 1 compete for the places that are left
   int need = keep - lo - (len - hi);
+  // from the boundary on, a thread's four tokens are one load where all four are the list's
+  const int lead = (int)((reinterpret_cast<uintptr_t>(w) >> 2) & 3), end = len + lead;
+  uint32_t keys[J][4];
+  auto token = [&](int s0, int j) { return s0 + j * kStep + 4 * tid - lead; };  // the first of the thread's
+  auto read = [&](int s0) {
+    float4 v[J];
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int i = token(s0, j);
+      v[j] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      if (i >= 0 && i + 4 <= len)
+        v[j] = *reinterpret_cast<const float4*>(w + i);
+      else if (i + 4 > 0 && i < len)
+        v[j] = make_float4(w[max(i, 0)], w[min(max(i + 1, 0), len - 1)], w[min(max(i + 2, 0), len - 1)], w[min(i + 3, len - 1)]);
+    }
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+      keys[j][0] = order_of(v[j].x), keys[j][1] = order_of(v[j].y), keys[j][2] = order_of(v[j].z), keys[j][3] = order_of(v[j].w);
+  };
+  const bool once = end <= kSpan;
+  if (once) read(0);
+  for (int i = tid; i < kBins; i += kSelectThreads) bins[i] = 0;
   uint32_t prefix = 0;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = tid; i < 256; i += kSelectThreads) bins[i] = 0;
+#pragma unroll
+  for (int pass = 0; pass < 3; ++pass) {
+    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, above_shift = pass == 0 ? 0 : pass == 1 ? 21 : 10;
+    const uint32_t mask = pass == 2 ? 1023u : 2047u;
     __syncthreads();
-    for (int i = lo + tid; i < hi; i += kSelectThreads) {
-      const uint32_t k = order_of(w[i]);
-      if (shift == 24 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&bins[(k >> shift) & 255], 1);
+    for (int s0 = 0; s0 < end; s0 += kSpan) {
+      if (!once) read(s0);
+#pragma unroll
+      for (int j = 0; j < J; ++j) {
+        if (s0 + j * kStep >= end) break;
+        const int i = token(s0, j);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (i + k >= lo && i + k < hi && (pass == 0 || keys[j][k] >> above_shift == prefix >> above_shift))
+            atomicAdd(&bins[(keys[j][k] >> shift) & mask], 1);
+      }
     }
     __syncthreads();
-    if (tid == 0) {  // the byte of the need-th largest
-      int x = 255, above = 0;
-      while (x > 0 && above + bins[x] < need) above += bins[x--];
-      found[0] = x, found[1] = above;
+    // the bin of the need-th largest: thread t has bins 2047 - 2 t and the next lower one
+    const int x = kBins - 1 - 2 * tid, c1 = bins[x], c0 = bins[x - 1];
+    bins[x] = bins[x - 1] = 0;
+    int upto = wave_scan(c0 + c1);
+    if (lane == 63) waves[wave] = upto;
+    __syncthreads();
+    upto += across(waves).x;
+    const int above = upto - c0 - c1;
+    if (above < need && need <= upto) {
+      const bool upper = need <= above + c1;
+      found[0] = upper ? x : x - 1, found[1] = upper ? above : above + c1;
     }
+    if (need == 0 && tid == 0) found[0] = mask, found[1] = 0;  // none of them: no key lies above all ones
     __syncthreads();
     prefix |= (uint32_t)found[0] << shift;
     need -= found[1];
-    __syncthreads();
   }
-  // the keys above `prefix` and the first `need` equal to it, in order
-  int base = 0, ties = 0;
-  for (int i0 = 0; i0 < len; i0 += kSelectThreads) {
-    const int i = i0 + tid;
-    const bool forced = i < lo || i >= hi;
-    const uint32_t k = i < len && !forced ? order_of(w[i]) : 0u;
-    const bool above = i < len && (forced || k > prefix), equal = i < len && !forced && k == prefix;
-    const uint64_t ab = __ballot(above), eb = __ballot(equal), before = (1ull << lane) - 1;
-    if (lane == 0) waves[wave] = __popcll(ab) | __popcll(eb) << 16;
-    __syncthreads();
-    int na = 0, ne = 0, all_a = 0, all_e = 0;
-    for (int x = 0; x < kSelectWaves; ++x) {
-      const int v = waves[x];
-      if (x < wave) na += v & 0xFFFF, ne += v >> 16;
-      all_a += v & 0xFFFF, all_e += v >> 16;
+  // the keys above `prefix` and the first `need` equal to it, in order. Counts of both are held in one word, above in its lower
+  // half (a span has at most 2^15)
+  static_assert(kSpan <= 1 << 15, "two counts in a word");
+  int above0 = 0, equal0 = 0;  // in the spans before
+  for (int s0 = 0; s0 < end; s0 += kSpan) {
+    if (!once) read(s0);
+    auto flag = [&](int i, uint32_t key) {
+      const bool forced = i < lo || i >= hi;
+      return i < 0 || i >= len ? 0 : forced || key > prefix ? 1 : key == prefix ? 1 << 16 : 0;
+    };
+    int before[J];  // of the wave's, in the same step
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      const int i = token(s0, j);
+      int n = 0;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) n += flag(i + k, keys[j][k]);
+      const int upto = wave_scan(n);
+      before[j] = upto - n;
+      if (lane == 63) counts[j * kSelectWaves + wave] = upto;
     }
-    // kept before token i: those above, and of the equal ones as many as there is need for
-    const int pa = na + __popcll(ab & before), pe = ties + ne + __popcll(eb & before);
-    if (above || (equal && pe < need)) kept[base + pa + min(pe, need) - min(ties, need)] = i;
-    base += all_a + min(ties + all_e, need) - min(ties, need);
-    ties += all_e;
+    __syncthreads();
+    const int2 two = lane < J * kSelectWaves / 2 ? reinterpret_cast<const int2*>(counts)[lane] : make_int2(0, 0);
+    const int upto = wave_scan(two.x + two.y), first = upto - two.x - two.y, second = upto - two.y;
+#pragma unroll
+    for (int j = 0; j < J; ++j) {
+      if (s0 + j * kStep >= end) break;
+      const int i = token(s0, j), at = j * kSelectWaves + wave;
+      const int past = before[j] + (at & 1 ? __builtin_amdgcn_readlane(second, at >> 1) : __builtin_amdgcn_readlane(first, at >> 1));
+      // kept before a token: those above, and of the equal ones as many as there is need for
+      int na = above0 + (past & 0xFFFF), ne = equal0 + (int)((uint32_t)past >> 16);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int f = flag(i + k, keys[j][k]);
+        if (f == 1 || (f && ne < need)) kept[na + min(ne, need)] = i + k;
+        na += f & 1, ne += f >> 16;
+      }
+    }
+    const int all = __builtin_amdgcn_readlane(upto, 63);
+    above0 += all & 0xFFFF, equal0 += (int)((uint32_t)all >> 16);
     __syncthreads();
   }
 }
 
 hipError_t launch_select_tokens(const SelectArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(select_tokens_kernel, dim3((unsigned)(a.B * a.H)), dim3(kSelectThreads), 0, s, a);
+  const dim3 grid((unsigned)(a.B * a.H)), block(kSelectThreads);
+  if (a.max_ctx + 3 <= 8 * kSelectThreads)
+    hipLaunchKernelGGL(select_tokens_kernel<2>, grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL(select_tokens_kernel<8>, grid, block, 0, s, a);
   return hipGetLastError();
 }
 
