@@ -676,9 +676,15 @@ __global__ __launch_bounds__(256) void weight_few_scores_kernel(TokenWeightsArgs
   for (int i = 0; i < kPiecePages; ++i) {
     const int x = __builtin_amdgcn_readlane(id, i);
     const uint8_t* rec = a.cv.pool + ((size_t)(uint32_t)((real >> i) & 1 ? x : 0) * H + h) * Lay::kBytes;
-    code[i] = *reinterpret_cast<const cd_u2_t*>(rec + kOffKCodes + 32 * t + 8 * quad);
+    // (each key is read once: past the caches, so that the scores stay in them)
+    code[i] = __builtin_nontemporal_load(reinterpret_cast<const cd_u2_t*>(rec + kOffKCodes + 32 * t + 8 * quad));
+    if constexpr (NG == 4) {
+      const cd_u4_t y = __builtin_nontemporal_load(reinterpret_cast<const cd_u4_t*>(rec + Lay::kOffKMeta + 16 * t));
 #pragma unroll
-    for (int g = 0; g < NG; ++g) meta[i][g] = reinterpret_cast<const uint32_t*>(rec + Lay::kOffKMeta + 4 * NG * t)[g];
+      for (int g = 0; g < 4; ++g) meta[i][g] = y[g];
+    } else {
+      meta[i][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(rec + Lay::kOffKMeta + 4 * t));
+    }
   }
   const FewOps& ops = reinterpret_cast<const FewOps*>(a.few)[(size_t)b * H + h];
   const float down = ops.down, down24 = down * 0x1p24f;
@@ -706,7 +712,7 @@ __global__ __launch_bounds__(256) void weight_few_scores_kernel(TokenWeightsArgs
   float m[ROWS], sum[ROWS];
 #pragma unroll
   for (int k = 0; k < ROWS; ++k) m[k] = kNone, sum[k] = 0.0f;
-  float* scores = a.scores + ((size_t)b * H + h) * a.page_cap * (kBlock * a.row_cap);
+  float* scores = a.scores + (((size_t)b * H + h) * a.page_cap + page0) * (kBlock * a.row_cap) + ROWS * quad * kBlock + t;
 #pragma unroll
   for (int i = 0; i < kPiecePages; ++i) {
     if (page0 + i >= pages) break;
@@ -746,7 +752,7 @@ __global__ __launch_bounds__(256) void weight_few_scores_kernel(TokenWeightsArgs
         m[k] = top;
       }
       sum[k] += __builtin_amdgcn_exp2f(x - m[k]);
-      if (ROWS * quad + k < a.row_cap) scores[((size_t)(page0 + i) * a.row_cap + ROWS * quad + k) * kBlock + t] = x;
+      if (ROWS * quad + k < a.row_cap) scores[i * (kBlock * a.row_cap) + k * kBlock] = x;
     }
   }
 #pragma unroll
