@@ -570,7 +570,10 @@ __global__ __launch_bounds__(256) void weight_join_kernel(TokenWeightsArgs a) {
 namespace {
 
 constexpr int kFewRows = 8;
-constexpr int kPieceTokens = 512, kPiecePages = kPieceTokens / kBlock / 4;  // of a block; pages of each of its four waves
+#ifndef ALONE_PER_CU
+#define ALONE_PER_CU 1
+#endif
+constexpr int kPieceTokens = 512;  // of a block
 constexpr int kJoinTokens = 1024;
 
 // The rows' operands for products of 16 rows x 16 tokens, with zeros where a row has no part in a group, so that one chain of
@@ -600,69 +603,108 @@ __device__ __forceinline__ cd_h8_t bits_of(uint32_t u, uint32_t uh, uint32_t v, 
 
 }  // namespace
 
-// Block: one (sequence, KV head). Thread: channel c, a sixteenth of the sum's terms (all loads on their way at once); then one
-// row of it. Bound by the latency of its loads.
-__global__ __launch_bounds__(1024) void weight_few_rows_kernel(TokenWeightsArgs a) {
-  __shared__ float q[kFewRows][kHeadDim], part[8][kFewRows][kHeadDim], top[16];
-  const int H = a.cv.num_kv_heads, h = blockIdx.x % H, b = blockIdx.x / H, c = threadIdx.x & 127, k = threadIdx.x >> 7;
-  const float* R = a.R_k + ((size_t)h * kHeadDim + 16 * k) * kHeadDim + c;
-  float x[16];
+namespace {
+
+struct FewLds {
+  float q[kFewRows][kHeadDim], part[8][kFewRows][kHeadDim], top[16];
+};
+
+// The operands of one (sequence, KV head) by T threads: thread (channel c, part k of the sum's terms), all its loads on their
+// way at once (R, given by rotation_part); then (channel, row). All threads of the block call it.
+template <int T>
+struct RotationPart {
+  float x[kHeadDim / (T / kHeadDim)];
+};
+template <int T>
+__device__ __forceinline__ void rotation_part(const TokenWeightsArgs& a, int h, RotationPart<T>& p) {
+  constexpr int kTerms = kHeadDim / (T / kHeadDim);
+  const float* R = a.R_k + ((size_t)h * kHeadDim + kTerms * (threadIdx.x >> 7)) * kHeadDim + (threadIdx.x & 127);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) x[i] = R[(size_t)i * kHeadDim];
-  const Span s = span_of(a, b);
-  const int rows = min(s.n * a.gq, kFewRows);
-  if (rows == 0 || s.ctx == 0) return;
-  {
-    const int tok = k / a.gq;
-    q[k][c] = k < rows ? bf16_bits_to_f32(a.q[(s.start + tok) * a.q_stride + (size_t)(h * a.gq + k - tok * a.gq) * kHeadDim + c]) : 0.0f;
+  for (int i = 0; i < kTerms; ++i) p.x[i] = R[(size_t)i * kHeadDim];
+}
+template <int T>
+__device__ __forceinline__ void few_operands(const TokenWeightsArgs& a, const Span& s, int h, const RotationPart<T>& p, FewLds& lds, FewOps& out) {
+  constexpr int kParts = T / kHeadDim, kTerms = kHeadDim / kParts, kEach = kFewRows / kParts;  // rows of a thread in the second half
+  const int c = threadIdx.x & 127, k = threadIdx.x >> 7, rows = min(s.n * a.gq, kFewRows);
+#pragma unroll
+  for (int i = 0; i < kEach; ++i) {
+    const int r = k + kParts * i, tok = r / a.gq;
+    lds.q[r][c] = r < rows ? bf16_bits_to_f32(a.q[(s.start + tok) * a.q_stride + (size_t)(h * a.gq + r - tok * a.gq) * kHeadDim + c]) : 0.0f;
   }
   __syncthreads();
-#pragma unroll
-  for (int r = 0; r < kFewRows; ++r) {
+  for (int r = 0; r < rows; ++r) {
     float d = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) d = __builtin_fmaf(q[r][16 * k + i], x[i], d);
-    part[k][r][c] = d;
+    for (int i = 0; i < kTerms; ++i) d = __builtin_fmaf(lds.q[r][kTerms * k + i], p.x[i], d);
+    lds.part[k][r][c] = d;
   }
   __syncthreads();
-  const int r = k;
-  float d = 0.0f;
+  float d[kEach], big = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) d += part[i][r][c];
-  d *= kLogit2;
-  float big = fabsf(d);
+  for (int i = 0; i < kEach; ++i) {
+    const int r = k + kParts * i;
+    d[i] = 0.0f;
+    if (r < rows) {
+#pragma unroll
+      for (int x = 0; x < kParts; ++x) d[i] += lds.part[x][r][c];
+    }
+    d[i] *= kLogit2;
+    big = fmaxf(big, fabsf(d[i]));
+  }
 #pragma unroll
   for (int step = 32; step > 0; step >>= 1) big = fmaxf(big, __shfl_xor(big, step));
-  if ((threadIdx.x & 63) == 0) top[threadIdx.x >> 6] = big;
+  if ((threadIdx.x & 63) == 0) lds.top[threadIdx.x >> 6] = big;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < 16; ++i) big = fmaxf(big, top[i]);
+  for (int i = 0; i < T / 64; ++i) big = fmaxf(big, lds.top[i]);
   // the largest element to 2^13 .. 2^14
   const uint32_t e = min(max(__float_as_uint(big) >> 23, 14u), 240u);
-  FewOps& out = reinterpret_cast<FewOps*>(a.few)[(size_t)b * H + h];
   const int g = c >> 5, pos = c >> 4, word = (c & 15) >> 1, element = ((word & 1) << 2) | ((pos & 1) << 1) | (c & 1);
-  const float y = d * __uint_as_float((267u - e) << 23), z = y * __uint_as_float((127u - 2 * (pos % 5)) << 23);
-  const _Float16 hi = (_Float16)z, lo = (_Float16)(z - (float)hi);
   const bool narrow = a.row_cap <= 4;
-  if (!narrow || r < 4) {
-    const int at = narrow ? 0 : g >> 1, lane = 16 * (word >> 1) + (narrow ? 4 * r + g : 2 * r + (g & 1));
-    reinterpret_cast<_Float16*>(&out.term[at][0][lane])[element] = hi;
-    reinterpret_cast<_Float16*>(&out.term[at][1][lane])[element] = lo;
-  }
-  float sum = y;  // over the group: 32 lanes
 #pragma unroll
-  for (int step = 16; step > 0; step >>= 1) sum += __shfl_xor(sum, step);
-  if ((c & 31) == 0) out.sum[r][g] = sum;
+  for (int i = 0; i < kEach; ++i) {
+    const int r = k + kParts * i;
+    const float y = d[i] * __uint_as_float((267u - e) << 23), z = y * __uint_as_float((127u - 2 * (pos % 5)) << 23);
+    const _Float16 hi = (_Float16)z, lo = (_Float16)(z - (float)hi);
+    if (!narrow || r < 4) {
+      const int at = narrow ? 0 : g >> 1, lane = 16 * (word >> 1) + (narrow ? 4 * r + g : 2 * r + (g & 1));
+      reinterpret_cast<_Float16*>(&out.term[at][0][lane])[element] = hi;
+      reinterpret_cast<_Float16*>(&out.term[at][1][lane])[element] = lo;
+    }
+    float sum = y;  // over the group: 32 lanes
+#pragma unroll
+    for (int step = 16; step > 0; step >>= 1) sum += __shfl_xor(sum, step);
+    if ((c & 31) == 0) out.sum[r][g] = sum;
+  }
   if (threadIdx.x == 0) out.down = __uint_as_float((e - 13u) << 23);
 }
 
-// Block: 512 tokens of one KV head, a wave eight pages of them; all loads of a wave are on their way at once. Lane: one token
-// of a page and ROWS rows, 1 (up to four of a KV head) or 2.
-template <int NG, int ROWS>
-__global__ __launch_bounds__(256) void weight_few_scores_kernel(TokenWeightsArgs a) {
+}  // namespace
+
+// Block: one (sequence, KV head). Bound by the latency of its loads.
+__global__ __launch_bounds__(1024) void weight_few_rows_kernel(TokenWeightsArgs a) {
+  __shared__ FewLds lds;
+  const int H = a.cv.num_kv_heads, h = blockIdx.x % H, b = blockIdx.x / H;
+  RotationPart<1024> R;
+  rotation_part(a, h, R);
+  const Span s = span_of(a, b);
+  if (s.n == 0 || s.ctx == 0) return;
+  few_operands<1024>(a, s, h, R, lds, reinterpret_cast<FewOps*>(a.few)[(size_t)b * H + h]);
+}
+
+// Block: 512 tokens of one KV head, a wave eight (four) pages of them; all loads of a wave are on their way at once. Lane: one token
+// of a page and ROWS rows, 1 (up to four of a KV head) or 2. ALONE: forms its operands itself, while the keys are on their
+// way, and has twice the waves for it.
+template <int NG, int ROWS, bool ALONE>
+__global__ __launch_bounds__(ALONE ? 512 : 256) void weight_few_scores_kernel(TokenWeightsArgs a) {
   using Lay = Rec<NG>;
-  __shared__ float2 both[4][kFewRows];
+  constexpr int kW = ALONE ? 8 : 4, kPiecePages = kPieceTokens / kBlock / kW;
+  __shared__ float2 both[kW][kFewRows];
+  __shared__ typename std::conditional<ALONE, FewLds, int>::type work;
+  __shared__ typename std::conditional<ALONE, FewOps, int>::type own;
   const int H = a.cv.num_kv_heads, h = blockIdx.x % H, piece = blockIdx.x / H % a.pieces, b = blockIdx.x / H / a.pieces;
+  RotationPart<512> R;
+  if constexpr (ALONE) rotation_part(a, h, R);
   const Span s = span_of(a, b);
   if (kPieceTokens * piece >= s.ctx || s.n == 0) return;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, t = l & 15, quad = l >> 4;
@@ -686,7 +728,13 @@ __global__ __launch_bounds__(256) void weight_few_scores_kernel(TokenWeightsArgs
       meta[i][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(rec + Lay::kOffKMeta + 4 * t));
     }
   }
-  const FewOps& ops = reinterpret_cast<const FewOps*>(a.few)[(size_t)b * H + h];
+  const FewOps* from = reinterpret_cast<const FewOps*>(a.few) + ((size_t)b * H + h);
+  if constexpr (ALONE) {
+    few_operands<512>(a, s, h, R, work, own);
+    __syncthreads();
+    from = &own;
+  }
+  const FewOps& ops = *from;
   const float down = ops.down, down24 = down * 0x1p24f;
   cd_h8_t A[2][4];  // [high, low][group]
   float Q[ROWS][4];
@@ -765,9 +813,9 @@ __global__ __launch_bounds__(256) void weight_few_scores_kernel(TokenWeightsArgs
   if (threadIdx.x < 4 * ROWS) {
     float top = kNone, all = 0.0f;
 #pragma unroll
-    for (int x = 0; x < 4; ++x) top = fmaxf(top, both[x][threadIdx.x].x);
+    for (int x = 0; x < kW; ++x) top = fmaxf(top, both[x][threadIdx.x].x);
 #pragma unroll
-    for (int x = 0; x < 4; ++x) all += both[x][threadIdx.x].y * __builtin_amdgcn_exp2f(both[x][threadIdx.x].x - top);
+    for (int x = 0; x < kW; ++x) all += both[x][threadIdx.x].y * __builtin_amdgcn_exp2f(both[x][threadIdx.x].x - top);
     a.stats[(((size_t)b * H + h) * a.pieces + piece) * kFewRows + threadIdx.x] = make_float2(top, all);
   }
 }
@@ -850,18 +898,29 @@ TokenWeightsPlan make_token_weights_plan(int B, int Hq, int H, int total_q, int 
 
 namespace {
 
+template <int NG, bool ALONE>
+hipError_t launch_scores(const TokenWeightsArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((long long)a.B * a.cv.num_kv_heads * a.pieces));
+  if (a.row_cap <= 4)
+    hipLaunchKernelGGL((weight_few_scores_kernel<NG, 1, ALONE>), grid, dim3(ALONE ? 512 : 256), 0, s, a);
+  else
+    hipLaunchKernelGGL((weight_few_scores_kernel<NG, 2, ALONE>), grid, dim3(ALONE ? 512 : 256), 0, s, a);
+  return hipGetLastError();
+}
+
 template <int NG>
 hipError_t launch_few(const TokenWeightsArgs& a, hipStream_t s) {
   const long long H = a.cv.num_kv_heads;
-  hipLaunchKernelGGL(weight_few_rows_kernel, dim3((unsigned)(a.B * H)), dim3(1024), 0, s, a);
-  hipError_t e = hipGetLastError();
+  hipError_t e;
+  // While every compute unit has at most ALONE_PER_CU blocks, each rotates its own queries: a launch less
+  if (a.B * H * a.pieces <= ALONE_PER_CU * num_cus()) {
+    e = launch_scores<NG, true>(a, s);
+  } else {
+    hipLaunchKernelGGL(weight_few_rows_kernel, dim3((unsigned)(a.B * H)), dim3(1024), 0, s, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    e = launch_scores<NG, false>(a, s);
+  }
   if (e != hipSuccess) return e;
-  const dim3 grid((unsigned)(a.B * H * a.pieces));
-  if (a.row_cap <= 4)
-    hipLaunchKernelGGL((weight_few_scores_kernel<NG, 1>), grid, dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL((weight_few_scores_kernel<NG, 2>), grid, dim3(256), 0, s, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
   const long long joins = ((long long)a.page_cap * kBlock + kJoinTokens - 1) / kJoinTokens;
   hipLaunchKernelGGL(weight_few_join_kernel, dim3((unsigned)(a.B * H * joins)), dim3(256), 0, s, a);
   return hipGetLastError();

@@ -747,9 +747,10 @@ def int2kv_tree_attention(cache: Int2KVCache, q: torch.Tensor, q_starts: torch.T
 # Eviction: the weight that tokens receive, those that stay, their move
 def _lists(t: torch.Tensor, dtypes, batch: int, heads: int, least: int, name: str):
     """(pointer, elements between lists) of [batch, heads, n] lists, n at least `least`."""
-    if t.dim() != 3 or t.shape[0] != batch or t.shape[1] != heads or t.shape[2] < least:
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != batch or shape[1] != heads or shape[2] < least:
         raise ValueError(f"{name} must be [batch, num_kv_heads, at least {least}]")
-    return _ptr(t, dtypes, name), t.shape[2]
+    return _ptr(t, dtypes, name), shape[2]
 
 
 def int2kv_token_weights_workspace_bytes(batch: int, num_q_heads: int, num_kv_heads: int, total_q: int, max_q: int,
@@ -831,9 +832,10 @@ def int2kv_move_tokens(cache: Int2KVCache, block_table: torch.Tensor, kept: torc
     theirs to out_weights (in place: by default weights themselves; else new, zeros behind kept_lens). Returns
     out_weights."""
     B, H = kept_lens.numel(), cache.num_kv_heads
-    for t, name in ((block_table, "block_table"), (out_table, "out_table")):
-        if t is not None and (t.dim() != 2 or t.shape[0] != B):
-            raise ValueError(f"{name} must be [batch, max_blocks]")
+    shape = block_table.shape
+    out_shape = shape if out_table is None else out_table.shape
+    if len(shape) != 2 or shape[0] != B or len(out_shape) != 2 or out_shape[0] != B:
+        raise ValueError("block_table and out_table must be [batch, max_blocks]")
     if out_weights is not None and weights is None:
         raise ValueError("out_weights needs weights")
     in_place = out_table is None or out_table.data_ptr() == block_table.data_ptr()
@@ -849,9 +851,9 @@ def int2kv_move_tokens(cache: Int2KVCache, block_table: torch.Tensor, kept: torc
         need = int2kv_move_tokens_workspace_bytes(B, H, cache.group_size, max_kept)
         workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=cache.pool.device)
     st = load_library().int2kv_move_tokens(
-        cache.desc, _ptr(block_table, _I32, "block_table"), block_table.shape[1], kp, ks, _ptr(kept_lens, _I32, "kept_lens"), B,
-        max_kept, _ptr(out_table, _I32, "out_table"), 0 if out_table is None else out_table.shape[1], wp, ws, op, os_,
-        _ptr(workspace, (torch.uint8,), "workspace"), 0 if workspace is None else workspace.numel(), _stream())
+        cache.desc, _ptr(block_table, _I32, "block_table"), shape[1], kp, ks, _ptr(kept_lens, _I32, "kept_lens"), B, max_kept,
+        _ptr(out_table, _I32, "out_table"), out_shape[1], wp, ws, op, os_, _ptr(workspace, (torch.uint8,), "workspace"),
+        0 if workspace is None else workspace.numel(), _stream())
     _check(st, "int2kv_move_tokens")
     return out_weights
 
