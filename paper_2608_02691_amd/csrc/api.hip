@@ -842,6 +842,7 @@ int int2kv_token_weights(const int2kv_cache* cache, const uint16_t* q, int64_t q
     const uint64_t len = ((uint64_t)batch * H - 1) * (uint64_t)weights_stride * 4 + (uint64_t)max_ctx * 4;
     if ((x < y ? y - x : x - y) < len) return fail(INT2KV_EINVAL, "weights_out overlaps weights_in without being it");
   }
+  if (max_ctx > INT32_MAX - (1 << 18)) return fail(INT2KV_EUNSUPPORTED, "max_ctx must be at most 2^31 - 2^18 - 1");
   const TokenWeightsPlan plan = make_token_weights_plan(batch, num_q_heads, H, total_q, max_q, max_ctx);
   // a launch holds 2^32 - 1 threads
   if ((int64_t)batch * H * plan.ranges > UINT32_MAX / 512 / (plan.chunks > 1 ? plan.chunks : 1) ||

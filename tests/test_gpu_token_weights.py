@@ -25,7 +25,7 @@ def test_decode_steps(heads, gq, group):
     check(WeightsCall(seqs, heads, gq, group, seed=gq, pad=1, fused=gq == 4), f"{heads} x {gq}, {group}")
 
 
-@pytest.mark.parametrize("n,ctx", [(2, 2), (2, 300), (7, 40), (8, 8), (9, 500), (31, 33), (32, 32), (33, 700), (64, 64), (65, 1030), (150, 150), (200, 201)])
+@pytest.mark.parametrize("n,ctx", [(3, 4500), (20, 3000), (64, 2500), (64, 5), (2, 2), (2, 300), (7, 40), (8, 8), (9, 500), (31, 33), (32, 32), (33, 700), (64, 64), (65, 1030), (150, 150), (200, 201)])
 @pytest.mark.parametrize("gq", [1, 4, 5])
 def test_several_tokens(n, ctx, gq):
     check(WeightsCall([(n, ctx), (1, 70)], 1, gq, 32 if n % 2 else 128, seed=n), f"{n} of {ctx} x {gq}")
@@ -118,6 +118,16 @@ def test_sizes_of_scores(q_scale, k_scale, n):
     c = WeightsCall([(n, 700), (n, 90)], 1, 4, seed=13, q_scale=q_scale, k_scale=k_scale)
     c.q[0, 1] *= 0.001
     check(c, f"{q_scale}, {k_scale}")
+
+
+@pytest.mark.parametrize("n,pad", [(2, 0), (12, 0), (70, 0), (70, 5)])
+def test_only_late_pages_exist(n, pad):
+    """Rows whose every score lies far from zero, and none over the first tokens: their weights still sum to one."""
+    c = WeightsCall([(n, 900), (n, 300)], 1, 4, seed=19, q_scale=30.0, k_scale=4.0, first=True)
+    c.table[0, :-4 - (n + 15) // 16] = -1  # rows see the last pages only: from one token to n
+    c.table[1, :] = np.where(np.arange(c.table.shape[1]) == 12 + pad, c.table[1], -1)
+    got = check(c, "late pages")
+    assert abs(float(got[0].double().sum()) - 4 * n) < 1e-3 * n
 
 
 @pytest.mark.parametrize("n", [1, 10])
