@@ -456,7 +456,8 @@ int int2kv_tree_attention(const int2kv_cache* cache, const uint16_t* q, int64_t 
  *     p_ij = softmax over what token i sees of (q_ij R_K) k^_s^T / sqrt(d).
  * One token a sequence: a decode step; the last tokens of a prompt: their vote on the rest; all of them.
  *   q .. max_ctx, R_k : as int2kv_chunk_attention (with max_q 0 the sums only decay; q, R_k may be NULL)
- *   weights_in   : fp32, KV head h of sequence b at (b H_kv + h) weights_stride, or NULL: zeros
+ *   weights_in   : fp32, KV head h of sequence b at (b H_kv + h) weights_stride, or NULL: zeros. The
+ *                  entries of tokens that are new count too: zero, unless the caller wants otherwise
  *   decay        : factor of weights_in, finite
  *   weights_out  : fp32 as weights_in, which it may be, without otherwise overlapping it. Tokens from
  *                  min(ctx_lens[b], max_ctx) on are left as they were; tokens in blocks outside the
@@ -505,7 +506,8 @@ int int2kv_select_tokens(const float* weights, int64_t weights_stride, int batch
  *   workspace    : in place int2kv_move_tokens_workspace_bytes(...) bytes, 16-byte aligned; else NULL
  * A row whose old token lies outside the table or in a block outside the cache is left as it was, as
  * are rows behind the last kept one, pages whose new block lies outside the cache, and weights beyond
- * a stride. */
+ * a stride. In place that holds for weights behind the last kept one too: clear them before tokens are
+ * appended there and int2kv_token_weights adds to their sums. */
 size_t int2kv_move_tokens_workspace_bytes(int batch, int num_kv_heads, int group_size, int max_kept);
 int int2kv_move_tokens(const int2kv_cache* cache, const int32_t* block_table, int max_blocks_per_seq,
                        const int32_t* kept, int64_t kept_stride, const int32_t* kept_lens, int batch,

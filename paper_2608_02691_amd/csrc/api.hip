@@ -808,7 +808,7 @@ int int2kv_tree_attention(const int2kv_cache* cache, const uint16_t* q, int64_t 
 size_t int2kv_token_weights_workspace_bytes(int batch, int num_q_heads, int num_kv_heads, int total_q, int max_q,
                                             int max_ctx) {
   if (batch <= 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads || total_q < 0 || max_q < 0 || max_ctx < 0 ||
-      (int64_t)total_q * num_q_heads > INT32_MAX)
+      (int64_t)total_q * num_q_heads > INT32_MAX || max_ctx > INT32_MAX - (1 << 18))
     return 0;
   return make_token_weights_plan(batch, num_q_heads, num_kv_heads, total_q, max_q < total_q ? max_q : total_q, max_ctx).total;
 }

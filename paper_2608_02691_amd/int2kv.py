@@ -829,8 +829,8 @@ def int2kv_move_tokens(cache: Int2KVCache, block_table: torch.Tensor, kept: torc
                        out_weights: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """Writes the rows of the kept tokens to the front: token j of KV head h becomes the old token kept[b, h, j] (int32
     [batch, H_kv, at least max_kept]), in the blocks of out_table, or without it in place. With weights fp32 [batch, H_kv, n],
-    theirs to out_weights (in place: by default weights themselves; else new, zeros behind kept_lens). Returns
-    out_weights."""
+    theirs to out_weights (in place: by default weights themselves, whose entries behind kept_lens stay as they were; else
+    new, zeros there). Returns out_weights."""
     B, H = kept_lens.numel(), cache.num_kv_heads
     shape = block_table.shape
     out_shape = shape if out_table is None else out_table.shape
