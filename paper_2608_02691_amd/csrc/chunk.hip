@@ -451,11 +451,12 @@ struct OwnSource {
   __device__ __forceinline__ void refetch(int u) { fetch(u); }
   __device__ __forceinline__ bool partial(int u) const { return TREE || kUnit * u + kUnit - 1 > tok_tile; }
   __device__ __forceinline__ bool masked(int u) const { return TREE || kUnit * u + kUnit - 1 > tok_min; }
-  // (the lane half's 8 never crosses a word)
-  __device__ __forceinline__ bool sees(int u, int t) const { return sees_token(u, t + 8 * hh, t); }
-  __device__ __forceinline__ bool sees_token(int u, int t) const { return sees_token(u, t, t); }
-  __device__ __forceinline__ bool sees_token(int u, int t, int t0) const {
-    if constexpr (TREE) return (path_word(path, 2 * u + (t0 >> 5)) >> (t & 31)) & 1;
+  __device__ __forceinline__ bool sees(int u, int t) const {  // (the lane half's 8 never crosses a word)
+    if constexpr (TREE) return (path_word(path, 2 * u + (t >> 5)) >> ((t + 8 * hh) & 31)) & 1;
+    return kUnit * u + t + 8 * hh <= tok;
+  }
+  __device__ __forceinline__ bool sees_token(int u, int t) const {
+    if constexpr (TREE) return (path_word(path, 2 * u + (t >> 5)) >> (t & 31)) & 1;
     return kUnit * u + t <= tok;
   }
 };
@@ -812,7 +813,7 @@ hipError_t launch_chunk_attention(ChunkArgs a, const ChunkPlan& p, uint8_t* ws, 
   a.tile_start = reinterpret_cast<int32_t*>(ws + p.off_starts);
   a.tiles = reinterpret_cast<ChunkTile*>(ws + p.off_tiles);
   a.part = reinterpret_cast<float*>(ws + p.off_part);
-  return a.parents ? launch_pieces<true>(a, p, s) : launch_pieces<false>(a, p, s);
+  return !a.parents ? launch_pieces<false>(a, p, s) : launch_pieces<true>(a, p, s);
 }
 
 }  // namespace int2kv

@@ -208,8 +208,6 @@ struct ChunkArgs {
                                     // a prompt of 2,011 tokens 72 us, with the flag 69)
   const uint16_t *k_new, *v_new;
   const float* mu;
-  const int32_t *tree_starts, *parents;  // trees: offsets of their rows in k_new [B + 1], parents [total_tree]; or null
-  int total_tree, max_tree;
   uint16_t* out;                    // bf16 [total_q, Hq, 128]
   // plan and workspace
   int bm, resident, per_cu, min_piece, max_tiles, max_items, max_slots;
@@ -219,6 +217,8 @@ struct ChunkArgs {
   int32_t* tile_start;              // [B] (the same) the sequences' first tiles
   ChunkTile* tiles;                 // [max_tiles]
   float* part;                      // [max_slots, H, bm * kChunkPartStride]
+  const int32_t *tree_starts, *parents;  // trees: offsets of their rows in k_new [B + 1], parents [total_tree]; or null
+  int total_tree, max_tree;
 };
 struct ChunkPlan {
   int waves, bm, resident, min_piece, max_tiles, max_items, max_slots;
