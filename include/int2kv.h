@@ -466,8 +466,8 @@ int int2kv_tree_attention(const int2kv_cache* cache, const uint16_t* q, int64_t 
  *   workspace    : int2kv_token_weights_workspace_bytes(...) bytes, 256-byte aligned; enough for every
  *                  call within the same bounds, nothing kept between calls, calls that overlap need one each
  * fp32 throughout: products run on the matrix cores in terms that keep fp32's precision, statistics and
- * sums in fp32 (a weight is off by about 1e-6 of itself and the scores' size times 1e-7). Stored scales
- * and zeros have to be finite. Deterministic; no atomics on results. */
+ * sums in fp32 (a weight is off by about 1e-6 of itself and the scores' size times 1e-7). Queries and the
+ * scales and zeros of the cached tokens have to be finite. Deterministic; no atomics on results. */
 size_t int2kv_token_weights_workspace_bytes(int batch, int num_q_heads, int num_kv_heads, int total_q, int max_q,
                                             int max_ctx);
 int int2kv_token_weights(const int2kv_cache* cache, const uint16_t* q, int64_t q_stride, const int32_t* q_starts,

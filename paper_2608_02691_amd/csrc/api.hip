@@ -846,7 +846,7 @@ int int2kv_token_weights(const int2kv_cache* cache, const uint16_t* q, int64_t q
   const TokenWeightsPlan plan = make_token_weights_plan(batch, num_q_heads, H, total_q, max_q, max_ctx);
   // a launch holds 2^32 - 1 threads
   if ((int64_t)batch * H * plan.ranges > UINT32_MAX / 512 / (plan.chunks > 1 ? plan.chunks : 1) ||
-      (int64_t)batch * H * plan.seq_tiles > UINT32_MAX / 256)
+      (int64_t)batch * H * plan.seq_tiles > UINT32_MAX / 256 || (plan.few && (int64_t)batch * H > UINT32_MAX / 1024))
     return fail(INT2KV_EUNSUPPORTED, "too many row tiles or token ranges for one launch");
   if (!workspace || workspace_bytes < plan.total)
     return fail(INT2KV_EWORKSPACE, "workspace smaller than int2kv_token_weights_workspace_bytes()");
@@ -868,7 +868,7 @@ int int2kv_select_tokens(const float* weights, int64_t weights_stride, int batch
     return fail(INT2KV_EINVAL, "budget must hold sink + recent tokens");
   if (kept_stride < (budget < max_ctx ? budget : max_ctx)) return fail(INT2KV_EINVAL, "kept_stride must hold min(budget, max_ctx) tokens");
   if ((int64_t)batch * num_kv_heads > UINT32_MAX / 1024) return fail(INT2KV_EUNSUPPORTED, "too many lists for one launch");
-  if (max_ctx > INT32_MAX - 4096) return fail(INT2KV_EUNSUPPORTED, "max_ctx must be below 2^31 - 4096");
+  if (max_ctx > INT32_MAX - (1 << 18)) return fail(INT2KV_EUNSUPPORTED, "max_ctx must be at most 2^31 - 2^18 - 1");
   if (!ctx_lens || !kept_lens || (max_ctx > 0 && !weights) || (max_ctx > 0 && budget > 0 && !kept)) return fail(INT2KV_EINVAL, "NULL pointer argument");
   if (!aligned(weights, 4) || !aligned(kept, 4) || !aligned(ctx_lens, 4) || !aligned(kept_lens, 4))
     return fail(INT2KV_EINVAL, "weights, ctx_lens, kept and kept_lens must be 4-byte aligned");

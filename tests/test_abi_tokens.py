@@ -89,6 +89,7 @@ def test_token_weights_bounds():
     assert _weights(max_ctx=0)[0] == K.INT2KV_OK
     assert _weights(total=1 << 30)[0] == K.INT2KV_EUNSUPPORTED
     assert _weights(B=1 << 24, max_ctx=1 << 20, stride=1 << 20, wi=None)[0] == K.INT2KV_EUNSUPPORTED
+    assert _weights(B=1 << 21, max_q=4, wi=None, wb=1 << 60)[0] == K.INT2KV_EUNSUPPORTED  # (1,024 threads a sequence and KV head)
     assert _weights(B=1, max_ctx=2 ** 31 - 1, stride=1 << 31, wi=None, wb=1 << 60)[0] == K.INT2KV_EUNSUPPORTED
     for bad in ((0, 4, 2, 8, 8, 64), (2, 3, 2, 8, 8, 64), (2, 4, 2, -1, 8, 64), (2, 4, 2, 8, 8, -1), (2, 4, 2, 1 << 30, 8, 64),
                 (2, 4, 2, 8, 8, 2 ** 31 - 1)):
@@ -126,7 +127,8 @@ def test_select_tokens_refusals(kw, word):
 
 def test_select_tokens_bounds():
     assert _select(B=1 << 22, H=2)[0] == K.INT2KV_EUNSUPPORTED
-    assert _select(max_ctx=2 ** 31 - 4095, ws=1 << 31)[0] == K.INT2KV_EUNSUPPORTED
+    for max_ctx in (2 ** 31 - 1, 2 ** 31 - 4097, 2 ** 31 - 2 ** 18):  # a span's step past the list has to fit 32 bits too
+        assert _select(max_ctx=max_ctx, ws=1 << 31)[0] == K.INT2KV_EUNSUPPORTED
 
 
 def _move(cache=GOOD, **kw):
