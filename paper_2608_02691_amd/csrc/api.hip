@@ -898,7 +898,7 @@ int int2kv_move_tokens(const int2kv_cache* cache, const int32_t* block_table, in
   if (weights && (weights_stride <= 0 || out_weights_stride < max_kept))
     return fail(INT2KV_EINVAL, "weights_stride must be positive, out_weights_stride at least max_kept");
   if (max_kept == 0) return ok();
-  if ((int64_t)batch * H > UINT32_MAX / 64 / pages) return fail(INT2KV_EUNSUPPORTED, "too many pages for one launch");
+  if ((int64_t)batch * H > UINT32_MAX / 256 * 4 / pages) return fail(INT2KV_EUNSUPPORTED, "too many pages for one launch");
   if (!block_table || !kept || !kept_lens) return fail(INT2KV_EINVAL, "NULL pointer argument");
   if (!aligned(block_table, 4) || !aligned(kept, 4) || !aligned(kept_lens, 4) || !aligned(out_table, 4) || !aligned(weights, 4) || !aligned(out_weights, 4))
     return fail(INT2KV_EINVAL, "tables, lists and weights must be 4-byte aligned");
