@@ -690,30 +690,30 @@ __global__ __launch_bounds__(1024) void weight_few_rows_kernel(TokenWeightsArgs 
   few_operands<1024>(a, s, h, R, lds, reinterpret_cast<FewOps*>(a.few)[(size_t)b * H + h]);
 }
 
-// Block: 512 tokens of one KV head, a wave eight (four) pages of them; all loads of a wave are on their way at once. Lane: one token
-// of a page and ROWS rows, 1 (up to four of a KV head) or 2. ALONE: forms its operands itself, while the keys are on their
-// way, and has twice the waves for it.
-template <int NG, int ROWS, bool ALONE>
-__global__ __launch_bounds__(ALONE ? 512 : 256) void weight_few_scores_kernel(TokenWeightsArgs a) {
+// Block: W waves with PAGES pages of one KV head each; all loads of a wave are on their way at once. Lane: one token of a page
+// and ROWS rows, 1 (up to four of a KV head) or 2. ALONE: forms its operands itself, while the keys are on their way. WHOLE: the
+// block has the whole context, so that scores and statistics stay in registers and LDS, and forms the sums too.
+template <int NG, int ROWS, int W, int PAGES, bool ALONE, bool WHOLE>
+__global__ __launch_bounds__(64 * W) void weight_few_scores_kernel(TokenWeightsArgs a) {
   using Lay = Rec<NG>;
-  constexpr int kW = ALONE ? 8 : 4, kPiecePages = kPieceTokens / kBlock / kW;
-  __shared__ float2 both[kW][kFewRows];
+  static_assert(WHOLE ? ALONE && W <= 16 && PAGES % 4 == 0 : W * PAGES * kBlock == kPieceTokens, "a lane of sixteen a wave; pieces");
+  __shared__ float2 both[W][kFewRows];
   __shared__ typename std::conditional<ALONE, FewLds, int>::type work;
   __shared__ typename std::conditional<ALONE, FewOps, int>::type own;
-  const int H = a.cv.num_kv_heads, h = blockIdx.x % H, piece = blockIdx.x / H % a.pieces, b = blockIdx.x / H / a.pieces;
-  RotationPart<512> R;
+  const int H = a.cv.num_kv_heads, h = blockIdx.x % H, piece = WHOLE ? 0 : blockIdx.x / H % a.pieces, b = WHOLE ? blockIdx.x / H : blockIdx.x / H / a.pieces;
+  RotationPart<64 * W> R;
   if constexpr (ALONE) rotation_part(a, h, R);
   const Span s = span_of(a, b);
-  if (kPieceTokens * piece >= s.ctx || s.n == 0) return;
+  if (kPieceTokens * piece >= s.ctx || (!WHOLE && s.n == 0)) return;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, t = l & 15, quad = l >> 4;
-  const int page0 = kPieceTokens / kBlock * piece + kPiecePages * w, pages = (s.ctx + kBlock - 1) / kBlock;
+  const int page0 = W * PAGES * piece + PAGES * w, pages = (s.ctx + kBlock - 1) / kBlock;
   int id = -1;
-  if (l < kPiecePages && page0 + l < pages) id = a.table[(size_t)b * a.max_blocks + page0 + l];
+  if (l < PAGES && page0 + l < pages) id = a.table[(size_t)b * a.max_blocks + page0 + l];
   const uint32_t real = (uint32_t)__ballot(id >= 0 && id < a.cv.num_blocks);
-  cd_u2_t code[kPiecePages];
-  uint32_t meta[kPiecePages][NG];
+  cd_u2_t code[PAGES];
+  uint32_t meta[PAGES][NG];
 #pragma unroll
-  for (int i = 0; i < kPiecePages; ++i) {
+  for (int i = 0; i < PAGES; ++i) {
     const int x = __builtin_amdgcn_readlane(id, i);
     const uint8_t* rec = a.cv.pool + ((size_t)(uint32_t)((real >> i) & 1 ? x : 0) * H + h) * Lay::kBytes;
     // (each key is read once: past the caches, so that the scores stay in them)
@@ -726,9 +726,17 @@ __global__ __launch_bounds__(ALONE ? 512 : 256) void weight_few_scores_kernel(To
       meta[i][0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(rec + Lay::kOffKMeta + 4 * t));
     }
   }
+  // WHOLE: a lane's tokens in the sums are those of pages 4 j + quad
+  const size_t at = ((size_t)b * H + h) * a.w_stride;
+  const int token0 = kBlock * (page0 + quad) + t;
+  float before[WHOLE ? PAGES / 4 : 1], kept[WHOLE ? PAGES : 1][ROWS];
+  if constexpr (WHOLE) {
+#pragma unroll
+    for (int j = 0; j < PAGES / 4; ++j) before[j] = a.w_in && token0 + 64 * j < s.ctx ? a.w_in[at + token0 + 64 * j] : 0.0f;
+  }
   const FewOps* from = reinterpret_cast<const FewOps*>(a.few) + ((size_t)b * H + h);
   if constexpr (ALONE) {
-    few_operands<512>(a, s, h, R, work, own);
+    few_operands<64 * W>(a, s, h, R, work, own);
     __syncthreads();
     from = &own;
   }
@@ -758,9 +766,14 @@ __global__ __launch_bounds__(ALONE ? 512 : 256) void weight_few_scores_kernel(To
   float m[ROWS], sum[ROWS];
 #pragma unroll
   for (int k = 0; k < ROWS; ++k) m[k] = kNone, sum[k] = 0.0f;
-  float* scores = a.scores + (((size_t)b * H + h) * a.page_cap + page0) * (kBlock * a.row_cap) + ROWS * quad * kBlock + t;
+  float* scores = WHOLE ? nullptr : a.scores + (((size_t)b * H + h) * a.page_cap + page0) * (kBlock * a.row_cap) + ROWS * quad * kBlock + t;
 #pragma unroll
-  for (int i = 0; i < kPiecePages; ++i) {
+  for (int i = 0; i < PAGES; ++i) {
+    if constexpr (WHOLE) {
+#pragma unroll
+      for (int k = 0; k < ROWS; ++k) kept[i][k] = -INFINITY;
+      if (page0 + i >= pages) continue;
+    }
     if (page0 + i >= pages) break;
     const uint32_t u = code[i].x, v = code[i].y, uh = u >> 10, vh = v >> 10;
     const cd_h8_t c[4] = {bits_of<0>(u, uh, v, vh), bits_of<2>(u, uh, v, vh), bits_of<4>(u, uh, v, vh), bits_of<6>(u, uh, v, vh)};
@@ -798,7 +811,10 @@ __global__ __launch_bounds__(ALONE ? 512 : 256) void weight_few_scores_kernel(To
         m[k] = top;
       }
       sum[k] += __builtin_amdgcn_exp2f(x - m[k]);
-      if (ROWS * quad + k < a.row_cap) scores[i * (kBlock * a.row_cap) + k * kBlock] = x;
+      if constexpr (WHOLE)
+        kept[i][k] = x;
+      else if (ROWS * quad + k < a.row_cap)
+        scores[i * (kBlock * a.row_cap) + k * kBlock] = x;
     }
   }
 #pragma unroll
@@ -808,12 +824,33 @@ __global__ __launch_bounds__(ALONE ? 512 : 256) void weight_few_scores_kernel(To
     if (t == 0) both[w][ROWS * quad + k] = make_float2(top, all);
   }
   __syncthreads();
-  if (threadIdx.x < 4 * ROWS) {
+  if constexpr (WHOLE) {
+    float lse[ROWS];
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      const float2 v = t < W ? both[min(t, W - 1)][ROWS * quad + k] : make_float2(kNone, 0.0f);
+      const float top = row_max16(v.x), all = row_sum16(v.y * __builtin_amdgcn_exp2f(v.x - top));
+      lse[k] = all == 0.0f ? INFINITY : top + __builtin_amdgcn_logf(all);
+    }
+#pragma unroll
+    for (int j = 0; j < PAGES / 4; ++j) {
+      float mine = 0.0f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x = __builtin_amdgcn_exp2f(kept[4 * j + i][0] - lse[0]);
+        if constexpr (ROWS == 2) x += __builtin_amdgcn_exp2f(kept[4 * j + i][1] - lse[1]);
+        x += __shfl_xor(x, 16);
+        x += __shfl_xor(x, 32);
+        mine = quad == i ? x : mine;
+      }
+      if (token0 + 64 * j < s.ctx) a.w_out[at + token0 + 64 * j] = a.w_in ? __builtin_fmaf(a.decay, before[j], mine) : mine;
+    }
+  } else if (threadIdx.x < 4 * ROWS) {
     float top = kNone, all = 0.0f;
 #pragma unroll
-    for (int x = 0; x < kW; ++x) top = fmaxf(top, both[x][threadIdx.x].x);
+    for (int x = 0; x < W; ++x) top = fmaxf(top, both[x][threadIdx.x].x);
 #pragma unroll
-    for (int x = 0; x < kW; ++x) all += both[x][threadIdx.x].y * __builtin_amdgcn_exp2f(both[x][threadIdx.x].x - top);
+    for (int x = 0; x < W; ++x) all += both[x][threadIdx.x].y * __builtin_amdgcn_exp2f(both[x][threadIdx.x].x - top);
     a.stats[(((size_t)b * H + h) * a.pieces + piece) * kFewRows + threadIdx.x] = make_float2(top, all);
   }
 }
@@ -896,29 +933,33 @@ TokenWeightsPlan make_token_weights_plan(int B, int Hq, int H, int total_q, int 
 
 namespace {
 
-template <int NG, bool ALONE>
+// W, PAGES, ALONE, WHOLE: as weight_few_scores_kernel
+template <int NG, int W, int PAGES, bool ALONE, bool WHOLE>
 hipError_t launch_scores(const TokenWeightsArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)((long long)a.B * a.cv.num_kv_heads * a.pieces));
+  const long long BH = (long long)a.B * a.cv.num_kv_heads;
+  if (!ALONE) {
+    hipLaunchKernelGGL(weight_few_rows_kernel, dim3((unsigned)BH), dim3(1024), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  const dim3 grid((unsigned)(BH * (WHOLE ? 1 : a.pieces)));
   if (a.row_cap <= 4)
-    hipLaunchKernelGGL((weight_few_scores_kernel<NG, 1, ALONE>), grid, dim3(ALONE ? 512 : 256), 0, s, a);
+    hipLaunchKernelGGL((weight_few_scores_kernel<NG, 1, W, PAGES, ALONE, WHOLE>), grid, dim3(64 * W), 0, s, a);
   else
-    hipLaunchKernelGGL((weight_few_scores_kernel<NG, 2, ALONE>), grid, dim3(ALONE ? 512 : 256), 0, s, a);
+    hipLaunchKernelGGL((weight_few_scores_kernel<NG, 2, W, PAGES, ALONE, WHOLE>), grid, dim3(64 * W), 0, s, a);
   return hipGetLastError();
 }
-
 template <int NG>
 hipError_t launch_few(const TokenWeightsArgs& a, hipStream_t s) {
   const long long H = a.cv.num_kv_heads;
-  hipError_t e;
+  // Contexts that a block holds take one launch and keep no scores in memory (32 + 8 heads): 500 tokens of 256 sequences 35 us, in
+  // pieces 48; 1,000 of one 11 and 13, of 64 20 and 29 (40 + 8 heads); 2,000 of 128 61 and 68
+  if (a.max_ctx <= 8 * 4 * kBlock) return launch_scores<NG, 8, 4, true, true>(a, s);
+  if (a.max_ctx <= 16 * 4 * kBlock) return launch_scores<NG, 16, 4, true, true>(a, s);
+  if (a.max_ctx <= 16 * 8 * kBlock) return launch_scores<NG, 16, 8, true, true>(a, s);
   // While every compute unit has at most one block, each rotates its own queries, a launch less: 16,000 tokens of one sequence (32 + 8
   // heads) 16.5 us, with the launch 18.2; 32,000, twice the blocks, 26.1 and 20.5
-  if (a.B * H * a.pieces <= num_cus()) {
-    e = launch_scores<NG, true>(a, s);
-  } else {
-    hipLaunchKernelGGL(weight_few_rows_kernel, dim3((unsigned)(a.B * H)), dim3(1024), 0, s, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    e = launch_scores<NG, false>(a, s);
-  }
+  const hipError_t e = a.B * H * a.pieces <= num_cus() ? launch_scores<NG, 8, 4, true, false>(a, s) : launch_scores<NG, 4, 8, false, false>(a, s);
   if (e != hipSuccess) return e;
   const long long joins = ((long long)a.page_cap * kBlock + kJoinTokens - 1) / kJoinTokens;
   hipLaunchKernelGGL(weight_few_join_kernel, dim3((unsigned)(a.B * H * joins)), dim3(256), 0, s, a);
