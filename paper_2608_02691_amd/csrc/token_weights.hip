@@ -694,7 +694,7 @@ __global__ __launch_bounds__(1024) void weight_few_rows_kernel(TokenWeightsArgs 
 // and ROWS rows, 1 (up to four of a KV head) or 2. ALONE: forms its operands itself, while the keys are on their way. WHOLE: the
 // block has the whole context, so that scores and statistics stay in registers and LDS, and forms the sums too.
 template <int NG, int ROWS, int W, int PAGES, bool ALONE, bool WHOLE>
-__global__ __launch_bounds__(64 * W) void weight_few_scores_kernel(TokenWeightsArgs a) {
+__global__ __launch_bounds__(64 * W, 4) void weight_few_scores_kernel(TokenWeightsArgs a) {
   using Lay = Rec<NG>;
   static_assert(WHOLE ? ALONE && W <= 16 && PAGES % 4 == 0 : W * PAGES * kBlock == kPieceTokens, "a lane of sixteen a wave; pieces");
   __shared__ float2 both[W][kFewRows];
@@ -729,7 +729,7 @@ __global__ __launch_bounds__(64 * W) void weight_few_scores_kernel(TokenWeightsA
   // WHOLE: a lane's tokens in the sums are those of pages 4 j + quad
   const size_t at = ((size_t)b * H + h) * a.w_stride;
   const int token0 = kBlock * (page0 + quad) + t;
-  float before[WHOLE ? PAGES / 4 : 1], kept[WHOLE ? PAGES : 1][ROWS];
+  float before[WHOLE ? PAGES / 4 : 1], kept[PAGES][ROWS];
   if constexpr (WHOLE) {
 #pragma unroll
     for (int j = 0; j < PAGES / 4; ++j) before[j] = a.w_in && token0 + 64 * j < s.ctx ? a.w_in[at + token0 + 64 * j] : 0.0f;
@@ -763,18 +763,9 @@ __global__ __launch_bounds__(64 * W) void weight_few_scores_kernel(TokenWeightsA
     if constexpr (NG == 1) Q[k][0] = (Q[k][0] + Q[k][1]) + (Q[k][2] + Q[k][3]);
     lim[k] = row < s.n * a.gq ? s.limit(row / a.gq) : 0;
   }
-  float m[ROWS], sum[ROWS];
-#pragma unroll
-  for (int k = 0; k < ROWS; ++k) m[k] = kNone, sum[k] = 0.0f;
   float* scores = WHOLE ? nullptr : a.scores + (((size_t)b * H + h) * a.page_cap + page0) * (kBlock * a.row_cap) + ROWS * quad * kBlock + t;
 #pragma unroll
   for (int i = 0; i < PAGES; ++i) {
-    if constexpr (WHOLE) {
-#pragma unroll
-      for (int k = 0; k < ROWS; ++k) kept[i][k] = -INFINITY;
-      if (page0 + i >= pages) continue;
-    }
-    if (page0 + i >= pages) break;
     const uint32_t u = code[i].x, v = code[i].y, uh = u >> 10, vh = v >> 10;
     const cd_h8_t c[4] = {bits_of<0>(u, uh, v, vh), bits_of<2>(u, uh, v, vh), bits_of<4>(u, uh, v, vh), bits_of<6>(u, uh, v, vh)};
     const int token = kBlock * (page0 + i) + t;
@@ -804,23 +795,27 @@ __global__ __launch_bounds__(64 * W) void weight_few_scores_kernel(TokenWeightsA
       }
       x = __builtin_fmaf(x, down24, z);
       x = (real >> i) & 1 && token < lim[k] ? x : -INFINITY;
-      // the reference moves when a score exceeds it by 2^40, which fp32's sums have room for
-      if (__any(x > m[k] + 40.0f)) {
-        const float top = fmaxf(m[k], x);
-        sum[k] *= __builtin_amdgcn_exp2f(m[k] - top);
-        m[k] = top;
-      }
-      sum[k] += __builtin_amdgcn_exp2f(x - m[k]);
-      if constexpr (WHOLE)
-        kept[i][k] = x;
-      else if (ROWS * quad + k < a.row_cap)
-        scores[i * (kBlock * a.row_cap) + k * kBlock] = x;
+      kept[i][k] = x;
     }
+  }
+  if constexpr (!WHOLE) {  // (here, so that the products of several pages may overlap)
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k)
+      if (ROWS * quad + k < a.row_cap) {
+#pragma unroll
+        for (int i = 0; i < PAGES; ++i)
+          if (page0 + i < pages) scores[i * (kBlock * a.row_cap) + k * kBlock] = kept[i][k];
+      }
   }
 #pragma unroll
   for (int k = 0; k < ROWS; ++k) {
-    const float top = row_max16(m[k]);
-    const float all = row_sum16(sum[k] * __builtin_amdgcn_exp2f(m[k] - top));
+    float top = kNone, all = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PAGES; ++i) top = fmaxf(top, kept[i][k]);
+    top = row_max16(top);
+#pragma unroll
+    for (int i = 0; i < PAGES; ++i) all += __builtin_amdgcn_exp2f(kept[i][k] - top);
+    all = row_sum16(all);
     if (t == 0) both[w][ROWS * quad + k] = make_float2(top, all);
   }
   __syncthreads();
