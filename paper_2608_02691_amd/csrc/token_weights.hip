@@ -308,6 +308,7 @@ __global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a)
   __shared__ __align__(16) RowTile lds[kSlots];
   __shared__ float2 both[2][4][kRows], stats[PASS == 1 ? kChunkTiles : 1][kRows];
   __shared__ float top_of[4][kRows];
+  __shared__ float2 unused[PASS == 1 ? 64 : 1];
   // Heads come first, so that the blocks of a head share an XCD's L2, then ranges: the engines of an XCD take
   // blocks in turn, which by sequences of different lengths leaves some with more to do. Last chunks go first: those that most ranges see
   const int H = a.cv.num_kv_heads, BH = a.B * H, other = blockIdx.x / H, bh = other / a.ranges % a.B * H + blockIdx.x % H;
@@ -359,14 +360,15 @@ __global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a)
   bool pending = false;
   auto scores = [&](const RowTile& ops, auto&& beside, auto&& middle) {
     if constexpr (PASS == 2) middle();  // (in the middle it would cost the second pass registers it does not have)
-    cd_h8_t group = ops.group[n], op[2][2][2];  // [quarter][high, low]
-    if (hh) group = cd_h8_t{};
+    const cd_h8_t group = ops.group[n];  // (the other lane half's tokens have zeros there)
+    cd_h8_t op[2][2][2];  // [quarter][high, low]
     auto read = [&](int q) {
 #pragma unroll
       for (int x = 0; x < 2; ++x) op[q & 1][0][x] = ops.hi[2 * q + x][l], op[q & 1][1][x] = ops.lo[2 * q + x][l];
     };
     read(0);
     cd_f16_t D[2];
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int q = 0; q < 4; ++q)
 #pragma unroll
@@ -386,9 +388,10 @@ __global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a)
           for (int r = 0; r < 16; ++r) X[v][r] = __builtin_fmaf(tok[v].scale[NG == 4 ? g : 0], D[v][r], X[v][r]);
         }
         // products and vector instructions in turn: a wave issues in order, and each product waits for the one before
-        if (q == 0)
+        if (q == 0) {
+          if (u == 0) __builtin_amdgcn_sched_group_barrier(0x402, 8, 0);
           in_turn<5, 8>();
-        else
+        } else
           in_turn<4, 4>();
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -413,9 +416,10 @@ __global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a)
   auto sums = [&](int i, int t) {
     if (i > 2) return;
     if (i == 2) {
-      if (PASS == 2 || !pending) return;
-      const float all = fold(v, false);
-      if ((l & 1) == 0) both[t & 1][w][fold_row(l)] = make_float2(0.0f, all);
+      if (PASS == 2) return;
+      // (by the address, not by a branch, into which the compiler would move the exponentials, behind the products)
+      float2* to = pending ? &both[t & 1][w][fold_row(l)] : &unused[l];
+      *to = make_float2(0.0f, fold(v, false));  // lanes of a pair the same
       return;
     }
 #pragma unroll
