@@ -582,8 +582,9 @@ constexpr int kJoinTokens = 1024;
 // products forms several groups' sums. Up to four rows: operand row 4 j + g is group g of row j, and D's registers are the four groups of
 // one row. Up to eight: operand row 2 j + g % 2, two D, for g / 2. A lane's eight channels (lane = 16 quad + operand
 // row): positions 2 g, 2 g + 1 of words 2 quad, 2 quad + 1.
-// Codes are used as they lie: as an fp16 number their bits at 2 p are the subnormal code 2^(2 p - 24), which the matrix cores take
-// exactly, and the queries' operands carry 2^(-2 p). So one AND makes two channels.
+// Codes are normal numbers: taken as they lie, as subnormal ones code 2^(2 p - 24), they would spare an instruction for two
+// channels, but the matrix cores align a product by its operands' exponents, and the leading zeros of a subnormal one cost the
+// sum as many of its last bits (weights off by 8e-6 of themselves in place of 5e-7).
 struct FewOps {
   cd_h8_t term[2][2][64];  // [group / 2 (up to eight rows)][high, low]
   float sum[kFewRows][4];  // of a row's channels of each group
@@ -593,14 +594,11 @@ struct FewOps {
 __device__ __forceinline__ cd_f4_t product16(const cd_h8_t& x, const cd_h8_t& y, const cd_f4_t& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0);
 }
-// Positions P, P + 1 (both below 5 or not) of two words
+// Positions P, P + 1 of two words
 template <int P>
-__device__ __forceinline__ uint32_t bits_at(uint32_t w, uint32_t hi) {
-  return P < 5 ? w & in_sgpr((3u << 2 * P) * 0x10001u) : hi & in_sgpr((3u << (2 * P - 10)) * 0x10001u);
-}
-template <int P>
-__device__ __forceinline__ cd_h8_t bits_of(uint32_t u, uint32_t uh, uint32_t v, uint32_t vh) {
-  return __builtin_bit_cast(cd_h8_t, cd_u4_t{bits_at<P>(u, uh), bits_at<P + 1>(u, uh), bits_at<P>(v, vh), bits_at<P + 1>(v, vh)});
+__device__ __forceinline__ cd_h8_t codes_of(uint32_t u, uint32_t uh, uint32_t v, uint32_t vh) {
+  const cd_h2_t a = land_position<P>(u, uh), b = land_position<P + 1>(u, uh), c = land_position<P>(v, vh), d = land_position<P + 1>(v, vh);
+  return cd_h8_t{a.x, a.y, b.x, b.y, c.x, c.y, d.x, d.y};
 }
 
 }  // namespace
@@ -666,8 +664,8 @@ __device__ __forceinline__ void few_operands(const TokenWeightsArgs& a, const Sp
 #pragma unroll
   for (int i = 0; i < kEach; ++i) {
     const int r = k + kParts * i;
-    const float y = d[i] * __uint_as_float((267u - e) << 23), z = y * __uint_as_float((127u - 2 * (pos % 5)) << 23);
-    const _Float16 hi = (_Float16)z, lo = (_Float16)(z - (float)hi);
+    const float y = d[i] * __uint_as_float((267u - e) << 23);
+    const _Float16 hi = (_Float16)y, lo = (_Float16)(y - (float)hi);
     if (!narrow || r < 4) {
       const int at = narrow ? 0 : g >> 1, lane = 16 * (word >> 1) + (narrow ? 4 * r + g : 2 * r + (g & 1));
       reinterpret_cast<_Float16*>(&out.term[at][0][lane])[element] = hi;
@@ -745,7 +743,7 @@ __global__ __launch_bounds__(64 * W, 4) void weight_few_scores_kernel(TokenWeigh
     from = &own;
   }
   const FewOps& ops = *from;
-  const float down = ops.down, down24 = down * 0x1p24f;
+  const float down = ops.down;
   cd_h8_t A[2][4];  // [high, low][group]
   float Q[ROWS][4];
   int lim[ROWS];
@@ -771,7 +769,7 @@ __global__ __launch_bounds__(64 * W, 4) void weight_few_scores_kernel(TokenWeigh
 #pragma unroll
   for (int i = 0; i < PAGES; ++i) {
     const uint32_t u = code[i].x, v = code[i].y, uh = u >> 10, vh = v >> 10;
-    const cd_h8_t c[4] = {bits_of<0>(u, uh, v, vh), bits_of<2>(u, uh, v, vh), bits_of<4>(u, uh, v, vh), bits_of<6>(u, uh, v, vh)};
+    const cd_h8_t c[4] = {codes_of<0>(u, uh, v, vh), codes_of<2>(u, uh, v, vh), codes_of<4>(u, uh, v, vh), codes_of<6>(u, uh, v, vh)};
     const int token = kBlock * (page0 + i) + t;
     cd_f4_t D[ROWS];
 #pragma unroll
@@ -797,7 +795,7 @@ __global__ __launch_bounds__(64 * W, 4) void weight_few_scores_kernel(TokenWeigh
         x = f16_bits_to_f32(meta[i][0] & 0xFFFFu) * ((d[0] + d[1]) + (d[2] + d[3]));
         z = f16_bits_to_f32(meta[i][0] >> 16) * Q[k][0];
       }
-      x = __builtin_fmaf(x, down24, z);
+      x = __builtin_fmaf(x, down, z);
       x = (real >> i) & 1 && token < lim[k] ? x : -INFINITY;
       kept[i][k] = x;
     }

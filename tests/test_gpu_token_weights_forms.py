@@ -4,6 +4,7 @@ import numpy as np
 import pytest
 import torch
 
+from _chunk import stored_rows
 from _tokens import K, WeightsCall, assert_weights_close, dev
 
 pytestmark = pytest.mark.gpu
@@ -125,3 +126,50 @@ def test_many_sequences_are_repeatable(length):
     total = (first - 0.75 * torch.where(torch.arange(length, device="cuda") < dev(c.lens)[:, None, None], dev(c.w), 0)).double().sum(-1)
     # each of the `length` differences is off by a rounding of its parts and the weight's own error: 2^-22 of sums up to a few tens
     assert torch.allclose(total, torch.full_like(total, 4.0), atol=length * 2.0 ** -18)
+
+
+def typical_error(c):
+    """Norms over all weights [.., tokens] of the sums and of what their error comes to in fp32, with no running sums. With s_g D_g
+    and z_g Q_g the parts of a score x (base 2): each part and x are sums in which at most 8 roundings of that size count (a
+    group's products come in two terms, each of which may round up to four times; fma chains over the groups). A rounding is
+    uniform within half a step, at most 2^-24 of the value, thus 2^-24 / sqrt(3) in the root mean square, and the score is off
+    by delta = sqrt(8 / 3) 2^-24 sqrt(sum_g (s_g D_g)^2 + (z_g Q_g)^2 + x^2). A weight is off by ln 2 of that of itself, and by as much
+    again for its row's log sum, a mean of such errors; the logarithm, the exponential and the sum add 2^-22."""
+    D, PAGE = 128, 16
+    want, off, q, ng = 0.0, 0.0, c.q.double().numpy(), D // c.group
+    for b, (n, ctx) in enumerate(c.seqs):
+        if ctx == 0 or n == 0:
+            continue
+        kc, _ = stored_rows(c.pool, c.table[b], ctx)
+        for h in range(c.H):
+            z, w, e = c._zeros(b, ctx, h), np.zeros(ctx), np.zeros(ctx)
+            for j in range(h * c.gq, (h + 1) * c.gq):
+                qr = q[c.starts[b]:c.starts[b] + n, j] @ c.R_k[h].astype(np.float64) / np.sqrt(D) * np.log2(np.e)
+                x = qr @ kc[:, h].T
+                parts = x ** 2
+                for g in range(ng):
+                    s = slice(g * c.group, (g + 1) * c.group)
+                    Q = qr[:, s].sum(1)[:, None] * z[None, :, g]
+                    parts += (qr[:, s] @ kc[:, h, s].T - Q) ** 2 + Q ** 2
+                x = np.where(np.arange(ctx) < ctx - n + np.arange(n)[:, None] + 1, x, -np.inf)
+                p = np.exp2(x - x.max(1, keepdims=True))
+                p /= p.sum(1, keepdims=True)
+                w += p.sum(0)
+                e += (p * (2 * np.log(2) * np.sqrt(8 / 3) * 2.0 ** -24 * np.sqrt(parts) + 2.0 ** -22)).sum(0)
+            want, off = want + (w ** 2).sum(), off + (e ** 2).sum()
+    return np.sqrt(want), np.sqrt(off)
+
+
+@pytest.mark.parametrize("seqs,heads,gq,group", [
+    ([(1, 31)] * 6, 2, 4, 32), ([(1, 400)] * 4, 2, 4, 128), ([(1, 900), (1, 700)], 4, 5, 32), ([(1, 2000)] * 2, 2, 8, 128),
+    ([(1, 1500)] * 4, 2, 1, 32), ([(2, 600)] * 3, 2, 3, 32), ([(12, 600)] * 2, 2, 4, 32), ([(12, 600)] * 2, 2, 4, 128)])
+def test_typical_errors_are_those_of_fp32(seqs, heads, gq, group):
+    """The worst case above leaves room for terms that lose bits everywhere; the norm of the error does not."""
+    c = calls(seqs, heads, gq, group, seed=31, first=True)
+    ref, _ = c.reference()
+    want, most = typical_error(c)
+    for max_ctx in (c.max_ctx, LONG):
+        got = c.call(max_ctx=max_ctx, out=torch.zeros(c.shape, device="cuda")).double().cpu().numpy()
+        err = np.sqrt(((got - ref) ** 2).sum())
+        print(f"max_ctx {max_ctx}: {err / want:.2e} of the weights, {err / most:.3f} of the bound")
+        assert err <= most, (max_ctx, err / want, most / want)
