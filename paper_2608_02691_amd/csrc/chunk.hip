@@ -643,7 +643,7 @@ __global__ __launch_bounds__(64 * NW, 2) void chunk_attn_kernel(ChunkArgs a) {
         d[0] = make_float4(e[4 * q], f[4 * q], e[4 * q + 1], f[4 * q + 1]);
         d[1] = make_float4(e[4 * q + 2], f[4 * q + 2], e[4 * q + 3], f[4 * q + 3]);
       }
-    if (hh == 0) reinterpret_cast<float2*>(part + (size_t)a.bm * kHeadDim)[rt] = make_float2(TREE && absent ? kAbsent : st.thr < 0.0f ? kNone : st.m, all);
+    if (hh == 0) reinterpret_cast<float2*>(part + (size_t)a.bm * kHeadDim)[rt] = make_float2(st.thr < 0.0f ? kNone : st.m, TREE && absent ? kAbsent : all);
   }
 }
 
@@ -660,6 +660,7 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
   const size_t stride = (size_t)H * a.bm * kChunkPartStride, ml_at = (size_t)a.bm * kHeadDim;
   const float* part = a.part + ((size_t)tile.slot * H + h) * a.bm * kChunkPartStride;
   float o[8] = {}, all = 0.0f, top = kNone;
+  bool absent = false;
   for (int p0 = 0; p0 < tile.pieces; p0 += 4) {
     float2 ml[4];
     float4 u[4], v[4];
@@ -681,6 +682,7 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       if (p0 + i >= tile.pieces) continue;
+      if (TREE) absent |= ml[i].y == kAbsent;
       const float f = __builtin_amdgcn_exp2f(ml[i].x - top);
       all = __builtin_fmaf(ml[i].y, f, all);
       o[0] = __builtin_fmaf(u[i].x, f, o[0]), o[1] = __builtin_fmaf(u[i].y, f, o[1]);
@@ -689,7 +691,7 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(ChunkArgs a) {
       o[6] = __builtin_fmaf(v[i].z, f, o[6]), o[7] = __builtin_fmaf(v[i].w, f, o[7]);
     }
   }
-  if (TREE && top >= kAbsent) {  // whatever the other pieces hold
+  if (TREE && absent) {  // whatever the other pieces hold
     all = 0.0f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) o[j] = 0.0f;

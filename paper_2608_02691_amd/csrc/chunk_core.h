@@ -417,7 +417,7 @@ __device__ __forceinline__ int pos_channel(int pos) { return code_channel(pos >>
 __device__ __forceinline__ int row_position(int m) { return (m & 3) | ((m & 4) << 1) | ((m & 8) >> 1) | (m & 16); }
 
 // ---- Trees: a token sees the tokens on its path, itself, its parent and so on to one whose parent is -1
-constexpr float kAbsent = 1.0e30f;  // running maximum of a partial whose row has no path: nothing else counts beside it
+constexpr float kAbsent = -1.0f;  // sum of a partial whose row has no path: sums of probabilities are never below zero, also where scores are infinite
 typedef uint32_t path_t __attribute__((ext_vector_type(kTreeMost / 32)));  // bit t % 32 of word t / 32: token t lies on it
 // The path of token t of a tree whose parents lie in LDS; nothing on it for a token that has none. A parent outside [-1, t)
 // ends a walk that way, so each takes at most kTreeMost steps.

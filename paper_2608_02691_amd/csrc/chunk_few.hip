@@ -434,7 +434,7 @@ __global__ __launch_bounds__(64 * kFewWaves, 2) void chunk_few_kernel(ChunkArgs 
       d[0] = make_float4(O[0][8 * x], O[0][8 * x + 1], O[0][8 * x + 2], O[0][8 * x + 3]);
       d[1] = make_float4(O[0][8 * x + 4], O[0][8 * x + 5], O[0][8 * x + 6], O[0][8 * x + 7]);
     }
-    if (w == 0 && hh == 0) reinterpret_cast<float2*>(part + (size_t)a.bm * kHeadDim)[n] = make_float2(TREE && absent ? kAbsent : thr < 0.0f ? kNone : m, all);
+    if (w == 0 && hh == 0) reinterpret_cast<float2*>(part + (size_t)a.bm * kHeadDim)[n] = make_float2(thr < 0.0f ? kNone : m, TREE && absent ? kAbsent : all);
   }
 }
 
