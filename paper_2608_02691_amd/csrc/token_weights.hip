@@ -20,6 +20,8 @@ namespace {
 
 constexpr int kRows = 32;                                     // rows of a tile
 constexpr int kChunkTiles = 32;                               // row tiles of a block at most
+constexpr float kSure = 60.0f;  // ref lies above a row's largest score by less than this; sums reach 2^-66 of the largest term
+constexpr float kFar = 100.0f;  // scores above ref by more than this are summed relative to their own maximum
 static_assert(kRangeTokens == 4 * 64, "the waves' tokens");
 
 struct Span {
@@ -104,7 +106,7 @@ struct RowTile {
   float ref[kRows];        // near the row's largest score over the first tokens: its sums are formed relative to it
   float lse[kRows];        // L_r; infinite for rows that see nothing and behind the last one, so that their weights are zero
   float down;              // what brings the scores back to size
-  uint32_t unsure;         // not zero: some row's ref names no score of its own
+  uint32_t unsure;         // not zero: some row's ref names no score of its own, or may lie far above it
   float pad[62];
 };
 constexpr int kTileBytes = sizeof(RowTile), kPieces = kTileBytes / 1024;
@@ -139,6 +141,9 @@ __device__ __forceinline__ Share share_of(const TokenWeightsArgs& a, int bh, int
 // matrix cores, R_K in three bf16 terms that sum to it exactly. A tile's rows are scaled by one power of two that brings
 // the largest element to 2^7 .. 2^8: what the low terms lose, 2^-24, is 2^-31 of it, and a group's sum fits fp16. The
 // last wave forms the rows' scores over the sequence's first 32 tokens, in one fp16 term: their maximum is where the first pass starts.
+// Its roundings, 2^-11 of a query and of a key, may come to many powers of two where scores are large: up to 2^-10 sum |q'_c k_c|, at
+// most 2^-10 128 max |q'| max |k|. Above a row's scores by 126 and more it would leave nothing of the row's sums, so tiles in which the
+// bound passes kSure are summed relative to their own maxima.
 // Bound by the operands it writes, 17 KB a tile: 14,200 tokens of 32 + 8 heads 95 us, 3.7 TB/s. Blocks of several tiles bring R_K
 // once: with one tile each, whole prompts of 4 x 4,000 tokens take 1,448 us, with up to eight 1,380.
 template <int NG>
@@ -165,6 +170,7 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
     R[kk][0] = pack_terms(x), R[kk][1] = pack_terms(y), R[kk][2] = pack_terms(z);
   }
   uint32_t real = 0;
+  float key_top = 0x1p-14f;  // (below it fp16's steps no longer shrink)
   if (w == 3) {
     Token<NG> first;
     first.load(a, b, h, n, s.ctx, hh);
@@ -173,9 +179,15 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
     for (int x = 0; x < 8; ++x) {
       cd_h8_t k;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) k[j] = (_Float16)__builtin_fmaf((float)first.code[x][j], first.scale[x * NG / 8], first.low[x * NG / 8]);
+      for (int j = 0; j < 8; ++j) {
+        const float y = __builtin_fmaf((float)first.code[x][j], first.scale[x * NG / 8], first.low[x * NG / 8]);
+        key_top = first.real ? fmaxf(key_top, fabsf(y)) : key_top;
+        k[j] = (_Float16)y;
+      }
       keys[x][l] = k;
     }
+#pragma unroll
+    for (int step = 32; step > 0; step >>= 1) key_top = fmaxf(key_top, __shfl_xor(key_top, step));
   }
   const int t0 = at * tiles_per_block, t1 = min(tiles, t0 + tiles_per_block), rows = s.n * a.gq;
   // a tile's rows on their way to LDS as the products take them, a quarter by each wave; the last one's again behind the last
@@ -243,7 +255,7 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
       m = pair_max(m) * down;
       const bool good = fabsf(m) < 1.0e30f;
       if (hh == 0) tile.ref[n] = good ? m : 0.0f;
-      const bool unsure = __any(lim > 0 && !good);
+      const bool unsure = __any(lim > 0 && (!good || 0.125f * big * key_top > kSure));
       if (l == 0) tile.unsure = unsure;
     }
 #pragma unroll
@@ -269,7 +281,6 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
 namespace {
 
 constexpr int kSlots = 4;
-constexpr float kFar = 100.0f;  // scores above ref by more than this are summed relative to their own maximum
 
 // Sums over the 32 lanes of a half for all sixteen registers: halves of what is left change places, so that a lane ends with the
 // sum of one register, lane_register()
