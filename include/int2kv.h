@@ -461,7 +461,7 @@ int int2kv_tree_attention(const int2kv_cache* cache, const uint16_t* q, int64_t 
  *   decay        : factor of weights_in, finite
  *   weights_out  : fp32 as weights_in, which it may be, without otherwise overlapping it. Tokens from
  *                  min(ctx_lens[b], max_ctx) on are left as they were; tokens in blocks outside the
- *                  cache receive nothing
+ *                  cache, or behind the table's end, receive nothing: their sums only decay
  *   weights_stride : at least max_ctx
  *   workspace    : int2kv_token_weights_workspace_bytes(...) bytes, 256-byte aligned; enough for every
  *                  call within the same bounds, nothing kept between calls, calls that overlap need one each

@@ -25,7 +25,7 @@ constexpr float kFar = 100.0f;  // scores above ref by more than this are summed
 static_assert(kRangeTokens == 4 * 64, "the waves' tokens");
 
 struct Span {
-  int start, n, ctx, past;  // as Seq
+  int start, n, ctx, past;  // as Seq (but the table does not cut ctx)
   int tile0;                // first of the sequence's row tiles
   __device__ __forceinline__ int limit(int i) const { return max(min(ctx, past + i + 1), 0); }
 };
@@ -36,8 +36,7 @@ __device__ __forceinline__ Span span_of(const TokenWeightsArgs& a, int b) {
   const int end = min(max(a.starts[b + 1], 0), a.total_q);
   const int count = max(end - s.start, 0), len = max(a.lens[b], 0);
   s.n = min(count, a.max_q);
-  const long long room = (long long)a.max_blocks * kBlock;
-  s.ctx = min(len, (int)(room < a.max_ctx ? room : a.max_ctx));
+  s.ctx = min(len, a.max_ctx);  // tokens behind the table's end lie in no block: their sums decay with the others
   s.past = len - count;
   s.tile0 = (int)((long long)s.start * a.gq / kRows) + b;
   return s;
@@ -70,7 +69,7 @@ struct Token {
   bool real;
   __device__ __forceinline__ void load(const TokenWeightsArgs& a, int b, int h, int token, int ctx, int hh) {
     int id = -1;
-    if (token < ctx) id = a.table[(size_t)b * a.max_blocks + token / kBlock];
+    if (token < ctx && token / kBlock < a.max_blocks) id = a.table[(size_t)b * a.max_blocks + token / kBlock];
     real = id >= 0 && id < a.cv.num_blocks;
     const uint8_t* rec = a.cv.pool + ((size_t)(uint32_t)(real ? id : 0) * a.cv.num_kv_heads + h) * Rec<NG>::kBytes;
     const int t = token & 15;
@@ -727,7 +726,7 @@ __global__ __launch_bounds__(64 * W, 4) void weight_few_scores_kernel(TokenWeigh
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, t = l & 15, quad = l >> 4;
   const int page0 = W * PAGES * piece + PAGES * w, pages = (s.ctx + kBlock - 1) / kBlock;
   int id = -1;
-  if (l < PAGES && page0 + l < pages) id = a.table[(size_t)b * a.max_blocks + page0 + l];
+  if (l < PAGES && page0 + l < min(pages, a.max_blocks)) id = a.table[(size_t)b * a.max_blocks + page0 + l];
   const uint32_t real = (uint32_t)__ballot(id >= 0 && id < a.cv.num_blocks);
   cd_u2_t code[PAGES];
   uint32_t meta[PAGES][NG];
