@@ -485,7 +485,7 @@ int int2kv_token_weights(const int2kv_cache* cache, const uint16_t* q, int64_t q
  *   kept         : int32, list of KV head h of sequence b at (b num_kv_heads + h) kept_stride;
  *                  kept_lens[b] = min(ctx_lens[b], max_ctx, budget) entries are written
  *   kept_stride  : at least min(budget, max_ctx)
- *   kept_lens    : int32 [batch] */
+ *   kept_lens    : int32 [batch]; neither it nor kept may overlap weights, ctx_lens or the other */
 int int2kv_select_tokens(const float* weights, int64_t weights_stride, int batch, int num_kv_heads,
                          const int32_t* ctx_lens, int max_ctx, int budget, int sink, int recent, int32_t* kept,
                          int64_t kept_stride, int32_t* kept_lens, hipStream_t stream);

@@ -644,6 +644,12 @@ bool rows_meet(const Rows& a, const Rows& b) {
   return d < a.len() || a.step() - d < b.len();
 }
 
+// Whether two ranges of bytes meet
+bool spans_meet(const void* a, uint64_t a_len, const void* b, uint64_t b_len) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a_len && b_len && x < y + b_len && y < x + a_len;
+}
+
 bool valid_stride(int64_t stride, int heads) { return stride >= (int64_t)heads * kHeadDim && stride % 8 == 0 && stride <= INT32_MAX; }
 
 // Attention of new tokens over the cache and their own rows: checks, plan and launch. The names of the caller's rows are for
@@ -872,6 +878,12 @@ int int2kv_select_tokens(const float* weights, int64_t weights_stride, int batch
   if (!ctx_lens || !kept_lens || (max_ctx > 0 && !weights) || (max_ctx > 0 && budget > 0 && !kept)) return fail(INT2KV_EINVAL, "NULL pointer argument");
   if (!aligned(weights, 4) || !aligned(kept, 4) || !aligned(ctx_lens, 4) || !aligned(kept_lens, 4))
     return fail(INT2KV_EINVAL, "weights, ctx_lens, kept and kept_lens must be 4-byte aligned");
+  // every work-group reads its sequence's length and its own weights, and writes its list; one of a sequence's writes the new length
+  const uint64_t more = (uint64_t)batch * num_kv_heads - 1, lens = 4ull * batch, longest = budget < max_ctx ? budget : max_ctx;
+  const uint64_t w_len = max_ctx > 0 ? 4 * (more * weights_stride + max_ctx) : 0, kept_len = longest > 0 ? 4 * (more * kept_stride + longest) : 0;
+  if (spans_meet(kept_lens, lens, ctx_lens, lens) || spans_meet(kept_lens, lens, weights, w_len) || spans_meet(kept_lens, lens, kept, kept_len) ||
+      spans_meet(kept, kept_len, ctx_lens, lens) || spans_meet(kept, kept_len, weights, w_len))
+    return fail(INT2KV_EINVAL, "kept and kept_lens must not overlap weights, ctx_lens or each other");
   SelectArgs a{weights, weights_stride, ctx_lens, batch, num_kv_heads, max_ctx, budget, sink, recent, kept, kept_stride, kept_lens};
   return hip_status(launch_select_tokens(a, stream), "select_tokens");
 }
