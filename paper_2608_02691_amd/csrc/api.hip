@@ -851,8 +851,9 @@ int int2kv_token_weights(const int2kv_cache* cache, const uint16_t* q, int64_t q
   if (max_ctx > INT32_MAX - (1 << 18)) return fail(INT2KV_EUNSUPPORTED, "max_ctx must be at most 2^31 - 2^18 - 1");
   const TokenWeightsPlan plan = make_token_weights_plan(batch, num_q_heads, H, total_q, max_q, max_ctx);
   // a launch holds 2^32 - 1 threads
-  if ((int64_t)batch * H * plan.ranges > UINT32_MAX / 512 / (plan.chunks > 1 ? plan.chunks : 1) ||
-      (int64_t)batch * H * plan.seq_tiles > UINT32_MAX / 256 || (plan.few && (int64_t)batch * H > UINT32_MAX / 1024))
+  const int seq_tiles = plan.slab_tiles > 0 ? plan.slab_tiles : plan.seq_tiles;
+  if ((int64_t)batch * H * plan.ranges > UINT32_MAX / 512 / (plan.slab_chunks > 1 ? plan.slab_chunks : 1) ||
+      (int64_t)batch * H * seq_tiles > UINT32_MAX / 256 || (plan.few && (int64_t)batch * H > UINT32_MAX / 1024))
     return fail(INT2KV_EUNSUPPORTED, "too many row tiles or token ranges for one launch");
   if (!workspace || workspace_bytes < plan.total)
     return fail(INT2KV_EWORKSPACE, "workspace smaller than int2kv_token_weights_workspace_bytes()");

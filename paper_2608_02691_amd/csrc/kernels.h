@@ -247,11 +247,14 @@ struct TokenWeightsArgs {
   int64_t w_stride;
   float decay;
   // plan and workspace
-  int seq_tiles, ranges, tiles;     // row tiles of a sequence at most; token ranges; all row tiles
+  int seq_tiles, ranges, tiles;     // row tiles of a sequence at most; token ranges; all row tiles (of a slab)
   int chunks, chunk_tiles;          // chunks of a sequence's row tiles
+  int chunk0, slab_tiles;           // slabs: the first chunk; tiles of a sequence (0: all of them, one behind the other)
+  bool last;                        // no slab follows
   uint8_t* ops;                     // [tiles, H] row tiles
   float2* stats;                    // [ranges, tiles, H, 32] maximum and sum of a row over a range
-  float* part;                      // [chunks, B, H, ranges * kRangeTokens] where there are several
+  float* part;                      // [chunks, B, H, ranges * kRangeTokens] where there are several, or slabs; else null
+  float* run;                       // [B, H, ranges * kRangeTokens] sums of the slabs before
   // few rows a sequence (stats: [B, H, pieces, 8])
   int pieces, page_cap, row_cap;    // pieces and pages of a sequence, rows of a KV head, each at most
   uint8_t* few;                     // [B, H] row operands
@@ -259,8 +262,8 @@ struct TokenWeightsArgs {
 };
 struct TokenWeightsPlan {
   bool few;
-  int seq_tiles, ranges, tiles, chunks, chunk_tiles, pieces, page_cap, row_cap;
-  size_t off_ops, off_stats, off_part, off_few, off_few_stats, off_scores, total;
+  int seq_tiles, ranges, tiles, chunks, chunk_tiles, slab_chunks, slab_tiles, pieces, page_cap, row_cap;
+  size_t off_ops, off_stats, off_part, off_run, off_few, off_few_stats, off_scores, total;
 };
 constexpr int kRangeTokens = 256;
 TokenWeightsPlan make_token_weights_plan(int B, int Hq, int H, int total_q, int max_q, int max_ctx);

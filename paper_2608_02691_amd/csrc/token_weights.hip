@@ -20,16 +20,18 @@ namespace {
 
 constexpr int kRows = 32;                                     // rows of a tile
 constexpr int kChunkTiles = 32;                               // row tiles of a block at most
+constexpr size_t kSlabBytes = size_t(1) << 30;                // of the workspace, beyond which row tiles are taken in slabs
 constexpr float kSure = 60.0f;  // ref lies above a row's largest score by less than this; sums reach 2^-66 of the largest term
 constexpr float kFar = 100.0f;  // scores above ref by more than this are summed relative to their own maximum
 static_assert(kRangeTokens == 4 * 64, "the waves' tokens");
 
 struct Span {
   int start, n, ctx, past;  // as Seq (but the table does not cut ctx)
-  int tile0;                // first of the sequence's row tiles
+  int tile0;                // place of the sequence's first row tile (in slabs: as if there were one)
   __device__ __forceinline__ int limit(int i) const { return max(min(ctx, past + i + 1), 0); }
 };
-// The tiles of sequence b start at start * gq / 32 + b: never before the end of the one before.
+// The tiles of sequence b start at start * gq / 32 + b: never before the end of the one before. In slabs every sequence has the
+// same number of places, for its tiles from the slab's first one on.
 __device__ __forceinline__ Span span_of(const TokenWeightsArgs& a, int b) {
   Span s;
   s.start = min(max(a.starts[b], 0), a.total_q);
@@ -38,7 +40,7 @@ __device__ __forceinline__ Span span_of(const TokenWeightsArgs& a, int b) {
   s.n = min(count, a.max_q);
   s.ctx = min(len, a.max_ctx);  // tokens behind the table's end lie in no block: their sums decay with the others
   s.past = len - count;
-  s.tile0 = (int)((long long)s.start * a.gq / kRows) + b;
+  s.tile0 = a.slab_tiles > 0 ? b * a.slab_tiles - a.chunk0 * a.chunk_tiles : (int)((long long)s.start * a.gq / kRows) + b;
   return s;
 }
 
@@ -154,9 +156,9 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
   const int H = a.cv.num_kv_heads, blocks = (a.seq_tiles + tiles_per_block - 1) / tiles_per_block;
   const int h = blockIdx.x % H, at = blockIdx.x / H % blocks, b = blockIdx.x / H / blocks;
   const Span s = span_of(a, b);
-  const int tiles = (s.n * a.gq + kRows - 1) / kRows;
+  const int slab0 = a.chunk0 * a.chunk_tiles, tiles = min((s.n * a.gq + kRows - 1) / kRows, slab0 + a.seq_tiles), t0 = slab0 + at * tiles_per_block;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, hh = l >> 5;
-  if (at * tiles_per_block >= tiles || s.ctx == 0) return;
+  if (t0 >= tiles || s.ctx == 0) return;
   cd_u4_t R[8][3];  // of column 32 w + n, rows 16 kk + 8 hh ..
 #pragma unroll
   for (int kk = 0; kk < 8; ++kk) {
@@ -188,7 +190,7 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
 #pragma unroll
     for (int step = 32; step > 0; step >>= 1) key_top = fmaxf(key_top, __shfl_xor(key_top, step));
   }
-  const int t0 = at * tiles_per_block, t1 = min(tiles, t0 + tiles_per_block), rows = s.n * a.gq;
+  const int t1 = min(tiles, t0 + tiles_per_block), rows = s.n * a.gq;
   // a tile's rows on their way to LDS as the products take them, a quarter by each wave; the last one's again behind the last
   auto fetch = [&](int t) {
     const int row = min(kRows * t + n, rows - 1), tok = quotient(row, a.gq);
@@ -326,18 +328,18 @@ __global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a)
   // blocks in turn, which by sequences of different lengths leaves some with more to do. Last chunks go first: those that most ranges see
   const int H = a.cv.num_kv_heads, BH = a.B * H, other = blockIdx.x / H, bh = other / a.ranges % a.B * H + blockIdx.x % H;
   const Span s = span_of(a, bh / H);
-  const Share me = share_of(a, bh, other % a.ranges, a.chunks - 1 - other / a.ranges / a.B, s);
-  if (me.t0 >= me.t1 && (PASS == 1 || a.chunks > 1 || me.first >= s.ctx)) return;
+  const Share me = share_of(a, bh, other % a.ranges, a.chunk0 + a.chunks - 1 - other / a.ranges / a.B, s);
+  if (me.t0 >= me.t1 && (PASS == 1 || a.part || me.first >= s.ctx)) return;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, hh = l >> 5, token0 = me.first + 64 * w;
   // ---- Row tiles on their way to LDS, tile t in slot t % kSlots. Half way through a tile (at its start) the next one has landed for every wave
   // and the one before is done with, so that no wave waits between tiles.
-  const uint8_t* tiles = a.ops + ((size_t)s.tile0 * H + me.h) * kTileBytes + 16 * l;
+  const uint8_t* tiles = a.ops + ((size_t)(s.tile0 + me.t0) * H + me.h) * kTileBytes + 16 * l;
   const size_t stride = (size_t)H * kTileBytes;
   const uint32_t lds0 = (uint32_t)(uintptr_t)&lds[0];
   auto slot = [&](int t) -> const RowTile& { return lds[t & (kSlots - 1)]; };
   auto issue = [&](int t) {  // 17 pieces by four waves: the first has one more
     if (t >= me.t1) return;
-    for (int c = w; c < kPieces; c += 4) ap_dma16(tiles + t * stride + 1024 * c, lds0 + (uint32_t)((t & (kSlots - 1)) * kTileBytes + 1024 * c));
+    for (int c = w; c < kPieces; c += 4) ap_dma16(tiles + (t - me.t0) * stride + 1024 * c, lds0 + (uint32_t)((t & (kSlots - 1)) * kTileBytes + 1024 * c));
   };
   // until tile t has landed, with what came after it, up to `after` tiles, on its way
   auto landed = [&](int t, auto after) {
@@ -529,8 +531,8 @@ __global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a)
       float x = pair_sum(sum[u]);
       if (!tok[u].real) x = 0.0f;
       if (hh || t >= s.ctx) continue;
-      if (a.chunks > 1) {
-        a.part[((size_t)me.chunk * BH + bh) * ((size_t)a.ranges * kRangeTokens) + t] = x;
+      if (a.part) {
+        a.part[((size_t)(me.chunk - a.chunk0) * BH + bh) * ((size_t)a.ranges * kRangeTokens) + t] = x;
       } else {
         const size_t at = (size_t)bh * a.w_stride + t;
         a.w_out[at] = a.w_in ? __builtin_fmaf(a.decay, a.w_in[at], x) : x;
@@ -543,7 +545,7 @@ __global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a)
 __global__ __launch_bounds__(256) void weight_lse_kernel(TokenWeightsArgs a) {
   __shared__ float2 part[8][kRows];
   const int H = a.cv.num_kv_heads, n = threadIdx.x & 31, k = threadIdx.x >> 5;
-  const int h = blockIdx.x % H, t = blockIdx.x / H % a.seq_tiles, b = blockIdx.x / H / a.seq_tiles;
+  const int h = blockIdx.x % H, t = a.chunk0 * a.chunk_tiles + blockIdx.x / H % a.seq_tiles, b = blockIdx.x / H / a.seq_tiles;
   const Span s = span_of(a, b);
   const int rows = s.n * a.gq, row = kRows * t + n;
   if (kRows * t >= rows || s.ctx == 0) return;
@@ -569,15 +571,20 @@ __global__ __launch_bounds__(256) void weight_lse_kernel(TokenWeightsArgs a) {
   reinterpret_cast<RowTile*>(a.ops + ((size_t)(s.tile0 + t) * H + h) * kTileBytes)->lse[n] = sum == 0.0f ? INFINITY : m + __builtin_amdgcn_logf(sum);
 }
 
-// ---- The chunks' sums, and the running ones: 8 us for up to 16 chunks of 4 x 4,096 tokens and 8 heads
+// ---- The chunks' sums, behind those of the slabs before, and the running ones: 8 us for up to 16 chunks of 4 x 4,096 tokens and 8 heads
 __global__ __launch_bounds__(256) void weight_join_kernel(TokenWeightsArgs a) {
   const int BH = a.B * a.cv.num_kv_heads, bh = blockIdx.x % BH, range = blockIdx.x / BH, t = kRangeTokens * range + threadIdx.x;
   const Span s = span_of(a, bh / a.cv.num_kv_heads);
   if (t >= s.ctx) return;
-  float sum = 0.0f;
+  const size_t places = (size_t)a.ranges * kRangeTokens;
+  float sum = a.chunk0 > 0 ? a.run[bh * places + t] : 0.0f;
   for (int x = 0; x < a.chunks; ++x) {
-    const Share share = share_of(a, bh, range, x, s);
-    if (share.t0 < share.t1) sum += a.part[((size_t)x * BH + bh) * ((size_t)a.ranges * kRangeTokens) + t];
+    const Share share = share_of(a, bh, range, a.chunk0 + x, s);
+    if (share.t0 < share.t1) sum += a.part[((size_t)x * BH + bh) * places + t];
+  }
+  if (!a.last) {
+    a.run[bh * places + t] = sum;
+    return;
   }
   const size_t at = (size_t)bh * a.w_stride + t;
   a.w_out[at] = a.w_in ? __builtin_fmaf(a.decay, a.w_in[at], sum) : sum;
@@ -938,15 +945,39 @@ TokenWeightsPlan make_token_weights_plan(int B, int Hq, int H, int total_q, int 
     tiles /= 2;
     if (cost(tiles) < cost(p.chunk_tiles)) p.chunk_tiles = tiles;
   }
-  p.chunks = (int)chunks(p.chunk_tiles);
+  p.chunks = p.slab_chunks = (int)chunks(p.chunk_tiles);
   auto up = [](size_t x) { return (x + 255) & ~size_t(255); };
   size_t off = 0;
-  p.off_ops = off, off = up(off + (size_t)p.tiles * H * kTileBytes);
-  p.off_stats = off, off = up(off + (size_t)p.ranges * p.tiles * H * kRows * sizeof(float2));
+  auto lay = [&](size_t tiles, size_t parts, size_t runs) {
+    off = 0;
+    p.off_ops = off, off = up(off + tiles * H * kTileBytes);
+    p.off_stats = off, off = up(off + (size_t)p.ranges * tiles * H * kRows * sizeof(float2));
+    p.off_part = off, off = up(off + parts * kRangeTokens * sizeof(float));
+    p.off_run = off, off = up(off + runs * kRangeTokens * sizeof(float));
+    return off;
+  };
   // (a smaller call may take shorter chunks: fewer than twice as many as there are places, and one a range)
   const long long most = ranges * chunks(kChunkTiles), shorter = 2 * places + ranges;
-  p.off_part = off, off = up(off + (size_t)(most > shorter ? most : shorter) * kRangeTokens * sizeof(float));
-  p.total = off;
+  const size_t whole = lay(p.tiles, (size_t)(most > shorter ? most : shorter), 0);
+  // A row's statistics take 8 bytes a range, so that those of whole prompts would grow with the square of their length (32 + 8 heads:
+  // 32,768 tokens 1.8 GB, 131,072 21.6). Beyond kSlabBytes, or what one chunk of every sequence takes where that is more, the chunks are
+  // taken a slab at a time, as many as have room; sums are added up in the same order. One prompt of 32,768 tokens 18.7 ms either way, of
+  // 65,536 74.4 ms and 72.8 with all statistics at once, of 131,072 294 and 287.
+  const size_t least = lay((size_t)B * kChunkTiles, ranges, ranges), room = least > kSlabBytes ? least : kSlabBytes;
+  if (whole <= room) {
+    p.total = lay(p.tiles, (size_t)(most > shorter ? most : shorter), 0);
+  } else {
+    auto slab = [&](long long n) { return lay((size_t)B * n * p.chunk_tiles, (size_t)(ranges * n), ranges); };
+    long long n = 1, beyond = (long long)p.chunks + 1;  // n chunks have room
+    while (beyond - n > 1) {
+      const long long mid = (n + beyond) / 2;
+      if (slab(mid) <= room) n = mid;
+      else beyond = mid;
+    }
+    slab(n);
+    p.slab_chunks = (int)n, p.slab_tiles = (int)n * p.chunk_tiles, p.tiles = B * p.slab_tiles;
+    p.total = room;
+  }
   // few rows: a call within these bounds may have them, whether or not this one does
   off = 0;
   p.off_few = off, off = up(off + (size_t)B * H * sizeof(FewOps));
@@ -991,8 +1022,9 @@ hipError_t launch_few(const TokenWeightsArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+// The chunks chunk0 .. chunk0 + chunks - 1
 template <int NG>
-hipError_t launch_many(const TokenWeightsArgs& a, hipStream_t s) {
+hipError_t launch_slab(const TokenWeightsArgs& a, hipStream_t s) {
   const long long BH = (long long)a.B * a.cv.num_kv_heads;
   hipError_t e = hipSuccess;
   if (a.seq_tiles > 0) {
@@ -1008,20 +1040,33 @@ hipError_t launch_many(const TokenWeightsArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((weight_scan_kernel<NG, 2>), shares, dim3(256), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  if (a.chunks != 1) {
+  if (a.part) {
     hipLaunchKernelGGL(weight_join_kernel, dim3((unsigned)(BH * a.ranges)), dim3(kRangeTokens), 0, s, a);
     e = hipGetLastError();
   }
   return e;
 }
 
+template <int NG>
+hipError_t launch_many(TokenWeightsArgs a, const TokenWeightsPlan& p, hipStream_t s) {
+  for (int c = 0;;) {
+    a.chunk0 = c, a.chunks = min(p.slab_chunks, p.chunks - c), a.last = c + a.chunks == p.chunks;
+    a.seq_tiles = min(a.chunks * p.chunk_tiles, p.seq_tiles - c * p.chunk_tiles);
+    const hipError_t e = launch_slab<NG>(a, s);
+    c += a.chunks;
+    if (e != hipSuccess || a.last) return e;
+  }
+}
+
 }  // namespace
 
 hipError_t launch_token_weights(TokenWeightsArgs a, const TokenWeightsPlan& p, uint8_t* ws, hipStream_t s) {
-  a.seq_tiles = p.seq_tiles, a.ranges = p.ranges, a.chunks = p.chunks, a.chunk_tiles = p.chunk_tiles, a.tiles = p.tiles;
+  a.ranges = p.ranges, a.chunk_tiles = p.chunk_tiles, a.tiles = p.tiles, a.slab_tiles = p.slab_tiles;
   a.ops = ws + p.off_ops;
   a.stats = reinterpret_cast<float2*>(ws + p.off_stats);
-  a.part = reinterpret_cast<float*>(ws + p.off_part);
+  // one chunk of all rows writes the results itself
+  a.part = p.chunks == 1 && p.slab_tiles == 0 ? nullptr : reinterpret_cast<float*>(ws + p.off_part);
+  a.run = reinterpret_cast<float*>(ws + p.off_run);
   if (p.few) {
     a.few = ws + p.off_few;
     a.stats = reinterpret_cast<float2*>(ws + p.off_few_stats);
@@ -1029,7 +1074,7 @@ hipError_t launch_token_weights(TokenWeightsArgs a, const TokenWeightsPlan& p, u
     a.pieces = p.pieces, a.page_cap = p.page_cap, a.row_cap = p.row_cap;
     return a.cv.groups == 4 ? launch_few<4>(a, s) : launch_few<1>(a, s);
   }
-  return a.cv.groups == 4 ? launch_many<4>(a, s) : launch_many<1>(a, s);
+  return a.cv.groups == 4 ? launch_many<4>(a, p, s) : launch_many<1>(a, p, s);
 }
 
 }  // namespace int2kv
