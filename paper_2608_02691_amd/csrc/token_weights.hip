@@ -171,7 +171,7 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
     R[kk][0] = pack_terms(x), R[kk][1] = pack_terms(y), R[kk][2] = pack_terms(z);
   }
   uint32_t real = 0;
-  float key_top = 0x1p-14f;  // (below it fp16's steps no longer shrink)
+  float key_top = 0x1p-14f;  // the largest element of the lane's part of the keys (below 2^-14 fp16's steps no longer shrink)
   if (w == 3) {
     Token<NG> first;
     first.load(a, b, h, n, s.ctx, hh);
@@ -187,8 +187,6 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
       }
       keys[x][l] = k;
     }
-#pragma unroll
-    for (int step = 32; step > 0; step >>= 1) key_top = fmaxf(key_top, __shfl_xor(key_top, step));
   }
   const int t1 = min(tiles, t0 + tiles_per_block), rows = s.n * a.gq;
   // a tile's rows on their way to LDS as the products take them, a quarter by each wave; the last one's again behind the last
@@ -256,7 +254,7 @@ __global__ __launch_bounds__(256) void weight_rows_kernel(TokenWeightsArgs a, in
       m = pair_max(m) * down;
       const bool good = fabsf(m) < 1.0e30f;
       if (hh == 0) tile.ref[n] = good ? m : 0.0f;
-      const bool unsure = __any(lim > 0 && (!good || 0.125f * big * key_top > kSure));
+      const bool unsure = __any((lim > 0 && !good) || 0.125f * big * key_top > kSure);
       if (l == 0) tile.unsure = unsure;
     }
 #pragma unroll
@@ -333,13 +331,13 @@ __global__ __launch_bounds__(256, 2) void weight_scan_kernel(TokenWeightsArgs a)
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = l & 31, hh = l >> 5, token0 = me.first + 64 * w;
   // ---- Row tiles on their way to LDS, tile t in slot t % kSlots. Half way through a tile (at its start) the next one has landed for every wave
   // and the one before is done with, so that no wave waits between tiles.
-  const uint8_t* tiles = a.ops + ((size_t)(s.tile0 + me.t0) * H + me.h) * kTileBytes + 16 * l;
+  const uint8_t* tiles = a.ops + ((ptrdiff_t)s.tile0 * H + me.h) * kTileBytes + 16 * l;  // of tile 0, which a slab may not hold
   const size_t stride = (size_t)H * kTileBytes;
   const uint32_t lds0 = (uint32_t)(uintptr_t)&lds[0];
   auto slot = [&](int t) -> const RowTile& { return lds[t & (kSlots - 1)]; };
   auto issue = [&](int t) {  // 17 pieces by four waves: the first has one more
     if (t >= me.t1) return;
-    for (int c = w; c < kPieces; c += 4) ap_dma16(tiles + (t - me.t0) * stride + 1024 * c, lds0 + (uint32_t)((t & (kSlots - 1)) * kTileBytes + 1024 * c));
+    for (int c = w; c < kPieces; c += 4) ap_dma16(tiles + t * stride + 1024 * c, lds0 + (uint32_t)((t & (kSlots - 1)) * kTileBytes + 1024 * c));
   };
   // until tile t has landed, with what came after it, up to `after` tiles, on its way
   auto landed = [&](int t, auto after) {
