@@ -465,11 +465,13 @@ int int2kv_tree_attention(const int2kv_cache* cache, const uint16_t* q, int64_t 
  *   weights_stride : at least max_ctx
  *   workspace    : int2kv_token_weights_workspace_bytes(...) bytes, 256-byte aligned; enough for every
  *                  call within the same bounds, nothing kept between calls, calls that overlap need one each.
- *                  Up to 8 rows (n_b H_q / H_kv, by max_q) of a KV head: mostly their scores, 4 bytes a row
- *                  and token. More: 17 KiB of operands for every 32 rows of a KV head and 8 bytes of statistics
- *                  for each row and 256 tokens of max_ctx (a prompt of 16,384 tokens, 32 + 8 heads: 0.6 GB);
- *                  where that passes 1 GiB the rows are taken in parts, one behind the other, so that it
- *                  stays at 1 GiB or, if that is more, what 1,024 rows of every sequence and KV head take
+ *                  Up to 8 rows (n_b H_q / H_kv, by max_q) of a KV head, which read the keys once: mostly
+ *                  their scores, 4 bytes a row and token. More, which read the keys twice (64 sequences of
+ *                  8,000 tokens, 4 KV heads: 8 rows 71 us, 12 or 16 rows 175): 17 KiB of operands for every
+ *                  32 rows of a KV head and 8 bytes of statistics for each row and 256 tokens of max_ctx (a
+ *                  prompt of 16,384 tokens, 32 + 8 heads: 0.6 GB); where that passes 1 GiB the rows are
+ *                  taken in parts, one behind the other, so that it stays at 1 GiB or, if that is more,
+ *                  what 1,024 rows of every sequence and KV head take
  * fp32 throughout: products run on the matrix cores in terms that keep fp32's precision, statistics and
  * sums in fp32 (a weight is off by about 1e-6 of itself and the scores' size times 1e-7). Queries and the
  * scales and zeros of the cached tokens have to be finite. Deterministic; no atomics on results. */

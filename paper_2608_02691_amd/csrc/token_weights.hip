@@ -590,7 +590,8 @@ __global__ __launch_bounds__(256) void weight_join_kernel(TokenWeightsArgs a) {
 
 // ---- Few rows a sequence (decode steps): up to kFewRows rows of one KV head. The scores are formed once and kept; the second
 // pass goes over them and not over the keys: 64 sequences of 512 to 32,768 tokens with five rows 188 us, by the kernels above about
-// three times as much (64 x 2 tokens of 8,000: 120 and 362 us; 2 of 1,000: 12 and 19).
+// three times as much (64 x 2 tokens of 8,000: 120 and 362 us; 2 of 1,000: 12 and 19). More rows than that have only those, at a tile
+// of 32: 64 x 1 token of 8,000 and 4 KV heads, 8 rows 71 us, 12 or 16 rows 175.
 namespace {
 
 constexpr int kFewRows = 8;

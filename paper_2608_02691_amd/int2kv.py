@@ -765,7 +765,7 @@ def int2kv_token_weights(cache: Int2KVCache, q: torch.Tensor, q_starts: torch.Te
     """decay * weights plus the attention weight that each cached token receives from the queries q bf16 [total, H_q, 128],
     the last tokens of every sequence (in the cache already), summed over them and the KV head's query heads. Returns fp32
     [batch, H_kv, n], n at least max_ctx (a new `out`: max_ctx, or as `weights`; zeros behind the lengths); `out` may be
-    `weights`."""
+    `weights`. The workspace of whole prompts is at most 1 GiB, or what 1,024 rows of every sequence and KV head take."""
     total, Hq, H, B = q.shape[0], q.shape[1], cache.num_kv_heads, ctx_lens.numel()
     if q_starts.numel() != B + 1:
         raise ValueError("q_starts must hold batch + 1 offsets")
@@ -798,7 +798,8 @@ def int2kv_select_tokens(weights: torch.Tensor, ctx_lens: torch.Tensor, max_ctx:
                          kept: Optional[torch.Tensor] = None, kept_lens: Optional[torch.Tensor] = None):
     """(kept int32 [batch, H_kv, n], kept_lens int32 [batch]): the tokens of each sequence and KV head that stay, ascending:
     the first `sink`, the last `recent`, and the largest weights (fp32 [batch, H_kv, at least max_ctx]) of the others, up to
-    `budget`. Entries behind kept_lens[b] are left as they were (-1 in a new `kept`)."""
+    `budget`. Entries behind kept_lens[b] are left as they were (-1 in a new `kept`). `kept` and `kept_lens` may not be memory that
+    the call reads: the new lengths do not replace ctx_lens in place."""
     if weights.dim() != 3:
         raise ValueError("weights must be [batch, num_kv_heads, at least max_ctx]")
     B, H = weights.shape[0], weights.shape[1]
