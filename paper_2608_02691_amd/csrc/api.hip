@@ -644,10 +644,22 @@ bool rows_meet(const Rows& a, const Rows& b) {
   return d < a.len() || a.step() - d < b.len();
 }
 
-// Whether two ranges of bytes meet
-bool spans_meet(const void* a, uint64_t a_len, const void* b, uint64_t b_len) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return a_len && b_len && x < y + b_len && y < x + a_len;
+// n lists of `len` bytes, `step` apart
+struct Lists {
+  const void* p;
+  uint64_t n, step, len;
+  uintptr_t first() const { return reinterpret_cast<uintptr_t>(p); }
+  uintptr_t end() const { return first() + (n - 1) * step + len; }
+};
+
+// Whether two sets of lists share a byte: lists of one step may lie in each other's gaps, and a single one in another's; lists
+// of different steps count as sharing where their spans meet
+bool lists_meet(const Lists& a, const Lists& b) {
+  if (!a.len || !b.len || a.first() >= b.end() || b.first() >= a.end()) return false;
+  if ((a.n == 1 && b.n == 1) || (a.n > 1 && b.n > 1 && a.step != b.step)) return true;
+  const uint64_t step = a.n > 1 ? a.step : b.step;
+  const uint64_t d = (b.first() >= a.first() ? b.first() - a.first() : step - (a.first() - b.first()) % step) % step;
+  return d < a.len || step - d < b.len;
 }
 
 bool valid_stride(int64_t stride, int heads) { return stride >= (int64_t)heads * kHeadDim && stride % 8 == 0 && stride <= INT32_MAX; }
@@ -880,10 +892,10 @@ int int2kv_select_tokens(const float* weights, int64_t weights_stride, int batch
   if (!aligned(weights, 4) || !aligned(kept, 4) || !aligned(ctx_lens, 4) || !aligned(kept_lens, 4))
     return fail(INT2KV_EINVAL, "weights, ctx_lens, kept and kept_lens must be 4-byte aligned");
   // every work-group reads its sequence's length and its own weights, and writes its list; one of a sequence's writes the new length
-  const uint64_t more = (uint64_t)batch * num_kv_heads - 1, lens = 4ull * batch, longest = budget < max_ctx ? budget : max_ctx;
-  const uint64_t w_len = max_ctx > 0 ? 4 * (more * weights_stride + max_ctx) : 0, kept_len = longest > 0 ? 4 * (more * kept_stride + longest) : 0;
-  if (spans_meet(kept_lens, lens, ctx_lens, lens) || spans_meet(kept_lens, lens, weights, w_len) || spans_meet(kept_lens, lens, kept, kept_len) ||
-      spans_meet(kept, kept_len, ctx_lens, lens) || spans_meet(kept, kept_len, weights, w_len))
+  const uint64_t n = (uint64_t)batch * num_kv_heads, longest = budget < max_ctx ? budget : max_ctx;
+  const Lists w{weights, n, 4 * (uint64_t)weights_stride, 4 * (uint64_t)max_ctx}, k{kept, n, 4 * (uint64_t)kept_stride, 4 * longest};
+  const Lists lens{ctx_lens, 1, 0, 4 * (uint64_t)batch}, new_lens{kept_lens, 1, 0, 4 * (uint64_t)batch};
+  if (lists_meet(new_lens, lens) || lists_meet(new_lens, w) || lists_meet(new_lens, k) || lists_meet(k, lens) || lists_meet(k, w))
     return fail(INT2KV_EINVAL, "kept and kept_lens must not overlap weights, ctx_lens or each other");
   SelectArgs a{weights, weights_stride, ctx_lens, batch, num_kv_heads, max_ctx, budget, sink, recent, kept, kept_stride, kept_lens};
   return hip_status(launch_select_tokens(a, stream), "select_tokens");

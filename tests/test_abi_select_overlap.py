@@ -20,3 +20,11 @@ def _select(w=W, kept=KEPT, lens=LENS, klens=KLENS, budget=32):
 def test_outputs_over_inputs_are_refused(kw):
     st, msg = _select(**kw)
     assert st == K.INT2KV_EINVAL and b"overlap" in msg, msg
+
+
+@pytest.mark.parametrize("kw", [
+    dict(kept=W + 4 * 24), dict(kept=W + 4 * (64 - 1)), dict(kept=W - 4), dict(klens=W + 4 * 63), dict(klens=W + 4 * (64 + 39) - 4), dict(klens=W - 4)])
+def test_lists_in_gaps_that_are_too_small(kw):
+    """Lists of one stride, a list of new lengths: the weights' gaps do not hold them."""
+    st = K.load_library().int2kv_select_tokens(W, 64, 2, 2, LENS, 40, 25, 4, 8, kw.get("kept", KEPT), 64, kw.get("klens", KLENS), None)
+    assert st == K.INT2KV_EINVAL and b"overlap" in K.load_library().int2kv_last_error()
