@@ -434,7 +434,8 @@ int int2kv_chunk_attention(const int2kv_cache* cache, const uint16_t* q, int64_t
  *                  every token of the trees is a query
  *   total_tree, max_tree : rows of k_tree, v_tree and parents; host-side upper bound of T_b, at most
  *                  INT2KV_MAX_TREE
- *   k_tree, v_tree, mu : as k_new, v_new and mu of int2kv_chunk_attention
+ *   k_tree, v_tree, mu : as k_new, v_new and mu of int2kv_chunk_attention (NULL, as parents, only where
+ *                  total_tree is 0)
  *   workspace    : int2kv_tree_attention_workspace_bytes(...) bytes, 256-byte aligned; enough for every
  *                  call within the same bounds, nothing kept between calls, calls that overlap need one each
  * Numerics and ranges as int2kv_chunk_attention. Deterministic; no atomics on results. */

@@ -811,7 +811,8 @@ int int2kv_tree_attention(const int2kv_cache* cache, const uint16_t* q, int64_t 
     return fail(INT2KV_EUNSUPPORTED, "total_tree * num_kv_heads must be below 2^31");
   if (max_q > 0 && total_q > 0) {
     if (!tree_starts || !aligned(tree_starts, 4)) return fail(INT2KV_EINVAL, "NULL pointer argument: tree_starts");
-    if (!parents || !k_tree || !v_tree || !mu) return fail(INT2KV_EINVAL, "NULL pointer argument: parents, k_tree, v_tree and mu");
+    if (total_tree > 0 && (!parents || !k_tree || !v_tree || !mu))
+      return fail(INT2KV_EINVAL, "NULL pointer argument: parents, k_tree, v_tree and mu");
     if (!aligned(parents, 4)) return fail(INT2KV_EINVAL, "parents must be 4-byte aligned");
   }
   ChunkArgs a{};
@@ -820,6 +821,8 @@ int int2kv_tree_attention(const int2kv_cache* cache, const uint16_t* q, int64_t 
   a.table = block_table, a.max_blocks = max_blocks_per_seq, a.lens = ctx_lens, a.max_ctx = max_ctx;
   a.R_k = R_k, a.R_v = R_v, a.own = true, a.k_new = k_tree, a.v_new = v_tree, a.mu = mu, a.out = out;
   a.tree_starts = tree_starts, a.parents = parents, a.total_tree = total_tree, a.max_tree = max_tree < total_tree ? max_tree : total_tree;
+  // trees without a token: queries in front of them get zeros, and nothing of rows and parents is read (a.parents also names the form)
+  if (total_tree == 0) a.k_new = a.v_new = nullptr, a.mu = nullptr, a.parents = tree_starts;
   return chunk_attention(cache, a, "k_tree, v_tree", total_tree, workspace, workspace_bytes, stream);
 }
 
