@@ -922,7 +922,7 @@ int int2kv_move_tokens(const int2kv_cache* cache, const int32_t* block_table, in
   const int pages = (int)(((int64_t)max_kept + kBlock - 1) / kBlock);
   if (kept_stride < max_kept) return fail(INT2KV_EINVAL, "kept_stride must be at least max_kept");
   if (out_max_blocks < pages) return fail(INT2KV_EINVAL, "the result's table must hold max_kept tokens");
-  if (!weights != !out_weights) return fail(INT2KV_EINVAL, "weights and out_weights go together");
+  if (max_kept > 0 && !weights != !out_weights) return fail(INT2KV_EINVAL, "weights and out_weights go together");
   if (weights && (weights_stride <= 0 || out_weights_stride < max_kept))
     return fail(INT2KV_EINVAL, "weights_stride must be positive, out_weights_stride at least max_kept");
   if (max_kept == 0) return ok();

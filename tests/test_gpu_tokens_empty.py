@@ -19,3 +19,20 @@ def test_queries_without_trees(seqs, gq, max_tree):
     got = c.call(out=out, max_tree=max_tree)
     torch.cuda.synchronize()
     assert bool((got[:-2] == 0).all()) and bool((got[-2:] == 3.0).all())
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+def test_moves_of_nothing(in_place):
+    """max_kept 0, with sums and without: the cache and the sums stay as they were, new sums are empty."""
+    pool = dev(np.random.default_rng(0).integers(0, 256, (8, 3, 1536)).astype(np.uint8))
+    cache, before = K.Int2KVCache(8, 3, pool=pool), pool.clone()
+    table, other = dev(np.arange(4, dtype=np.int32).reshape(2, 2)), dev(np.arange(4, 8, dtype=np.int32).reshape(2, 2))
+    kept, lens = torch.zeros((2, 3, 0), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    w = torch.rand((2, 3, 30), device="cuda")
+    sums = w.clone()
+    out = None if in_place else other
+    assert K.int2kv_move_tokens(cache, table, kept, lens, 0, out_table=out) is None
+    got = K.int2kv_move_tokens(cache, table, kept, lens, 0, out_table=out, weights=w)
+    torch.cuda.synchronize()
+    assert torch.equal(pool, before) and torch.equal(w, sums)
+    assert got.data_ptr() == w.data_ptr() if in_place else got.shape == (2, 3, 0)
